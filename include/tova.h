@@ -417,6 +417,179 @@ int tova_decode_step_static(const tova_config* cfg, void* K, void* V, int32_t* p
                             int32_t n_live, const void* q, const void* k, const void* v, int32_t pos,
                             float* out, int32_t* evicted_pos, int32_t* status, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Around the decode step: rotary positions, the 8-bit state, drafted tokens.
+ *
+ * What a model that decodes speculatively over a bounded state needs beside the
+ * step itself.  The calls below follow the general conventions above (device
+ * pointers, 16-byte aligned unless said otherwise, caller-owned memory, the
+ * device of the pointers current, argument errors found on the host before
+ * anything is launched); they take plain tensors, keep nothing between calls,
+ * and may run on any stream.  Token-major layouts: [T,B,...] for T prompt
+ * tokens, [N,B,...] for the N drafted tokens ("nodes") of every sequence.
+ * Results do not depend on earlier calls; two calls may share buffers only
+ * when ordered, their workspaces among them.
+ * ------------------------------------------------------------------------- */
+
+/* Rotary position embedding of q and k: makes the post-RoPE q and k that the
+ * calls above take.  Pair i of a head at position p turns by the angle p w_i,
+ *   (a, b) -> m (a cos - b sin, b cos + a sin),  w_i = base^(-2 i / rotary_dim),
+ * i < rotary_dim / 2; components from rotary_dim on pass through.  Pairs are
+ * (i, i + rotary_dim/2) in the half layout, (2i, 2i+1) in the interleaved one.
+ * Scalings for contexts beyond the one trained on (original_context tokens),
+ * by `factor` >= 1:
+ *   TOVA_ROPE_PLAIN    none, m = 1 (factor ignored);
+ *   TOVA_ROPE_LINEAR   w_i / factor;
+ *   TOVA_ROPE_NTK      base * factor^(rotary_dim / (rotary_dim - 2));
+ *   TOVA_ROPE_YARN     (arXiv 2309.00071) pairs that turn more than blend_high
+ *          (0: 32) times over original_context stay, those that turn less than
+ *          blend_low (0: 1) times become w_i / factor, a linear ramp over the
+ *          pair index (from the lower bound rounded down to the upper one
+ *          rounded up) between; m = 0.1 ln(factor) + 1;
+ *   TOVA_ROPE_BANDS    by wavelength 2 pi / w_i: below original_context /
+ *          blend_high (0: 4) it stays, above original_context / blend_low
+ *          (0: 1) it becomes w_i / factor, between the two blended linearly in
+ *          original_context / wavelength.
+ * amplitude > 0 replaces m.  The frequencies are formed once, on the host, in 64
+ * bits; the handle holds them and no device memory.
+ *   tova_rope_apply   q [T,B,H,D], k [T,B,Hkv,D] or NULL; *_stride: elements
+ *          between consecutive (token, sequence) rows, 0 = contiguous, a
+ *          multiple of 16 bytes (q and k may be slices of one projection);
+ *          positions [T,B] int32, or NULL: first_pos + token index; results in
+ *          the type of the input, from fp32 arithmetic and angles formed in 64
+ *          bits; an output may be its own input, but not overlap it otherwise.
+ *          inverse != 0 turns by -p w_i and keeps m: the transposed map, which
+ *          takes a gradient of the results to the gradient of the inputs. */
+#define TOVA_ROPE_HALF 0
+#define TOVA_ROPE_INTERLEAVED 1
+#define TOVA_ROPE_PLAIN 0
+#define TOVA_ROPE_LINEAR 1
+#define TOVA_ROPE_NTK 2
+#define TOVA_ROPE_YARN 3
+#define TOVA_ROPE_BANDS 4
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim; /* head_dim in {64,128}                     */
+  int32_t dtype;                                  /* of q, k and the results                  */
+  int32_t rotary_dim;                             /* even, 2..head_dim; 0 = head_dim          */
+  int32_t layout;                                 /* TOVA_ROPE_HALF or TOVA_ROPE_INTERLEAVED  */
+  int32_t scaling;                                /* TOVA_ROPE_PLAIN ... TOVA_ROPE_BANDS      */
+  double base;                                    /* > 1; 0 = 10000                           */
+  double factor;                                  /* >= 1; 0 = 1                              */
+  double blend_low, blend_high;                   /* 0 = the defaults above                   */
+  double amplitude;                               /* 0 = m as above                           */
+  int32_t original_context;                       /* >= 1 for YARN and BANDS                  */
+} tova_rope_config;
+typedef struct tova_rope tova_rope;               /* opaque host handle                       */
+int tova_rope_init(tova_rope** out, const tova_rope_config* cfg);
+int tova_rope_apply(const tova_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    int32_t n_tokens, const int32_t* positions, int32_t first_pos, int32_t inverse, void* q_out,
+                    int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* cuda_stream);
+int tova_rope_destroy(tova_rope* r);
+
+/* A state in 8 bits: half the bytes of a bf16 state per step and per sequence.
+ * codes k, v [B,Hkv,capacity,D] one byte each, scales [B,Hkv,capacity] fp32, one
+ * for each row of K and of V:
+ *   a = max |x_d|,  Q = 127 (int8) or 448 (e4m3),  scale = fp32(a / Q),
+ *   code_d = nearest(fp32(x_d * fp32(Q / a))), ties to even,  value = code_d * scale.
+ * Rows with a < 2^-100 store zeros; rows with an infinity or NaN store scale NaN
+ * and read back as NaN.  Codes and scales are a function of the rows alone.
+ *   tova_quant_write   rows k, v [T,B,Hkv,D] (strides as for tova_rope_apply)
+ *          go to slots [T,B] int32, or NULL: first_slot + token, which must lie
+ *          in the state.  A listed slot outside 0..capacity-1 skips the row;
+ *          where a call lists a slot of a sequence twice, the later token's row
+ *          stands.  All other rows stay as they are.
+ *   tova_quant_read    the rows of those slots as k, v [T,B,Hkv,D] in cfg->dtype,
+ *          fp32(code * scale) rounded to it; a slot outside the state gives
+ *          zeros.  k or v may be NULL. */
+#define TOVA_FORMAT_PLAIN 0 /* rows in cfg->dtype, no scales (tova_tree_attention only) */
+#define TOVA_FORMAT_INT8 1
+#define TOVA_FORMAT_E4M3 2
+typedef struct {
+  int32_t batch, n_kv_heads, head_dim, capacity; /* head_dim in {64,128}                      */
+  int32_t dtype;                                 /* of the rows written and read              */
+  int32_t format;                                /* TOVA_FORMAT_INT8 or TOVA_FORMAT_E4M3      */
+} tova_quant_config;
+int tova_quant_write(const tova_quant_config* cfg, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     int32_t n_tokens, const int32_t* slots, int32_t first_slot, void* k_codes, float* k_scale,
+                     void* v_codes, float* v_scale, void* cuda_stream);
+int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const float* k_scale, const void* v_codes,
+                    const float* v_scale, int32_t n_tokens, const int32_t* slots, int32_t first_slot, void* k,
+                    void* v, void* cuda_stream);
+
+/* Attention of a tree of drafted tokens over a state, which is only read: node i
+ * of a sequence attends to the state's rows, to itself and to the nodes above
+ * it (Eq. 4 and 7 with the candidates that it would have if the nodes above it
+ * had been settled and no row dropped meanwhile; exact while the state has free
+ * rows for them).
+ *   K, V [B,Hkv,capacity,D]   in cfg->dtype (TOVA_FORMAT_PLAIN), or codes with
+ *                             k_scale, v_scale [B,Hkv,capacity]
+ *   lens [B] int32 or NULL    rows each sequence holds, 0..n_live (clamped to
+ *                             it); NULL: n_live in all.  Rows behind are not
+ *                             read for values: they may hold anything
+ *   n_live                    the most rows any sequence holds, 0..capacity
+ *   n_nodes                   N, 0..256; 1 = a plain step that drops nothing
+ *   parents [N,B] int32       -1 (hangs below the last settled token) or an
+ *                             earlier node's index; NULL: a chain, parent i-1.
+ *                             Any other value makes the node, and those below
+ *                             it, padding: output 0
+ *   q [N,B,H,D], k, v [N,B,Hkv,D], out [N,B,H,D]   all in cfg->dtype
+ * Logits, soft-max and sums are fp32; fp32 configurations form every product in
+ * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the
+ * result is.  The result does not depend on n_live, lens, other sequences or the
+ * GPU beyond the order of fp32 sums, and is the same bits every time.
+ *   tova_tree_workspace_bytes   device bytes that a call with this shape needs
+ *          for partial results (0 is possible: none; an invalid configuration
+ *          gives (size_t)-1).  It asks the current device for its SM count.
+ *   tova_cache_tree_attention   the same over the live rows of a cache (format
+ *          and geometry are the cache's).  Waits for a pending deferred eviction.
+ *          Refused (TOVA_ERR_UNSUPPORTED) under position compression, whose keys
+ *          are not rotated. */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim, capacity; /* as in tova_config               */
+  int32_t dtype;                                            /* of q, k, v, out, and plain states */
+  int32_t format;                                           /* TOVA_FORMAT_* of K and V          */
+  float sm_scale;                                           /* 0 selects 1/sqrt(head_dim)        */
+} tova_tree_config;
+size_t tova_tree_workspace_bytes(const tova_tree_config* cfg, int32_t n_live, int32_t n_nodes);
+int tova_tree_attention(const tova_tree_config* cfg, const void* K, const void* V, const float* k_scale,
+                        const float* v_scale, const int32_t* lens, int32_t n_live, const void* q, const void* k,
+                        const void* v, int32_t n_nodes, const int32_t* parents, void* out, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream);
+size_t tova_cache_tree_workspace_bytes(const tova_cache* c, int32_t n_nodes);
+int tova_cache_tree_attention(tova_cache* c, const void* q, const void* k, const void* v, int32_t n_nodes,
+                              const int32_t* parents, void* out, void* workspace, size_t workspace_bytes,
+                              void* cuda_stream);
+
+/* Which drafted tokens become real, from given random numbers, so that the
+ * tokens are distributed as if drawn from the target one by one.
+ *   target [N+1,B,V]   probabilities, cfg->dtype; row 0 after the last settled
+ *                      token, row 1+i after node i
+ *   draft [N+1,B,V] or NULL   row r: what the children of that node were drawn
+ *                      from, independently of one another (only rows of nodes
+ *                      that have children are read, so a chain may pass N rows);
+ *                      NULL: drafts proposed with certainty
+ *   tokens, parents [N,B] int32 (parents as for tova_tree_attention)
+ *   u [N,B], u_sample [B] fp32 in [0,1)
+ * The walk starts at the root.  Children of a node are tried in index order, with
+ * S = 0, Z = 1 at first: a child with token x is accepted when u Z q(x) < r(x),
+ * r = max(0, p - S q); else S += Z and Z = sum of the new r.  (NULL draft: q(x) =
+ * 1, r is p with the tokens already tried struck out, Z -= r(x) instead.)  Where
+ * no child is accepted, the last token is the smallest x at which the running sum
+ * of r exceeds u_sample times its whole (of p where r is zero everywhere).
+ * Comparisons and sums are in 64 bits.
+ *   n_accepted [B]; path [N,B] (may be NULL): the accepted nodes, then -1;
+ *   tokens_out [N+1,B]: their tokens, then the last token, then -1.  A row of p
+ *   without any positive entry gives the last token -1.
+ * A token outside 0..V-1 is never accepted.  N = 0 draws one token. */
+typedef struct {
+  int32_t batch, n_nodes, vocab; /* n_nodes 0..1024                                    */
+  int32_t dtype;                 /* of the probabilities                               */
+  int64_t row_stride;            /* elements between the rows of two sequences; 0 = V  */
+} tova_verify_config;
+int tova_verify_draft(const tova_verify_config* cfg, const void* target, const void* draft, const int32_t* tokens,
+                      const int32_t* parents, const float* u, const float* u_sample, int32_t* n_accepted,
+                      int32_t* path, int32_t* tokens_out, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

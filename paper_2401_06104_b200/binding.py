@@ -22,6 +22,9 @@ TOVA_POLICY_TOVA_HEAD = 2
 TOVA_POLICY_H2O_LAYER = 3
 TOVA_POLICY_H2O_HEAD = 4
 TOVA_POS_AUTO = -1       # "the previous token's position + 1"
+TOVA_ROPE_HALF, TOVA_ROPE_INTERLEAVED = 0, 1
+TOVA_ROPE_PLAIN, TOVA_ROPE_LINEAR, TOVA_ROPE_NTK, TOVA_ROPE_YARN, TOVA_ROPE_BANDS = 0, 1, 2, 3, 4
+TOVA_FORMAT_PLAIN, TOVA_FORMAT_INT8, TOVA_FORMAT_E4M3 = 0, 1, 2
 
 
 class TovaError(RuntimeError):
@@ -35,6 +38,30 @@ class tova_config(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("sm_scale", ctypes.c_float), ("evict", ctypes.c_int32)]
+
+
+class tova_rope_config(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("blend_low", ctypes.c_double), ("blend_high", ctypes.c_double),
+                ("amplitude", ctypes.c_double), ("original_context", ctypes.c_int32)]
+
+
+class tova_quant_config(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("dtype", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class tova_tree_config(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("format", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
+
+
+class tova_verify_config(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_nodes", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -109,6 +136,29 @@ def lib() -> ctypes.CDLL:
         L.tova_decode_step_static.restype = ctypes.c_int
         L.tova_decode_step_static.argtypes = [ctypes.POINTER(tova_config), vp, vp, vp, i32, vp, vp, vp,
                                               i32, vp, vp, vp, vp]
+        sz = ctypes.c_size_t
+        L.tova_rope_init.restype = ctypes.c_int
+        L.tova_rope_init.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(tova_rope_config)]
+        L.tova_rope_apply.restype = ctypes.c_int
+        L.tova_rope_apply.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, i32, vp, i64, vp, i64, vp]
+        L.tova_rope_destroy.restype = ctypes.c_int
+        L.tova_rope_destroy.argtypes = [vp]
+        L.tova_quant_write.restype = ctypes.c_int
+        L.tova_quant_write.argtypes = [ctypes.POINTER(tova_quant_config), vp, i64, vp, i64, i32, vp, i32, vp, vp, vp,
+                                       vp, vp]
+        L.tova_quant_read.restype = ctypes.c_int
+        L.tova_quant_read.argtypes = [ctypes.POINTER(tova_quant_config), vp, vp, vp, vp, i32, vp, i32, vp, vp, vp]
+        L.tova_tree_workspace_bytes.restype = sz
+        L.tova_tree_workspace_bytes.argtypes = [ctypes.POINTER(tova_tree_config), i32, i32]
+        L.tova_tree_attention.restype = ctypes.c_int
+        L.tova_tree_attention.argtypes = [ctypes.POINTER(tova_tree_config), vp, vp, vp, vp, vp, i32, vp, vp, vp, i32,
+                                          vp, vp, vp, sz, vp]
+        L.tova_cache_tree_workspace_bytes.restype = sz
+        L.tova_cache_tree_workspace_bytes.argtypes = [vp, i32]
+        L.tova_cache_tree_attention.restype = ctypes.c_int
+        L.tova_cache_tree_attention.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.tova_verify_draft.restype = ctypes.c_int
+        L.tova_verify_draft.argtypes = [ctypes.POINTER(tova_verify_config), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.tova_strerror.restype = ctypes.c_char_p
         L.tova_strerror.argtypes = [ctypes.c_int]
         _lib = L
@@ -307,6 +357,25 @@ class TovaCache:
     def tova_cache_launches(self) -> int:
         return int(lib().tova_cache_launches(self._h))
 
+    def tova_cache_tree_workspace_bytes(self, n_nodes: int) -> int:
+        n = int(lib().tova_cache_tree_workspace_bytes(self._h, int(n_nodes)))
+        if n == _NO_SIZE:
+            raise TovaError(-2, "tova_cache_tree_workspace_bytes rejected the shape")
+        return n
+
+    def tova_cache_tree_attention(self, q, k, v, n_nodes: int, out, workspace=None, parents=None, stream=None) -> None:
+        """Attention of the drafted tokens q [N,B,H,D], k and v [N,B,Hkv,D] over this state and their tree; out
+        [N,B,H,D] in the cache's dtype, workspace of tova_cache_tree_workspace_bytes(n_nodes) bytes."""
+        c, N = self.cfg, int(n_nodes)
+        row = N * c.batch * c.head_dim
+        for x, n in ((q, row * c.n_q_heads), (k, row * c.n_kv_heads), (v, row * c.n_kv_heads), (out, row * c.n_q_heads)):
+            _need(x, n, self.tdtype, self.device)
+        _need(parents, N * c.batch, torch.int32, self.device)
+        with _on(self.device):
+            _check(lib().tova_cache_tree_attention(self._h, _a(q), _a(k), _a(v), N, _a(parents), _a(out), _a(workspace),
+                                                   _bytes(workspace), _raw_stream(self.device, stream)),
+                   "tova_cache_tree_attention")
+
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
             lib().tova_cache_destroy(self._h)
@@ -329,6 +398,211 @@ def tova_decode_step_static(cfg: tova_config, K, V, positions, n_live: int, q, k
     _check(lib().tova_decode_step_static(ctypes.byref(cfg), _p(K), _p(V), _p(positions), int(n_live),
                                          _p(q), _p(k), _p(v), int(pos), _p(out), _p(evicted_pos),
                                          _p(status), _stream(stream)), "tova_decode_step_static")
+
+
+# -- around the decode step: rotary positions, the 8-bit state, drafted tokens ------------------------------------
+# These take torch tensors of any origin, so their types, sizes and devices are checked here before their addresses
+# reach the library; the current device is switched to the tensors' where it is another.
+
+_NO_SIZE = ctypes.c_size_t(-1).value
+_TORCH_TYPE = {TOVA_DTYPE_BF16: torch.bfloat16, TOVA_DTYPE_FP32: torch.float32}
+_CODE_TYPES = {TOVA_FORMAT_INT8: (torch.int8, torch.uint8), TOVA_FORMAT_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8)}
+_byref = ctypes.byref
+
+
+def _a(t):
+    return None if t is None else t.data_ptr()
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _need(t, numel: int, dtype, device) -> None:
+    """A contiguous device tensor of at least `numel` elements of `dtype` (or of one of several); None passes."""
+    if t is None:
+        return
+    if not (t.dtype is dtype or (type(dtype) is tuple and t.dtype in dtype)):
+        raise TypeError(f"expected a tensor of {dtype}, got {t.dtype}")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"expected a tensor on {device}, got {t.device}")
+    if not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"expected a contiguous tensor of at least {numel} elements, got {tuple(t.shape)}"
+                         f"{'' if t.is_contiguous() else ' (not contiguous)'}")
+
+
+def _rows(t, n_tokens: int, batch: int, heads: int, dim: int, dtype, device) -> int:
+    """Checks [T,B,heads,dim] with contiguous heads and evenly spaced (token, sequence) rows; their element stride."""
+    if t.dtype is not dtype:
+        raise TypeError(f"expected a tensor of {dtype}, got {t.dtype}")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"expected a tensor on {device}, got {t.device}")
+    T, B, H, D = t.shape
+    if T < n_tokens or B != batch or H != heads or D != dim:
+        raise ValueError(f"expected [{n_tokens},{batch},{heads},{dim}], got {tuple(t.shape)}")
+    s0, s1, s2, s3 = t.stride()
+    if n_tokens * batch == 1:
+        s0 = s1 = heads * dim
+    elif batch == 1:
+        s1 = s0
+    elif n_tokens == 1:
+        s0 = s1 * batch
+    if s0 != s1 * batch or (s2 != dim and heads > 1) or (s3 != 1 and dim > 1):
+        raise ValueError(f"rows of {tuple(t.shape)} with strides {t.stride()} are not evenly spaced with contiguous heads")
+    return s1
+
+
+class _on:
+    """Makes `device` current for the calls inside, where it is not already."""
+    __slots__ = ("want", "was")
+
+    def __init__(self, device):
+        self.want = device.index
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.want != self.was:
+            torch.cuda.set_device(self.want)
+
+    def __exit__(self, *exc):
+        if self.want != self.was:
+            torch.cuda.set_device(self.was)
+
+
+def _raw_stream(device, stream) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+class TovaRope:
+    """Rotary positions of q and k; holds the frequencies (host memory only)."""
+
+    def __init__(self, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int = TOVA_DTYPE_BF16,
+                 rotary_dim: int = 0, layout: int = TOVA_ROPE_HALF, base: float = 10000.0,
+                 scaling: int = TOVA_ROPE_PLAIN, factor: float = 1.0, original_context: int = 0,
+                 blend_low: float = 0.0, blend_high: float = 0.0, amplitude: float = 0.0):
+        self.cfg = tova_rope_config(batch, n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, layout, scaling, base,
+                                    factor, blend_low, blend_high, amplitude, original_context)
+        h = ctypes.c_void_p()
+        _check(lib().tova_rope_init(_byref(h), _byref(self.cfg)), "tova_rope_init")
+        self._h = h
+        self._dims = (batch, n_q_heads, n_kv_heads, head_dim, _TORCH_TYPE[dtype])
+
+    def tova_rope_apply(self, q, k, n_tokens: int, q_out, k_out, positions=None, first_pos: int = 0,
+                        inverse: bool = False, stream=None) -> None:
+        """q [T,B,H,D] and k [T,B,Hkv,D] (or None) into q_out, k_out; all may be evenly strided over (T, B).  inverse:
+        the transposed map, for gradients."""
+        B, H, Hkv, D, t = self._dims
+        dev = q.device
+        qs, qos = _rows(q, n_tokens, B, H, D, t, dev), _rows(q_out, n_tokens, B, H, D, t, dev)
+        ks = kos = 0
+        if k is not None or k_out is not None:
+            if k is None or k_out is None:
+                raise ValueError("k and k_out come together")
+            ks, kos = _rows(k, n_tokens, B, Hkv, D, t, dev), _rows(k_out, n_tokens, B, Hkv, D, t, dev)
+        _need(positions, n_tokens * B, torch.int32, dev)
+        with _on(dev):
+            _check(lib().tova_rope_apply(self._h, _a(q), qs, _a(k), ks, n_tokens, _a(positions), first_pos,
+                                         1 if inverse else 0, _a(q_out), qos, _a(k_out), kos, _raw_stream(dev, stream)),
+                   "tova_rope_apply")
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h:
+            lib().tova_rope_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _need_state(cfg, format, codes, scale, dtype, device) -> None:
+    rows = cfg.batch * cfg.n_kv_heads * cfg.capacity
+    _need(codes, rows * cfg.head_dim, dtype if format == TOVA_FORMAT_PLAIN else _CODE_TYPES.get(format), device)
+    _need(scale, rows, torch.float32, device)
+
+
+def tova_quant_write(cfg: tova_quant_config, k, v, n_tokens: int, k_codes, k_scale, v_codes, v_scale, slots=None,
+                     first_slot: int = 0, stream=None) -> None:
+    """Rows k, v [T,B,Hkv,D] (evenly strided over (T, B)) into the 8-bit state: codes [B,Hkv,cap,D], scales
+    [B,Hkv,cap]; slots [T,B] int32 or None = first_slot + token."""
+    t, dev, B, H, D = _TORCH_TYPE.get(cfg.dtype), k.device, cfg.batch, cfg.n_kv_heads, cfg.head_dim
+    ks, vs = _rows(k, n_tokens, B, H, D, t, dev), _rows(v, n_tokens, B, H, D, t, dev)
+    _need_state(cfg, cfg.format, k_codes, k_scale, None, dev)
+    _need_state(cfg, cfg.format, v_codes, v_scale, None, dev)
+    _need(slots, n_tokens * B, torch.int32, dev)
+    with _on(dev):
+        _check(lib().tova_quant_write(_byref(cfg), _a(k), ks, _a(v), vs, n_tokens, _a(slots), first_slot, _a(k_codes),
+                                      _a(k_scale), _a(v_codes), _a(v_scale), _raw_stream(dev, stream)), "tova_quant_write")
+
+
+def tova_quant_read(cfg: tova_quant_config, k_codes, k_scale, v_codes, v_scale, n_tokens: int, k, v, slots=None,
+                    first_slot: int = 0, stream=None) -> None:
+    """The state's rows at slots [T,B] (None: first_slot + token) as k, v [T,B,Hkv,D] in cfg.dtype; k or v may be None."""
+    if k is None and v is None:
+        return
+    t, dev, B = _TORCH_TYPE.get(cfg.dtype), (k if k is not None else v).device, cfg.batch
+    n = n_tokens * B * cfg.n_kv_heads * cfg.head_dim
+    _need(k, n, t, dev)
+    _need(v, n, t, dev)
+    _need_state(cfg, cfg.format, k_codes, k_scale, None, dev)
+    _need_state(cfg, cfg.format, v_codes, v_scale, None, dev)
+    _need(slots, n_tokens * B, torch.int32, dev)
+    with _on(dev):
+        _check(lib().tova_quant_read(_byref(cfg), _a(k_codes), _a(k_scale), _a(v_codes), _a(v_scale), n_tokens,
+                                     _a(slots), first_slot, _a(k), _a(v), _raw_stream(dev, stream)), "tova_quant_read")
+
+
+def tova_tree_workspace_bytes(cfg: tova_tree_config, n_live: int, n_nodes: int) -> int:
+    n = int(lib().tova_tree_workspace_bytes(_byref(cfg), int(n_live), int(n_nodes)))
+    if n == _NO_SIZE:
+        raise TovaError(-2, "tova_tree_workspace_bytes rejected the shape")
+    return n
+
+
+def tova_tree_attention(cfg: tova_tree_config, K, V, n_live: int, q, k, v, n_nodes: int, out, workspace=None,
+                        parents=None, lens=None, k_scale=None, v_scale=None, stream=None) -> None:
+    """Attention of N drafted tokens q [N,B,H,D], k, v [N,B,Hkv,D] over a state K, V [B,Hkv,cap,D] (or its codes with
+    their scales) and the tree parents [N,B] (None: a chain); lens [B] int32 (None: n_live rows each).  out [N,B,H,D]
+    in the type of q."""
+    t, dev, B, N = _TORCH_TYPE.get(cfg.dtype), q.device, cfg.batch, n_nodes
+    nq, nk = N * B * cfg.n_q_heads * cfg.head_dim, N * B * cfg.n_kv_heads * cfg.head_dim
+    _need_state(cfg, cfg.format, K, k_scale, t, dev)
+    _need_state(cfg, cfg.format, V, v_scale, t, dev)
+    _need(q, nq, t, dev)
+    _need(k, nk, t, dev)
+    _need(v, nk, t, dev)
+    _need(out, nq, t, dev)
+    _need(parents, N * B, torch.int32, dev)
+    _need(lens, B, torch.int32, dev)
+    with _on(dev):
+        _check(lib().tova_tree_attention(_byref(cfg), _a(K), _a(V), _a(k_scale), _a(v_scale), _a(lens), n_live, _a(q),
+                                         _a(k), _a(v), N, _a(parents), _a(out), _a(workspace), _bytes(workspace),
+                                         _raw_stream(dev, stream)), "tova_tree_attention")
+
+
+def tova_verify_draft(cfg: tova_verify_config, target, draft, tokens, u, u_sample, n_accepted, path, tokens_out,
+                      parents=None, stream=None) -> None:
+    """Which drafted tokens [N,B] the target's probabilities [N+1,B,V] accept, given u [N,B] and u_sample [B]; see
+    include/tova.h.  draft: probabilities the children were drawn from, or None.  n_accepted [B], path [N,B] or None,
+    tokens_out [N+1,B], int32."""
+    t, dev, B, N = _TORCH_TYPE.get(cfg.dtype), target.device, cfg.batch, cfg.n_nodes
+    ld = cfg.row_stride or cfg.vocab
+    need = ((N + 1) * B - 1) * ld + cfg.vocab
+    _need(target, need, t, dev)
+    _need(draft, (max(N, 1) * B - 1) * ld + cfg.vocab if parents is None else need, t, dev)
+    _need(tokens, N * B, torch.int32, dev)
+    _need(parents, N * B, torch.int32, dev)
+    _need(u, N * B, torch.float32, dev)
+    _need(u_sample, B, torch.float32, dev)
+    _need(n_accepted, B, torch.int32, dev)
+    _need(path, N * B, torch.int32, dev)
+    _need(tokens_out, (N + 1) * B, torch.int32, dev)
+    with _on(dev):
+        _check(lib().tova_verify_draft(_byref(cfg), _a(target), _a(draft), _a(tokens), _a(parents), _a(u), _a(u_sample),
+                                       _a(n_accepted), _a(path), _a(tokens_out), _raw_stream(dev, stream)),
+               "tova_verify_draft")
 
 
 def to_device(x, dtype: int, device="cuda:0") -> torch.Tensor:

@@ -1474,6 +1474,45 @@ int tova_cache_read_scores(const tova_cache* c, float* scores, void* cuda_stream
                          static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? TOVA_OK : TOVA_ERR_CUDA;
 }
 
+namespace {
+tova_tree_config tree_config_of(const tova_cache& c) {
+  tova_tree_config t{};
+  t.batch = c.cfg.batch;
+  t.n_q_heads = c.cfg.n_q_heads;
+  t.n_kv_heads = c.cfg.n_kv_heads;
+  t.head_dim = c.cfg.head_dim;
+  t.capacity = c.cfg.capacity;
+  t.dtype = c.cfg.dtype;
+  t.format = TOVA_FORMAT_PLAIN;
+  t.sm_scale = c.cfg.sm_scale;
+  return t;
+}
+}  // namespace
+
+size_t tova_cache_tree_workspace_bytes(const tova_cache* c, int32_t n_nodes) {
+  if (!c) return (size_t)-1;
+  const tova_tree_config t = tree_config_of(*c);
+  // (enough for every length that the state goes through)
+  size_t most = 0;
+  for (int64_t n = 1; n < 2 * (int64_t)t.capacity; n *= 2) {
+    const size_t bytes = tova_tree_workspace_bytes(&t, (int32_t)std::min<int64_t>(n, t.capacity), n_nodes);
+    if (bytes == (size_t)-1) return bytes;
+    most = std::max(most, bytes);
+  }
+  return most;
+}
+
+int tova_cache_tree_attention(tova_cache* c, const void* q, const void* k, const void* v, int32_t n_nodes,
+                              const int32_t* parents, void* out, void* workspace, size_t workspace_bytes,
+                              void* cuda_stream) {
+  if (!c) return TOVA_ERR_NULL;
+  if (c->poscomp_ws) return TOVA_ERR_UNSUPPORTED;
+  if (tova_cache_join(c, cuda_stream) != TOVA_OK) return TOVA_ERR_CUDA;
+  const tova_tree_config t = tree_config_of(*c);
+  return tova_tree_attention(&t, c->base + c->lay.K, c->base + c->lay.V, nullptr, nullptr, nullptr, c->len, q, k, v, n_nodes,
+                             parents, out, workspace, workspace_bytes, cuda_stream);
+}
+
 int32_t tova_cache_units(const tova_cache* c) { return c ? (c->units > 0 ? c->units : 1) : -1; }
 
 int32_t tova_cache_len(const tova_cache* c) { return c ? c->len : -1; }

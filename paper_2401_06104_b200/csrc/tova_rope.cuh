@@ -1,0 +1,139 @@
+// Rotary position embedding of queries and keys (sm_100a): what turns a projection's q and k into the ones the decode
+// step takes ("callers pass post-RoPE q and k").
+//
+// Pair i of a head, i < rotary_dim / 2, at position p:  (a, b) -> m (a c - b s, b c + a s),  c = cos(p w_i),
+// s = sin(p w_i), with w_i the pair's frequency and m the factor on both (1 unless the scaling asks for another).  A
+// pair is (i, i + rotary_dim/2) in the half layout, (2i, 2i + 1) in the interleaved one; the components from
+// rotary_dim on pass through.  The inverse turns by -p w_i and keeps m: it is the transposed map, so it is also what
+// a gradient of the result goes through.
+//
+// The map reads and writes every component once and does three operations on it: DRAM bound.  A block takes a few
+// tokens; their cosines and sines are formed once - the angle as a fraction of a turn in 64 bits, since p w_i in 32
+// bits is off by whole degrees at far positions, then sincospi in 32 - and serve all H + Hkv heads from shared memory.
+#pragma once
+
+#include "tova_device.cuh"
+
+namespace tova {
+
+constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_MAX_PAIRS = 64;    // head_dim <= 128
+constexpr int ROPE_MAX_TOKENS = 4;    // tokens per block
+
+struct RopeParams {
+  const void* x[2];             // q, k: element strides between the rows of consecutive (token, sequence) pairs
+  void* y[2];
+  long long x_stride[2], y_stride[2];
+  int heads[2];                 // heads of q, of k (0: no k)
+  const int32_t* positions;     // [T,B] or NULL: first_pos + token
+  long long rows;               // T * B
+  int first_pos, B, D, rot, tokens_per_block;
+  float factor, sign;           // m; +1, or -1 for the inverse
+  double turns[ROPE_MAX_PAIRS]; // w_i / 2 pi
+};
+
+template <typename T>
+__device__ __forceinline__ uint4 rope_pack(const float (&f)[Vec16<T>::N]);
+template <>
+__device__ __forceinline__ uint4 rope_pack<float>(const float (&f)[4]) {
+  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+template <>
+__device__ __forceinline__ uint4 rope_pack<__nv_bfloat16>(const float (&f)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);   // the result's one rounding
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// VEC: units of 16 bytes (rotary_dim a multiple of 2 vectors in the half layout, of one in the interleaved one);
+// otherwise a unit is one pair, or one component of the rest.  grid = ceil(rows / tokens_per_block).
+template <typename T, bool HALF, bool VEC>
+__global__ void __launch_bounds__(ROPE_THREADS) tova_rope_kernel(const __grid_constant__ RopeParams p) {
+  constexpr int N = Vec16<T>::N;
+  __shared__ __align__(16) float cs[ROPE_MAX_TOKENS][ROPE_MAX_PAIRS], sn[ROPE_MAX_TOKENS][ROPE_MAX_PAIRS];
+  const long long row0 = (long long)blockIdx.x * p.tokens_per_block;
+  const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
+  const int half = p.rot >> 1;
+  for (int i = threadIdx.x; i < n_tok * half; i += ROPE_THREADS) {
+    const int t = i / half, j = i - t * half;
+    const long long row = row0 + t;
+    const double pos = p.positions ? (double)p.positions[row] : (double)p.first_pos + (double)(row / p.B);
+    double a = pos * p.turns[j];
+    a -= rint(a);
+    float s, c;
+    sincospif((float)(2.0 * a), &s, &c);
+    cs[t][j] = c * p.factor;
+    sn[t][j] = s * p.factor * p.sign;
+  }
+  __syncthreads();
+  const int turning = VEC ? (HALF ? half / N : p.rot / N) : half;       // units that turn, per head
+  const int passing = VEC ? (p.D - p.rot) / N : p.D - p.rot;            // units that pass through
+  const int per_head = turning + passing;
+  const int per_tok = (p.heads[0] + p.heads[1]) * per_head;
+  const int total = n_tok * per_tok;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < total; i += ROPE_THREADS) {
+    const int t = i / per_tok;
+    int rem = i - t * per_tok;
+    int h = rem / per_head;
+    const int u = rem - h * per_head;
+    const int which = h >= p.heads[0];
+    if (which) h -= p.heads[0];
+    const T* x = static_cast<const T*>(p.x[which]) + (row0 + t) * p.x_stride[which] + (long long)h * p.D;
+    T* y = static_cast<T*>(p.y[which]) + (row0 + t) * p.y_stride[which] + (long long)h * p.D;
+    if constexpr (VEC) {
+      if (u >= turning) {
+        const int d = p.rot + (u - turning) * N;
+        *reinterpret_cast<uint4*>(y + d) = *reinterpret_cast<const uint4*>(x + d);
+      } else if constexpr (HALF) {
+        const int d = u * N;
+        const uint4 wa = *reinterpret_cast<const uint4*>(x + d), wb = *reinterpret_cast<const uint4*>(x + half + d);
+        float a[N], b[N], ya[N], yb[N];
+        Vec16<T>::unpack(wa, a);
+        Vec16<T>::unpack(wb, b);
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+          const float4 c4 = *reinterpret_cast<const float4*>(&cs[t][d + e]);
+          const float4 s4 = *reinterpret_cast<const float4*>(&sn[t][d + e]);
+          const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            ya[e + k] = a[e + k] * c[k] - b[e + k] * s[k];
+            yb[e + k] = b[e + k] * c[k] + a[e + k] * s[k];
+          }
+        }
+        *reinterpret_cast<uint4*>(y + d) = rope_pack<T>(ya);
+        *reinterpret_cast<uint4*>(y + half + d) = rope_pack<T>(yb);
+      } else {
+        const int d = u * N;
+        const uint4 w = *reinterpret_cast<const uint4*>(x + d);
+        float a[N];
+        Vec16<T>::unpack(w, a);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          const float c = cs[t][(d + e) >> 1], s = sn[t][(d + e) >> 1];
+          const float lo = a[e] * c - a[e + 1] * s;
+          a[e + 1] = a[e + 1] * c + a[e] * s;
+          a[e] = lo;
+        }
+        *reinterpret_cast<uint4*>(y + d) = rope_pack<T>(a);
+      }
+    } else {
+      if (u >= turning) {
+        const int d = p.rot + u - turning;
+        y[d] = x[d];
+      } else {
+        const int da = HALF ? u : 2 * u, db = HALF ? u + half : 2 * u + 1;
+        const float a = (float)x[da], b = (float)x[db], c = cs[t][u], s = sn[t][u];
+        y[da] = (T)(a * c - b * s);
+        y[db] = (T)(b * c + a * s);
+      }
+    }
+  }
+}
+
+}  // namespace tova

@@ -1,0 +1,337 @@
+// Attention of drafted tokens over a state (sm_100a).
+//
+// N drafted tokens of a sequence (nodes) hang below its last settled token as a tree, parents[i] < i, -1 for the root.
+// A node sees the state's live rows, its ancestors and itself:
+//   o_i = sum_j p_ij v_j,  p_ij = softmax_j(scale q_i k_j)  over j in state rows + {i, parent(i), parent(parent(i)), ...}
+// A node whose parent is neither -1 nor an earlier node, and every node below it, is padding: it sees nothing, o = 0.
+// The state is only read.  N = 1 is a plain step without eviction.
+//
+// The rows of the product are the M = N G pairs (node, query head) that share a KV head; its columns the state's rows,
+// then the drafted tokens.  The state's bytes are what cannot be avoided, and M of these rows use each of them: few
+// rows leave the kernel waiting for memory, many for the contractions.  The columns are cut into `splits` runs so that
+// even one sequence gives every SM something to do; a run's (max, sum, weighted sum) go through the caller's
+// workspace and a second kernel joins them.  One run writes the result itself.
+#pragma once
+
+#include "tova_quant.cuh"
+
+namespace tova {
+
+constexpr int TREE_MAX_NODES = 256;
+constexpr int TREE_ANC_WORDS = TREE_MAX_NODES / 32;
+constexpr float TREE_PADDING = -1.f;     // the sum that stands for "a padding node" in a partial result
+
+struct TreeParams {
+  const void* q;               // [N,B,H,D]
+  const void* k_new;           // [N,B,Hkv,D]
+  const void* v_new;
+  const void* K;               // [B,Hkv,cap,D]
+  const void* V;
+  const float* k_scale;        // [B,Hkv,cap], 8-bit states
+  const float* v_scale;
+  const int32_t* lens;         // [B] or NULL: n_live rows in every sequence
+  const int32_t* parents;      // [N,B] or NULL: a chain
+  void* out;                   // [N,B,H,D]
+  float2* part_ml;             // [splits][B,Hkv,M] running max (base 2), sum
+  float* part_acc;             // [splits][B,Hkv,M][D]
+  int N, B, H, Hkv, G, M, cap, n_live;
+  int splits, split_cols;      // columns of a run (a multiple of the kernel's tile); the last run also has the drafts
+  float scale2;                // scale * log2(e)
+};
+
+__device__ __forceinline__ int tree_len(const TreeParams& p, int b) {
+  return p.lens ? max(0, min(p.lens[b], p.n_live)) : p.n_live;
+}
+
+// Ancestor bits of every node, one thread per node: anc[i][w] bit j says that node 32 w + j is i or above it.  All
+// zero for padding.  par_s holds the sequence's parents; the walk goes strictly down in index, so it ends.
+__device__ __forceinline__ void tree_ancestors(const TreeParams& p, int b, int* par_s, uint32_t (*anc)[TREE_ANC_WORDS],
+                                               int threads) {
+  for (int i = threadIdx.x; i < p.N; i += threads) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
+  __syncthreads();
+  const int words = (p.N + 31) >> 5;
+  for (int i = threadIdx.x; i < p.N; i += threads) {
+    uint32_t w[TREE_ANC_WORDS];
+#pragma unroll
+    for (int k = 0; k < TREE_ANC_WORDS; ++k) w[k] = 0;
+    int j = i;
+    bool real = true;
+    while (j >= 0) {
+#pragma unroll
+      for (int k = 0; k < TREE_ANC_WORDS; ++k) w[k] |= (j >> 5) == k ? 1u << (j & 31) : 0u;
+      const int up = par_s[j];
+      if (up < -1 || up >= j) { real = false; break; }
+      j = up;
+    }
+    for (int k = 0; k < words; ++k) anc[i][k] = 0;
+#pragma unroll
+    for (int k = 0; k < TREE_ANC_WORDS; ++k)
+      if (k < words) anc[i][k] = real ? w[k] : 0u;
+  }
+  __syncthreads();
+}
+
+// Four consecutive values (aligned to four) as floats.
+__device__ __forceinline__ float4 tree_load4(const float* x) { return *reinterpret_cast<const float4*>(x); }
+__device__ __forceinline__ float4 tree_load4(const __nv_bfloat16* x) {
+  const uint2 w = *reinterpret_cast<const uint2*>(x);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xffff0000u));
+}
+
+template <typename T>
+__device__ __forceinline__ void tree_store4(T* dst, float a, float b, float c, float d);
+template <>
+__device__ __forceinline__ void tree_store4<float>(float* dst, float a, float b, float c, float d) {
+  *reinterpret_cast<float4*>(dst) = make_float4(a, b, c, d);
+}
+template <>
+__device__ __forceinline__ void tree_store4<__nv_bfloat16>(__nv_bfloat16* dst, float a, float b, float c, float d) {
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(a, b), hi = __floats2bfloat162_rn(c, d);   // the result's one rounding
+  *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Plain-ALU kernel: every product in fp32.  Serves fp32 queries, whose results the tensor cores' bf16 operands could
+// not give.  A block takes 32 rows of the product and a run of columns in tiles of 32: logits with 2 x 4 outputs a
+// thread, the weighted sum with 8 rows x (D/32) columns a thread... both from shared memory in fp32.
+// grid = (ceil(M / 32), splits, B * Hkv).
+constexpr int TREE_ALU_THREADS = 128;
+constexpr int TREE_ALU_ROWS = 32;
+constexpr int TREE_ALU_COLS = 32;
+
+template <int D>
+inline size_t tree_alu_smem_bytes() {
+  return sizeof(float) * (2 * TREE_ALU_ROWS * (D + 4) + TREE_ALU_COLS * D + TREE_ALU_ROWS * (TREE_ALU_COLS + 4));
+}
+
+template <typename T, int D, int FMT>
+__global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const __grid_constant__ TreeParams p) {
+  constexpr int R = TREE_ALU_ROWS, C = TREE_ALU_COLS;
+  constexpr int LD = D + 4;                      // row stride of Q and K in shared memory: rows 4 banks apart
+  constexpr int LP = C + 4;
+  extern __shared__ __align__(16) float tree_alu_smem[];
+  float* q_s = tree_alu_smem;                    // [R][LD]
+  float* k_s = q_s + R * LD;                     // [C][LD]
+  float* v_s = k_s + C * LD;                     // [C][D]
+  float* p_s = v_s + C * D;                      // [R][LP]
+  __shared__ int par_s[TREE_MAX_NODES];
+  __shared__ uint32_t anc_s[TREE_MAX_NODES][TREE_ANC_WORDS];
+  __shared__ float m_s[R], corr_s[R];
+
+  const int tid = threadIdx.x;
+  const int b = blockIdx.z / p.Hkv, hk = blockIdx.z % p.Hkv;
+  const int split = blockIdx.y, row0 = blockIdx.x * R;
+  const int len = tree_len(p, b);
+  const bool last = split == p.splits - 1;
+  const int c0 = split * p.split_cols;
+  const int c1 = last ? len : min(len, c0 + p.split_cols);
+  const int n_state = c1 > c0 ? (c1 - c0 + C - 1) / C : 0;
+  const int n_draft = last ? (p.N + C - 1) / C : 0;
+
+  if (last) tree_ancestors(p, b, par_s, anc_s, TREE_ALU_THREADS);
+  // Q rows, scaled into the base-2 domain
+  for (int i = tid; i < R * (D / 4); i += TREE_ALU_THREADS) {
+    const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+    const int m = row0 + r;
+    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (m < p.M) {
+      const int n = m / p.G, g = m - n * p.G;
+      const T* src = static_cast<const T*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
+      w = tree_load4(src);
+    }
+    *reinterpret_cast<float4*>(q_s + r * LD + d) = make_float4(w.x * p.scale2, w.y * p.scale2, w.z * p.scale2, w.w * p.scale2);
+  }
+  // logits: thread -> rows 2 (tid / 8), +1; columns tid % 8 + 8 k.  Weighted sum: rows 8 (tid / 32) ..+7, D/32 columns.
+  const int lr = (tid >> 3) * 2, lc = tid & 7;
+  const int orow = (tid >> 5) * 8, oc = (tid & 31) * (D / 32);
+  float acc[8][D / 32];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) acc[i][j] = 0.f;
+  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+
+  for (int tile = 0; tile < n_state + n_draft; ++tile) {
+    const bool draft = tile >= n_state;
+    const int j0 = draft ? (tile - n_state) * C : c0 + tile * C;      // first column of the tile, in its own numbering
+    const int jn = draft ? p.N : c1;
+    __syncthreads();
+    for (int i = tid; i < C * (D / 4); i += TREE_ALU_THREADS) {
+      const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+      const int j = j0 + r;
+      float4 kf = make_float4(0.f, 0.f, 0.f, 0.f), vf = kf;
+      if (j < jn) {
+        if (draft || FMT == FORMAT_PLAIN) {
+          const long long at = draft ? (((long long)j * p.B + b) * p.Hkv + hk) * D + d
+                                     : ((long long)blockIdx.z * p.cap + j) * D + d;
+          const T* kp = static_cast<const T*>(draft ? p.k_new : p.K) + at;
+          const T* vp = static_cast<const T*>(draft ? p.v_new : p.V) + at;
+          kf = tree_load4(kp);
+          vf = tree_load4(vp);
+        } else if constexpr (FMT != FORMAT_PLAIN) {
+          const long long row = (long long)blockIdx.z * p.cap + j;
+          float a[4];
+          const float ks = p.k_scale[row], vs = p.v_scale[row];
+          quant_unpack4<FMT>(*reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.K) + row * D + d), a);
+          kf = make_float4(a[0] * ks, a[1] * ks, a[2] * ks, a[3] * ks);
+          quant_unpack4<FMT>(*reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.V) + row * D + d), a);
+          vf = make_float4(a[0] * vs, a[1] * vs, a[2] * vs, a[3] * vs);
+        }
+      }
+      *reinterpret_cast<float4*>(k_s + r * LD + d) = kf;
+      *reinterpret_cast<float4*>(v_s + r * D + d) = vf;
+    }
+    __syncthreads();
+    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+    for (int d = 0; d < D; d += 4) {
+      const float4 q0 = *reinterpret_cast<const float4*>(q_s + lr * LD + d);
+      const float4 q1 = *reinterpret_cast<const float4*>(q_s + (lr + 1) * LD + d);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float4 kk = *reinterpret_cast<const float4*>(k_s + (lc + 8 * k) * LD + d);
+        s[0][k] = fmaf(q0.x, kk.x, fmaf(q0.y, kk.y, fmaf(q0.z, kk.z, fmaf(q0.w, kk.w, s[0][k]))));
+        s[1][k] = fmaf(q1.x, kk.x, fmaf(q1.y, kk.y, fmaf(q1.z, kk.z, fmaf(q1.w, kk.w, s[1][k]))));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int m = row0 + lr + i;
+      const uint32_t see = draft ? (m < p.M ? anc_s[m / p.G][j0 >> 5] : 0u) : 0u;
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = lc + 8 * k;
+        const bool vis = draft ? ((see >> c) & 1u) != 0 : j0 + c < jn;
+        if (!vis) s[i][k] = -INFINITY;
+        top = fmaxf(top, s[i][k]);
+      }
+#pragma unroll
+      for (int o = 4; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float m_new = fmaxf(m_run[i], top);
+      const float base = m_new == -INFINITY ? 0.f : m_new;
+      const float corr = exp2f(m_run[i] - base);       // 0 while nothing has been seen
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float e = exp2f(s[i][k] - base);
+        sum += e;
+        p_s[(lr + i) * LP + lc + 8 * k] = e;
+      }
+#pragma unroll
+      for (int o = 4; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l_run[i] = l_run[i] * corr + sum;
+      m_run[i] = m_new;
+      if (lc == 0) corr_s[lr + i] = corr;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float corr = corr_s[orow + i];
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) acc[i][j] *= corr;
+    }
+    if (!draft) {
+#pragma unroll 4
+      for (int c = 0; c < C; ++c) {
+        float v[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) v[j] = v_s[c * D + oc + j];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float w = p_s[(orow + i) * LP + c];
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) acc[i][j] = fmaf(w, v[j], acc[i][j]);
+        }
+      }
+    } else {
+      // Drafts that a row does not see may hold anything: 0 times an infinity must not reach the sum.
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float w = p_s[(orow + i) * LP + c];
+          if (w != 0.f) {
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) acc[i][j] = fmaf(w, v_s[c * D + oc + j], acc[i][j]);
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (lc == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int m = row0 + lr + i;
+      float l = l_run[i];
+      if (last && m < p.M) {
+        const int n = m / p.G;
+        if (((anc_s[n][n >> 5] >> (n & 31)) & 1u) == 0) l = TREE_PADDING;
+      }
+      m_s[lr + i] = m_run[i];
+      corr_s[lr + i] = l;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int m = row0 + orow + i;
+    if (m >= p.M) continue;
+    const float l = corr_s[orow + i];
+    if (p.splits == 1) {
+      const float r = l == 0.f ? 0.f : 1.f / l;
+      const int n = m / p.G, g = m - n * p.G;
+      T* dst = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + oc;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) dst[j] = (T)(l == TREE_PADDING ? 0.f : acc[i][j] * r);
+    } else {
+      const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
+      if ((tid & 31) == 0) p.part_ml[at] = make_float2(m_s[orow + i], l);
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) p.part_acc[at * D + oc + j] = acc[i][j];
+    }
+  }
+}
+
+// Joins the runs' partial results: o = sum_s 2^(m_s - m) acc_s / sum_s 2^(m_s - m) l_s.  One warp per row of the
+// product; grid = ceil(B Hkv M / 8), 256 threads.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) tova_tree_merge_kernel(const __grid_constant__ TreeParams p) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long rows = (long long)p.B * p.Hkv * p.M;
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  float m = -INFINITY;
+  bool pad = false;
+  for (int s = lane; s < p.splits; s += 32) {
+    const float2 ml = p.part_ml[s * rows + row];
+    m = fmaxf(m, ml.x);
+    if (s == p.splits - 1) pad = ml.y == TREE_PADDING;
+  }
+  m = warp_max(m);
+  pad = __any_sync(0xffffffffu, pad) != 0;
+  const float base = m == -INFINITY ? 0.f : m;
+  constexpr int E = D / 32;
+  float acc[E], l = 0.f;
+#pragma unroll
+  for (int j = 0; j < E; ++j) acc[j] = 0.f;
+  for (int s = 0; s < p.splits; ++s) {
+    const float2 ml = p.part_ml[s * rows + row];
+    if (ml.x == -INFINITY) continue;                 // a run without a visible column
+    const float w = exp2f(ml.x - base);
+    l += w * ml.y;
+    const float* a = p.part_acc + (s * rows + row) * D + lane * E;
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] = fmaf(w, a[j], acc[j]);
+  }
+  const int bh = (int)(row / p.M), mm = (int)(row - (long long)bh * p.M);
+  const int b = bh / p.Hkv, hk = bh - b * p.Hkv, n = mm / p.G, g = mm - n * p.G;
+  T* dst = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + lane * E;
+  const float r = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int j = 0; j < E; ++j) dst[j] = (T)(pad ? 0.f : acc[j] * r);
+}
+
+}  // namespace tova

@@ -1,0 +1,264 @@
+// Verification of drafted tokens against the target's probabilities, from given random numbers (sm_100a).
+//
+// A sequence's drafted tokens form a tree (a chain is one): node i carries token x_i and hangs below node parents[i],
+// or below the last settled token (the root).  Row 0 of the target's probabilities p is the distribution after the
+// root, row 1 + i the one after node i; row r of the draft's probabilities q is the distribution that the children of
+// that node were drawn from.  The walk starts at the root.  At a node with target p and draft q its children are
+// tried in index order:
+//   r_0 = p, Z_0 = 1;   child with token x is accepted when   u Z_j q(x) < r_j(x);
+//   rejected:           r_{j+1} = max(0, r_j - Z_j q),  Z_{j+1} = sum of r_{j+1}
+// and the walk goes on at the accepted child.  Where no child is accepted the last token is drawn from r (from p where
+// r is zero everywhere), by the smallest x whose running sum exceeds u_sample times the whole.  The tokens are then
+// distributed as if they had been drawn from p one by one, provided each child was drawn from q.  Unnormalised
+// residuals nest: r_j = max(0, p - S_j q) with S_j = Z_0 + ... + Z_{j-1}, so the kernel keeps the scalar S and never
+// stores a residual.  Without q the drafts are taken as certain (q = 1 at the child's own token): r_{j+1} is r_j with
+// x struck out, Z_{j+1} = Z_j - r_j(x), and no row is read before the last token is drawn.
+//
+// Every comparison and sum is in 64 bits (u q is exact there), so that the decisions do not depend on the order of
+// the sums.  What has to be read is a few scalars along the walk and the rows where a rejection meets another child
+// or the walk ends: the time is the latency of a chain of small steps.  One cluster of blocks per sequence: the
+// scalars of all nodes are fetched at once at the start, every block walks the same path, and the blocks share out
+// the vocabulary where a row has to be summed; partial sums travel through distributed shared memory.
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "tova_device.cuh"
+
+namespace tova {
+
+constexpr int VERIFY_THREADS = 512;
+constexpr int VERIFY_WARPS = VERIFY_THREADS / 32;
+constexpr int VERIFY_CLUSTER = 8;
+constexpr int VERIFY_MAX_NODES = 1024;
+
+struct VerifyParams {
+  const void* target;         // [N+1,B,row_stride] probabilities
+  const void* draft;          // the same layout, or NULL
+  const int32_t* tokens;      // [N,B]
+  const int32_t* parents;     // [N,B] or NULL: a chain
+  const float* u;             // [N,B]
+  const float* u_sample;      // [B]
+  int32_t* n_accepted;        // [B]
+  int32_t* path;              // [N,B] or NULL
+  int32_t* tokens_out;        // [N+1,B]
+  long long row_stride;
+  int B, N, V;
+};
+
+// Dynamic shared memory: per node p(x), q(x), u (floats), token, parent.
+inline size_t verify_smem_bytes(int N) { return (size_t)N * 20; }
+
+template <typename T>
+__device__ __forceinline__ float verify_load(const void* p, long long i) {
+  return (float)static_cast<const T*>(p)[i];
+}
+
+// The weight that the last token is drawn with, or a term of Z: max(0, p - S q); NaN counts as zero.
+__device__ __forceinline__ double verify_weight(float p, float q, double S) {
+  const double w = (double)p - S * (double)q;
+  return w > 0.0 ? w : 0.0;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __grid_constant__ VerifyParams p) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  extern __shared__ __align__(16) unsigned char verify_smem[];
+  float* px_s = reinterpret_cast<float*>(verify_smem);
+  float* qx_s = px_s + p.N;
+  float* u_s = qx_s + p.N;
+  int* tok_s = reinterpret_cast<int*>(u_s + p.N);
+  int* par_s = tok_s + p.N;
+  __shared__ double inbox[2][VERIFY_CLUSTER];     // partial sums of the cluster's blocks, double-buffered
+  __shared__ double warp_part[VERIFY_WARPS];
+  __shared__ int cmd_s, row_s, node_s, count_s, last_child_s;
+  __shared__ double S_s;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = blockIdx.y;
+  const int rank = (int)cluster.block_rank(), nc = (int)cluster.num_blocks();
+  const int N = p.N, V = p.V;
+
+  for (int i = tid; i < N; i += VERIFY_THREADS) {
+    const long long at = (long long)i * p.B + b;
+    int par = p.parents ? p.parents[at] : i - 1;
+    if (par < -1 || par >= i) par = -2;                       // padding: never reached
+    const int tok = p.tokens[at];
+    const bool ok = par >= -1 && (unsigned)tok < (unsigned)V;
+    const long long row = ((long long)(par + 1) * p.B + b) * p.row_stride;
+    par_s[i] = par;
+    tok_s[i] = tok;
+    u_s[i] = p.u[at];
+    px_s[i] = ok ? verify_load<T>(p.target, row + tok) : 0.f;   // a token outside the vocabulary is never accepted
+    qx_s[i] = ok ? (p.draft ? verify_load<T>(p.draft, row + tok) : 1.f) : 0.f;
+  }
+  if (tid == 0) { row_s = 0; node_s = -1; count_s = 0; last_child_s = -1; S_s = 0.0; cmd_s = 0; }
+  cluster.sync();     // every block of the cluster runs before any writes into another's inbox
+
+  // This block's share of the vocabulary, and every warp's share of that: contiguous, in order.
+  const int per_block = ((V + nc - 1) / nc + 7) / 8 * 8;
+  const int v0 = min(V, rank * per_block), v1 = min(V, v0 + per_block);
+  const int per_warp = ((v1 - v0 + VERIFY_WARPS - 1) / VERIFY_WARPS + 31) / 32 * 32;
+  const int w0 = min(v1, v0 + warp * per_warp), w1 = min(v1, w0 + per_warp);
+
+  int turn = 0;                       // exchanges so far
+  // The sum over the cluster of one value per thread, in a fixed order; the block's prefix before this warp and the
+  // cluster's before this block come with it.
+  auto cluster_sum = [&](double x, double& before_block, double& before_warp) -> double {
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (lane == 0) warp_part[warp] = x;
+    __syncthreads();
+    double block = 0.0;
+    before_warp = 0.0;
+    for (int i = 0; i < VERIFY_WARPS; ++i) {
+      if (i == warp) before_warp = block;
+      block += warp_part[i];
+    }
+    if (tid < nc) *cluster.map_shared_rank(&inbox[turn & 1][rank], tid) = block;
+    cluster.sync();
+    double all = 0.0;
+    before_block = 0.0;
+    for (int i = 0; i < nc; ++i) {
+      if (i == rank) before_block = all;
+      all += inbox[turn & 1][i];
+    }
+    ++turn;
+    return all;
+  };
+
+  double Z = 1.0;
+  for (;;) {
+    // Warp 0 walks until a row's sum is needed (cmd 1) or the walk ends (cmd 2); every block does the same steps.
+    if (warp == 0) {
+      int node = node_s, count = count_s, from = last_child_s + 1;
+      double S = S_s;
+      int cmd = 0;
+      if (from < node + 1) from = node + 1;     // children come after their parent
+      auto next_child = [&](int start) {
+        for (int i0 = start; i0 < N; i0 += 32) {
+          const int i = i0 + lane;
+          const unsigned m = __ballot_sync(0xffffffffu, i < N && par_s[i] == node);
+          if (m) return i0 + __ffs(m) - 1;
+        }
+        return -1;
+      };
+      int c = next_child(from);
+      while (cmd == 0) {
+        if (c < 0) { cmd = 2; break; }
+        const double pr = (double)px_s[c], qr = (double)qx_s[c];
+        double r;
+        if (p.draft) {
+          r = verify_weight(px_s[c], qx_s[c], S);
+        } else {                                 // struck out if an earlier child carried the same token
+          bool again = false;
+          for (int i = node + 1 + lane; i < c; i += 32) again |= par_s[i] == node && tok_s[i] == tok_s[c];
+          r = __any_sync(0xffffffffu, again) ? 0.0 : (pr > 0.0 ? pr : 0.0);
+        }
+        if ((double)u_s[c] * qr * Z < r) {
+          if (rank == 0 && lane == 0) {
+            if (p.path) p.path[(long long)count * p.B + b] = c;
+            p.tokens_out[(long long)count * p.B + b] = tok_s[c];
+          }
+          ++count;
+          node = c;
+          S = 0.0;
+          Z = 1.0;
+          c = next_child(c + 1);
+          continue;
+        }
+        const int more = next_child(c + 1);
+        if (p.draft) {
+          S += Z;
+          if (more >= 0) cmd = 1;
+          from = c;                              // the child just rejected
+        } else {
+          Z -= r;
+        }
+        if (cmd == 0) c = more;
+      }
+      __syncwarp();
+      if (lane == 0) { cmd_s = cmd; node_s = node; count_s = count; last_child_s = from; S_s = S; }
+    }
+    __syncthreads();
+    if (cmd_s == 2) break;
+    const long long row = ((long long)(node_s + 1) * p.B + b) * p.row_stride;
+    const double S = S_s;
+    double sum = 0.0, bb, bw;
+    for (int i = w0 + lane; i < w1; i += 32)
+      sum += verify_weight(verify_load<T>(p.target, row + i), verify_load<T>(p.draft, row + i), S);
+    Z = cluster_sum(sum, bb, bw);
+    __syncthreads();
+  }
+
+  // The last token.
+  const int node = node_s, count = count_s;
+  const double S = S_s;
+  const long long row = ((long long)(node + 1) * p.B + b) * p.row_stride;
+  auto struck = [&](int x) {     // without q: tokens of the node's children, all rejected
+    for (int i = node + 1; i < N; ++i)
+      if (par_s[i] == node && tok_s[i] == x) return true;
+    return false;
+  };
+  bool plain = false;            // r was zero everywhere: drawn from p
+  double before_block = 0.0, before_warp = 0.0, all = 0.0, mine = 0.0;
+  auto weight = [&](int i) -> double {
+    const float pr = verify_load<T>(p.target, row + i);
+    if (plain) return pr > 0.f ? (double)pr : 0.0;
+    if (p.draft) return S > 0.0 ? verify_weight(pr, verify_load<T>(p.draft, row + i), S) : (pr > 0.f ? (double)pr : 0.0);
+    return pr > 0.f && !struck(i) ? (double)pr : 0.0;
+  };
+  for (int attempt = 0; attempt < 2; ++attempt) {
+    double sum = 0.0;
+    for (int i = w0 + lane; i < w1; i += 32) sum += weight(i);
+    mine = sum;
+    all = cluster_sum(sum, before_block, before_warp);
+    if (all > 0.0 || plain) break;
+    __syncthreads();
+    plain = true;
+  }
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  // The warp whose stretch of the running sum holds the target: at or before it below or equal, after it above.  The
+  // prefixes are added up the same way in every warp, so exactly one warp finds it (the target lies below the whole).
+  float us = p.u_sample[b];
+  us = us >= 0.f ? fminf(us, 0x1.fffffep-1f) : 0.f;
+  const double goal = (double)us * all;
+  const double lo = before_block + before_warp, hi = before_block + (before_warp + mine);
+  int found = -1;
+  if (mine > 0.0 && lo <= goal && goal < hi) {
+    double run = lo;
+    int last_some = -1;
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+      const int i = i0 + lane;
+      const double w = i < w1 ? weight(i) : 0.0;
+      double inc = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      const unsigned m = __ballot_sync(0xffffffffu, w > 0.0 && run + inc > goal);
+      if (m) { found = i0 + __ffs(m) - 1; break; }
+      const unsigned some = __ballot_sync(0xffffffffu, w > 0.0);
+      if (some) last_some = i0 + 31 - __clz(some);
+      run += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (found < 0) found = last_some;     // the stretch's sum in another order fell short of the goal
+    if (lane == 0) p.tokens_out[(long long)count * p.B + b] = found;
+  }
+  if (rank == 0) {
+    if (tid == 0) {
+      p.n_accepted[b] = count;
+      if (!(all > 0.0)) p.tokens_out[(long long)count * p.B + b] = -1;    // no probability anywhere
+    }
+    for (int i = count + tid; i < N; i += VERIFY_THREADS) {
+      if (p.path) p.path[(long long)i * p.B + b] = -1;
+      p.tokens_out[(long long)(i + 1) * p.B + b] = -1;
+    }
+  }
+  cluster.sync();     // no block leaves while another may still write into its inbox
+}
+
+}  // namespace tova
