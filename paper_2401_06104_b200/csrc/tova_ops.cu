@@ -7,10 +7,12 @@
 #include <atomic>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "tova_quant.cuh"
 #include "tova_rope.cuh"
 #include "tova_tree.cuh"
+#include "tova_tree_mma.cuh"
 #include "tova_verify.cuh"
 
 namespace {
@@ -290,20 +292,30 @@ int tree_check(const tova_tree_config* c, int32_t n_live, int32_t n_nodes) {
   return TOVA_OK;
 }
 
+// Which kernel serves a call and how its columns are cut.
+enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64 };
 struct TreePlan {
-  int row_blocks, splits, split_cols;
+  int kernel, row_blocks, splits, split_cols;
   size_t ml_bytes, bytes;
 };
 
 TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count) {
   TreePlan t{};
   const int M = n_nodes * (c.n_q_heads / c.n_kv_heads);
-  const int rows = tova::TREE_ALU_ROWS, cols = tova::TREE_ALU_COLS;
+  int rows = tova::TREE_ALU_ROWS, cols = tova::TREE_ALU_COLS;
+  if (c.dtype == TOVA_DTYPE_BF16) {
+    t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : TREE_MMA_64;
+    rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    cols = tova::TREE_MMA_COLS;
+  }
   t.row_blocks = (M + rows - 1) / rows;
   const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;
   const int tiles = std::max(1, (n_live + cols - 1) / cols);
+  // Enough runs for two rounds of resident blocks (two per SM), but no run shorter than two tiles unless the GPU would
+  // stay half empty.
   long long want = (4LL * sm_count + whole - 1) / whole;
-  want = std::max(1LL, std::min<long long>(want, (tiles + 3) / 4));
+  const int shortest = whole * (tiles / 2) >= sm_count ? 2 : 1;
+  want = std::max(1LL, std::min<long long>(want, tiles / shortest));
   const int per = (int)((tiles + want - 1) / want);
   t.split_cols = per * cols;
   t.splits = (tiles + per - 1) / per;
@@ -315,24 +327,56 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
   return t;
 }
 
-template <typename T, int D, int FMT>
-cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
-  static std::atomic<bool> configured[64];
+template <typename Kernel>
+cudaError_t tree_start(Kernel kern, std::atomic<bool>* configured, size_t smem, int threads, const tova::TreeParams& p,
+                       const TreePlan& t, cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  const size_t smem = tova::tree_alu_smem_bytes<D>();
   if (!configured[dev & 63]) {
-    e = cudaFuncSetAttribute(tova::tova_tree_alu_kernel<T, D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
     if (e != cudaSuccess) return e;
     configured[dev & 63] = true;
   }
-  const dim3 grid((unsigned)t.row_blocks, (unsigned)t.splits, (unsigned)(p.B * p.Hkv));
-  tova::tova_tree_alu_kernel<T, D, FMT><<<grid, tova::TREE_ALU_THREADS, smem, st>>>(p);
-  if ((e = cudaGetLastError()) != cudaSuccess || t.splits == 1) return e;
-  const long long rows = (long long)p.B * p.Hkv * p.M;
-  tova::tova_tree_merge_kernel<T, D><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(p);
+  kern<<<dim3((unsigned)t.row_blocks, (unsigned)t.splits, (unsigned)(p.B * p.Hkv)), threads, smem, st>>>(p);
   return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t tree_merge(const tova::TreeParams& p, cudaStream_t st) {
+  const long long rows = (long long)p.B * p.Hkv * p.M;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3((unsigned)((rows + 7) / 8));
+  lc.blockDim = dim3(256);
+  lc.stream = st;
+  cudaLaunchAttribute at[1];      // its blocks may come up while the first kernel's last ones still run
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  return cudaLaunchKernelEx(&lc, tova::tova_tree_merge_kernel<T, D>, p);
+}
+
+template <int D, int FMT, int MT, int WR>
+cudaError_t tree_start_mma(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
+  static std::atomic<bool> configured[64];
+  return tree_start(tova::tova_tree_mma_kernel<D, FMT, MT, WR>, configured, tova::TreeMmaShape<D, FMT, MT, WR>::SMEM,
+                    tova::TREE_MMA_THREADS, p, t, st);
+}
+
+template <typename T, int D, int FMT>
+cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
+  cudaError_t e;
+  if constexpr (std::is_same<T, float>::value) {
+    static std::atomic<bool> configured[64];
+    e = tree_start(tova::tova_tree_alu_kernel<T, D, FMT>, configured, tova::tree_alu_smem_bytes<D>(), tova::TREE_ALU_THREADS, p, t, st);
+  } else {
+    e = t.kernel == TREE_MMA_16 ? tree_start_mma<D, FMT, 1, 1>(p, t, st)
+        : t.kernel == TREE_MMA_32 ? tree_start_mma<D, FMT, 1, 2>(p, t, st) : tree_start_mma<D, FMT, 2, 2>(p, t, st);
+  }
+  if (e != cudaSuccess || t.splits == 1) return e;
+  return tree_merge<T, D>(p, st);
 }
 template <typename T, int D>
 cudaError_t tree_launch_f(int format, const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {

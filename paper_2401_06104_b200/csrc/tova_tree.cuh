@@ -43,14 +43,11 @@ __device__ __forceinline__ int tree_len(const TreeParams& p, int b) {
   return p.lens ? max(0, min(p.lens[b], p.n_live)) : p.n_live;
 }
 
-// Ancestor bits of every node, one thread per node: anc[i][w] bit j says that node 32 w + j is i or above it.  All
-// zero for padding.  par_s holds the sequence's parents; the walk goes strictly down in index, so it ends.
-__device__ __forceinline__ void tree_ancestors(const TreeParams& p, int b, int* par_s, uint32_t (*anc)[TREE_ANC_WORDS],
-                                               int threads) {
-  for (int i = threadIdx.x; i < p.N; i += threads) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
-  __syncthreads();
-  const int words = (p.N + 31) >> 5;
-  for (int i = threadIdx.x; i < p.N; i += threads) {
+// Ancestor bits of nodes n0..n1-1, one thread per node: bit j of word w of anc[(i - n0) * TREE_ANC_WORDS ..] says that
+// node 32 w + j is i or above it.  All zero for padding.  par_s holds the sequence's parents; the walk goes strictly down
+// in index, so it ends.  (The caller has made par_s visible; the results are visible after the barrier here.)
+__device__ __forceinline__ void tree_ancestor_bits(int N, int n0, int n1, const int* par_s, uint32_t* anc, int tid, int threads) {
+  for (int i = n0 + tid; i < n1; i += threads) {
     uint32_t w[TREE_ANC_WORDS];
 #pragma unroll
     for (int k = 0; k < TREE_ANC_WORDS; ++k) w[k] = 0;
@@ -63,12 +60,29 @@ __device__ __forceinline__ void tree_ancestors(const TreeParams& p, int b, int* 
       if (up < -1 || up >= j) { real = false; break; }
       j = up;
     }
-    for (int k = 0; k < words; ++k) anc[i][k] = 0;
 #pragma unroll
-    for (int k = 0; k < TREE_ANC_WORDS; ++k)
-      if (k < words) anc[i][k] = real ? w[k] : 0u;
+    for (int k = 0; k < TREE_ANC_WORDS; ++k) anc[(i - n0) * TREE_ANC_WORDS + k] = real ? w[k] : 0u;
   }
   __syncthreads();
+}
+__device__ __forceinline__ void tree_ancestors(const TreeParams& p, int b, int* par_s, uint32_t (*anc)[TREE_ANC_WORDS],
+                                               int threads) {
+  for (int i = threadIdx.x; i < p.N; i += threads) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
+  __syncthreads();
+  tree_ancestor_bits(p.N, 0, p.N, par_s, &anc[0][0], threadIdx.x, threads);
+}
+
+// Zeroes the infinities and NaN among eight bf16 values; true if there were any.
+__device__ __forceinline__ bool tree_drop_odd(uint4& w) {
+  uint32_t* x = reinterpret_cast<uint32_t*>(&w);
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (x[i] & 0x00007f80u) == 0x00007f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
+    odd |= lo | hi;
+    x[i] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+  }
+  return odd;
 }
 
 // Four consecutive values (aligned to four) as floats.

@@ -1,0 +1,580 @@
+// Attention of drafted tokens over a state on warp-level matrix instructions (see tova_tree.cuh for the operation):
+// bf16 queries, up to 64 rows of the product per block, states in bf16, int8 or e4m3.
+//
+// With few rows the kernel's only hard limit is the state's bytes, so everything else hides behind their copies: a
+// block of four warps runs down its columns in tiles of 64, copied ahead (cp.async, several stages) into swizzled
+// shared memory.  WR groups of warps share out the rows, the 4 / WR warps of a group the tile's columns; every warp
+// keeps a running maximum, sum and O of its own over the columns it has seen, and the warps are joined once, at the
+// end, through shared memory.  O is rescaled only when some row's maximum moved.
+//
+// 8-bit states are converted on the way from shared memory to the matrix instructions' operands, each code once per
+// row group: int8 by pasting its 7 low bits and its sign bit behind the exponent of 128 (two bf16 numbers whose
+// difference is the code), e4m3 by shifting exponent and mantissa into bf16's and multiplying by 2^120; both exact.
+// The row's scale goes onto the logit and onto the weight, never onto a converted operand.  So that a thread's operand
+// elements are neighbouring bytes, the order of the contraction index (over D for the logits) and of O's columns is a
+// permutation of the natural one - the sums do not care, the operands of the other side follow it.
+#pragma once
+
+#include "tova_mma.cuh"
+#include "tova_tc.cuh"     // ex2_approx
+#include "tova_tree.cuh"
+
+namespace tova {
+
+constexpr int TREE_MMA_THREADS = 128;
+constexpr int TREE_MMA_COLS = 64;      // columns of a tile
+
+template <int D, int FMT, int MT, int WR>
+struct TreeMmaShape {
+  static constexpr int WK = 4 / WR;                     // warps that share out a tile's columns
+  static constexpr int KS = TREE_MMA_COLS / WK;         // columns of a warp
+  static constexpr int NB = KS / 8;
+  static constexpr int ROWS = 16 * MT * WR;             // rows of the product per block
+  static constexpr int ROW_BYTES = D * (FMT == FORMAT_PLAIN ? 2 : 1);
+  static constexpr int TILE = TREE_MMA_COLS * ROW_BYTES;
+  static constexpr int STAGE = 2 * TILE + (FMT == FORMAT_PLAIN ? 0 : 2 * TREE_MMA_COLS * 4);
+  // 48 to 100 KiB in flight per block, two blocks per SM: about twice what the memory's latency asks for
+  static constexpr int STAGES = FMT == FORMAT_PLAIN ? 3 : (D == 128 ? 5 : 8);
+  static constexpr int Q_BYTES = ROWS * D * 2;
+  static constexpr int SMEM = STAGES * STAGE + Q_BYTES;
+  static constexpr int DRAFT_TILE = TREE_MMA_COLS * D * 2;
+  // the ring's room is taken over by the drafts (two tiles, parents, ancestor bits), then by the joining of the warps
+  static_assert(2 * DRAFT_TILE + TREE_MAX_NODES * 4 + ROWS * TREE_ANC_WORDS * 4 + 16 <= STAGES * STAGE, "drafts fit the ring");
+  static_assert(WK * ROWS * (D * 4 + 8) <= STAGES * STAGE, "partial results fit the ring");
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Bytes ia and ib of the eight bytes (a, b) as two bf16 numbers, ia in the low half.
+template <int FMT>
+__device__ __forceinline__ uint32_t tree_codes2(uint32_t a, uint32_t b, int ia, int ib) {
+  if constexpr (FMT == FORMAT_INT8) {
+    const uint32_t x = __byte_perm(a, b, (uint32_t)(ia | (ib << 8)));            // code in the low byte of each half
+    const uint32_t lo = (x & 0x007f007fu) | 0x43004300u;                         // 128 + low seven bits
+    const uint32_t hi = (x & 0x00800080u) | 0x43004300u;                         // 128, or 256 for a negative code
+    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&lo), *reinterpret_cast<const __nv_bfloat162*>(&hi));
+    return *reinterpret_cast<const uint32_t*>(&d);
+  } else {
+    const uint32_t x = __byte_perm(a, b, (uint32_t)((ia << 4) | (ib << 12)));    // code in the high byte of each half
+    const uint32_t w = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u);
+    const uint32_t up = 0x7b807b80u;                                             // 2^120: from exponent bias 7 to 127
+    const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&up));
+    return *reinterpret_cast<const uint32_t*>(&d);
+  }
+}
+
+// Byte offset of 16-byte chunk `ch` of row `row` in a tile.  bf16 rows: the low three chunk bits turn with the row, so
+// that eight rows' chunks (one ldmatrix) fall into different banks.  8-bit rows: both readers below - eight lanes on two
+// neighbouring rows x four chunks, or on four rows two apart x two chunks - find eight different chunks of a 128-byte line.
+template <int ROW_BYTES>
+__device__ __forceinline__ uint32_t tree_off16(int row, int ch) {
+  return (uint32_t)(row * ROW_BYTES + ((ch ^ (row & 7)) << 4));
+}
+template <int D>
+__device__ __forceinline__ uint32_t tree_off8(int row, int ch) {
+  if constexpr (D == 128) return (uint32_t)(row * 128 + ((ch ^ (((row >> 1) & 3) << 1) ^ ((row & 1) << 2)) << 4));
+  else return (uint32_t)((row >> 1) * 128 + (((((row & 1) << 2) | ch) ^ (((row >> 1) & 3) << 1)) << 4));
+}
+
+template <int D, int FMT, int MT, int WR>
+__global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(const __grid_constant__ TreeParams p) {
+  using S = TreeMmaShape<D, FMT, MT, WR>;
+  constexpr int C = TREE_MMA_COLS, KS = S::KS, NB = S::NB, OB = D / 8;
+  constexpr bool PLAIN = FMT == FORMAT_PLAIN;
+  extern __shared__ __align__(128) unsigned char tree_smem[];
+  unsigned char* ring = tree_smem;
+  uint4* q_s = reinterpret_cast<uint4*>(tree_smem + S::STAGES * S::STAGE);    // operand order: [row tile][step][lane]
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int wr = warp / S::WK, wk = warp % S::WK;
+  const int lr = lane >> 2, lc = lane & 3;
+  const int b = blockIdx.z / p.Hkv, hk = blockIdx.z % p.Hkv;
+  const int split = blockIdx.y, row0 = blockIdx.x * S::ROWS;
+  const int len = tree_len(p, b);
+  const bool last = split == p.splits - 1;
+  const int c0 = split * p.split_cols;
+  const int c1 = last ? len : min(len, c0 + p.split_cols);
+  const int n_tiles = c1 > c0 ? (c1 - c0 + C - 1) / C : 0;
+  const uint32_t ring_a = smem_addr(ring);
+
+  const unsigned char* Kg = static_cast<const unsigned char*>(p.K) + (long long)blockIdx.z * p.cap * S::ROW_BYTES;
+  const unsigned char* Vg = static_cast<const unsigned char*>(p.V) + (long long)blockIdx.z * p.cap * S::ROW_BYTES;
+  const float* ksg = PLAIN ? nullptr : p.k_scale + (long long)blockIdx.z * p.cap;
+  const float* vsg = PLAIN ? nullptr : p.v_scale + (long long)blockIdx.z * p.cap;
+
+  auto load_tile = [&](int i) {
+    const int j0 = c0 + i * C;
+    const uint32_t st = ring_a + (i % S::STAGES) * S::STAGE;
+    constexpr int CH = S::ROW_BYTES / 16;
+#pragma unroll
+    for (int x = 0; x < C * CH / TREE_MMA_THREADS; ++x) {
+      const int e = x * TREE_MMA_THREADS + tid;
+      const int row = e / CH, ch = e % CH;
+      const bool in = j0 + row < c1;                       // columns behind the run are zeros, whatever lies there
+      const long long at = (long long)(in ? j0 + row : c0) * S::ROW_BYTES + ch * 16;
+      const uint32_t off = PLAIN ? tree_off16<S::ROW_BYTES>(row, ch) : tree_off8<D>(row, ch);
+      cp_async16(st + off, Kg + at, in ? 16u : 0u);
+      cp_async16(st + S::TILE + off, Vg + at, in ? 16u : 0u);
+    }
+    if constexpr (!PLAIN) {
+      const int row = tid & 63;
+      const bool in = j0 + row < c1;
+      cp_async4(st + 2 * S::TILE + tid * 4, (tid < 64 ? ksg : vsg) + (in ? j0 + row : c0), in ? 4u : 0u);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < S::STAGES - 1; ++i) {
+    if (i < n_tiles) load_tile(i);
+    cp_async_commit();
+  }
+
+  // Q in operand order.  Step ks of the contraction: natural order (bf16 states) k = 16 ks + 2 lc + {0,1}, + 8; permuted
+  // (8-bit states), with ks = 4 i + w: d = 64 i + 16 lc + 4 w + {0,1}, {2,3}.
+  for (int e = tid; e < (S::ROWS / 16) * (D / 16) * 32; e += TREE_MMA_THREADS) {
+    const int l = e & 31, ks = (e >> 5) % (D / 16), rt = (e >> 5) / (D / 16);
+    const int r = l >> 2, c = l & 3;
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int m = row0 + rt * 16 + r + 8 * h;
+      if (m < p.M) {
+        const int n = m / p.G, g = m - n * p.G;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D;
+        const int d = PLAIN ? 16 * ks + 2 * c : 64 * (ks >> 2) + 16 * c + 4 * (ks & 3);
+        w[h] = *reinterpret_cast<const uint32_t*>(src + d);
+        w[2 + h] = *reinterpret_cast<const uint32_t*>(src + d + (PLAIN ? 8 : 2));
+      }
+    }
+    q_s[e] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+
+  float o[MT][OB][4];
+  float m_run[MT][2], l_run[MT][2];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+#pragma unroll
+    for (int j = 0; j < OB; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[t][j][e] = 0.f;
+    m_run[t][0] = m_run[t][1] = -INFINITY;
+    l_run[t][0] = l_run[t][1] = 0.f;
+  }
+
+  // Soft-max of one tile's logits s (scaled, masked): weights in place, running values updated, O rescaled if needed.
+  auto softmax = [&](float (&s)[MT][NB][4]) {
+    float corr[MT][2];
+    bool moved = false;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) top = fmaxf(top, fmaxf(s[t][n][2 * h], s[t][n][2 * h + 1]));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const float m_new = fmaxf(m_run[t][h], top);
+        const float base = m_new == -INFINITY ? 0.f : m_new;
+        corr[t][h] = ex2_approx(m_run[t][h] - base);
+        moved |= m_new != m_run[t][h];
+        m_run[t][h] = m_new;
+        float sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          s[t][n][2 * h] = ex2_approx(s[t][n][2 * h] - base);
+          s[t][n][2 * h + 1] = ex2_approx(s[t][n][2 * h + 1] - base);
+          sum += s[t][n][2 * h] + s[t][n][2 * h + 1];
+        }
+        l_run[t][h] = l_run[t][h] * corr[t][h] + sum;      // (this thread's columns; the row's four threads add up at the end)
+      }
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int j = 0; j < OB; ++j) {
+          o[t][j][0] *= corr[t][0];
+          o[t][j][1] *= corr[t][0];
+          o[t][j][2] *= corr[t][1];
+          o[t][j][3] *= corr[t][1];
+        }
+    }
+  };
+  auto q_frag = [&](int t, int ks, uint32_t (&a)[4]) {
+    const uint4 w = q_s[((wr * MT + t) * (D / 16) + ks) * 32 + lane];
+    a[0] = w.x; a[1] = w.y; a[2] = w.z; a[3] = w.w;
+  };
+  const int kb = wk * KS;      // this warp's first column within a tile
+
+  for (int i = 0; i < n_tiles; ++i) {
+    cp_async_wait<S::STAGES - 2>();
+    __syncthreads();
+    if (i + S::STAGES - 1 < n_tiles) load_tile(i + S::STAGES - 1);
+    cp_async_commit();
+    const unsigned char* stp = ring + (i % S::STAGES) * S::STAGE;
+    const uint32_t st = smem_addr(stp);
+    float s[MT][NB][4];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t][n][e] = 0.f;
+    if constexpr (PLAIN) {
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        uint32_t a[MT][4];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) q_frag(t, ks, a[t]);
+#pragma unroll
+        for (int n = 0; n < NB; n += 2) {
+          uint32_t f[4];
+          ldmatrix_x4(f, st + tree_off16<S::ROW_BYTES>(kb + n * 8 + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            mma_bf16(s[t][n], a[t], f[0], f[1]);
+            mma_bf16(s[t][n + 1], a[t], f[2], f[3]);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int hf = 0; hf < D / 64; ++hf) {
+        uint4 kw[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) kw[n] = *reinterpret_cast<const uint4*>(stp + tree_off8<D>(kb + n * 8 + lr, 4 * hf + lc));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t a[MT][4];
+#pragma unroll
+          for (int t = 0; t < MT; ++t) q_frag(t, 4 * hf + w, a[t]);
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+            const uint32_t x = w == 0 ? kw[n].x : w == 1 ? kw[n].y : w == 2 ? kw[n].z : kw[n].w;
+            const uint32_t b0 = tree_codes2<FMT>(x, x, 0, 1), b1 = tree_codes2<FMT>(x, x, 2, 3);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) mma_bf16(s[t][n], a[t], b0, b1);
+          }
+        }
+      }
+    }
+    const float* ks_s = reinterpret_cast<const float*>(stp + 2 * S::TILE);
+    const int left = c1 - (c0 + i * C) - kb;             // columns of this warp's share that exist
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int col = n * 8 + 2 * lc + e;
+        const float f = PLAIN ? p.scale2 : p.scale2 * ks_s[kb + col];
+        const bool in = col < left;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          s[t][n][e] = in ? s[t][n][e] * f : -INFINITY;
+          s[t][n][2 + e] = in ? s[t][n][2 + e] * f : -INFINITY;
+        }
+      }
+    softmax(s);
+    if constexpr (!PLAIN) {
+      const float* vs_s = ks_s + C;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float f = vs_s[kb + n * 8 + 2 * lc + e];
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            s[t][n][e] *= f;
+            s[t][n][2 + e] *= f;
+          }
+        }
+    }
+#pragma unroll
+    for (int kk = 0; kk < KS / 16; ++kk) {
+      uint32_t a[MT][4];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        a[t][0] = pack_bf16(s[t][2 * kk][0], s[t][2 * kk][1]);
+        a[t][1] = pack_bf16(s[t][2 * kk][2], s[t][2 * kk][3]);
+        a[t][2] = pack_bf16(s[t][2 * kk + 1][0], s[t][2 * kk + 1][1]);
+        a[t][3] = pack_bf16(s[t][2 * kk + 1][2], s[t][2 * kk + 1][3]);
+      }
+      if constexpr (PLAIN) {
+#pragma unroll
+        for (int j = 0; j < OB; j += 2) {
+          uint32_t f[4];
+          ldmatrix_x4_trans(f, st + S::TILE + tree_off16<S::ROW_BYTES>(kb + kk * 16 + (lane & 15), j + (lane >> 4)));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            mma_bf16(o[t][j], a[t], f[0], f[1]);
+            mma_bf16(o[t][j + 1], a[t], f[2], f[3]);
+          }
+        }
+      } else {
+        // rows (columns of the product) 2 lc, 2 lc + 1, + 8, + 9; bytes (D/8) lr ..: O's column block j is their byte j
+        uint32_t vw[4][D / 32];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = kb + kk * 16 + 2 * lc + (r & 1) + 8 * (r >> 1);
+          if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(stp + S::TILE + tree_off8<D>(row, lr));
+            vw[r][0] = x.x; vw[r][1] = x.y; vw[r][2] = x.z; vw[r][3] = x.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(stp + S::TILE + tree_off8<D>(row, lr >> 1) + (lr & 1) * 8);
+            vw[r][0] = x.x; vw[r][1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < OB; ++j) {
+          const uint32_t b0 = tree_codes2<FMT>(vw[0][j >> 2], vw[1][j >> 2], j & 3, 4 + (j & 3));
+          const uint32_t b1 = tree_codes2<FMT>(vw[2][j >> 2], vw[3][j >> 2], j & 3, 4 + (j & 3));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) mma_bf16(o[t][j], a[t], b0, b1);
+        }
+      }
+    }
+  }
+  cp_async_wait<0>();
+
+  // The drafts: tiles of 64 more columns, in bf16, masked by ancestry.
+  uint32_t real = 0;        // bit 2 t + h: this thread's row is a node's, not padding
+  if (last) {
+    __syncthreads();
+    unsigned char* dk = ring;
+    unsigned char* dv = ring + S::DRAFT_TILE;
+    int* par_s = reinterpret_cast<int*>(ring + 2 * S::DRAFT_TILE);
+    uint32_t* anc_s = reinterpret_cast<uint32_t*>(par_s + TREE_MAX_NODES);     // [node of this block][words]
+    int* odd_s = reinterpret_cast<int*>(anc_s + S::ROWS * TREE_ANC_WORDS);     // some value of the tile is not finite
+    const int n0 = row0 / p.G, n1 = min(p.N, (min(p.M, row0 + S::ROWS) - 1) / p.G + 1);
+    for (int i = tid; i < p.N; i += TREE_MMA_THREADS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
+    __syncthreads();
+    tree_ancestor_bits(p.N, n0, n1, par_s, anc_s, tid, TREE_MMA_THREADS);
+    for (int j0 = 0; j0 < p.N; j0 += C) {
+      if (tid == 0) *odd_s = 0;
+      __syncthreads();
+      bool odd = false;
+      for (int e = tid; e < C * (D / 8); e += TREE_MMA_THREADS) {
+        const int row = e / (D / 8), ch = e % (D / 8);
+        uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
+        if (j0 + row < p.N) {
+          const long long at = (((long long)(j0 + row) * p.B + b) * p.Hkv + hk) * D + ch * 8;
+          kw = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_new) + at);
+          vw = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.v_new) + at);
+          odd |= tree_drop_odd(vw);
+        }
+        *reinterpret_cast<uint4*>(dk + tree_off16<2 * D>(row, ch)) = kw;
+        *reinterpret_cast<uint4*>(dv + tree_off16<2 * D>(row, ch)) = vw;
+      }
+      if (odd) *odd_s = 1;
+      __syncthreads();
+      const int jw = j0 + kb;                 // this warp's first draft
+      if (jw < p.N) {
+        float s[MT][NB][4];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][n][e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          uint32_t a[MT][4];
+#pragma unroll
+          for (int t = 0; t < MT; ++t) q_frag(t, ks, a[t]);
+#pragma unroll
+          for (int n = 0; n < NB; n += 2) {
+            uint32_t f[4];
+            if constexpr (PLAIN) {
+              ldmatrix_x4(f, smem_addr(dk) + tree_off16<2 * D>(kb + n * 8 + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)));
+            } else {
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const uint2 w = *reinterpret_cast<const uint2*>(
+                    dk + tree_off16<2 * D>(kb + (n + x) * 8 + lr, 8 * (ks >> 2) + 2 * lc + ((ks & 3) >> 1)) + (ks & 1) * 8);
+                f[2 * x] = w.x;
+                f[2 * x + 1] = w.y;
+              }
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              mma_bf16(s[t][n], a[t], f[0], f[1]);
+              mma_bf16(s[t][n + 1], a[t], f[2], f[3]);
+            }
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int m = row0 + (wr * MT + t) * 16 + lr + 8 * h;
+            const uint32_t* anc = anc_s + (min(m, p.M - 1) / p.G - n0) * TREE_ANC_WORDS;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+              const int col = jw + n * 8 + 2 * lc;          // even: both columns are in one word
+              const uint32_t see = col < p.N && m < p.M ? anc[col >> 5] >> (col & 31) : 0u;
+              s[t][n][2 * h] = (see & 1u) ? s[t][n][2 * h] * p.scale2 : -INFINITY;
+              s[t][n][2 * h + 1] = (see & 2u) ? s[t][n][2 * h + 1] * p.scale2 : -INFINITY;
+            }
+          }
+        softmax(s);
+#pragma unroll
+        for (int kk = 0; kk < KS / 16; ++kk) {
+          uint32_t a[MT][4];
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            a[t][0] = pack_bf16(s[t][2 * kk][0], s[t][2 * kk][1]);
+            a[t][1] = pack_bf16(s[t][2 * kk][2], s[t][2 * kk][3]);
+            a[t][2] = pack_bf16(s[t][2 * kk + 1][0], s[t][2 * kk + 1][1]);
+            a[t][3] = pack_bf16(s[t][2 * kk + 1][2], s[t][2 * kk + 1][3]);
+          }
+          if constexpr (PLAIN) {
+#pragma unroll
+            for (int j = 0; j < OB; j += 2) {
+              uint32_t f[4];
+              ldmatrix_x4_trans(f, smem_addr(dv) + tree_off16<2 * D>(kb + kk * 16 + (lane & 15), j + (lane >> 4)));
+#pragma unroll
+              for (int t = 0; t < MT; ++t) {
+                mma_bf16(o[t][j], a[t], f[0], f[1]);
+                mma_bf16(o[t][j + 1], a[t], f[2], f[3]);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < OB; j += 2) {               // O's columns (D/8) lr + j, + 1 of four drafts
+              uint32_t w[4];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int row = kb + kk * 16 + 2 * lc + (r & 1) + 8 * (r >> 1);
+                const int d = OB * lr + j;
+                w[r] = *reinterpret_cast<const uint32_t*>(dv + tree_off16<2 * D>(row, d >> 3) + (d & 7) * 2);
+              }
+#pragma unroll
+              for (int t = 0; t < MT; ++t) {
+                mma_bf16(o[t][j], a[t], __byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+                mma_bf16(o[t][j + 1], a[t], __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
+              }
+            }
+          }
+        }
+        if (*odd_s) {
+          // Values that are not finite were left out of the contraction, where a weight of zero would not have kept them
+          // from the rows that do not see them; they are added here to the rows that do.
+          for (int x = 0; x < KS && jw + x < p.N; ++x) {
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.v_new) + (((long long)(jw + x) * p.B + b) * p.Hkv + hk) * D;
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float mine = 0.f;
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e)
+                    if (n == (x >> 3) && e == (x & 1)) mine = s[t][n][2 * h + e];
+                const float w = __shfl_sync(0xffffffffu, mine, (lane & ~3) | ((x & 7) >> 1));
+                if (w == 0.f) continue;
+#pragma unroll
+                for (int j = 0; j < OB; ++j)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const float v = __bfloat162float(src[PLAIN ? 8 * j + 2 * lc + e : OB * (2 * lc + e) + j]);
+                    if (!isfinite(v)) o[t][j][2 * h + e] += w * v;
+                  }
+              }
+          }
+        }
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int m = row0 + (wr * MT + t) * 16 + lr + 8 * h;
+        if (m < p.M) {
+          const int n = m / p.G;
+          real |= ((anc_s[(n - n0) * TREE_ANC_WORDS + (n >> 5)] >> (n & 31)) & 1u) << (2 * t + h);
+        }
+      }
+  }
+  pdl_launch_dependents();
+
+  // Join the warps that shared out the columns: maxima and sums first, then O scaled to the common maximum.
+  __syncthreads();
+  float* o_s = reinterpret_cast<float*>(ring);                       // [WK][ROWS][D]
+  float2* ml_s = reinterpret_cast<float2*>(ring + S::WK * S::ROWS * D * 4);   // [WK][ROWS]
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float l = l_run[t][h];
+      l += __shfl_xor_sync(0xffffffffu, l, 1);
+      l += __shfl_xor_sync(0xffffffffu, l, 2);
+      const int r = (wr * MT + t) * 16 + lr + 8 * h;
+      if (lc == 0) ml_s[wk * S::ROWS + r] = make_float2(m_run[t][h], last && !((real >> (2 * t + h)) & 1u) ? TREE_PADDING : l);
+    }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = (wr * MT + t) * 16 + lr + 8 * h;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < S::WK; ++w) top = fmaxf(top, ml_s[w * S::ROWS + r].x);
+      const float f = top == -INFINITY ? 0.f : ex2_approx(m_run[t][h] - top);
+      float* dst = o_s + (wk * S::ROWS + r) * D;
+#pragma unroll
+      for (int j = 0; j < OB; ++j) {
+        if constexpr (PLAIN) {
+          *reinterpret_cast<float2*>(dst + 8 * j + 2 * lc) = make_float2(o[t][j][2 * h] * f, o[t][j][2 * h + 1] * f);
+        } else {
+          dst[OB * (2 * lc) + j] = o[t][j][2 * h] * f;
+          dst[OB * (2 * lc + 1) + j] = o[t][j][2 * h + 1] * f;
+        }
+      }
+    }
+  __syncthreads();
+  for (int e = tid; e < S::ROWS * (D / 4); e += TREE_MMA_THREADS) {
+    const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+    const int m = row0 + r;
+    if (m >= p.M) continue;
+    float top = -INFINITY, l = 0.f;
+    bool pad = false;
+#pragma unroll
+    for (int w = 0; w < S::WK; ++w) top = fmaxf(top, ml_s[w * S::ROWS + r].x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < S::WK; ++w) {
+      const float2 ml = ml_s[w * S::ROWS + r];
+      pad |= ml.y == TREE_PADDING;
+      if (ml.x != -INFINITY) l += ml.y * ex2_approx(ml.x - top);
+      const float4 x = *reinterpret_cast<const float4*>(o_s + (w * S::ROWS + r) * D + d);
+      acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+    }
+    if (p.splits == 1) {
+      const float f = l == 0.f ? 0.f : 1.f / l;
+      const int n = m / p.G, g = m - n * p.G;
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
+      if (pad) tree_store4<__nv_bfloat16>(dst, 0.f, 0.f, 0.f, 0.f);
+      else tree_store4<__nv_bfloat16>(dst, acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+    } else {
+      const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
+      if (d == 0) p.part_ml[at] = make_float2(top, pad ? TREE_PADDING : l);
+      *reinterpret_cast<float4*>(p.part_acc + at * D + d) = acc;
+    }
+  }
+}
+
+}  // namespace tova
