@@ -368,13 +368,13 @@ class TovaCache:
         [N,B,H,D] in the cache's dtype, workspace of tova_cache_tree_workspace_bytes(n_nodes) bytes."""
         c, N = self.cfg, int(n_nodes)
         row = N * c.batch * c.head_dim
+        dev = self.mem.get_device()
         for x, n in ((q, row * c.n_q_heads), (k, row * c.n_kv_heads), (v, row * c.n_kv_heads), (out, row * c.n_q_heads)):
-            _need(x, n, self.tdtype, self.device)
-        _need(parents, N * c.batch, torch.int32, self.device)
-        with _on(self.device):
-            _check(lib().tova_cache_tree_attention(self._h, _a(q), _a(k), _a(v), N, _a(parents), _a(out), _a(workspace),
-                                                   _bytes(workspace), _raw_stream(self.device, stream)),
-                   "tova_cache_tree_attention")
+            _need(x, n, self.tdtype, dev)
+        _need(parents, N * c.batch, torch.int32, dev)
+        _need_workspace(workspace, dev)
+        _call(lib().tova_cache_tree_attention, "tova_cache_tree_attention", dev, stream, self._h, _a(q), _a(k), _a(v), N,
+              _a(parents), _a(out), _a(workspace), _bytes(workspace))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
@@ -418,59 +418,60 @@ def _bytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
-def _need(t, numel: int, dtype, device) -> None:
-    """A contiguous device tensor of at least `numel` elements of `dtype` (or of one of several); None passes."""
-    if t is None:
-        return
-    if not (t.dtype is dtype or (type(dtype) is tuple and t.dtype in dtype)):
+def _misfit(t, numel, dtype, device: int):
+    if t.dtype is not dtype and not (type(dtype) is tuple and t.dtype in dtype):
         raise TypeError(f"expected a tensor of {dtype}, got {t.dtype}")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"expected a tensor on {device}, got {t.device}")
-    if not t.is_contiguous() or t.numel() < numel:
-        raise ValueError(f"expected a contiguous tensor of at least {numel} elements, got {tuple(t.shape)}"
-                         f"{'' if t.is_contiguous() else ' (not contiguous)'}")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"expected a tensor on the GPU of the other arguments, got one on {t.device}")
+    raise ValueError(f"expected a contiguous tensor of at least {numel} elements, got {tuple(t.shape)} with strides {t.stride()}")
 
 
-def _rows(t, n_tokens: int, batch: int, heads: int, dim: int, dtype, device) -> int:
+def _need(t, numel: int, dtype, device: int) -> None:
+    """A contiguous tensor of at least `numel` elements of `dtype` (or of one of several) on GPU `device`; None passes."""
+    if t is not None and not ((t.dtype is dtype or (type(dtype) is tuple and t.dtype in dtype)) and t.get_device() == device >= 0
+                              and t.is_contiguous() and t.numel() >= numel):
+        _misfit(t, numel, dtype, device)
+
+
+def _need_workspace(t, device: int) -> None:
+    if t is not None and not (t.get_device() == device >= 0 and t.is_contiguous()):
+        _misfit(t, 0, t.dtype, device)
+
+
+def _rows(t, n_tokens: int, batch: int, heads: int, dim: int, dtype, device: int) -> int:
     """Checks [T,B,heads,dim] with contiguous heads and evenly spaced (token, sequence) rows; their element stride."""
-    if t.dtype is not dtype:
-        raise TypeError(f"expected a tensor of {dtype}, got {t.dtype}")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"expected a tensor on {device}, got {t.device}")
+    if t.dtype is not dtype or t.get_device() != device or device < 0:
+        _misfit(t, 0, dtype, device)
     T, B, H, D = t.shape
     if T < n_tokens or B != batch or H != heads or D != dim:
         raise ValueError(f"expected [{n_tokens},{batch},{heads},{dim}], got {tuple(t.shape)}")
     s0, s1, s2, s3 = t.stride()
-    if n_tokens * batch == 1:
-        s0 = s1 = heads * dim
-    elif batch == 1:
-        s1 = s0
-    elif n_tokens == 1:
-        s0 = s1 * batch
-    if s0 != s1 * batch or (s2 != dim and heads > 1) or (s3 != 1 and dim > 1):
+    if batch == 1:
+        s1 = s0 if n_tokens > 1 else heads * dim
+    elif n_tokens > 1 and s0 != s1 * batch:
+        s1 = -1
+    if s1 < heads * dim or (s2 != dim and heads > 1) or s3 != 1:
         raise ValueError(f"rows of {tuple(t.shape)} with strides {t.stride()} are not evenly spaced with contiguous heads")
     return s1
 
 
-class _on:
-    """Makes `device` current for the calls inside, where it is not already."""
-    __slots__ = ("want", "was")
-
-    def __init__(self, device):
-        self.want = device.index
-
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.want != self.was:
-            torch.cuda.set_device(self.want)
-
-    def __exit__(self, *exc):
-        if self.want != self.was:
-            torch.cuda.set_device(self.was)
+_raw_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _raw_stream(device, stream) -> int:
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _call(fn, what: str, device: int, stream, *args) -> None:
+    """fn(*args, stream) with `device` current (switched to where it is not already); the stream is the caller's, or the
+    current one of that device."""
+    was = torch.cuda.current_device()
+    if was != device:
+        torch.cuda.set_device(device)
+    try:
+        rc = fn(*args, _raw_current_stream(device) if stream is None else stream.cuda_stream)
+    finally:
+        if was != device:
+            torch.cuda.set_device(was)
+    if rc != 0:
+        raise TovaError(rc, what)
 
 
 class TovaRope:
@@ -492,7 +493,7 @@ class TovaRope:
         """q [T,B,H,D] and k [T,B,Hkv,D] (or None) into q_out, k_out; all may be evenly strided over (T, B).  inverse:
         the transposed map, for gradients."""
         B, H, Hkv, D, t = self._dims
-        dev = q.device
+        dev = q.get_device()
         qs, qos = _rows(q, n_tokens, B, H, D, t, dev), _rows(q_out, n_tokens, B, H, D, t, dev)
         ks = kos = 0
         if k is not None or k_out is not None:
@@ -500,10 +501,8 @@ class TovaRope:
                 raise ValueError("k and k_out come together")
             ks, kos = _rows(k, n_tokens, B, Hkv, D, t, dev), _rows(k_out, n_tokens, B, Hkv, D, t, dev)
         _need(positions, n_tokens * B, torch.int32, dev)
-        with _on(dev):
-            _check(lib().tova_rope_apply(self._h, _a(q), qs, _a(k), ks, n_tokens, _a(positions), first_pos,
-                                         1 if inverse else 0, _a(q_out), qos, _a(k_out), kos, _raw_stream(dev, stream)),
-                   "tova_rope_apply")
+        _call(lib().tova_rope_apply, "tova_rope_apply", dev, stream, self._h, _a(q), qs, _a(k), ks, n_tokens, _a(positions),
+              first_pos, 1 if inverse else 0, _a(q_out), qos, _a(k_out), kos)
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
@@ -527,14 +526,13 @@ def tova_quant_write(cfg: tova_quant_config, k, v, n_tokens: int, k_codes, k_sca
                      first_slot: int = 0, stream=None) -> None:
     """Rows k, v [T,B,Hkv,D] (evenly strided over (T, B)) into the 8-bit state: codes [B,Hkv,cap,D], scales
     [B,Hkv,cap]; slots [T,B] int32 or None = first_slot + token."""
-    t, dev, B, H, D = _TORCH_TYPE.get(cfg.dtype), k.device, cfg.batch, cfg.n_kv_heads, cfg.head_dim
+    t, dev, B, H, D = _TORCH_TYPE.get(cfg.dtype), k.get_device(), cfg.batch, cfg.n_kv_heads, cfg.head_dim
     ks, vs = _rows(k, n_tokens, B, H, D, t, dev), _rows(v, n_tokens, B, H, D, t, dev)
     _need_state(cfg, cfg.format, k_codes, k_scale, None, dev)
     _need_state(cfg, cfg.format, v_codes, v_scale, None, dev)
     _need(slots, n_tokens * B, torch.int32, dev)
-    with _on(dev):
-        _check(lib().tova_quant_write(_byref(cfg), _a(k), ks, _a(v), vs, n_tokens, _a(slots), first_slot, _a(k_codes),
-                                      _a(k_scale), _a(v_codes), _a(v_scale), _raw_stream(dev, stream)), "tova_quant_write")
+    _call(lib().tova_quant_write, "tova_quant_write", dev, stream, _byref(cfg), _a(k), ks, _a(v), vs, n_tokens, _a(slots),
+          first_slot, _a(k_codes), _a(k_scale), _a(v_codes), _a(v_scale))
 
 
 def tova_quant_read(cfg: tova_quant_config, k_codes, k_scale, v_codes, v_scale, n_tokens: int, k, v, slots=None,
@@ -542,16 +540,15 @@ def tova_quant_read(cfg: tova_quant_config, k_codes, k_scale, v_codes, v_scale, 
     """The state's rows at slots [T,B] (None: first_slot + token) as k, v [T,B,Hkv,D] in cfg.dtype; k or v may be None."""
     if k is None and v is None:
         return
-    t, dev, B = _TORCH_TYPE.get(cfg.dtype), (k if k is not None else v).device, cfg.batch
+    t, dev, B = _TORCH_TYPE.get(cfg.dtype), (k if k is not None else v).get_device(), cfg.batch
     n = n_tokens * B * cfg.n_kv_heads * cfg.head_dim
     _need(k, n, t, dev)
     _need(v, n, t, dev)
     _need_state(cfg, cfg.format, k_codes, k_scale, None, dev)
     _need_state(cfg, cfg.format, v_codes, v_scale, None, dev)
     _need(slots, n_tokens * B, torch.int32, dev)
-    with _on(dev):
-        _check(lib().tova_quant_read(_byref(cfg), _a(k_codes), _a(k_scale), _a(v_codes), _a(v_scale), n_tokens,
-                                     _a(slots), first_slot, _a(k), _a(v), _raw_stream(dev, stream)), "tova_quant_read")
+    _call(lib().tova_quant_read, "tova_quant_read", dev, stream, _byref(cfg), _a(k_codes), _a(k_scale), _a(v_codes),
+          _a(v_scale), n_tokens, _a(slots), first_slot, _a(k), _a(v))
 
 
 def tova_tree_workspace_bytes(cfg: tova_tree_config, n_live: int, n_nodes: int) -> int:
@@ -566,7 +563,7 @@ def tova_tree_attention(cfg: tova_tree_config, K, V, n_live: int, q, k, v, n_nod
     """Attention of N drafted tokens q [N,B,H,D], k, v [N,B,Hkv,D] over a state K, V [B,Hkv,cap,D] (or its codes with
     their scales) and the tree parents [N,B] (None: a chain); lens [B] int32 (None: n_live rows each).  out [N,B,H,D]
     in the type of q."""
-    t, dev, B, N = _TORCH_TYPE.get(cfg.dtype), q.device, cfg.batch, n_nodes
+    t, dev, B, N = _TORCH_TYPE.get(cfg.dtype), q.get_device(), cfg.batch, n_nodes
     nq, nk = N * B * cfg.n_q_heads * cfg.head_dim, N * B * cfg.n_kv_heads * cfg.head_dim
     _need_state(cfg, cfg.format, K, k_scale, t, dev)
     _need_state(cfg, cfg.format, V, v_scale, t, dev)
@@ -576,10 +573,9 @@ def tova_tree_attention(cfg: tova_tree_config, K, V, n_live: int, q, k, v, n_nod
     _need(out, nq, t, dev)
     _need(parents, N * B, torch.int32, dev)
     _need(lens, B, torch.int32, dev)
-    with _on(dev):
-        _check(lib().tova_tree_attention(_byref(cfg), _a(K), _a(V), _a(k_scale), _a(v_scale), _a(lens), n_live, _a(q),
-                                         _a(k), _a(v), N, _a(parents), _a(out), _a(workspace), _bytes(workspace),
-                                         _raw_stream(dev, stream)), "tova_tree_attention")
+    _need_workspace(workspace, dev)
+    _call(lib().tova_tree_attention, "tova_tree_attention", dev, stream, _byref(cfg), _a(K), _a(V), _a(k_scale),
+          _a(v_scale), _a(lens), n_live, _a(q), _a(k), _a(v), N, _a(parents), _a(out), _a(workspace), _bytes(workspace))
 
 
 def tova_verify_draft(cfg: tova_verify_config, target, draft, tokens, u, u_sample, n_accepted, path, tokens_out,
@@ -587,7 +583,7 @@ def tova_verify_draft(cfg: tova_verify_config, target, draft, tokens, u, u_sampl
     """Which drafted tokens [N,B] the target's probabilities [N+1,B,V] accept, given u [N,B] and u_sample [B]; see
     include/tova.h.  draft: probabilities the children were drawn from, or None.  n_accepted [B], path [N,B] or None,
     tokens_out [N+1,B], int32."""
-    t, dev, B, N = _TORCH_TYPE.get(cfg.dtype), target.device, cfg.batch, cfg.n_nodes
+    t, dev, B, N = _TORCH_TYPE.get(cfg.dtype), target.get_device(), cfg.batch, cfg.n_nodes
     ld = cfg.row_stride or cfg.vocab
     need = ((N + 1) * B - 1) * ld + cfg.vocab
     _need(target, need, t, dev)
@@ -599,10 +595,8 @@ def tova_verify_draft(cfg: tova_verify_config, target, draft, tokens, u, u_sampl
     _need(n_accepted, B, torch.int32, dev)
     _need(path, N * B, torch.int32, dev)
     _need(tokens_out, (N + 1) * B, torch.int32, dev)
-    with _on(dev):
-        _check(lib().tova_verify_draft(_byref(cfg), _a(target), _a(draft), _a(tokens), _a(parents), _a(u), _a(u_sample),
-                                       _a(n_accepted), _a(path), _a(tokens_out), _raw_stream(dev, stream)),
-               "tova_verify_draft")
+    _call(lib().tova_verify_draft, "tova_verify_draft", dev, stream, _byref(cfg), _a(target), _a(draft), _a(tokens),
+          _a(parents), _a(u), _a(u_sample), _a(n_accepted), _a(path), _a(tokens_out))
 
 
 def to_device(x, dtype: int, device="cuda:0") -> torch.Tensor:

@@ -13,6 +13,7 @@
 #include "tova_rope.cuh"
 #include "tova_tree.cuh"
 #include "tova_tree_mma.cuh"
+#include "tova_tree_tc.cuh"
 #include "tova_verify.cuh"
 
 namespace {
@@ -293,7 +294,7 @@ int tree_check(const tova_tree_config* c, int32_t n_live, int32_t n_nodes) {
 }
 
 // Which kernel serves a call and how its columns are cut.
-enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64 };
+enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64, TREE_TC_1, TREE_TC_2 };
 struct TreePlan {
   int kernel, row_blocks, splits, split_cols;
   size_t ml_bytes, bytes;
@@ -303,22 +304,24 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
   TreePlan t{};
   const int M = n_nodes * (c.n_q_heads / c.n_kv_heads);
   int rows = tova::TREE_ALU_ROWS, cols = tova::TREE_ALU_COLS;
+  int resident = 2 * sm_count, shortest = 2;     // blocks at a time; tiles worth a block's set-up
   if (c.dtype == TOVA_DTYPE_BF16) {
-    t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : TREE_MMA_64;
-    rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : M <= 64 ? TREE_MMA_64 : M <= 128 ? TREE_TC_1 : TREE_TC_2;
+    rows = M <= 64 ? 64 : M <= 128 ? tova::TREE_TC_ROWS : 2 * tova::TREE_TC_ROWS;
     cols = tova::TREE_MMA_COLS;
+    if (t.kernel == TREE_TC_2) resident = sm_count;
+    if (M > 64) shortest = 8;
   }
   t.row_blocks = (M + rows - 1) / rows;
   const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;
   const int tiles = std::max(1, (n_live + cols - 1) / cols);
-  // Enough runs for two rounds of resident blocks (two per SM), but no run shorter than two tiles unless the GPU would
-  // stay half empty.
-  long long want = (4LL * sm_count + whole - 1) / whole;
-  const int shortest = whole * (tiles / 2) >= sm_count ? 2 : 1;
+  long long want = (2LL * resident + whole - 1) / whole;
+  if (whole * (tiles / shortest) < resident) shortest = 1;
   want = std::max(1LL, std::min<long long>(want, tiles / shortest));
   const int per = (int)((tiles + want - 1) / want);
   t.split_cols = per * cols;
   t.splits = (tiles + per - 1) / per;
+  if (t.splits > 1) t.splits += 1;               // a run of its own for the drafts: it does not wait for a run of rows
   if (t.splits > 1) {
     const size_t n = (size_t)t.splits * c.batch * c.n_kv_heads * M;
     t.ml_bytes = (n * sizeof(float2) + 255) / 256 * 256;
@@ -347,8 +350,9 @@ template <typename T, int D>
 cudaError_t tree_merge(const tova::TreeParams& p, cudaStream_t st) {
   const long long rows = (long long)p.B * p.Hkv * p.M;
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3((unsigned)((rows + 7) / 8));
-  lc.blockDim = dim3(256);
+  constexpr int ROWS = tova::TREE_MERGE_THREADS / 32;
+  lc.gridDim = dim3((unsigned)((rows + ROWS - 1) / ROWS));
+  lc.blockDim = dim3(tova::TREE_MERGE_THREADS);
   lc.stream = st;
   cudaLaunchAttribute at[1];      // its blocks may come up while the first kernel's last ones still run
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -365,6 +369,13 @@ cudaError_t tree_start_mma(const tova::TreeParams& p, const TreePlan& t, cudaStr
                     tova::TREE_MMA_THREADS, p, t, st);
 }
 
+template <int D, int FMT, int NT>
+cudaError_t tree_start_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
+  static std::atomic<bool> configured[64];
+  using S = tova::TreeTcShape<D, FMT, NT>;
+  return tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, p, t, st);
+}
+
 template <typename T, int D, int FMT>
 cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
   cudaError_t e;
@@ -372,8 +383,13 @@ cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream
     static std::atomic<bool> configured[64];
     e = tree_start(tova::tova_tree_alu_kernel<T, D, FMT>, configured, tova::tree_alu_smem_bytes<D>(), tova::TREE_ALU_THREADS, p, t, st);
   } else {
-    e = t.kernel == TREE_MMA_16 ? tree_start_mma<D, FMT, 1, 1>(p, t, st)
-        : t.kernel == TREE_MMA_32 ? tree_start_mma<D, FMT, 1, 2>(p, t, st) : tree_start_mma<D, FMT, 2, 2>(p, t, st);
+    switch (t.kernel) {
+      case TREE_MMA_16: e = tree_start_mma<D, FMT, 1, 1>(p, t, st); break;
+      case TREE_MMA_32: e = tree_start_mma<D, FMT, 1, 2>(p, t, st); break;
+      case TREE_MMA_64: e = tree_start_mma<D, FMT, 2, 2>(p, t, st); break;
+      case TREE_TC_1: e = tree_start_tc<D, FMT, 1>(p, t, st); break;
+      default: e = tree_start_tc<D, FMT, 2>(p, t, st); break;
+    }
   }
   if (e != cudaSuccess || t.splits == 1) return e;
   return tree_merge<T, D>(p, st);

@@ -43,33 +43,27 @@ __device__ __forceinline__ int tree_len(const TreeParams& p, int b) {
   return p.lens ? max(0, min(p.lens[b], p.n_live)) : p.n_live;
 }
 
-// Ancestor bits of nodes n0..n1-1, one thread per node: bit j of word w of anc[(i - n0) * TREE_ANC_WORDS ..] says that
-// node 32 w + j is i or above it.  All zero for padding.  par_s holds the sequence's parents; the walk goes strictly down
-// in index, so it ends.  (The caller has made par_s visible; the results are visible after the barrier here.)
-__device__ __forceinline__ void tree_ancestor_bits(int N, int n0, int n1, const int* par_s, uint32_t* anc, int tid, int threads) {
-  for (int i = n0 + tid; i < n1; i += threads) {
-    uint32_t w[TREE_ANC_WORDS];
+// Ancestor bits of node i: bit j of word w says that node 32 w + j is i or above it; all zero for padding.  par holds the
+// sequence's parents (or it is a chain); the walk goes strictly down in index, so it ends.
+template <int WORDS>
+__device__ __forceinline__ void tree_ancestor_bits(int i, bool chain, const int* par, uint32_t* anc) {
+  uint32_t w[WORDS];
 #pragma unroll
-    for (int k = 0; k < TREE_ANC_WORDS; ++k) w[k] = 0;
-    int j = i;
-    bool real = true;
-    while (j >= 0) {
+  for (int k = 0; k < WORDS; ++k) w[k] = chain ? (i >= 32 * k + 31 ? 0xffffffffu : i >= 32 * k ? (2u << (i & 31)) - 1u : 0u) : 0u;
+  int j = chain ? -1 : i;
+  while (j >= 0) {
 #pragma unroll
-      for (int k = 0; k < TREE_ANC_WORDS; ++k) w[k] |= (j >> 5) == k ? 1u << (j & 31) : 0u;
-      const int up = par_s[j];
-      if (up < -1 || up >= j) { real = false; break; }
-      j = up;
+    for (int k = 0; k < WORDS; ++k) w[k] |= (j >> 5) == k ? 1u << (j & 31) : 0u;
+    const int up = par[j];
+    if (up < -1 || up >= j) {
+#pragma unroll
+      for (int k = 0; k < WORDS; ++k) w[k] = 0;
+      break;
     }
-#pragma unroll
-    for (int k = 0; k < TREE_ANC_WORDS; ++k) anc[(i - n0) * TREE_ANC_WORDS + k] = real ? w[k] : 0u;
+    j = up;
   }
-  __syncthreads();
-}
-__device__ __forceinline__ void tree_ancestors(const TreeParams& p, int b, int* par_s, uint32_t (*anc)[TREE_ANC_WORDS],
-                                               int threads) {
-  for (int i = threadIdx.x; i < p.N; i += threads) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
-  __syncthreads();
-  tree_ancestor_bits(p.N, 0, p.N, par_s, &anc[0][0], threadIdx.x, threads);
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) anc[k] = w[k];
 }
 
 // Zeroes the infinities and NaN among eight bf16 values; true if there were any.
@@ -91,6 +85,25 @@ __device__ __forceinline__ float4 tree_load4(const __nv_bfloat16* x) {
   const uint2 w = *reinterpret_cast<const uint2*>(x);
   return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
                      __uint_as_float(w.y & 0xffff0000u));
+}
+
+// Adds the values that tree_drop_odd took out, of the drafts whose bits are set, to a row's components d0..d0+E-1 before
+// normalisation: a positive weight times an infinity or NaN is that again.
+template <int WORDS, int E>
+__device__ __forceinline__ void tree_add_odd(const TreeParams& p, int b, int hk, const uint32_t* anc, int D, int d0, float* acc) {
+  for (int j = 0; j < p.N; ++j) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k)
+      if (k == (j >> 5)) word = anc[k];
+    if (!((word >> (j & 31)) & 1u)) continue;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.v_new) + (((long long)j * p.B + b) * p.Hkv + hk) * D + d0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float v = __bfloat162float(src[e]);
+      if (!isfinite(v)) acc[e] += v;
+    }
+  }
 }
 
 template <typename T>
@@ -143,7 +156,11 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
   const int n_state = c1 > c0 ? (c1 - c0 + C - 1) / C : 0;
   const int n_draft = last ? (p.N + C - 1) / C : 0;
 
-  if (last) tree_ancestors(p, b, par_s, anc_s, TREE_ALU_THREADS);
+  if (last) {
+    for (int i = tid; i < p.N; i += TREE_ALU_THREADS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
+    __syncthreads();
+    for (int i = tid; i < p.N; i += TREE_ALU_THREADS) tree_ancestor_bits<TREE_ANC_WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
+  }
   // Q rows, scaled into the base-2 domain
   for (int i = tid; i < R * (D / 4); i += TREE_ALU_THREADS) {
     const int r = i / (D / 4), d = (i % (D / 4)) * 4;
@@ -309,14 +326,15 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
 }
 
 // Joins the runs' partial results: o = sum_s 2^(m_s - m) acc_s / sum_s 2^(m_s - m) l_s.  One warp per row of the
-// product; grid = ceil(B Hkv M / 8), 256 threads.
+// product, its lanes first over the runs, then over D; grid = ceil(B Hkv M / 4), 128 threads.
+constexpr int TREE_MERGE_THREADS = 128;
 template <typename T, int D>
-__global__ void __launch_bounds__(256) tova_tree_merge_kernel(const __grid_constant__ TreeParams p) {
-  pdl_wait();
+__global__ void __launch_bounds__(TREE_MERGE_THREADS) tova_tree_merge_kernel(const __grid_constant__ TreeParams p) {
   const int lane = threadIdx.x & 31;
   const long long rows = (long long)p.B * p.Hkv * p.M;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long row = (long long)blockIdx.x * (TREE_MERGE_THREADS / 32) + (threadIdx.x >> 5);
   if (row >= rows) return;
+  pdl_wait();
   float m = -INFINITY;
   bool pad = false;
   for (int s = lane; s < p.splits; s += 32) {
@@ -331,15 +349,25 @@ __global__ void __launch_bounds__(256) tova_tree_merge_kernel(const __grid_const
   float acc[E], l = 0.f;
 #pragma unroll
   for (int j = 0; j < E; ++j) acc[j] = 0.f;
-  for (int s = 0; s < p.splits; ++s) {
-    const float2 ml = p.part_ml[s * rows + row];
-    if (ml.x == -INFINITY) continue;                 // a run without a visible column
-    const float w = exp2f(ml.x - base);
-    l += w * ml.y;
-    const float* a = p.part_acc + (s * rows + row) * D + lane * E;
+  const float* src = p.part_acc + row * D + lane * E;
+  for (int s0 = 0; s0 < p.splits; s0 += 32) {
+    // lane's run: its factor, and its share of the sum.  (A run without a visible column has the factor 0 and zeros.)
+    float w = 0.f;
+    if (s0 + lane < p.splits) {
+      const float2 ml = p.part_ml[(s0 + lane) * rows + row];
+      w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - base);
+      if (w != 0.f) l += w * ml.y;
+    }
+    const int n = min(32, p.splits - s0);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float f = __shfl_sync(0xffffffffu, w, i);
+      const float* a = src + (s0 + i) * rows * D;
 #pragma unroll
-    for (int j = 0; j < E; ++j) acc[j] = fmaf(w, a[j], acc[j]);
+      for (int j = 0; j < E; ++j) acc[j] = fmaf(f, a[j], acc[j]);
+    }
   }
+  l = warp_sum(l);
   const int bh = (int)(row / p.M), mm = (int)(row - (long long)bh * p.M);
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv, n = mm / p.G, g = mm - n * p.G;
   T* dst = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + lane * E;

@@ -1,11 +1,12 @@
 // Attention of drafted tokens over a state on warp-level matrix instructions (see tova_tree.cuh for the operation):
-// bf16 queries, up to 64 rows of the product per block, states in bf16, int8 or e4m3.
+// bf16 queries, up to 64 rows of the product (nodes x query heads of a KV head), states in bf16, int8 or e4m3.
 //
 // With few rows the kernel's only hard limit is the state's bytes, so everything else hides behind their copies: a
 // block of four warps runs down its columns in tiles of 64, copied ahead (cp.async, several stages) into swizzled
 // shared memory.  WR groups of warps share out the rows, the 4 / WR warps of a group the tile's columns; every warp
 // keeps a running maximum, sum and O of its own over the columns it has seen, and the warps are joined once, at the
-// end, through shared memory.  O is rescaled only when some row's maximum moved.
+// end, through shared memory.  O is rescaled only when some row's maximum moved.  The drafts are one more tile, copied
+// ahead like the others.  The weights are summed as they were rounded to bf16, so that what multiplies V adds up to one.
 //
 // 8-bit states are converted on the way from shared memory to the matrix instructions' operands, each code once per
 // row group: int8 by pasting its 7 low bits and its sign bit behind the exponent of 128 (two bf16 numbers whose
@@ -23,6 +24,7 @@ namespace tova {
 
 constexpr int TREE_MMA_THREADS = 128;
 constexpr int TREE_MMA_COLS = 64;      // columns of a tile
+constexpr int TREE_MMA_NODES = 64;     // M <= 64, so there are no more nodes than that: the drafts are one tile
 
 template <int D, int FMT, int MT, int WR>
 struct TreeMmaShape {
@@ -37,9 +39,10 @@ struct TreeMmaShape {
   static constexpr int STAGES = FMT == FORMAT_PLAIN ? 3 : (D == 128 ? 5 : 8);
   static constexpr int Q_BYTES = ROWS * D * 2;
   static constexpr int SMEM = STAGES * STAGE + Q_BYTES;
-  static constexpr int DRAFT_TILE = TREE_MMA_COLS * D * 2;
-  // the ring's room is taken over by the drafts (two tiles, parents, ancestor bits), then by the joining of the warps
-  static_assert(2 * DRAFT_TILE + TREE_MAX_NODES * 4 + ROWS * TREE_ANC_WORDS * 4 + 16 <= STAGES * STAGE, "drafts fit the ring");
+  // the drafts take one stage (bf16 states), or one for their keys and one for their values (8-bit states)
+  static constexpr int DRAFT_STAGES = FMT == FORMAT_PLAIN ? 1 : 2;
+  static_assert(TREE_MMA_COLS * D * 2 * (FMT == FORMAT_PLAIN ? 2 : 1) <= STAGE && STAGES > DRAFT_STAGES, "drafts fit the ring");
+  // the ring's room is taken over by the joining of the warps
   static_assert(WK * ROWS * (D * 4 + 8) <= STAGES * STAGE, "partial results fit the ring");
 };
 
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   const int wr = warp / S::WK, wk = warp % S::WK;
   const int lr = lane >> 2, lc = lane & 3;
   const int b = blockIdx.z / p.Hkv, hk = blockIdx.z % p.Hkv;
-  const int split = blockIdx.y, row0 = blockIdx.x * S::ROWS;
+  const int split = blockIdx.y;
   const int len = tree_len(p, b);
   const bool last = split == p.splits - 1;
   const int c0 = split * p.split_cols;
@@ -115,10 +118,31 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   const float* ksg = PLAIN ? nullptr : p.k_scale + (long long)blockIdx.z * p.cap;
   const float* vsg = PLAIN ? nullptr : p.v_scale + (long long)blockIdx.z * p.cap;
 
+  // Draft `row`'s chunk `ch` of k_new or v_new.
+  auto draft_src = [&](const void* x, int row, int ch) {
+    return static_cast<const unsigned char*>(x) + ((((long long)min(row, p.N - 1) * p.B + b) * p.Hkv + hk) * D + ch * 8) * 2;
+  };
+  const int n_loads = n_tiles + (last ? S::DRAFT_STAGES : 0);
   auto load_tile = [&](int i) {
     const int j0 = c0 + i * C;
     const uint32_t st = ring_a + (i % S::STAGES) * S::STAGE;
     constexpr int CH = S::ROW_BYTES / 16;
+    if (i >= n_tiles) {
+      constexpr int DC = D / 8;
+#pragma unroll
+      for (int x = 0; x < C * DC / TREE_MMA_THREADS; ++x) {
+        const int e = x * TREE_MMA_THREADS + tid;
+        const int row = e / DC, ch = e % DC;
+        const uint32_t off = tree_off16<2 * D>(row, ch), size = row < p.N ? 16u : 0u;
+        if (PLAIN) {
+          cp_async16(st + off, draft_src(p.k_new, row, ch), size);
+          cp_async16(st + S::TILE + off, draft_src(p.v_new, row, ch), size);
+        } else {
+          cp_async16(st + off, draft_src(i == n_tiles ? p.k_new : p.v_new, row, ch), size);
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int x = 0; x < C * CH / TREE_MMA_THREADS; ++x) {
       const int e = x * TREE_MMA_THREADS + tid;
@@ -137,10 +161,19 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   };
 #pragma unroll
   for (int i = 0; i < S::STAGES - 1; ++i) {
-    if (i < n_tiles) load_tile(i);
+    if (i < n_loads) load_tile(i);
     cp_async_commit();
   }
 
+  __shared__ int par_s[TREE_MMA_NODES];
+  __shared__ uint32_t anc_s[TREE_MMA_NODES][2];      // ancestor bits of every node
+  __shared__ int odd_s;                              // some draft's value is not finite
+  if (last) {
+    if (tid < p.N) par_s[tid] = p.parents ? p.parents[(long long)tid * p.B + b] : tid - 1;
+    if (tid == 0) odd_s = 0;
+    __syncthreads();
+    if (tid < p.N) tree_ancestor_bits<2>(tid, p.parents == nullptr, par_s, anc_s[tid]);
+  }
   // Q in operand order.  Step ks of the contraction: natural order (bf16 states) k = 16 ks + 2 lc + {0,1}, + 8; permuted
   // (8-bit states), with ks = 4 i + w: d = 64 i + 16 lc + 4 w + {0,1}, {2,3}.
   for (int e = tid; e < (S::ROWS / 16) * (D / 16) * 32; e += TREE_MMA_THREADS) {
@@ -149,7 +182,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int m = row0 + rt * 16 + r + 8 * h;
+      const int m = rt * 16 + r + 8 * h;
       if (m < p.M) {
         const int n = m / p.G, g = m - n * p.G;
         const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D;
@@ -173,7 +206,8 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
     l_run[t][0] = l_run[t][1] = 0.f;
   }
 
-  // Soft-max of one tile's logits s (scaled, masked): weights in place, running values updated, O rescaled if needed.
+  // Soft-max of one tile's logits s (scaled, masked): weights in place, running maximum updated, sum and O rescaled if it
+  // moved.
   auto softmax = [&](float (&s)[MT][NB][4]) {
     float corr[MT][2];
     bool moved = false;
@@ -191,14 +225,12 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
         corr[t][h] = ex2_approx(m_run[t][h] - base);
         moved |= m_new != m_run[t][h];
         m_run[t][h] = m_new;
-        float sum = 0.f;
+        l_run[t][h] *= corr[t][h];
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           s[t][n][2 * h] = ex2_approx(s[t][n][2 * h] - base);
           s[t][n][2 * h + 1] = ex2_approx(s[t][n][2 * h + 1] - base);
-          sum += s[t][n][2 * h] + s[t][n][2 * h + 1];
         }
-        l_run[t][h] = l_run[t][h] * corr[t][h] + sum;      // (this thread's columns; the row's four threads add up at the end)
       }
     if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
@@ -212,6 +244,19 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
         }
     }
   };
+  // Two neighbouring weights as operand elements, times the columns' value scales f (8-bit states); added to the running
+  // sum as rounded.  (The sum is this thread's; a row's four threads add up at the end.)
+  auto weight2 = [&](float w0, float w1, float f0, float f1, float r0, float r1, float& sum) -> uint32_t {
+    if constexpr (PLAIN) {
+      const uint32_t u = pack_bf16(w0, w1);
+      sum += __uint_as_float(u << 16) + __uint_as_float(u & 0xffff0000u);
+      return u;
+    } else {
+      const uint32_t u = pack_bf16(w0 * f0, w1 * f1);
+      sum += (f0 != 0.f ? __uint_as_float(u << 16) * r0 : w0) + (f1 != 0.f ? __uint_as_float(u & 0xffff0000u) * r1 : w1);
+      return u;
+    }
+  };
   auto q_frag = [&](int t, int ks, uint32_t (&a)[4]) {
     const uint4 w = q_s[((wr * MT + t) * (D / 16) + ks) * 32 + lane];
     a[0] = w.x; a[1] = w.y; a[2] = w.z; a[3] = w.w;
@@ -221,7 +266,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   for (int i = 0; i < n_tiles; ++i) {
     cp_async_wait<S::STAGES - 2>();
     __syncthreads();
-    if (i + S::STAGES - 1 < n_tiles) load_tile(i + S::STAGES - 1);
+    if (i + S::STAGES - 1 < n_loads) load_tile(i + S::STAGES - 1);
     cp_async_commit();
     const unsigned char* stp = ring + (i % S::STAGES) * S::STAGE;
     const uint32_t st = smem_addr(stp);
@@ -286,29 +331,23 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
         }
       }
     softmax(s);
-    if constexpr (!PLAIN) {
-      const float* vs_s = ks_s + C;
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float f = vs_s[kb + n * 8 + 2 * lc + e];
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            s[t][n][e] *= f;
-            s[t][n][2 + e] *= f;
-          }
-        }
-    }
 #pragma unroll
     for (int kk = 0; kk < KS / 16; ++kk) {
       uint32_t a[MT][4];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        a[t][0] = pack_bf16(s[t][2 * kk][0], s[t][2 * kk][1]);
-        a[t][1] = pack_bf16(s[t][2 * kk][2], s[t][2 * kk][3]);
-        a[t][2] = pack_bf16(s[t][2 * kk + 1][0], s[t][2 * kk + 1][1]);
-        a[t][3] = pack_bf16(s[t][2 * kk + 1][2], s[t][2 * kk + 1][3]);
+      for (int x = 0; x < 2; ++x) {
+        const int n = 2 * kk + x;
+        float f[2] = {1.f, 1.f}, r[2] = {1.f, 1.f};
+        if constexpr (!PLAIN) {
+          const float2 w = *reinterpret_cast<const float2*>(ks_s + C + kb + n * 8 + 2 * lc);
+          f[0] = w.x; f[1] = w.y;
+          r[0] = __frcp_rn(w.x); r[1] = __frcp_rn(w.y);
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          a[t][2 * x] = weight2(s[t][n][0], s[t][n][1], f[0], f[1], r[0], r[1], l_run[t][0]);
+          a[t][2 * x + 1] = weight2(s[t][n][2], s[t][n][3], f[0], f[1], r[0], r[1], l_run[t][1]);
+        }
       }
       if constexpr (PLAIN) {
 #pragma unroll
@@ -347,165 +386,120 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   }
   cp_async_wait<0>();
 
-  // The drafts: tiles of 64 more columns, in bf16, masked by ancestry.
+  // The drafts: up to 64 more columns, in bf16, masked by ancestry.
   uint32_t real = 0;        // bit 2 t + h: this thread's row is a node's, not padding
   if (last) {
-    __syncthreads();
-    unsigned char* dk = ring;
-    unsigned char* dv = ring + S::DRAFT_TILE;
-    int* par_s = reinterpret_cast<int*>(ring + 2 * S::DRAFT_TILE);
-    uint32_t* anc_s = reinterpret_cast<uint32_t*>(par_s + TREE_MAX_NODES);     // [node of this block][words]
-    int* odd_s = reinterpret_cast<int*>(anc_s + S::ROWS * TREE_ANC_WORDS);     // some value of the tile is not finite
-    const int n0 = row0 / p.G, n1 = min(p.N, (min(p.M, row0 + S::ROWS) - 1) / p.G + 1);
-    for (int i = tid; i < p.N; i += TREE_MMA_THREADS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
-    __syncthreads();
-    tree_ancestor_bits(p.N, n0, n1, par_s, anc_s, tid, TREE_MMA_THREADS);
-    for (int j0 = 0; j0 < p.N; j0 += C) {
-      if (tid == 0) *odd_s = 0;
-      __syncthreads();
-      bool odd = false;
-      for (int e = tid; e < C * (D / 8); e += TREE_MMA_THREADS) {
-        const int row = e / (D / 8), ch = e % (D / 8);
-        uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
-        if (j0 + row < p.N) {
-          const long long at = (((long long)(j0 + row) * p.B + b) * p.Hkv + hk) * D + ch * 8;
-          kw = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_new) + at);
-          vw = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.v_new) + at);
-          odd |= tree_drop_odd(vw);
-        }
-        *reinterpret_cast<uint4*>(dk + tree_off16<2 * D>(row, ch)) = kw;
-        *reinterpret_cast<uint4*>(dv + tree_off16<2 * D>(row, ch)) = vw;
+    unsigned char* dk = ring + (n_tiles % S::STAGES) * S::STAGE;
+    unsigned char* dv = PLAIN ? dk + S::TILE : ring + ((n_tiles + 1) % S::STAGES) * S::STAGE;
+    // A draft that a row does not see may hold anything, and 0 times an infinity is not 0: values that are not finite
+    // are taken out (each thread looks at the chunks it copied) and added at the end to the rows that see them.
+#pragma unroll
+    for (int x = 0; x < C * (D / 8) / TREE_MMA_THREADS; ++x) {
+      const int e = x * TREE_MMA_THREADS + tid;
+      uint4* at = reinterpret_cast<uint4*>(dv + tree_off16<2 * D>(e / (D / 8), e % (D / 8)));
+      uint4 w = *at;
+      if (tree_drop_odd(w)) {
+        *at = w;
+        odd_s = 1;
       }
-      if (odd) *odd_s = 1;
-      __syncthreads();
-      const int jw = j0 + kb;                 // this warp's first draft
-      if (jw < p.N) {
-        float s[MT][NB][4];
+    }
+    __syncthreads();
+    if (kb < p.N) {           // this warp has drafts
+      float s[MT][NB][4];
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t][n][e] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        uint32_t a[MT][4];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) q_frag(t, ks, a[t]);
+#pragma unroll
+        for (int n = 0; n < NB; n += 2) {
+          uint32_t f[4];
+          if constexpr (PLAIN) {
+            ldmatrix_x4(f, smem_addr(dk) + tree_off16<2 * D>(kb + n * 8 + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)));
+          } else {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint2 w = *reinterpret_cast<const uint2*>(
+                  dk + tree_off16<2 * D>(kb + (n + x) * 8 + lr, 8 * (ks >> 2) + 2 * lc + ((ks & 3) >> 1)) + (ks & 1) * 8);
+              f[2 * x] = w.x;
+              f[2 * x + 1] = w.y;
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            mma_bf16(s[t][n], a[t], f[0], f[1]);
+            mma_bf16(s[t][n + 1], a[t], f[2], f[3]);
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int m = (wr * MT + t) * 16 + lr + 8 * h;
+          const uint32_t* anc = anc_s[min(m, p.M - 1) / p.G];
+          const uint32_t a0 = m < p.M ? anc[0] : 0u, a1 = m < p.M ? anc[1] : 0u;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+            const int col = kb + n * 8 + 2 * lc;          // even: both columns are in one word
+            const uint32_t see = (col < 32 ? a0 : a1) >> (col & 31);
+            s[t][n][2 * h] = (see & 1u) ? s[t][n][2 * h] * p.scale2 : -INFINITY;
+            s[t][n][2 * h + 1] = (see & 2u) ? s[t][n][2 * h + 1] * p.scale2 : -INFINITY;
+          }
+        }
+      softmax(s);
+#pragma unroll
+      for (int kk = 0; kk < KS / 16; ++kk) {
+        uint32_t a[MT][4];
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
+          for (int x = 0; x < 2; ++x) {
+            a[t][2 * x] = weight2(s[t][2 * kk + x][0], s[t][2 * kk + x][1], 1.f, 1.f, 1.f, 1.f, l_run[t][0]);
+            a[t][2 * x + 1] = weight2(s[t][2 * kk + x][2], s[t][2 * kk + x][3], 1.f, 1.f, 1.f, 1.f, l_run[t][1]);
+          }
+        if constexpr (PLAIN) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][n][e] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          uint32_t a[MT][4];
-#pragma unroll
-          for (int t = 0; t < MT; ++t) q_frag(t, ks, a[t]);
-#pragma unroll
-          for (int n = 0; n < NB; n += 2) {
+          for (int j = 0; j < OB; j += 2) {
             uint32_t f[4];
-            if constexpr (PLAIN) {
-              ldmatrix_x4(f, smem_addr(dk) + tree_off16<2 * D>(kb + n * 8 + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)));
-            } else {
+            ldmatrix_x4_trans(f, smem_addr(dv) + tree_off16<2 * D>(kb + kk * 16 + (lane & 15), j + (lane >> 4)));
 #pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                const uint2 w = *reinterpret_cast<const uint2*>(
-                    dk + tree_off16<2 * D>(kb + (n + x) * 8 + lr, 8 * (ks >> 2) + 2 * lc + ((ks & 3) >> 1)) + (ks & 1) * 8);
-                f[2 * x] = w.x;
-                f[2 * x + 1] = w.y;
-              }
+            for (int t = 0; t < MT; ++t) {
+              mma_bf16(o[t][j], a[t], f[0], f[1]);
+              mma_bf16(o[t][j + 1], a[t], f[2], f[3]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < OB; j += 2) {               // O's columns (D/8) lr + j, + 1 of four drafts
+            uint32_t w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int row = kb + kk * 16 + 2 * lc + (r & 1) + 8 * (r >> 1);
+              const int d = OB * lr + j;
+              w[r] = *reinterpret_cast<const uint32_t*>(dv + tree_off16<2 * D>(row, d >> 3) + (d & 7) * 2);
             }
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-              mma_bf16(s[t][n], a[t], f[0], f[1]);
-              mma_bf16(s[t][n + 1], a[t], f[2], f[3]);
+              mma_bf16(o[t][j], a[t], __byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+              mma_bf16(o[t][j + 1], a[t], __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
             }
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int m = row0 + (wr * MT + t) * 16 + lr + 8 * h;
-            const uint32_t* anc = anc_s + (min(m, p.M - 1) / p.G - n0) * TREE_ANC_WORDS;
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-              const int col = jw + n * 8 + 2 * lc;          // even: both columns are in one word
-              const uint32_t see = col < p.N && m < p.M ? anc[col >> 5] >> (col & 31) : 0u;
-              s[t][n][2 * h] = (see & 1u) ? s[t][n][2 * h] * p.scale2 : -INFINITY;
-              s[t][n][2 * h + 1] = (see & 2u) ? s[t][n][2 * h + 1] * p.scale2 : -INFINITY;
-            }
-          }
-        softmax(s);
-#pragma unroll
-        for (int kk = 0; kk < KS / 16; ++kk) {
-          uint32_t a[MT][4];
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            a[t][0] = pack_bf16(s[t][2 * kk][0], s[t][2 * kk][1]);
-            a[t][1] = pack_bf16(s[t][2 * kk][2], s[t][2 * kk][3]);
-            a[t][2] = pack_bf16(s[t][2 * kk + 1][0], s[t][2 * kk + 1][1]);
-            a[t][3] = pack_bf16(s[t][2 * kk + 1][2], s[t][2 * kk + 1][3]);
-          }
-          if constexpr (PLAIN) {
-#pragma unroll
-            for (int j = 0; j < OB; j += 2) {
-              uint32_t f[4];
-              ldmatrix_x4_trans(f, smem_addr(dv) + tree_off16<2 * D>(kb + kk * 16 + (lane & 15), j + (lane >> 4)));
-#pragma unroll
-              for (int t = 0; t < MT; ++t) {
-                mma_bf16(o[t][j], a[t], f[0], f[1]);
-                mma_bf16(o[t][j + 1], a[t], f[2], f[3]);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < OB; j += 2) {               // O's columns (D/8) lr + j, + 1 of four drafts
-              uint32_t w[4];
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int row = kb + kk * 16 + 2 * lc + (r & 1) + 8 * (r >> 1);
-                const int d = OB * lr + j;
-                w[r] = *reinterpret_cast<const uint32_t*>(dv + tree_off16<2 * D>(row, d >> 3) + (d & 7) * 2);
-              }
-#pragma unroll
-              for (int t = 0; t < MT; ++t) {
-                mma_bf16(o[t][j], a[t], __byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
-                mma_bf16(o[t][j + 1], a[t], __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
-              }
-            }
-          }
-        }
-        if (*odd_s) {
-          // Values that are not finite were left out of the contraction, where a weight of zero would not have kept them
-          // from the rows that do not see them; they are added here to the rows that do.
-          for (int x = 0; x < KS && jw + x < p.N; ++x) {
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.v_new) + (((long long)(jw + x) * p.B + b) * p.Hkv + hk) * D;
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float mine = 0.f;
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                  for (int e = 0; e < 2; ++e)
-                    if (n == (x >> 3) && e == (x & 1)) mine = s[t][n][2 * h + e];
-                const float w = __shfl_sync(0xffffffffu, mine, (lane & ~3) | ((x & 7) >> 1));
-                if (w == 0.f) continue;
-#pragma unroll
-                for (int j = 0; j < OB; ++j)
-#pragma unroll
-                  for (int e = 0; e < 2; ++e) {
-                    const float v = __bfloat162float(src[PLAIN ? 8 * j + 2 * lc + e : OB * (2 * lc + e) + j]);
-                    if (!isfinite(v)) o[t][j][2 * h + e] += w * v;
-                  }
-              }
           }
         }
       }
-      __syncthreads();
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int m = row0 + (wr * MT + t) * 16 + lr + 8 * h;
-        if (m < p.M) {
-          const int n = m / p.G;
-          real |= ((anc_s[(n - n0) * TREE_ANC_WORDS + (n >> 5)] >> (n & 31)) & 1u) << (2 * t + h);
-        }
+        const int m = (wr * MT + t) * 16 + lr + 8 * h;
+        if (m < p.M) real |= (uint32_t)((anc_s[m / p.G][0] | anc_s[m / p.G][1]) != 0) << (2 * t + h);
       }
   }
   pdl_launch_dependents();
@@ -548,7 +542,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   __syncthreads();
   for (int e = tid; e < S::ROWS * (D / 4); e += TREE_MMA_THREADS) {
     const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-    const int m = row0 + r;
+    const int m = r;
     if (m >= p.M) continue;
     float top = -INFINITY, l = 0.f;
     bool pad = false;
@@ -563,9 +557,14 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
       const float4 x = *reinterpret_cast<const float4*>(o_s + (w * S::ROWS + r) * D + d);
       acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
     }
+    const int n = m / p.G, g = m - n * p.G;
+    if (last && odd_s && !pad) {
+      float v[4] = {acc.x, acc.y, acc.z, acc.w};
+      tree_add_odd<2, 4>(p, b, hk, anc_s[n], D, d, v);
+      acc = make_float4(v[0], v[1], v[2], v[3]);
+    }
     if (p.splits == 1) {
       const float f = l == 0.f ? 0.f : 1.f / l;
-      const int n = m / p.G, g = m - n * p.G;
       __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
       if (pad) tree_store4<__nv_bfloat16>(dst, 0.f, 0.f, 0.f, 0.f);
       else tree_store4<__nv_bfloat16>(dst, acc.x * f, acc.y * f, acc.z * f, acc.w * f);
