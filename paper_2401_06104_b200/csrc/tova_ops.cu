@@ -308,9 +308,9 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
   if (c.dtype == TOVA_DTYPE_BF16) {
     t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : M <= 64 ? TREE_MMA_64 : M <= 128 ? TREE_TC_1 : TREE_TC_2;
     rows = M <= 64 ? 64 : M <= 128 ? tova::TREE_TC_ROWS : 2 * tova::TREE_TC_ROWS;
-    cols = tova::TREE_MMA_COLS;
+    cols = M <= 64 ? tova::TREE_MMA_COLS : tova::TREE_TC_COLS;
     if (t.kernel == TREE_TC_2) resident = sm_count;
-    if (M > 64) shortest = 8;
+    if (M > 64) shortest = 4;
   }
   t.row_blocks = (M + rows - 1) / rows;
   const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;

@@ -1,19 +1,22 @@
 // Attention of drafted tokens over a state on the 5th-generation tensor cores (see tova_tree.cuh for the operation):
 // bf16 queries, more than 64 rows of the product (nodes x query heads of a KV head).
 //
-// A block takes NT tiles of 128 rows and runs down its columns in tiles of 64; row i of a tile is TMEM lane i.  Roles:
+// A block takes NT tiles of 128 rows and runs down its columns in tiles of 128; row i of a tile is TMEM lane i.  Roles:
 //   4 producer warps    K and V tiles into a ring of shared-memory slots in the 128-byte-swizzled layout the tensor cores
-//                       read: bf16 states by cp.async several slots ahead; 8-bit states through a raw ring (every thread
-//                       converts the chunks it copied itself, exactly, see tova_tree_mma.cuh); drafts, the last tiles,
-//                       by plain loads that take out infinities and NaN.  Columns behind the run are zeros.
-//   1 issuing thread    S = Q K^T (128 x 64, fp32 in TMEM, two buffers a row tile) one tile ahead of O += P V
-//   4 warps a row tile  one thread per row: logits from TMEM, mask, running maximum, weights as bf16 back into the logits'
-//                       columns as the A operand of O += P V.  The sum is taken over the rounded weights, so that the
+//                       read: bf16 states by cp.async, as far ahead as there are slots; 8-bit states through registers,
+//                       converted exactly (see tova_tree_mma.cuh); drafts, the last tiles, by plain loads that take out
+//                       infinities and NaN.  Columns behind the run are zeros, whatever lies there.
+//   1 issuing thread    S = Q K^T (128 x 128, fp32 in TMEM) and O += P V in the order PV_0(i) S_0(i+1) PV_1(i) S_1(i+1):
+//                       the tensor cores work on one row tile while the other's soft-max runs (two row tiles in a block,
+//                       or two blocks on an SM)
+//   4 warps a row tile  one thread per row: logits from TMEM, mask, running maximum, weights as bf16 back over the logits,
+//                       where they are the A operand of O += P V.  The sum is taken over the rounded weights, so that the
 //                       weights that multiply V add up to one.  The reference maximum moves only when a tile's exceeds it
 //                       by more than 2^8: weights up to 256 lose nothing in floating point, and O is almost never rescaled.
-// The roles meet through mbarriers.  One row tile: 256 TMEM columns and 113 KiB, two blocks per SM; two row tiles (more
-// than 128 rows): all 512 columns, one block per SM, and every K and V tile feeds both.  A barrier per S buffer and kind:
-// a waiter can then never be two phases behind.  Every wait is bounded; one that runs out leaves NaN in the block's rows.
+// A tile of 128 columns, not 64, because S = Q K^T reads both operands from shared memory: 8 KiB per 64 cycles of math
+// (128 x 128 x 16) are what shared memory delivers, 6 KiB per 32 cycles (128 x 64 x 16) are not.  TMEM: 256 columns per row
+// tile (S 128, O 128).  One row tile: two blocks per SM; two row tiles (more than 128 rows): one block per SM, and every K
+// and V tile feeds both.  Every wait is bounded; one that runs out leaves NaN in the block's rows.
 #pragma once
 
 #include "tova_tree_mma.cuh"
@@ -21,8 +24,7 @@
 namespace tova {
 
 constexpr int TREE_TC_ROWS = 128;      // rows of a tile
-constexpr int TREE_TC_COLS = 64;
-constexpr int TREE_TC_SCALE_TILES = 8; // tiles whose scales are kept: more than the ring reaches ahead
+constexpr int TREE_TC_COLS = 128;      // columns of a tile
 constexpr float TREE_TC_SLACK = 8.f;   // log2 of how far weights may exceed 1 before O is rescaled
 
 template <int D, int FMT, int NT>
@@ -31,15 +33,23 @@ struct TreeTcShape {
   static constexpr int THREADS = 32 * (SOFT_WARPS + 4 + 1);
   static constexpr int Q_BYTES = TREE_TC_ROWS * D * 2;            // per row tile
   static constexpr int SLOT = TREE_TC_COLS * D * 2;
-  static constexpr int RAW = FMT == FORMAT_PLAIN ? 0 : TREE_TC_COLS * D;
-  static constexpr int RAW_SLOTS = FMT == FORMAT_PLAIN ? 0 : (NT == 1 ? 3 : 6);
-  static constexpr int SCALES = FMT == FORMAT_PLAIN ? 0 : TREE_TC_SCALE_TILES * 2 * TREE_TC_COLS * 4;
-  static constexpr int SLOTS = NT == 1 ? (FMT == FORMAT_PLAIN ? 4 : 3) : (FMT == FORMAT_PLAIN ? 9 : 6);
-  static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + RAW_SLOTS * RAW + SCALES + 1024;
+  static constexpr int SLOTS = (NT == 1 ? 2 : 4) * (128 / D);
+  // Tiles whose scales are kept.  K of tile i takes the slot of K of tile i - SLOTS/2; S of that tile is complete then, so
+  // the soft-max of all tiles before it has passed: their scales may go.
+  static constexpr int SCALE_TILES = SLOTS / 2 + 2;
+  static constexpr int SCALES = FMT == FORMAT_PLAIN ? 0 : SCALE_TILES * 2 * TREE_TC_COLS * 4;
+  static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + SCALES + 1024;
   static constexpr int TMEM_COLS = 256 * NT;
   static constexpr int NODES = NT == 1 ? TREE_TC_ROWS : TREE_MAX_NODES;   // one row tile: M <= 128, so N <= 128
   static constexpr int WORDS = NODES / 32;
+  // after the last contraction Q and the ring hold the rows of O on their way out
+  static_assert(NT * TREE_TC_ROWS * D * 4 <= NT * Q_BYTES + SLOTS * SLOT, "O fits");
 };
+
+// The mbarrier receives this thread's arrival (counted in its initial count) once its cp.async so far have landed.
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
 
 template <int D, int FMT, int NT>
 __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, NT == 1 ? 2 : 1)
@@ -47,13 +57,13 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, NT == 1 ? 2 
   using S = TreeTcShape<D, FMT, NT>;
   constexpr bool PLAIN = FMT == FORMAT_PLAIN;
   constexpr int C = TREE_TC_COLS, R = TREE_TC_ROWS;
+  constexpr int PRODUCER = S::SOFT_WARPS, ISSUER = S::SOFT_WARPS + 4;      // first warp of each role
   extern __shared__ unsigned char tree_tc_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tree_tc_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* q_s = smem;                               // per row tile: boxes of [128 rows][128 bytes]
-  unsigned char* slot_s = q_s + NT * S::Q_BYTES;           // per slot: boxes of [64 rows][128 bytes]
-  unsigned char* raw_s = slot_s + S::SLOTS * S::SLOT;
-  float* scale_s = reinterpret_cast<float*>(raw_s + S::RAW_SLOTS * S::RAW);   // [tile % 8][k, v][64]
-  __shared__ __align__(8) uint64_t full[S::SLOTS], empty[S::SLOTS], bar_s[NT][2], bar_p[NT][2], bar_o[NT][2], bar_sc[TREE_TC_SCALE_TILES];
+  unsigned char* slot_s = q_s + NT * S::Q_BYTES;           // per slot: boxes of [128 rows][128 bytes]
+  float* scale_s = reinterpret_cast<float*>(slot_s + S::SLOTS * S::SLOT);   // [tile % SCALE_TILES][k, v][128]
+  __shared__ __align__(8) uint64_t full[S::SLOTS], empty[S::SLOTS], bar_q, bar_s[NT], bar_p[NT], bar_o[NT], bar_sc[S::SCALE_TILES];
   __shared__ uint32_t tmem_base_s;
   __shared__ int odd_s;
   __shared__ int par_s[S::NODES];
@@ -74,255 +84,246 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, NT == 1 ? 2 
       mbar_init(&full[i], 128);
       mbar_init(&empty[i], 1);
     }
-    for (int t = 0; t < NT; ++t)
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(&bar_s[t][i], 1);
-        mbar_init(&bar_p[t][i], R);
-        mbar_init(&bar_o[t][i], 1);
-      }
-    for (int i = 0; i < TREE_TC_SCALE_TILES; ++i) mbar_init(&bar_sc[i], 128);
+    mbar_init(&bar_q, R * NT);
+    for (int t = 0; t < NT; ++t) {
+      mbar_init(&bar_s[t], 1);
+      mbar_init(&bar_p[t], R);
+      mbar_init(&bar_o[t], 1);
+    }
+    for (int i = 0; i < S::SCALE_TILES; ++i) mbar_init(&bar_sc[i], 128);
     mbar_fence_init();
     odd_s = 0;
   }
-  if (warp == S::SOFT_WARPS + 4) {
+  if (warp == ISSUER) {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_s)), "r"(S::TMEM_COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (last)
-    for (int i = tid; i < p.N; i += S::THREADS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
-  // Q rows, K-major with the 128-byte swizzle; rows past the product are zeros.
-  for (int e = tid; e < NT * R * (D / 8); e += S::THREADS) {
-    const int r = e / (D / 8), ch = e % (D / 8);
-    const int m = row0 + r;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (m < p.M) {
-      const int nd = m / p.G, g = m - nd * p.G;
-      w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + (((long long)nd * p.B + b) * p.H + hk * p.G + g) * D + ch * 8);
-    }
-    *reinterpret_cast<uint4*>(q_s + (r / R) * S::Q_BYTES + (ch >> 3) * (R * 128) + (r % R) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = w;
-  }
-  fence_proxy_async_smem();      // the tensor cores read Q through the asynchronous proxy
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
-
-  // Order in which the tiles are copied and consumed: K0 | K1 V0 | K2 V1 | ... | K(n-1) V(n-2) | V(n-1).
-  auto pos_k = [&](int i) { return i == 0 ? 0 : 2 * i - 1; };
-  auto pos_v = [&](int i) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; };
   bool ok = true;
+  // Copies are made and consumed in the order K0 V0 K1 V1 ...: position 2 i is K of tile i, 2 i + 1 its V.
 
-  if (warp >= S::SOFT_WARPS && warp < S::SOFT_WARPS + 4) {
+  if (warp >= PRODUCER && warp < ISSUER) {
     // ============================== producers ==============================
-    const int pt = tid - S::SOFT_WARPS * 32;
-    const unsigned char* Kg = static_cast<const unsigned char*>(p.K) + (long long)blockIdx.z * p.cap * (PLAIN ? 2 * D : D);
-    const unsigned char* Vg = static_cast<const unsigned char*>(p.V) + (long long)blockIdx.z * p.cap * (PLAIN ? 2 * D : D);
-    auto decode = [&](int pos, bool& is_k, int& tile) {
-      if (pos == 0) { is_k = true; tile = 0; }
-      else if (pos == 2 * n - 1) { is_k = false; tile = n - 1; }
-      else { is_k = pos & 1; tile = is_k ? (pos + 1) / 2 : pos / 2 - 1; }
-    };
+    const int pt = tid - PRODUCER * 32;
     auto slot_free = [&](int pos) {
       return pos < S::SLOTS || mbar_wait_bounded(&empty[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS - 1) & 1));
     };
-    // One scale a thread and tile, fetched a tile early and stored with the tile's K (the slot that K goes to was freed
-    // by a tile less than TREE_TC_SCALE_TILES back, whose scales and all before them are used up).
-    auto scale_of = [&](int tile) {
-      const int j = c0 + tile * C + (pt & 63);
-      const float* src = (pt < 64 ? p.k_scale : p.v_scale) + (long long)blockIdx.z * p.cap;
-      return tile < n_state ? (j < c1 ? src[j] : 0.f) : 1.f;
-    };
-    float next_scale = PLAIN ? 0.f : scale_of(0);
-    auto scales = [&](int tile) {
-      scale_s[((tile % TREE_TC_SCALE_TILES) * 2 + (pt >> 6)) * C + (pt & 63)] = next_scale;
-      mbar_arrive(&bar_sc[tile % TREE_TC_SCALE_TILES]);
-      next_scale = scale_of(tile + 1);
-    };
-    auto draft = [&](int pos, bool is_k, int tile) {
+    // Where 16-byte chunk ch of row `row` lies in a slot.
+    auto place = [&](int row, int ch) { return (ch >> 3) * (C * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4); };
+    auto draft = [&](int pos) {
+      const bool is_k = !(pos & 1);
       unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
       const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_k ? p.k_new : p.v_new);
       bool odd = false;
 #pragma unroll 4
       for (int e = pt; e < C * (D / 8); e += 128) {
-        const int row = e / (D / 8), ch = e % (D / 8), j = (tile - n_state) * C + row;
+        const int row = e / (D / 8), ch = e % (D / 8), j = (pos / 2 - n_state) * C + row;
         uint4 w = make_uint4(0, 0, 0, 0);
         if (j < p.N) {
           w = *reinterpret_cast<const uint4*>(src + (((long long)j * p.B + b) * p.Hkv + hk) * D + ch * 8);
           if (!is_k) odd |= tree_drop_odd(w);
         }
-        *reinterpret_cast<uint4*>(dst + (ch >> 3) * (C * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = w;
+        *reinterpret_cast<uint4*>(dst + place(row, ch)) = w;
       }
       if (odd) odd_s = 1;
+      fence_proxy_async_smem();
+      mbar_arrive(&full[pos % S::SLOTS]);
     };
     if constexpr (PLAIN) {
-      constexpr int AHEAD = S::SLOTS - 2;
-      for (int pos = 0; pos < 2 * n + AHEAD && ok; ++pos) {
-        if (pos < 2 * n) {
-          bool is_k;
-          int tile;
-          decode(pos, is_k, tile);
-          ok = slot_free(pos);
-          if (!ok) break;
-          if (tile < n_state) {
-            const int j0 = c0 + tile * C;
-            const uint32_t dst = smem_addr(slot_s + (pos % S::SLOTS) * S::SLOT);
-            const unsigned char* g = is_k ? Kg : Vg;
-#pragma unroll
-            for (int x = 0; x < C * (D / 8) / 128; ++x) {
-              const int e = x * 128 + pt;
-              const int row = e / (D / 8), ch = e % (D / 8);
-              const bool in = j0 + row < c1;
-              cp_async16(dst + (ch >> 3) * (C * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4),
-                         g + (long long)(in ? j0 + row : c0) * (2 * D) + ch * 16, in ? 16u : 0u);
-            }
-          } else {
-            draft(pos, is_k, tile);
-          }
-        }
-        cp_async_commit();
-        if (pos >= AHEAD) {
-          cp_async_wait<AHEAD>();
-          fence_proxy_async_smem();
-          mbar_arrive(&full[(pos - AHEAD) % S::SLOTS]);
-        }
-      }
-      cp_async_wait<0>();
-    } else {
-      constexpr int AHEAD = S::RAW_SLOTS - 1;
-      constexpr int CHR = D / 16;                    // 16-byte chunks of a row of codes
-      constexpr int PER = C * CHR / 128;             // chunks of a thread
-      auto fetch = [&](int pos) {
-        bool is_k;
-        int tile;
-        decode(pos, is_k, tile);
-        if (tile >= n_state) return;
-        const int j0 = c0 + tile * C;
-        const unsigned char* g = is_k ? Kg : Vg;
-        const uint32_t dst = smem_addr(raw_s + (pos % S::RAW_SLOTS) * S::RAW);
-#pragma unroll
-        for (int x = 0; x < PER; ++x) {
-          const int e = x * 128 + pt;
-          const int row = e / CHR, ch = e % CHR;
-          const bool in = j0 + row < c1;
-          cp_async16(dst + e * 16, g + (long long)(in ? j0 + row : c0) * D + ch * 16, in ? 16u : 0u);
-        }
-      };
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        if (i < 2 * n) fetch(i);
-        cp_async_commit();
-      }
-      for (int pos = 0; pos < 2 * n; ++pos) {
-        bool is_k;
-        int tile;
-        decode(pos, is_k, tile);
-        if (pos + AHEAD < 2 * n) fetch(pos + AHEAD);
-        cp_async_commit();
+      const unsigned char* g[2] = {static_cast<const unsigned char*>(p.K) + (long long)blockIdx.z * p.cap * (2 * D),
+                                   static_cast<const unsigned char*>(p.V) + (long long)blockIdx.z * p.cap * (2 * D)};
+      constexpr int CH = D / 8, STEP = 128 / CH;           // a thread's chunks: one column, every STEP-th row
+      const int row_t = pt / CH, ch_t = pt % CH;
+      for (int pos = 0; pos < 2 * n && ok; ++pos) {
         ok = slot_free(pos);
         if (!ok) break;
-        if (is_k) scales(tile);
-        if (tile < n_state) {
-          cp_async_wait<AHEAD>();
-          unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
-          const unsigned char* src = raw_s + (pos % S::RAW_SLOTS) * S::RAW;
+        if (pos / 2 < n_state) {
+          const int j0 = c0 + (pos / 2) * C;
+          const uint32_t dst = smem_addr(slot_s + (pos % S::SLOTS) * S::SLOT);
+          const unsigned char* src = ((pos & 1) ? g[1] : g[0]) + ch_t * 16;
 #pragma unroll
-          for (int x = 0; x < PER; ++x) {
-            const int e = x * 128 + pt;
-            const int row = e / CHR, ch = (e % CHR) * 2;
-            const uint4 w = *reinterpret_cast<const uint4*>(src + e * 16);
-            const uint4 lo = make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
-                                        tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
-            const uint4 hi = make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
-                                        tree_codes2<FMT>(w.w, w.w, 0, 1), tree_codes2<FMT>(w.w, w.w, 2, 3));
-            unsigned char* line = dst + (ch >> 3) * (C * 128) + row * 128;
-            *reinterpret_cast<uint4*>(line + (((ch & 7) ^ (row & 7)) << 4)) = lo;
-            *reinterpret_cast<uint4*>(line + ((((ch & 7) + 1) ^ (row & 7)) << 4)) = hi;
+          for (int x = 0; x < C / STEP; ++x) {
+            const int row = x * STEP + row_t;
+            const bool in = j0 + row < c1;
+            cp_async16(dst + place(row, ch_t), src + (long long)(in ? j0 + row : c0) * (2 * D), in ? 16u : 0u);
           }
+          cp_async_arrive(&full[pos % S::SLOTS]);
         } else {
-          draft(pos, is_k, tile);
+          draft(pos);
+        }
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+    } else {
+      const unsigned char* g[2] = {static_cast<const unsigned char*>(p.K) + (long long)blockIdx.z * p.cap * D,
+                                   static_cast<const unsigned char*>(p.V) + (long long)blockIdx.z * p.cap * D};
+      constexpr int CH = D / 16, STEP = 128 / CH, PER = C / STEP;
+      const int row_t = pt / CH, ch_t = pt % CH;
+      uint4 raw[PER];                  // this thread's chunks of the position that comes next
+      auto fetch = [&](int pos) {
+        const int j0 = c0 + (pos / 2) * C;
+        const unsigned char* src = ((pos & 1) ? g[1] : g[0]) + ch_t * 16;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const int j = j0 + x * STEP + row_t;
+          raw[x] = pos / 2 < n_state && j < c1 ? *reinterpret_cast<const uint4*>(src + (long long)j * D) : make_uint4(0, 0, 0, 0);
+        }
+      };
+      // Two scales a thread and tile, fetched a tile early and stored with the tile's K.
+      float next_k, next_v;
+      auto fetch_scales = [&](int tile) {
+        const int j = c0 + tile * C + pt;
+        const bool in = j < c1;
+        next_k = tile < n_state ? (in ? p.k_scale[(long long)blockIdx.z * p.cap + j] : 0.f) : 1.f;
+        next_v = tile < n_state ? (in ? p.v_scale[(long long)blockIdx.z * p.cap + j] : 0.f) : 1.f;
+      };
+      fetch(0);
+      fetch_scales(0);
+      for (int pos = 0; pos < 2 * n; ++pos) {
+        const int tile = pos / 2;
+        ok = slot_free(pos);
+        if (!ok) break;
+        if (!(pos & 1)) {
+          float* sc = scale_s + (tile % S::SCALE_TILES) * 2 * C;
+          sc[pt] = next_k;
+          sc[C + pt] = next_v;
+          mbar_arrive(&bar_sc[tile % S::SCALE_TILES]);
+          fetch_scales(tile + 1);
+        }
+        if (tile >= n_state) {
+          draft(pos);
+          continue;
+        }
+        unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
+        uint4 now[PER];
+#pragma unroll
+        for (int x = 0; x < PER; ++x) now[x] = raw[x];
+        fetch(pos + 1);
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+          const int row = x * STEP + row_t;
+          const uint4 w = now[x];
+          *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t)) =
+              make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
+                         tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
+          *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + 1)) =
+              make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
+                         tree_codes2<FMT>(w.w, w.w, 0, 1), tree_codes2<FMT>(w.w, w.w, 2, 3));
         }
         fence_proxy_async_smem();
         mbar_arrive(&full[pos % S::SLOTS]);
       }
-      cp_async_wait<0>();
     }
-  } else if (warp == S::SOFT_WARPS + 4) {
+    named_barrier_sync(1, 32 * ISSUER);          // odd_s is final
+  } else if (warp == ISSUER) {
     // ============================== issuing thread ==============================
     if (lane == 0 && n > 0) {
       const uint32_t idesc_s = umma_idesc_bf16(R, C, false);
       const uint32_t idesc_o = umma_idesc_bf16(R, D, true);
       const uint32_t q_a = smem_addr(q_s), slot_a = smem_addr(slot_s);
-      auto issue_s = [&](int i) {
-        const int pos = pos_k(i);
+      // cp.async writes through the generic proxy: a tile that has landed is ordered before the tensor cores' reads by a
+      // proxy fence here, behind the wait.
+      auto landed = [&](int pos) {
         if (!mbar_wait_bounded(&full[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS) & 1))) return false;
-        tc_fence_after();
-        const uint32_t k_a = slot_a + (pos % S::SLOTS) * S::SLOT;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint64_t a = umma_desc_sw128(q_a + t * S::Q_BYTES + (ks >> 2) * (R * 128) + (ks & 3) * 32, 16, 1024);
-            const uint64_t bd = umma_desc_sw128(k_a + (ks >> 2) * (C * 128) + (ks & 3) * 32, 16, 1024);
-            umma_bf16(tmem + 256 * t + 64 * (i & 1), a, bd, idesc_s, ks > 0 ? 1u : 0u);
-          }
-          umma_commit(&bar_s[t][i & 1]);
-        }
-        umma_commit(&empty[pos % S::SLOTS]);
+        fence_proxy_async_smem();
         return true;
       };
-      ok = issue_s(0);
+      auto issue_s = [&](int t, int i) {
+        const uint32_t k_a = slot_a + ((2 * i) % S::SLOTS) * S::SLOT;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint64_t a = umma_desc_sw128(q_a + t * S::Q_BYTES + (ks >> 2) * (R * 128) + (ks & 3) * 32, 16, 1024);
+          const uint64_t bd = umma_desc_sw128(k_a + (ks >> 2) * (C * 128) + (ks & 3) * 32, 16, 1024);
+          umma_bf16(tmem + 256 * t, a, bd, idesc_s, ks > 0 ? 1u : 0u);
+        }
+        umma_commit(&bar_s[t]);
+        if (t == NT - 1) umma_commit(&empty[(2 * i) % S::SLOTS]);
+      };
+      ok = mbar_wait_bounded(&bar_q, 0u) && landed(0);
+      if (ok) {
+        tc_fence_after();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) issue_s(t, 0);
+      }
       for (int i = 0; i < n && ok; ++i) {
-        if (i + 1 < n && !(ok = issue_s(i + 1))) break;
-        const int pos = pos_v(i);
-        ok = mbar_wait_bounded(&full[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS) & 1));
-        const uint32_t v_a = slot_a + (pos % S::SLOTS) * S::SLOT;
+        const uint32_t v_a = slot_a + ((2 * i + 1) % S::SLOTS) * S::SLOT;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          ok = ok && mbar_wait_bounded(&bar_p[t][i & 1], (uint32_t)((i >> 1) & 1));
+          if (t == 0) ok = landed(2 * i + 1);
+          ok = ok && mbar_wait_bounded(&bar_p[t], (uint32_t)(i & 1));
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
           for (int kk = 0; kk < C / 16; ++kk)
-            umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + 64 * (i & 1) + kk * 8, umma_desc_sw128(v_a + kk * 2048, C * 128, 1024),
-                             idesc_o, (i > 0 || kk > 0) ? 1u : 0u);
-          umma_commit(&bar_o[t][i & 1]);
+            umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + kk * 8, umma_desc_sw128(v_a + kk * 2048, C * 128, 1024), idesc_o,
+                             (i > 0 || kk > 0) ? 1u : 0u);
+          if (t == NT - 1) umma_commit(&empty[(2 * i + 1) % S::SLOTS]);
+          if (i + 1 < n) {
+            if (t == 0) ok = landed(2 * i + 2);
+            if (!ok) break;
+            tc_fence_after();
+            issue_s(t, i + 1);
+          } else {
+            umma_commit(&bar_o[t]);
+          }
         }
-        if (ok) umma_commit(&empty[pos % S::SLOTS]);
       }
     }
   } else {
     // ============================== soft-max: one thread per row ==============================
     const int t = warp >> 2;
     const uint32_t base = tmem + 256 * t + ((uint32_t)((warp & 3) * 32) << 16);
-    const int m = row0 + t * R + (warp & 3) * 32 + lane;
-    const int node = m < p.M ? m / p.G : -1;
-    if (last) {
-      for (int i = tid; i < p.N; i += 32 * S::SOFT_WARPS) tree_ancestor_bits<S::WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
-      named_barrier_sync(2, 32 * S::SOFT_WARPS);
+    const int m0 = row0 + t * R + (warp & 3) * 32;       // the warp's first row
+    const int node = m0 + lane < p.M ? (m0 + lane) / p.G : -1;
+    // Q rows of the row tile, K-major with the 128-byte swizzle; rows past the product are zeros.
+    {
+      constexpr int CH = D / 8, STEP = 128 / CH;
+      const int x = tid & 127, row_t = x / CH, ch = x % CH;
+      const uint32_t dst = smem_addr(q_s + t * S::Q_BYTES) + (ch >> 3) * (R * 128);
+#pragma unroll 4
+      for (int k = 0; k < R / STEP; ++k) {
+        const int r = k * STEP + row_t, m = row0 + t * R + r;
+        const int nd = min(m, p.M - 1) / p.G, g = min(m, p.M - 1) - nd * p.G;
+        cp_async16(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
+                   static_cast<const __nv_bfloat16*>(p.q) + (((long long)nd * p.B + b) * p.H + hk * p.G + g) * D + ch * 8, m < p.M ? 16u : 0u);
+      }
+      cp_async_commit();
     }
+    if (last) {
+      for (int i = tid; i < p.N; i += 32 * S::SOFT_WARPS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
+      named_barrier_sync(2, 32 * S::SOFT_WARPS);
+      for (int i = tid; i < p.N; i += 32 * S::SOFT_WARPS) tree_ancestor_bits<S::WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
+    }
+    cp_async_wait<0>();
+    fence_proxy_async_smem();
+    mbar_arrive(&bar_q);
+    named_barrier_sync(2, 32 * S::SOFT_WARPS);
     const uint32_t* anc = anc_s[max(node, 0)];
     bool real = false;               // a node's row, not padding's or one behind the product
     if (last && node >= 0) {
 #pragma unroll
-      for (int k = 0; k < S::WORDS; ++k) real |= anc[k] != 0;       // (words past N's are zero: bits only go down from i)
+      for (int k = 0; k < S::WORDS; ++k) real |= anc[k] != 0;
     }
     float m_ref = -INFINITY, l = 0.f;
+    const uint64_t scale_2 = pack_f2(p.scale2, p.scale2);
     for (int i = 0; i < n; ++i) {
-      const uint32_t tm_s = base + 64 * (i & 1);
-      const float* sc = scale_s + (i % TREE_TC_SCALE_TILES) * 2 * C;
-      ok = mbar_wait_bounded(&bar_s[t][i & 1], (uint32_t)((i >> 1) & 1));
-      if constexpr (!PLAIN) ok = ok && mbar_wait_bounded(&bar_sc[i % TREE_TC_SCALE_TILES], (uint32_t)((i / TREE_TC_SCALE_TILES) & 1));
+      const float* sc = scale_s + (i % S::SCALE_TILES) * 2 * C;
+      ok = mbar_wait_bounded(&bar_s[t], (uint32_t)(i & 1));
+      if constexpr (!PLAIN) ok = ok && mbar_wait_bounded(&bar_sc[i % S::SCALE_TILES], (uint32_t)((i / S::SCALE_TILES) & 1));
       ok = __all_sync(0xffffffffu, ok) != 0;
       if (!ok) break;
       tc_fence_after();
-      // Half a row's logits at a time; the first half is read again after the maximum is known, which costs less than 32
-      // more registers a thread would.
+      // A quarter of a row's logits at a time, read once for the maximum and again for the weights: that costs less than 128
+      // registers a thread would.
       const int left = i < n_state ? c1 - (c0 + i * C) : C;
       float s[32];
       auto logits = [&](int h) {
-        tmem_ld32(tm_s + 32 * h, s);
+        tmem_ld32(base + 32 * h, s);
         if constexpr (!PLAIN) {
 #pragma unroll
           for (int c = 0; c < 32; c += 4) {
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, NT == 1 ? 2 
           }
         }
         if (i >= n_state) {
-          const int w = 2 * (i - n_state) + h;
+          const int w = 4 * (i - n_state) + h;
           const uint32_t see = real && w < S::WORDS ? anc[w] : 0u;
 #pragma unroll
           for (int c = 0; c < 32; ++c) s[c] = ((see >> c) & 1u) ? s[c] : -INFINITY;
@@ -340,112 +341,114 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, NT == 1 ? 2 
           for (int c = 0; c < 32; ++c) s[c] = 32 * h + c < left ? s[c] : -INFINITY;
         }
       };
-      auto top_of = [&]() {
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        logits(h);
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
         for (int c = 4; c < 32; c += 4)
 #pragma unroll
           for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[c + k]);
-        return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      };
-      logits(0);
-      float top = top_of();
-      logits(1);
-      top = fmaxf(top, top_of()) * p.scale2;
+        top = fmaxf(top, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+      }
+      top *= p.scale2;
       float corr = 1.f;
       if (top > m_ref + TREE_TC_SLACK || (m_ref == -INFINITY && top > -INFINITY)) {
         corr = ex2_approx(m_ref - top);
         m_ref = top;
         l *= corr;
       }
+      __syncwarp();
+      // O of the tiles so far was summed against the old reference.  (The last of them is complete: S of this tile was
+      // issued behind it.)
+      if (i > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          tmem_ld32(base + 128 + c, s);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[k] *= corr;
+          tmem_st32(base + 128 + c, s);
+        }
+      }
       const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-      const uint64_t scale_2 = pack_f2(p.scale2, p.scale2), mneg_2 = pack_f2(-ref, -ref);
+      const uint64_t mneg_2 = pack_f2(-ref, -ref);
       uint64_t sum2[2] = {pack_f2(0.f, 0.f), pack_f2(0.f, 0.f)};
-      float w[32];            // packed weights, two bf16 each
-      auto weights = [&](int h) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        logits(h);
+        uint32_t w[16];            // packed weights, two bf16 each
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float x0, x1;
           unpack_f2(fma_f2(pack_f2(s[2 * e], s[2 * e + 1]), scale_2, mneg_2), x0, x1);
           const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
-          uint32_t u;
           if constexpr (PLAIN) {
-            u = pack_bf16(e0, e1);
-            sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
+            w[e] = pack_bf16(e0, e1);
+            sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)));
           } else {
             // (the sum is over the weights as they were before the value scale went in: to divide it out again costs
             //  more than it gives)
             sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(e0, e1));
             const float2 f = *reinterpret_cast<const float2*>(sc + C + 32 * h + 2 * e);
-            u = pack_bf16(e0 * f.x, e1 * f.y);
+            w[e] = pack_bf16(e0 * f.x, e1 * f.y);
           }
-          w[16 * h + e] = __uint_as_float(u);
         }
-      };
-      weights(1);
-      logits(0);
-      weights(0);
+        tmem_st16(base + 16 * h, w);       // over logits that have been read
+      }
       float s0, s1;
       unpack_f2(add_f2(sum2[0], sum2[1]), s0, s1);
       l += s0 + s1;
-      if (i > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
-        // O of the tiles so far was summed against the old reference; the last of them has to be complete
-        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bar_o[t][(i - 1) & 1], (uint32_t)(((i - 1) >> 1) & 1))) != 0;
-        if (!ok) break;
-        tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < D; c += 32) {
-          float o[32];
-          tmem_ld32(base + 128 + c, o);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] *= corr;
-          tmem_st32(base + 128 + c, o);
-        }
-      }
-      tmem_st32(tm_s, w);
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(&bar_p[t][i & 1]);
+      mbar_arrive(&bar_p[t]);
     }
+    // Every row tile's last contraction: Q and the ring are then free for O's way out.
     if (ok && n > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bar_o[t][(n - 1) & 1], (uint32_t)(((n - 1) >> 1) & 1))) != 0;
+#pragma unroll
+      for (int x = 0; x < NT; ++x) ok = ok && mbar_wait_bounded(&bar_o[x], 0u);
+      ok = __all_sync(0xffffffffu, ok) != 0;
       tc_fence_after();
     }
-    named_barrier_sync(1, 32 * (S::SOFT_WARPS + 4));       // the producers' word on odd values
+    named_barrier_sync(1, 32 * ISSUER);          // odd_s is final; no thread is still copying
     pdl_launch_dependents();
     if (last && !real) l = TREE_PADDING;
-    const bool in = node >= 0;
-    const int g = in ? m - node * p.G : 0;
-    const float r = ok ? (l == TREE_PADDING || l == 0.f ? 0.f : 1.f / l) : __uint_as_float(0x7fc00000u);
-    const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
-    if (p.splits > 1 && in) p.part_ml[at] = make_float2(m_ref, ok ? l : __uint_as_float(0x7fc00000u));
+    if (!ok) l = __uint_as_float(0x7fc00000u);
+    const bool zero = n == 0 || l == TREE_PADDING || l == 0.f;
+    const float r = p.splits > 1 ? 1.f : (zero ? 0.f : 1.f / l);
+    const long long at0 = ((long long)split * gridDim.z + blockIdx.z) * p.M + m0;
+    if (p.splits > 1 && node >= 0) p.part_ml[at0 + lane] = make_float2(m_ref, l);
+    constexpr int OCH = D / 4;                   // 16-byte chunks of a row of O, turned with the row: no bank conflicts
+    unsigned char* stage = smem + (t * R + (warp & 3) * 32) * (D * 4);
 #pragma unroll
     for (int c = 0; c < D; c += 32) {
       float o[32];
-      tmem_ld32(base + 128 + c, o);      // (nothing was written there in a block without columns: o is not used then)
-      if (n == 0 || (l == TREE_PADDING && ok)) {
-#pragma unroll
-        for (int k = 0; k < 32; ++k) o[k] = 0.f;
-      }
+      tmem_ld32(base + 128 + c, o);              // (nothing was written there in a block without columns: not used then)
       if (last && odd_s && real) tree_add_odd<S::WORDS, 32>(p, b, hk, anc, D, c, o);
-      if (in && p.splits == 1) {
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)node * p.B + b) * p.H + hk * p.G + g) * D + c;
 #pragma unroll
-        for (int k = 0; k < 32; k += 8)
-          *reinterpret_cast<uint4*>(dst + k) = make_uint4(pack_bf16(o[k] * r, o[k + 1] * r), pack_bf16(o[k + 2] * r, o[k + 3] * r),
-                                                          pack_bf16(o[k + 4] * r, o[k + 5] * r), pack_bf16(o[k + 6] * r, o[k + 7] * r));
-      } else if (in) {
-        float* dst = p.part_acc + at * D + c;
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-      }
+      for (int k = 0; k < 32; k += 4)
+        *reinterpret_cast<float4*>(stage + lane * (D * 4) + ((((c + k) / 4) ^ (lane & (OCH - 1))) << 4)) =
+            zero ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[k] * r, o[k + 1] * r, o[k + 2] * r, o[k + 3] * r);
       __syncwarp();
     }
+    constexpr int AT_ONCE = 32 / OCH;            // rows a warp writes at a time
+#pragma unroll 4
+    for (int x = 0; x < 32; x += AT_ONCE) {
+      const int rr = x + lane / OCH, m = m0 + rr, ch = lane % OCH;
+      if (m >= p.M) break;
+      const float4 v = *reinterpret_cast<const float4*>(stage + rr * (D * 4) + ((ch ^ (rr & (OCH - 1))) << 4));
+      if (p.splits == 1) {
+        const int nd = m / p.G, g = m - nd * p.G;
+        tree_store4<__nv_bfloat16>(static_cast<__nv_bfloat16*>(p.out) + (((long long)nd * p.B + b) * p.H + hk * p.G + g) * D + ch * 4,
+                                   v.x, v.y, v.z, v.w);
+      } else {
+        *reinterpret_cast<float4*>(p.part_acc + (at0 + rr) * D + ch * 4) = v;
+      }
+    }
   }
-  if (warp >= S::SOFT_WARPS && warp < S::SOFT_WARPS + 4) named_barrier_sync(1, 32 * (S::SOFT_WARPS + 4));
   tc_fence_before();
   __syncthreads();
-  if (warp == S::SOFT_WARPS + 4)
+  if (warp == ISSUER)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS) : "memory");
 }
 
