@@ -16,6 +16,8 @@
 #include "tova_tree_tc.cuh"
 #include "tova_verify.cuh"
 
+int encode_state_map(CUtensorMap* map, void* base, const tova_config& cfg, int box_rows, long long rows_per_head);   // tova_api.cu
+
 namespace {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -297,42 +299,57 @@ int tree_check(const tova_tree_config* c, int32_t n_live, int32_t n_nodes) {
 enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64, TREE_TC_1, TREE_TC_2 };
 struct TreePlan {
   int kernel, row_blocks, splits, split_cols;
+  int blocks, least;             // tcgen05 kernel
   size_t ml_bytes, bytes;
 };
 
 TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count) {
   TreePlan t{};
   const int M = n_nodes * (c.n_q_heads / c.n_kv_heads);
-  int rows = tova::TREE_ALU_ROWS, cols = tova::TREE_ALU_COLS;
-  int resident = 2 * sm_count, shortest = 2;     // blocks at a time; tiles worth a block's set-up
-  if (c.dtype == TOVA_DTYPE_BF16) {
-    t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : M <= 64 ? TREE_MMA_64 : M <= 128 ? TREE_TC_1 : TREE_TC_2;
-    rows = M <= 64 ? 64 : M <= 128 ? tova::TREE_TC_ROWS : 2 * tova::TREE_TC_ROWS;
-    cols = M <= 64 ? tova::TREE_MMA_COLS : tova::TREE_TC_COLS;
-    if (t.kernel == TREE_TC_2) resident = sm_count;
-    if (M > 64) shortest = 4;
+  size_t part_rows;
+  if (c.dtype == TOVA_DTYPE_BF16 && M > 64) {
+    // More than 64 rows: the contractions, not the state's bytes, set the pace of a warp-level kernel.
+    t.kernel = M <= 128 ? TREE_TC_1 : TREE_TC_2;
+    const int rows = (M <= 128 ? 1 : 2) * tova::TREE_TC_ROWS;
+    const bool two = M <= 128 && c.format == TOVA_FORMAT_PLAIN;
+    t.row_blocks = (M + rows - 1) / rows;
+    t.splits = 1;
+    t.blocks = (two ? 2 : 1) * sm_count;
+    t.least = 4;                 // tiles of 128 columns: less than that does not pay for a block's set-up
+    part_rows = (size_t)2 * t.blocks * rows;
+  } else {
+    int rows = tova::TREE_ALU_ROWS, cols = tova::TREE_ALU_COLS;
+    if (c.dtype == TOVA_DTYPE_BF16) {
+      t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : TREE_MMA_64;
+      rows = 64;
+      cols = tova::TREE_MMA_COLS;
+    }
+    t.row_blocks = (M + rows - 1) / rows;
+    const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;
+    const int tiles = std::max(1, (n_live + cols - 1) / cols);
+    // Runs of columns for two rounds of resident blocks (two per SM), but none shorter than two tiles unless the GPU
+    // would stay half empty.
+    const int resident = 2 * sm_count, shortest = whole * (tiles / 2) < resident ? 1 : 2;
+    long long want = (2LL * resident + whole - 1) / whole;
+    want = std::max(1LL, std::min<long long>(want, tiles / shortest));
+    const int per = (int)((tiles + want - 1) / want);
+    t.split_cols = per * cols;
+    t.splits = (tiles + per - 1) / per;
+    if (t.splits > 1) t.splits += 1;               // a run of its own for the drafts: it does not wait for a run of rows
+    part_rows = t.splits > 1 ? (size_t)t.splits * c.batch * c.n_kv_heads * M : 0;
   }
-  t.row_blocks = (M + rows - 1) / rows;
-  const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;
-  const int tiles = std::max(1, (n_live + cols - 1) / cols);
-  long long want = (2LL * resident + whole - 1) / whole;
-  if (whole * (tiles / shortest) < resident) shortest = 1;
-  want = std::max(1LL, std::min<long long>(want, tiles / shortest));
-  const int per = (int)((tiles + want - 1) / want);
-  t.split_cols = per * cols;
-  t.splits = (tiles + per - 1) / per;
-  if (t.splits > 1) t.splits += 1;               // a run of its own for the drafts: it does not wait for a run of rows
-  if (t.splits > 1) {
-    const size_t n = (size_t)t.splits * c.batch * c.n_kv_heads * M;
-    t.ml_bytes = (n * sizeof(float2) + 255) / 256 * 256;
-    t.bytes = t.ml_bytes + n * c.head_dim * sizeof(float);
-  }
+  t.ml_bytes = (part_rows * sizeof(float2) + 255) / 256 * 256;
+  t.bytes = t.ml_bytes + part_rows * c.head_dim * sizeof(float);
   return t;
 }
 
-template <typename Kernel>
-cudaError_t tree_start(Kernel kern, std::atomic<bool>* configured, size_t smem, int threads, const tova::TreeParams& p,
-                       const TreePlan& t, cudaStream_t st) {
+inline dim3 tree_grid(const tova::TreeParams& p, const TreePlan& t) {
+  return dim3((unsigned)t.row_blocks, (unsigned)t.splits, (unsigned)(p.B * p.Hkv));
+}
+
+template <typename... Args>
+cudaError_t tree_start(void (*kern)(Args...), std::atomic<bool>* configured, size_t smem, int threads, dim3 grid, cudaStream_t st,
+                       const Args&... args) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -342,7 +359,7 @@ cudaError_t tree_start(Kernel kern, std::atomic<bool>* configured, size_t smem, 
     if (e != cudaSuccess) return e;
     configured[dev & 63] = true;
   }
-  kern<<<dim3((unsigned)t.row_blocks, (unsigned)t.splits, (unsigned)(p.B * p.Hkv)), threads, smem, st>>>(p);
+  kern<<<grid, threads, smem, st>>>(args...);
   return cudaGetLastError();
 }
 
@@ -366,14 +383,37 @@ template <int D, int FMT, int MT, int WR>
 cudaError_t tree_start_mma(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
   static std::atomic<bool> configured[64];
   return tree_start(tova::tova_tree_mma_kernel<D, FMT, MT, WR>, configured, tova::TreeMmaShape<D, FMT, MT, WR>::SMEM,
-                    tova::TREE_MMA_THREADS, p, t, st);
+                    tova::TREE_MMA_THREADS, tree_grid(p, t), st, p);
 }
 
 template <int D, int FMT, int NT>
-cudaError_t tree_start_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
+cudaError_t tree_run_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
   static std::atomic<bool> configured[64];
   using S = tova::TreeTcShape<D, FMT, NT>;
-  return tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, p, t, st);
+  // Tiled views of a bf16 state in boxes of 128 rows; where they cannot be had (fewer rows, 2^31 or more) the kernel
+  // copies every tile as it copies a sequence's last.
+  CUtensorMap map_k{}, map_v{};
+  tova::TreeParams q = p;
+  const long long rows = (long long)p.B * p.Hkv * p.cap;
+  if (FMT == tova::FORMAT_PLAIN && rows >= tova::TREE_TC_COLS && rows < (1LL << 31)) {
+    tova_config c{};
+    c.batch = p.B; c.n_kv_heads = p.Hkv; c.capacity = p.cap; c.head_dim = D;
+    q.tiled = encode_state_map(&map_k, const_cast<void*>(p.K), c, tova::TREE_TC_COLS, 0) == TOVA_OK &&
+              encode_state_map(&map_v, const_cast<void*>(p.V), c, tova::TREE_TC_COLS, 0) == TOVA_OK;
+  }
+  cudaError_t e = tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, dim3((unsigned)t.blocks), st, q, map_k, map_v);
+  if (e != cudaSuccess) return e;
+  constexpr int JOIN_ROWS = tova::TREE_TC_JOIN_THREADS / 32;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3((unsigned)(p.B * p.Hkv * t.row_blocks), (unsigned)((std::min(p.M, NT * tova::TREE_TC_ROWS) + JOIN_ROWS - 1) / JOIN_ROWS));
+  lc.blockDim = dim3(tova::TREE_TC_JOIN_THREADS);
+  lc.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  return cudaLaunchKernelEx(&lc, tova::tova_tree_tc_join_kernel<D, NT>, p);
 }
 
 template <typename T, int D, int FMT>
@@ -381,14 +421,15 @@ cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream
   cudaError_t e;
   if constexpr (std::is_same<T, float>::value) {
     static std::atomic<bool> configured[64];
-    e = tree_start(tova::tova_tree_alu_kernel<T, D, FMT>, configured, tova::tree_alu_smem_bytes<D>(), tova::TREE_ALU_THREADS, p, t, st);
+    e = tree_start(tova::tova_tree_alu_kernel<T, D, FMT>, configured, tova::tree_alu_smem_bytes<D>(), tova::TREE_ALU_THREADS,
+                   tree_grid(p, t), st, p);
   } else {
     switch (t.kernel) {
       case TREE_MMA_16: e = tree_start_mma<D, FMT, 1, 1>(p, t, st); break;
       case TREE_MMA_32: e = tree_start_mma<D, FMT, 1, 2>(p, t, st); break;
       case TREE_MMA_64: e = tree_start_mma<D, FMT, 2, 2>(p, t, st); break;
-      case TREE_TC_1: e = tree_start_tc<D, FMT, 1>(p, t, st); break;
-      default: e = tree_start_tc<D, FMT, 2>(p, t, st); break;
+      case TREE_TC_1: return tree_run_tc<D, FMT, 1>(p, t, st);
+      default: return tree_run_tc<D, FMT, 2>(p, t, st);
     }
   }
   if (e != cudaSuccess || t.splits == 1) return e;
@@ -437,6 +478,7 @@ extern "C" int tova_tree_attention(const tova_tree_config* cfg, const void* K, c
   p.N = n_nodes; p.B = cfg->batch; p.H = cfg->n_q_heads; p.Hkv = cfg->n_kv_heads;
   p.G = p.H / p.Hkv; p.M = p.N * p.G; p.cap = cfg->capacity; p.n_live = n_live;
   p.splits = t.splits; p.split_cols = t.split_cols;
+  p.row_blocks = t.row_blocks; p.blocks = t.blocks; p.least = t.least;
   const float scale = cfg->sm_scale == 0.f ? 1.f / std::sqrt((float)cfg->head_dim) : cfg->sm_scale;
   p.scale2 = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -1,22 +1,32 @@
 // Attention of drafted tokens over a state on the 5th-generation tensor cores (see tova_tree.cuh for the operation):
 // bf16 queries, more than 64 rows of the product (nodes x query heads of a KV head).
 //
-// A block takes NT tiles of 128 rows and runs down its columns in tiles of 128; row i of a tile is TMEM lane i.  Roles:
-//   4 producer warps    K and V tiles into a ring of shared-memory slots in the 128-byte-swizzled layout the tensor cores
-//                       read: bf16 states by cp.async, as far ahead as there are slots; 8-bit states through registers,
-//                       converted exactly (see tova_tree_mma.cuh); drafts, the last tiles, by plain loads that take out
-//                       infinities and NaN.  Columns behind the run are zeros, whatever lies there.
+// Work.  A job is up to NT x 128 rows of one KV head of one sequence against all their columns, in tiles of 128; the
+// drafts are its last tiles.  The tiles of all jobs, one behind the other, are dealt out evenly: every block (as many as fit
+// the GPU at a time) takes a run of `share` tiles and walks through the jobs in it.  A job that lies in one run is written
+// out; one cut by the end of a run leaves (reference, sum, weighted sum) of its pieces in the workspace, at most two a
+// block, and a second kernel joins them.  So lengths that differ cost nobody idle time, and hardly any job is cut.
+//
+// Roles in a block.  They meet through mbarriers only and run ahead of one another across jobs: while the rows of one job
+// are written out, the next one's Q, K and V are on their way and its first logits computed.
+//   producer warps      Q, then K and V tiles into a ring of shared-memory slots in the 128-byte-swizzled layout the tensor
+//                       cores read: bf16 states by tiled TMA, as far ahead as there are slots (by cp.async the two warps
+//                       could not keep up; values of rows behind a sequence's last are zeroed when they have landed,
+//                       whatever lies there); 8-bit states by bulk copies into a raw ring and an exact conversion (see
+//                       tova_tree_mma.cuh); drafts by plain loads that take out infinities and NaN.
 //   1 issuing thread    S = Q K^T (128 x 128, fp32 in TMEM) and O += P V in the order PV_0(i) S_0(i+1) PV_1(i) S_1(i+1):
 //                       the tensor cores work on one row tile while the other's soft-max runs (two row tiles in a block,
 //                       or two blocks on an SM)
-//   4 warps a row tile  one thread per row: logits from TMEM, mask, running maximum, weights as bf16 back over the logits,
-//                       where they are the A operand of O += P V.  The sum is taken over the rounded weights, so that the
-//                       weights that multiply V add up to one.  The reference maximum moves only when a tile's exceeds it
-//                       by more than 2^8: weights up to 256 lose nothing in floating point, and O is almost never rescaled.
+//   1 helper warp       ancestor bits of the next job's drafts, and whether one of their values is not finite
+//   8 warps a row tile  two threads a row, 64 columns each: logits from TMEM, weights as bf16 back over them, where they are
+//                       the A operand of O += P V.  The weights' reference is a whole number, set by a job's first tile
+//                       (which takes a pass for the maximum) and hardly ever moved again: floating point loses nothing on
+//                       weights above 1, so a later tile needs no maximum; only where a row's weights sum to more than 2^32
+//                       is the tile done over, with a factor of a power of two on what was summed before.  The sum is taken
+//                       over the rounded weights, so that the weights that multiply V add up to one.
 // A tile of 128 columns, not 64, because S = Q K^T reads both operands from shared memory: 8 KiB per 64 cycles of math
 // (128 x 128 x 16) are what shared memory delivers, 6 KiB per 32 cycles (128 x 64 x 16) are not.  TMEM: 256 columns per row
-// tile (S 128, O 128).  One row tile: two blocks per SM; two row tiles (more than 128 rows): one block per SM, and every K
-// and V tile feeds both.  Every wait is bounded; one that runs out leaves NaN in the block's rows.
+// tile (S 128, O 128).  Every wait is bounded; one that runs out leaves NaN in the rows that the block had yet to write.
 #pragma once
 
 #include "tova_tree_mma.cuh"
@@ -25,431 +35,774 @@ namespace tova {
 
 constexpr int TREE_TC_ROWS = 128;      // rows of a tile
 constexpr int TREE_TC_COLS = 128;      // columns of a tile
-constexpr float TREE_TC_SLACK = 8.f;   // log2 of how far weights may exceed 1 before O is rescaled
+constexpr float TREE_TC_MOST = 4294967296.f;   // a larger sum of a thread's weights moves the row's reference
 
 template <int D, int FMT, int NT>
 struct TreeTcShape {
-  static constexpr int SOFT_WARPS = 4 * NT;
-  static constexpr int THREADS = 32 * (SOFT_WARPS + 4 + 1);
-  static constexpr int Q_BYTES = TREE_TC_ROWS * D * 2;            // per row tile
+  static constexpr bool PLAIN = FMT == FORMAT_PLAIN;
+  static constexpr int SOFT_WARPS = 8 * NT;
+  static constexpr int PRODUCER_WARPS = PLAIN ? 2 : 4;
+  static constexpr int THREADS = 32 * (SOFT_WARPS + PRODUCER_WARPS + 2);
+  static constexpr int BLOCKS = PLAIN && NT == 1 ? 2 : 1;          // per SM
+  static constexpr int Q_BYTES = TREE_TC_ROWS * D * 2;             // per row tile
   static constexpr int SLOT = TREE_TC_COLS * D * 2;
-  static constexpr int SLOTS = (NT == 1 ? 2 : 4) * (128 / D);
-  // Tiles whose scales are kept.  K of tile i takes the slot of K of tile i - SLOTS/2; S of that tile is complete then, so
-  // the soft-max of all tiles before it has passed: their scales may go.
+  static constexpr int SLOTS = (PLAIN ? (NT == 1 ? 2 : 4) : 3) * (128 / D);
+  static constexpr int RAW = PLAIN ? 0 : TREE_TC_COLS * D;
+  static constexpr int RAW_SLOTS = PLAIN ? 0 : (NT == 1 ? 4 : 3) * (128 / D);
+  // Tiles whose scales are kept.  K of tile i takes the slot of a copy SLOTS positions back; when that has been consumed,
+  // the soft-max of tile i - SLOTS/2 - 1 has passed.
   static constexpr int SCALE_TILES = SLOTS / 2 + 2;
-  static constexpr int SCALES = FMT == FORMAT_PLAIN ? 0 : SCALE_TILES * 2 * TREE_TC_COLS * 4;
-  static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + SCALES + 1024;
+  static constexpr int SCALES = PLAIN ? 0 : SCALE_TILES * 2 * TREE_TC_COLS * 4;
+  static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + RAW_SLOTS * RAW + SCALES + 1024;
   static constexpr int TMEM_COLS = 256 * NT;
   static constexpr int NODES = NT == 1 ? TREE_TC_ROWS : TREE_MAX_NODES;   // one row tile: M <= 128, so N <= 128
   static constexpr int WORDS = NODES / 32;
-  // after the last contraction Q and the ring hold the rows of O on their way out
-  static_assert(NT * TREE_TC_ROWS * D * 4 <= NT * Q_BYTES + SLOTS * SLOT, "O fits");
 };
 
-// The mbarrier receives this thread's arrival (counted in its initial count) once its cp.async so far have landed.
-__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+// --- how the work is dealt out -----------------------------------------------------------------------------------
+// Tiles of a job of sequence b.
+__device__ __forceinline__ int tree_tc_tiles(const TreeParams& p, int b) {
+  return (tree_len(p, b) + TREE_TC_COLS - 1) / TREE_TC_COLS + (p.N + TREE_TC_COLS - 1) / TREE_TC_COLS;
+}
+// Tiles a block takes: an even share of all, but no fewer than `least`.
+__device__ __forceinline__ long long tree_tc_share(long long total, int blocks, int least) {
+  const long long even = (total + blocks - 1) / blocks;
+  return even > least ? even : least;
+}
+
+// Where a block is in its run.  Every role holds its own copy and steps through the same pieces.
+struct TreeTcRun {
+  long long at, end, base;      // next tile, end of the run, first tile of sequence b's jobs
+  int b, tiles;                 // sequence, tiles of each of its jobs
+  bool first;
+  // the current piece
+  int hk, rb, i0, i1, len, n_state, part;
+  bool last;                    // has the job's last tile
+
+  __device__ __forceinline__ bool next(const TreeParams& p, int block) {
+    if (at >= end) return false;
+    const int jobs = p.Hkv * p.row_blocks;        // of a sequence
+    while (at >= base + (long long)tiles * jobs) {
+      base += (long long)tiles * jobs;
+      ++b;
+      tiles = tree_tc_tiles(p, b);
+    }
+    const long long r = at - base;
+    const int job = (int)(r / tiles);
+    i0 = (int)(r - (long long)job * tiles);
+    i1 = (int)min((long long)tiles, i0 + (end - at));
+    hk = job / p.row_blocks;
+    rb = job - hk * p.row_blocks;
+    len = tree_len(p, b);
+    n_state = (len + TREE_TC_COLS - 1) / TREE_TC_COLS;
+    last = i1 == tiles;
+    part = i0 == 0 && last ? -1 : 2 * block + (first ? 0 : 1);
+    first = false;
+    at += i1 - i0;
+    return true;
+  }
+};
+
+// Four floats of shared memory as two pairs.  (Volatile: read again where they are needed again, instead of being kept in
+// registers that the rows need.)
+__device__ __forceinline__ void lds_f2x2(const float* x, uint64_t (&r)[2]) {
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(r[0]), "=l"(r[1]) : "r"(smem_addr(x)));
+}
+
+__device__ __forceinline__ void tma_load_2d_tile(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_addr(bar))
+      : "memory");
+}
+
+// 16 columns of this thread's TMEM lane times f (a power of two or 0: exact).
+__device__ __forceinline__ void tree_tc_scale16(uint32_t taddr, float f) {
+  uint32_t v[16];
+  tmem_ld16(taddr, v);
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+  tmem_st16(taddr, v);
 }
 
 template <int D, int FMT, int NT>
-__global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, NT == 1 ? 2 : 1)
-    tova_tree_tc_kernel(const __grid_constant__ TreeParams p) {
+__global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<D, FMT, NT>::BLOCKS)
+    tova_tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v) {
   using S = TreeTcShape<D, FMT, NT>;
-  constexpr bool PLAIN = FMT == FORMAT_PLAIN;
+  constexpr bool PLAIN = S::PLAIN;
   constexpr int C = TREE_TC_COLS, R = TREE_TC_ROWS;
-  constexpr int PRODUCER = S::SOFT_WARPS, ISSUER = S::SOFT_WARPS + 4;      // first warp of each role
+  constexpr int PRODUCER = S::SOFT_WARPS, ISSUER = PRODUCER + S::PRODUCER_WARPS, HELPER = ISSUER + 1;      // first warp of each role
+  constexpr int PT = 32 * S::PRODUCER_WARPS, SOFT = 32 * S::SOFT_WARPS;
   extern __shared__ unsigned char tree_tc_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tree_tc_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* q_s = smem;                               // per row tile: boxes of [128 rows][128 bytes]
   unsigned char* slot_s = q_s + NT * S::Q_BYTES;           // per slot: boxes of [128 rows][128 bytes]
-  float* scale_s = reinterpret_cast<float*>(slot_s + S::SLOTS * S::SLOT);   // [tile % SCALE_TILES][k, v][128]
-  __shared__ __align__(8) uint64_t full[S::SLOTS], empty[S::SLOTS], bar_q, bar_s[NT], bar_p[NT], bar_o[NT], bar_sc[S::SCALE_TILES];
+  unsigned char* raw_s = slot_s + S::SLOTS * S::SLOT;
+  float* scale_s = reinterpret_cast<float*>(raw_s + S::RAW_SLOTS * S::RAW);   // [tile % SCALE_TILES][k times the logits' scale, v][128]
+  __shared__ __align__(8) uint64_t full[S::SLOTS], empty[S::SLOTS], bar_sc[S::SCALE_TILES];
+  __shared__ __align__(8) uint64_t raw_full[PLAIN ? 1 : S::RAW_SLOTS], raw_empty[PLAIN ? 1 : S::RAW_SLOTS];
+  // Q landed, Q free again, S computed, weights written, O complete, ancestor bits there, ancestor bits free again, the
+  // two warps of 32 rows meet, a tile that has to be trimmed landed
+  __shared__ __align__(8) uint64_t bar_q, bar_qf, bar_s[NT], bar_p[NT], bar_o[NT], bar_a, bar_af, bar_pair[NT * 4], bar_trim;
   __shared__ uint32_t tmem_base_s;
-  __shared__ int odd_s;
-  __shared__ int par_s[S::NODES];
+  __shared__ int odd_s;                                    // some draft's value is not finite
+  __shared__ TreeTcRun run_s, soft_run_s[S::SOFT_WARPS];   // (the soft-max warps' registers are for the rows)
   __shared__ __align__(16) uint32_t anc_s[S::NODES][S::WORDS];     // ancestor bits of every node
+  __shared__ int par_s[S::NODES];
+  __shared__ float pair_s[NT * R][2];                      // what the two threads of a row tell each other
+  __shared__ int flag_s[NT * 4];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int b = blockIdx.z / p.Hkv, hk = blockIdx.z % p.Hkv;
-  const int split = blockIdx.y, row0 = blockIdx.x * (R * NT);
-  const int len = tree_len(p, b);
-  const bool last = split == p.splits - 1;
-  const int c0 = split * p.split_cols;
-  const int c1 = last ? len : min(len, c0 + p.split_cols);
-  const int n_state = c1 > c0 ? (c1 - c0 + C - 1) / C : 0;
-  const int n = n_state + (last ? (p.N + C - 1) / C : 0);  // tiles of this block
 
   if (tid == 0) {
     for (int i = 0; i < S::SLOTS; ++i) {
-      mbar_init(&full[i], 128);
+      mbar_init(&full[i], PT);
       mbar_init(&empty[i], 1);
     }
-    mbar_init(&bar_q, R * NT);
+    for (int i = 0; i < S::RAW_SLOTS; ++i) {
+      mbar_init(&raw_full[i], 1);
+      mbar_init(&raw_empty[i], PT);
+    }
+    mbar_init(&bar_q, PT);
+    mbar_init(&bar_trim, 1);
+    mbar_init(&bar_qf, 1);
     for (int t = 0; t < NT; ++t) {
       mbar_init(&bar_s[t], 1);
-      mbar_init(&bar_p[t], R);
+      mbar_init(&bar_p[t], 2 * R);
       mbar_init(&bar_o[t], 1);
     }
-    for (int i = 0; i < S::SCALE_TILES; ++i) mbar_init(&bar_sc[i], 128);
+    for (int i = 0; i < S::SCALE_TILES; ++i) mbar_init(&bar_sc[i], PT);
+    mbar_init(&bar_a, 32);
+    mbar_init(&bar_af, SOFT);
+    for (int i = 0; i < NT * 4; ++i) mbar_init(&bar_pair[i], 64);
     mbar_fence_init();
-    odd_s = 0;
   }
+  if (tid < NT * 4) flag_s[tid] = -1;
   if (warp == ISSUER) {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_s)), "r"(S::TMEM_COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (warp == HELPER) {
+    // The block's run: all tiles, its share of them, and the sequence that the share starts in.
+    const int jobs = p.Hkv * p.row_blocks;
+    TreeTcRun r;
+    long long total;
+    if (p.lens) {
+      long long x = 0;
+      for (int b = lane; b < p.B; b += 32) x += tree_tc_tiles(p, b);
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+      total = x * jobs;
+    } else {
+      total = (long long)tree_tc_tiles(p, 0) * jobs * p.B;
+    }
+    const long long share = tree_tc_share(total, gridDim.x, p.least);
+    r.at = min(total, blockIdx.x * share);
+    r.end = min(total, r.at + share);
+    r.base = 0;
+    r.b = 0;
+    if (r.at < r.end) {
+      if (p.lens) {
+        for (int b0 = 0;; b0 += 32) {           // (r.at < total, so some sequence holds it)
+          const long long mine = b0 + lane < p.B ? (long long)tree_tc_tiles(p, b0 + lane) * jobs : 0;
+          long long upto = mine;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+          }
+          const unsigned hit = __ballot_sync(0xffffffffu, r.base + upto > r.at);
+          if (hit) {
+            const int x = __ffs(hit) - 1;
+            r.b = b0 + x;
+            r.base += __shfl_sync(0xffffffffu, upto - mine, x);
+            break;
+          }
+          r.base += __shfl_sync(0xffffffffu, upto, 31);
+        }
+      } else {
+        const long long per = (long long)tree_tc_tiles(p, 0) * jobs;
+        r.b = (int)(r.at / per);
+        r.base = per * r.b;
+      }
+      r.tiles = tree_tc_tiles(p, r.b);
+    }
+    r.first = true;
+    if (lane == 0) run_s = r;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
+  TreeTcRun run = run_s;
   bool ok = true;
-  // Copies are made and consumed in the order K0 V0 K1 V1 ...: position 2 i is K of tile i, 2 i + 1 its V.
+  // Copies are made and consumed in the order Q K0 V0 K1 V1 ...; the counters go on from piece to piece.  Tile g (of the
+  // block's run) has K at ring position 2 g and V at 2 g + 1.
 
   if (warp >= PRODUCER && warp < ISSUER) {
     // ============================== producers ==============================
     const int pt = tid - PRODUCER * 32;
-    auto slot_free = [&](int pos) {
-      return pos < S::SLOTS || mbar_wait_bounded(&empty[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS - 1) & 1));
-    };
     // Where 16-byte chunk ch of row `row` lies in a slot.
     auto place = [&](int row, int ch) { return (ch >> 3) * (C * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4); };
-    auto draft = [&](int pos) {
-      const bool is_k = !(pos & 1);
-      unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
-      const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_k ? p.k_new : p.v_new);
-      bool odd = false;
-#pragma unroll 4
-      for (int e = pt; e < C * (D / 8); e += 128) {
-        const int row = e / (D / 8), ch = e % (D / 8), j = (pos / 2 - n_state) * C + row;
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (j < p.N) {
-          w = *reinterpret_cast<const uint4*>(src + (((long long)j * p.B + b) * p.Hkv + hk) * D + ch * 8);
-          if (!is_k) odd |= tree_drop_odd(w);
-        }
-        *reinterpret_cast<uint4*>(dst + place(row, ch)) = w;
-      }
-      if (odd) odd_s = 1;
-      fence_proxy_async_smem();
-      mbar_arrive(&full[pos % S::SLOTS]);
-    };
-    if constexpr (PLAIN) {
-      const unsigned char* g[2] = {static_cast<const unsigned char*>(p.K) + (long long)blockIdx.z * p.cap * (2 * D),
-                                   static_cast<const unsigned char*>(p.V) + (long long)blockIdx.z * p.cap * (2 * D)};
-      constexpr int CH = D / 8, STEP = 128 / CH;           // a thread's chunks: one column, every STEP-th row
-      const int row_t = pt / CH, ch_t = pt % CH;
-      for (int pos = 0; pos < 2 * n && ok; ++pos) {
-        ok = slot_free(pos);
-        if (!ok) break;
-        if (pos / 2 < n_state) {
-          const int j0 = c0 + (pos / 2) * C;
-          const uint32_t dst = smem_addr(slot_s + (pos % S::SLOTS) * S::SLOT);
-          const unsigned char* src = ((pos & 1) ? g[1] : g[0]) + ch_t * 16;
-#pragma unroll
-          for (int x = 0; x < C / STEP; ++x) {
-            const int row = x * STEP + row_t;
-            const bool in = j0 + row < c1;
-            cp_async16(dst + place(row, ch_t), src + (long long)(in ? j0 + row : c0) * (2 * D), in ? 16u : 0u);
-          }
-          cp_async_arrive(&full[pos % S::SLOTS]);
-        } else {
-          draft(pos);
-        }
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
-    } else {
-      const unsigned char* g[2] = {static_cast<const unsigned char*>(p.K) + (long long)blockIdx.z * p.cap * D,
-                                   static_cast<const unsigned char*>(p.V) + (long long)blockIdx.z * p.cap * D};
-      constexpr int CH = D / 16, STEP = 128 / CH, PER = C / STEP;
-      const int row_t = pt / CH, ch_t = pt % CH;
-      uint4 raw[PER];                  // this thread's chunks of the position that comes next
-      auto fetch = [&](int pos) {
-        const int j0 = c0 + (pos / 2) * C;
-        const unsigned char* src = ((pos & 1) ? g[1] : g[0]) + ch_t * 16;
-#pragma unroll
-        for (int x = 0; x < PER; ++x) {
-          const int j = j0 + x * STEP + row_t;
-          raw[x] = pos / 2 < n_state && j < c1 ? *reinterpret_cast<const uint4*>(src + (long long)j * D) : make_uint4(0, 0, 0, 0);
-        }
+    constexpr int QCH = D / 8, QSTEP = PT / QCH;           // a thread's chunks: one column, every STEP-th row
+    constexpr int CH = PLAIN ? D / 8 : D / 16, STEP = PT / CH, PER = C / STEP;
+    int g0 = 0, piece = 0, raw0 = 0;                       // tiles, pieces, raw copies before this piece
+    uint32_t trims = 0;
+    while (ok && run.next(p, blockIdx.x)) {
+      const int n = run.i1 - run.i0, bh = run.b * p.Hkv + run.hk;
+      auto slot_free = [&](int pos) {
+        return pos < S::SLOTS || mbar_wait_bounded(&empty[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS - 1) & 1));
       };
-      // Two scales a thread and tile, fetched a tile early and stored with the tile's K.
-      float next_k, next_v;
-      auto fetch_scales = [&](int tile) {
-        const int j = c0 + tile * C + pt;
-        const bool in = j < c1;
-        next_k = tile < n_state ? (in ? p.k_scale[(long long)blockIdx.z * p.cap + j] : 0.f) : 1.f;
-        next_v = tile < n_state ? (in ? p.v_scale[(long long)blockIdx.z * p.cap + j] : 0.f) : 1.f;
+      // Q rows, K-major with the 128-byte swizzle; rows past the product are zeros.  After the piece's first K and V, which
+      // need not wait for the piece before to be done with its Q.
+      auto load_q = [&]() {
+        ok = piece == 0 || mbar_wait_bounded(&bar_qf, (uint32_t)((piece - 1) & 1));
+        if (!ok) return;
+        const int row_q = pt / QCH, ch = pt % QCH;
+        const uint32_t dst = smem_addr(q_s) + (ch >> 3) * (R * 128);
+        const int m0 = run.rb * (R * NT);
+#pragma unroll 8
+        for (int k = 0; k < NT * R / QSTEP; ++k) {
+          const int r = k * QSTEP + row_q, m = m0 + r, mm = min(m, p.M - 1);
+          const int nd = mm / p.G, g = mm - nd * p.G;
+          cp_async16(dst + (r / R) * S::Q_BYTES + (r % R) * 128 + (((ch & 7) ^ (r & 7)) << 4),
+                     static_cast<const __nv_bfloat16*>(p.q) + (((long long)nd * p.B + run.b) * p.H + run.hk * p.G + g) * D + ch * 8, m < p.M ? 16u : 0u);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_proxy_async_smem();
+        mbar_arrive(&bar_q);
       };
-      fetch(0);
-      fetch_scales(0);
-      for (int pos = 0; pos < 2 * n; ++pos) {
-        const int tile = pos / 2;
-        ok = slot_free(pos);
-        if (!ok) break;
-        if (!(pos & 1)) {
-          float* sc = scale_s + (tile % S::SCALE_TILES) * 2 * C;
-          sc[pt] = next_k;
-          sc[C + pt] = next_v;
-          mbar_arrive(&bar_sc[tile % S::SCALE_TILES]);
-          fetch_scales(tile + 1);
-        }
-        if (tile >= n_state) {
-          draft(pos);
-          continue;
-        }
+      const unsigned char* src[2] = {static_cast<const unsigned char*>(p.K) + (long long)bh * p.cap * (PLAIN ? 2 * D : D),
+                                     static_cast<const unsigned char*>(p.V) + (long long)bh * p.cap * (PLAIN ? 2 * D : D)};
+      const int row_t = pt / CH, ch_t = pt % CH;           // this thread's chunks of a tile: one column, every STEP-th row
+      auto draft = [&](int x) {                            // x: position within the piece
+        const bool is_k = !(x & 1);
+        const int pos = 2 * g0 + x;
         unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
-        uint4 now[PER];
+        const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(is_k ? p.k_new : p.v_new);
+        const int j0 = (run.i0 + x / 2 - run.n_state) * C;
+        const int row_q = pt / QCH, ch = pt % QCH;
+        const __nv_bfloat16* at = from + (((long long)j0 * p.B + run.b) * p.Hkv + run.hk) * D + ch * 8;
+        constexpr int BATCH = 8;                           // loads in flight per thread
+        for (int k = 0; k < C / QSTEP; k += BATCH) {
+          uint4 w[BATCH];
 #pragma unroll
-        for (int x = 0; x < PER; ++x) now[x] = raw[x];
-        fetch(pos + 1);
+          for (int u = 0; u < BATCH; ++u) {
+            const int row = (k + u) * QSTEP + row_q;
+            w[u] = j0 + row < p.N ? *reinterpret_cast<const uint4*>(at + (long long)row * p.B * p.Hkv * D) : make_uint4(0, 0, 0, 0);
+          }
 #pragma unroll
-        for (int x = 0; x < PER; ++x) {
-          const int row = x * STEP + row_t;
-          const uint4 w = now[x];
-          *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t)) =
-              make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
-                         tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
-          *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + 1)) =
-              make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
-                         tree_codes2<FMT>(w.w, w.w, 0, 1), tree_codes2<FMT>(w.w, w.w, 2, 3));
+          for (int u = 0; u < BATCH; ++u) {
+            if (!is_k) tree_drop_odd(w[u]);
+            *reinterpret_cast<uint4*>(dst + place((k + u) * QSTEP + row_q, ch)) = w[u];
+          }
         }
         fence_proxy_async_smem();
         mbar_arrive(&full[pos % S::SLOTS]);
+      };
+      if constexpr (PLAIN) {
+        for (int x = 0; x < 2 * n && ok; ++x) {
+          const int pos = 2 * g0 + x, tile = run.i0 + x / 2;
+          ok = slot_free(pos);
+          if (!ok) break;
+          unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
+          if (tile >= run.n_state) {
+            draft(x);
+          } else if (p.tiled) {
+            // Rows behind the sequence's last come along: of K they give logits that are masked, of V they must be zeros.
+            const int valid = run.len - tile * C;
+            const bool trim = (x & 1) && valid < C;
+            uint64_t* bar = trim ? &bar_trim : &full[pos % S::SLOTS];
+            if (pt == 0) {
+              const int y = bh * p.cap + tile * C;
+              mbar_expect_tx(bar, S::SLOT);
+#pragma unroll
+              for (int c = 0; c < D / 64; ++c) tma_load_2d_tile(dst + c * (C * 128), (x & 1) ? &map_v : &map_k, c * 64, y, bar);
+            }
+            if (trim) {
+              ok = mbar_wait_bounded(&bar_trim, trims & 1u);
+              ++trims;
+              if (!ok) break;
+              for (int e = valid * QCH + pt; e < C * QCH; e += PT)
+                *reinterpret_cast<uint4*>(dst + place(e / QCH, e % QCH)) = make_uint4(0, 0, 0, 0);
+              fence_proxy_async_smem();
+              mbar_arrive(&full[pos % S::SLOTS]);
+            } else if (pt != 0) {
+              mbar_arrive(&full[pos % S::SLOTS]);
+            }
+          } else {
+            const unsigned char* from = ((x & 1) ? src[1] : src[0]) + ch_t * 16;
+#pragma unroll 8
+            for (int k = 0; k < PER; ++k) {
+              const int row = k * STEP + row_t, j = tile * C + row;
+              cp_async16(smem_addr(dst) + place(row, ch_t), from + (long long)min(j, run.len - 1) * (2 * D), j < run.len ? 16u : 0u);
+            }
+            cp_async_commit();
+            cp_async_wait<0>();
+            fence_proxy_async_smem();
+            mbar_arrive(&full[pos % S::SLOTS]);
+          }
+          if (x == 1) load_q();
+        }
+      } else {
+        // Raw copies run RAW_SLOTS - 1 ahead of the conversions; raw position rp = 2 (state tiles of the block so far) + x.
+        constexpr int AHEAD = S::RAW_SLOTS - 1;
+        const int n_raw = 2 * max(0, min(run.i1, run.n_state) - run.i0);
+        auto fetch = [&](int x) {
+          if (x >= n_raw || !ok) return;
+          const int rp = raw0 + x, j = (run.i0 + x / 2) * C;
+          if (rp >= S::RAW_SLOTS) ok = mbar_wait_bounded(&raw_empty[rp % S::RAW_SLOTS], (uint32_t)((rp / S::RAW_SLOTS - 1) & 1));
+          if (!ok) return;
+          const uint32_t bytes = (uint32_t)min(C, run.len - j) * D;
+          mbar_expect_tx(&raw_full[rp % S::RAW_SLOTS], bytes);
+          bulk_g2s(raw_s + (rp % S::RAW_SLOTS) * S::RAW, ((x & 1) ? src[1] : src[0]) + (long long)j * D, bytes, &raw_full[rp % S::RAW_SLOTS]);
+        };
+        // Two scales a thread and tile (columns behind the sequence's last get finite, positive ones: a masked logit is
+        // minus infinity), fetched a tile early and stored with the tile's K.
+        float next_k, next_v;
+        auto fetch_scales = [&](int tile) {
+          const int j = tile * C + pt;
+          const bool in = tile < run.n_state && j < run.len;
+          next_k = p.scale2 * (in ? p.k_scale[(long long)bh * p.cap + j] : 1.f);
+          next_v = in ? p.v_scale[(long long)bh * p.cap + j] : 1.f;
+        };
+        fetch_scales(run.i0);
+        if (pt == 0)
+          for (int x = 0; x < AHEAD; ++x) fetch(x);
+        for (int x = 0; x < 2 * n && ok; ++x) {
+          const int pos = 2 * g0 + x, tile = run.i0 + x / 2, g = g0 + x / 2;
+          if (pt == 0) fetch(x + AHEAD);
+          ok = ok && slot_free(pos);
+          if (!ok) break;
+          if (!(x & 1)) {
+            float* sc = scale_s + (g % S::SCALE_TILES) * 2 * C;
+            sc[pt] = next_k;
+            sc[C + pt] = next_v;
+            mbar_arrive(&bar_sc[g % S::SCALE_TILES]);
+            fetch_scales(tile + 1);
+          }
+          if (tile >= run.n_state) {
+            draft(x);
+          } else {
+            const int rp = raw0 + x, valid = run.len - tile * C;      // rows that were copied
+            ok = mbar_wait_bounded(&raw_full[rp % S::RAW_SLOTS], (uint32_t)((rp / S::RAW_SLOTS) & 1));
+            if (!ok) break;
+            unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
+            const unsigned char* raw = raw_s + (rp % S::RAW_SLOTS) * S::RAW + pt * 16;
+#pragma unroll 4
+            for (int k = 0; k < PER; ++k) {
+              const int row = k * STEP + row_t;
+              const uint4 w = row < valid ? *reinterpret_cast<const uint4*>(raw + k * (PT * 16)) : make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t)) =
+                  make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
+                             tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
+              *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + 1)) =
+                  make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
+                             tree_codes2<FMT>(w.w, w.w, 0, 1), tree_codes2<FMT>(w.w, w.w, 2, 3));
+            }
+            fence_proxy_async_smem();          // for the tensor cores' reads, and for the next copy into the raw slot
+            mbar_arrive(&full[pos % S::SLOTS]);
+            mbar_arrive(&raw_empty[rp % S::RAW_SLOTS]);
+          }
+          if (x == 1) load_q();
+        }
+        raw0 += n_raw;
       }
+      g0 += n;
+      ++piece;
     }
-    named_barrier_sync(1, 32 * ISSUER);          // odd_s is final
+    // (Bulk copies: where a wait ran out it took two seconds, and whatever was on its way has landed since.)
   } else if (warp == ISSUER) {
     // ============================== issuing thread ==============================
-    if (lane == 0 && n > 0) {
+    if (lane == 0) {
       const uint32_t idesc_s = umma_idesc_bf16(R, C, false);
       const uint32_t idesc_o = umma_idesc_bf16(R, D, true);
-      const uint32_t q_a = smem_addr(q_s), slot_a = smem_addr(slot_s);
-      // cp.async writes through the generic proxy: a tile that has landed is ordered before the tensor cores' reads by a
-      // proxy fence here, behind the wait.
-      auto landed = [&](int pos) {
-        if (!mbar_wait_bounded(&full[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS) & 1))) return false;
-        fence_proxy_async_smem();
-        return true;
-      };
-      auto issue_s = [&](int t, int i) {
-        const uint32_t k_a = slot_a + ((2 * i) % S::SLOTS) * S::SLOT;
+      // A descriptor's low word holds the address in units of 16 bytes, so stepping through an operand is an addition to
+      // that word.  (The tensor cores take a contraction every 64 cycles; forming each descriptor anew took this thread
+      // longer than that, beside the soft-max warps that share its scheduler.)
+      const uint64_t q_d = umma_desc_sw128(smem_addr(q_s), 16, 1024);
+      const uint64_t k_d = umma_desc_sw128(smem_addr(slot_s), 16, 1024), v_d = umma_desc_sw128(smem_addr(slot_s), C * 128, 1024);
+      auto at = [](uint64_t d, uint32_t bytes) { return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4)); };
+      // (What the producers wrote through the generic proxy they have fenced themselves, before they reported it: the fence
+      // takes hundreds of cycles, which this thread does not have.)
+      auto landed = [&](int pos) { return mbar_wait_bounded(&full[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS) & 1)); };
+      int g0 = 0, piece = 0;
+      while (ok && run.next(p, blockIdx.x)) {
+        const int n = run.i1 - run.i0;
+        auto issue_s = [&](int t, int x) {
+          const int pos = 2 * (g0 + x);
+          const uint64_t k_t = at(k_d, (pos % S::SLOTS) * S::SLOT);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const uint64_t a = umma_desc_sw128(q_a + t * S::Q_BYTES + (ks >> 2) * (R * 128) + (ks & 3) * 32, 16, 1024);
-          const uint64_t bd = umma_desc_sw128(k_a + (ks >> 2) * (C * 128) + (ks & 3) * 32, 16, 1024);
-          umma_bf16(tmem + 256 * t, a, bd, idesc_s, ks > 0 ? 1u : 0u);
-        }
-        umma_commit(&bar_s[t]);
-        if (t == NT - 1) umma_commit(&empty[(2 * i) % S::SLOTS]);
-      };
-      ok = mbar_wait_bounded(&bar_q, 0u) && landed(0);
-      if (ok) {
+          for (int ks = 0; ks < D / 16; ++ks)
+            umma_bf16(tmem + 256 * t, at(q_d, t * S::Q_BYTES + (ks >> 2) * (R * 128) + (ks & 3) * 32),
+                      at(k_t, (ks >> 2) * (C * 128) + (ks & 3) * 32), idesc_s, ks > 0 ? 1u : 0u);
+          umma_commit(&bar_s[t]);
+          if (t == NT - 1) {
+            umma_commit(&empty[pos % S::SLOTS]);
+            if (x == n - 1) umma_commit(&bar_qf);
+          }
+        };
+        ok = mbar_wait_bounded(&bar_q, (uint32_t)(piece & 1)) && landed(2 * g0);
+        if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int t = 0; t < NT; ++t) issue_s(t, 0);
-      }
-      for (int i = 0; i < n && ok; ++i) {
-        const uint32_t v_a = slot_a + ((2 * i + 1) % S::SLOTS) * S::SLOT;
+        for (int x = 0; x < n && ok; ++x) {
+          const int g = g0 + x, pos = 2 * g + 1;
+          const uint64_t v_t = at(v_d, (pos % S::SLOTS) * S::SLOT);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if (t == 0) ok = landed(2 * i + 1);
-          ok = ok && mbar_wait_bounded(&bar_p[t], (uint32_t)(i & 1));
-          if (!ok) break;
-          tc_fence_after();
-#pragma unroll
-          for (int kk = 0; kk < C / 16; ++kk)
-            umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + kk * 8, umma_desc_sw128(v_a + kk * 2048, C * 128, 1024), idesc_o,
-                             (i > 0 || kk > 0) ? 1u : 0u);
-          if (t == NT - 1) umma_commit(&empty[(2 * i + 1) % S::SLOTS]);
-          if (i + 1 < n) {
-            if (t == 0) ok = landed(2 * i + 2);
+          for (int t = 0; t < NT; ++t) {
+            if (t == 0) ok = landed(pos);
+            ok = ok && mbar_wait_bounded(&bar_p[t], (uint32_t)(g & 1));
             if (!ok) break;
             tc_fence_after();
-            issue_s(t, i + 1);
-          } else {
-            umma_commit(&bar_o[t]);
+            // (the weights of columns 64.. lie 64 TMEM columns up: each half of a row overwrites its own logits only)
+#pragma unroll
+            for (int kk = 0; kk < C / 16; ++kk)
+              umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + (kk >> 2) * 64 + (kk & 3) * 8,
+                               at(v_t, kk * 2048), idesc_o, (x > 0 || kk > 0) ? 1u : 0u);
+            if (t == NT - 1) umma_commit(&empty[pos % S::SLOTS]);
+            if (x + 1 < n) {
+              if (t == 0) ok = landed(pos + 1);
+              if (!ok) break;
+              tc_fence_after();
+              issue_s(t, x + 1);
+            } else {
+              umma_commit(&bar_o[t]);
+            }
           }
         }
+        g0 += n;
+        ++piece;
       }
+    }
+  } else if (warp == HELPER) {
+    // ============================== helper warp ==============================
+    int done = 0;                                          // pieces with drafts so far
+    while (run.next(p, blockIdx.x)) {
+      if (run.i1 <= run.n_state) continue;
+      if (done > 0 && !warp_wait(&bar_af, (uint32_t)((done - 1) & 1))) break;
+      for (int i = lane; i < p.N; i += 32) par_s[i] = p.parents ? p.parents[(long long)i * p.B + run.b] : i - 1;
+      __syncwarp();
+      for (int i = lane; i < p.N; i += 32) tree_ancestor_bits<S::WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
+      bool odd = false;
+#pragma unroll 4
+      for (int e = lane; e < p.N * (D / 8); e += 32) {
+        uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.v_new) +
+                                                  (((long long)(e / (D / 8)) * p.B + run.b) * p.Hkv + run.hk) * D + (e % (D / 8)) * 8);
+        odd |= tree_drop_odd(w);
+      }
+      odd = __any_sync(0xffffffffu, odd) != 0;
+      if (lane == 0) odd_s = odd;
+      mbar_arrive(&bar_a);
+      ++done;
     }
   } else {
-    // ============================== soft-max: one thread per row ==============================
-    const int t = warp >> 2;
-    const uint32_t base = tmem + 256 * t + ((uint32_t)((warp & 3) * 32) << 16);
-    const int m0 = row0 + t * R + (warp & 3) * 32;       // the warp's first row
-    const int node = m0 + lane < p.M ? (m0 + lane) / p.G : -1;
-    // Q rows of the row tile, K-major with the 128-byte swizzle; rows past the product are zeros.
-    {
-      constexpr int CH = D / 8, STEP = 128 / CH;
-      const int x = tid & 127, row_t = x / CH, ch = x % CH;
-      const uint32_t dst = smem_addr(q_s + t * S::Q_BYTES) + (ch >> 3) * (R * 128);
-#pragma unroll 4
-      for (int k = 0; k < R / STEP; ++k) {
-        const int r = k * STEP + row_t, m = row0 + t * R + r;
-        const int nd = min(m, p.M - 1) / p.G, g = min(m, p.M - 1) - nd * p.G;
-        cp_async16(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
-                   static_cast<const __nv_bfloat16*>(p.q) + (((long long)nd * p.B + b) * p.H + hk * p.G + g) * D + ch * 8, m < p.M ? 16u : 0u);
-      }
-      cp_async_commit();
-    }
-    if (last) {
-      for (int i = tid; i < p.N; i += 32 * S::SOFT_WARPS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
-      named_barrier_sync(2, 32 * S::SOFT_WARPS);
-      for (int i = tid; i < p.N; i += 32 * S::SOFT_WARPS) tree_ancestor_bits<S::WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
-    }
-    cp_async_wait<0>();
-    fence_proxy_async_smem();
-    mbar_arrive(&bar_q);
-    named_barrier_sync(2, 32 * S::SOFT_WARPS);
-    const uint32_t* anc = anc_s[max(node, 0)];
-    bool real = false;               // a node's row, not padding's or one behind the product
-    if (last && node >= 0) {
-#pragma unroll
-      for (int k = 0; k < S::WORDS; ++k) real |= anc[k] != 0;
-    }
-    float m_ref = -INFINITY, l = 0.f;
+    // ============================== soft-max: two threads per row ==============================
+    // Warps 0-3 of a row tile take the first 64 columns of its rows, warps 4-7 the others; a warp reaches the 32 TMEM
+    // lanes of its quarter (warp mod 4).
+    const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;
+    const int pair = t * 4 + quarter, row = t * R + quarter * 32 + lane;
+    const uint32_t base = tmem + 256 * t + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t mine = base + 64 * half;                // this thread's logits, and its weights
     const uint64_t scale_2 = pack_f2(p.scale2, p.scale2);
-    for (int i = 0; i < n; ++i) {
-      const float* sc = scale_s + (i % S::SCALE_TILES) * 2 * C;
-      ok = mbar_wait_bounded(&bar_s[t], (uint32_t)(i & 1));
-      if constexpr (!PLAIN) ok = ok && mbar_wait_bounded(&bar_sc[i % S::SCALE_TILES], (uint32_t)((i / S::SCALE_TILES) & 1));
-      ok = __all_sync(0xffffffffu, ok) != 0;
-      if (!ok) break;
-      tc_fence_after();
-      // A quarter of a row's logits at a time, read once for the maximum and again for the weights: that costs less than 128
-      // registers a thread would.
-      const int left = i < n_state ? c1 - (c0 + i * C) : C;
-      float s[32];
-      auto logits = [&](int h) {
-        tmem_ld32(base + 32 * h, s);
-        if constexpr (!PLAIN) {
+    volatile TreeTcRun& mr = soft_run_s[warp];
+    int g0 = 0, piece = 0, done = 0;
+    uint32_t met = 0;                    // phase of the pair's barrier
+    // The two warps that share 32 rows meet: what either wrote to shared memory before is there for both.
+    auto meet = [&]() {
+      mbar_arrive(&bar_pair[pair]);
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bar_pair[pair], met)) != 0;
+      met ^= 1u;
+    };
+    if (lane == 0) soft_run_s[warp] = run;
+    __syncwarp();
+    for (;;) {
+      int more = 0;
+      __syncwarp();
+      if (lane == 0) more = soft_run_s[warp].next(p, blockIdx.x);
+      __syncwarp();
+      if (!__shfl_sync(0xffffffffu, more, 0)) break;
+      const int n = mr.i1 - mr.i0;
+      const bool drafts = mr.i1 > mr.n_state;
+      const int m = mr.rb * (R * NT) + row;
+      const int node = m < p.M ? m / p.G : -1;
+      const uint32_t* anc = anc_s[max(node, 0)];
+      bool real = false, looked = false;         // a node's row, not padding's or one behind the product
+      auto look = [&]() {                        // the drafts' ancestor bits, from the first time they are needed
+        ok = __all_sync(0xffffffffu, ok && mbar_wait_bounded(&bar_a, (uint32_t)(done & 1))) != 0;
+        looked = true;
+        if (ok && node >= 0) {
 #pragma unroll
-          for (int c = 0; c < 32; c += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(sc + 32 * h + c);
-            s[c] *= f.x; s[c + 1] *= f.y; s[c + 2] *= f.z; s[c + 3] *= f.w;
-          }
-        }
-        if (i >= n_state) {
-          const int w = 4 * (i - n_state) + h;
-          const uint32_t see = real && w < S::WORDS ? anc[w] : 0u;
-#pragma unroll
-          for (int c = 0; c < 32; ++c) s[c] = ((see >> c) & 1u) ? s[c] : -INFINITY;
-        } else if (left < C) {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) s[c] = 32 * h + c < left ? s[c] : -INFINITY;
+          for (int k = 0; k < S::WORDS; ++k) real |= anc[k] != 0;
         }
       };
-      float top = -INFINITY;
+      float m_ref = -INFINITY, l = 0.f;
+      for (int x = 0; x < n && ok; ++x) {
+        const int i = mr.i0 + x, g = g0 + x;
+        const float* sc = scale_s + (g % S::SCALE_TILES) * 2 * C + 64 * half;
+        ok = mbar_wait_bounded(&bar_s[t], (uint32_t)(g & 1));
+        if constexpr (!PLAIN) ok = ok && mbar_wait_bounded(&bar_sc[g % S::SCALE_TILES], (uint32_t)((g / S::SCALE_TILES) & 1));
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (ok && i >= mr.n_state && !looked) look();
+        if (!ok) break;
+        tc_fence_after();
+        const int left = i < mr.n_state ? mr.len - i * C - 64 * half : 64;      // this half's columns that exist
+        const bool masked = i >= mr.n_state || left < 64;                       // the same for the whole warp
+        uint32_t see[2] = {0xffffffffu, 0xffffffffu};
+        if (masked) {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        logits(h);
-        float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-        for (int c = 4; c < 32; c += 4)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[c + k]);
-        top = fmaxf(top, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
-      }
-      top *= p.scale2;
-      float corr = 1.f;
-      if (top > m_ref + TREE_TC_SLACK || (m_ref == -INFINITY && top > -INFINITY)) {
-        corr = ex2_approx(m_ref - top);
-        m_ref = top;
-        l *= corr;
-      }
-      __syncwarp();
-      // O of the tiles so far was summed against the old reference.  (The last of them is complete: S of this tile was
-      // issued behind it.)
-      if (i > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
-#pragma unroll
-        for (int c = 0; c < D; c += 32) {
-          tmem_ld32(base + 128 + c, s);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) s[k] *= corr;
-          tmem_st32(base + 128 + c, s);
-        }
-      }
-      const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-      const uint64_t mneg_2 = pack_f2(-ref, -ref);
-      uint64_t sum2[2] = {pack_f2(0.f, 0.f), pack_f2(0.f, 0.f)};
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        logits(h);
-        uint32_t w[16];            // packed weights, two bf16 each
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float x0, x1;
-          unpack_f2(fma_f2(pack_f2(s[2 * e], s[2 * e + 1]), scale_2, mneg_2), x0, x1);
-          const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
-          if constexpr (PLAIN) {
-            w[e] = pack_bf16(e0, e1);
-            sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)));
-          } else {
-            // (the sum is over the weights as they were before the value scale went in: to divide it out again costs
-            //  more than it gives)
-            sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(e0, e1));
-            const float2 f = *reinterpret_cast<const float2*>(sc + C + 32 * h + 2 * e);
-            w[e] = pack_bf16(e0 * f.x, e1 * f.y);
+          for (int h = 0; h < 2; ++h) {
+            if (i >= mr.n_state) {
+              const int w = 4 * (i - mr.n_state) + 2 * half + h;
+              see[h] = real && w < S::WORDS ? anc[w] : 0u;
+            } else {
+              see[h] = left >= 32 * h + 32 ? 0xffffffffu : left > 32 * h ? (1u << (left - 32 * h)) - 1u : 0u;
+            }
           }
         }
-        tmem_st16(base + 16 * h, w);       // over logits that have been read
+        uint32_t w[32];            // packed weights, two bf16 each
+        float sum;
+        auto logits = [&](int h, uint32_t (&s)[32]) {
+          tmem_ld32_start(mine + 32 * h, s);
+          tmem_ld32_wait(s);
+          if (masked) {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) s[c] = ((see[h] >> c) & 1u) ? s[c] : 0xff800000u;
+          }
+        };
+        auto weights = [&]() {
+          const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+          const uint64_t mneg_2 = pack_f2(-ref, -ref);
+          uint64_t sum2[2] = {pack_f2(0.f, 0.f), pack_f2(0.f, 0.f)};
+          uint64_t kf[2] = {scale_2, scale_2}, vf[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t s[32];
+            logits(h, s);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              if constexpr (!PLAIN)
+                if (e % 2 == 0) {
+                  lds_f2x2(sc + 32 * h + 2 * e, kf);         // the logits' scale is in there
+                  lds_f2x2(sc + C + 32 * h + 2 * e, vf);
+                }
+              float x0, x1, e0, e1;
+              unpack_f2(fma_f2(pack_f2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), kf[e & 1], mneg_2), x0, x1);
+              e0 = ex2_approx(x0);
+              e1 = ex2_approx(x1);
+              if constexpr (PLAIN) {
+                const uint32_t u = pack_bf16(e0, e1);
+                sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
+                w[16 * h + e] = u;
+              } else {
+                // (the sum is over the weights as they were before the value scale went in: to divide it out again
+                //  costs more than it gives)
+                const uint64_t e2 = pack_f2(e0, e1);
+                sum2[e & 1] = add_f2(sum2[e & 1], e2);
+                unpack_f2(mul_f2(e2, vf[e & 1]), e0, e1);
+                w[16 * h + e] = pack_bf16(e0, e1);
+              }
+            }
+          }
+          float s0, s1;
+          unpack_f2(add_f2(sum2[0], sum2[1]), s0, s1);
+          sum = s0 + s1;
+        };
+        bool over = x == 0;              // the reference has to be found or moved
+        if (x > 0) {
+          weights();
+          // Both threads of a row have to agree on its reference: the pair of warps meets, and a row of either whose sum
+          // is too large (or not a number) sends both round again.
+          if (__any_sync(0xffffffffu, !(sum <= TREE_TC_MOST) || m_ref == -INFINITY)) flag_s[pair] = g;
+          meet();
+          if (!ok) break;
+          over = *reinterpret_cast<volatile int*>(&flag_s[pair]) == g;
+        }
+        if (over) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t s[32];
+            logits(h, s);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) top = fmaxf(top, __uint_as_float(s[c]) * (PLAIN ? p.scale2 : sc[32 * h + c]));
+          }
+          pair_s[row][half] = top;
+          meet();
+          if (!ok) break;
+          top = fmaxf(top, pair_s[row][half ^ 1]);
+          // (a reference that is right already stays: another row of the warp asked)
+          const bool beyond = top > m_ref + 16.f || (m_ref == -INFINITY && top > -INFINITY);
+          const float m_new = beyond ? ceilf(top) : m_ref;
+          const float corr = beyond ? ex2_approx(m_ref - m_new) : 1.f;       // a power of two, or 0
+          m_ref = m_new;
+          l *= corr;
+          if (x > 0) {
+            // O of the tiles so far, half the columns a thread.  (The last of them is complete: S of this tile was issued
+            // behind it.)
+#pragma unroll
+            for (int c = 0; c < D / 2; c += 16) tree_tc_scale16(base + 128 + half * (D / 2) + c, corr);
+          }
+          weights();
+          meet();                                  // (pair_s may be written again)
+          if (!ok) break;
+        }
+        l += sum;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t (&wh)[16] = *reinterpret_cast<uint32_t (*)[16]>(&w[16 * h]);
+          tmem_st16(mine + 16 * h, wh);                                      // over logits that have been read
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&bar_p[t]);
       }
-      float s0, s1;
-      unpack_f2(add_f2(sum2[0], sum2[1]), s0, s1);
-      l += s0 + s1;
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(&bar_p[t]);
-    }
-    // Every row tile's last contraction: Q and the ring are then free for O's way out.
-    if (ok && n > 0) {
-#pragma unroll
-      for (int x = 0; x < NT; ++x) ok = ok && mbar_wait_bounded(&bar_o[x], 0u);
-      ok = __all_sync(0xffffffffu, ok) != 0;
-      tc_fence_after();
-    }
-    named_barrier_sync(1, 32 * ISSUER);          // odd_s is final; no thread is still copying
-    pdl_launch_dependents();
-    if (last && !real) l = TREE_PADDING;
-    if (!ok) l = __uint_as_float(0x7fc00000u);
-    const bool zero = n == 0 || l == TREE_PADDING || l == 0.f;
-    const float r = p.splits > 1 ? 1.f : (zero ? 0.f : 1.f / l);
-    const long long at0 = ((long long)split * gridDim.z + blockIdx.z) * p.M + m0;
-    if (p.splits > 1 && node >= 0) p.part_ml[at0 + lane] = make_float2(m_ref, l);
-    constexpr int OCH = D / 4;                   // 16-byte chunks of a row of O, turned with the row: no bank conflicts
-    unsigned char* stage = smem + (t * R + (warp & 3) * 32) * (D * 4);
-#pragma unroll
-    for (int c = 0; c < D; c += 32) {
-      float o[32];
-      tmem_ld32(base + 128 + c, o);              // (nothing was written there in a block without columns: not used then)
-      if (last && odd_s && real) tree_add_odd<S::WORDS, 32>(p, b, hk, anc, D, c, o);
-#pragma unroll
-      for (int k = 0; k < 32; k += 4)
-        *reinterpret_cast<float4*>(stage + lane * (D * 4) + ((((c + k) / 4) ^ (lane & (OCH - 1))) << 4)) =
-            zero ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[k] * r, o[k + 1] * r, o[k + 2] * r, o[k + 3] * r);
-      __syncwarp();
-    }
-    constexpr int AT_ONCE = 32 / OCH;            // rows a warp writes at a time
-#pragma unroll 4
-    for (int x = 0; x < 32; x += AT_ONCE) {
-      const int rr = x + lane / OCH, m = m0 + rr, ch = lane % OCH;
-      if (m >= p.M) break;
-      const float4 v = *reinterpret_cast<const float4*>(stage + rr * (D * 4) + ((ch ^ (rr & (OCH - 1))) << 4));
-      if (p.splits == 1) {
-        const int nd = m / p.G, g = m - nd * p.G;
-        tree_store4<__nv_bfloat16>(static_cast<__nv_bfloat16*>(p.out) + (((long long)nd * p.B + b) * p.H + hk * p.G + g) * D + ch * 4,
-                                   v.x, v.y, v.z, v.w);
-      } else {
-        *reinterpret_cast<float4*>(p.part_acc + (at0 + rr) * D + ch * 4) = v;
+      if (drafts && ok && !looked) look();
+      if (ok) {
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bar_o[t], (uint32_t)(piece & 1))) != 0;
+        tc_fence_after();
       }
+      // The row's sum: both halves'.
+      if (ok) {
+        pair_s[row][half] = l;
+        meet();
+        l += pair_s[row][half ^ 1];
+        if (ok) meet();
+      }
+      if (mr.last && !real) l = TREE_PADDING;
+      if (!ok) l = __uint_as_float(0x7fc00000u);
+      const bool zero = l == TREE_PADDING || l == 0.f;
+      const float r = mr.part >= 0 ? 1.f : (zero ? 0.f : 1.f / l);
+      const long long at = (long long)mr.part * (R * NT) + row;
+      if (mr.part >= 0 && half == 0) p.part_ml[at] = make_float2(m_ref, l);
+      const int gq = max(node, 0);
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) +
+                           (((long long)gq * p.B + mr.b) * p.H + mr.hk * p.G + (max(m, 0) - gq * p.G)) * D + half * (D / 2);
+      float* acc = p.part_acc + at * D + half * (D / 2);
+#pragma unroll
+      for (int c = 0; c < D / 2; c += 32) {
+        float o[32];
+        if (ok) {
+          tmem_ld32(base + 128 + half * (D / 2) + c, o);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = __uint_as_float(0x7fc00000u);
+        }
+        if (drafts && odd_s && real && ok) tree_add_odd<S::WORDS, 32>(p, mr.b, mr.hk, anc, D, half * (D / 2) + c, o);
+        if (zero) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0.f;
+        }
+        if (node >= 0 && mr.part < 0) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 8)
+            *reinterpret_cast<uint4*>(out + c + k) = make_uint4(pack_bf16(o[k] * r, o[k + 1] * r), pack_bf16(o[k + 2] * r, o[k + 3] * r),
+                                                                pack_bf16(o[k + 4] * r, o[k + 5] * r), pack_bf16(o[k + 6] * r, o[k + 7] * r));
+        } else if (mr.part >= 0) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(acc + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+        }
+        __syncwarp();
+      }
+      tc_fence_before();                 // O has been read: the next piece's first weights are reported behind this
+      if (drafts) {
+        mbar_arrive(&bar_af);
+        ++done;
+      }
+      g0 += n;
+      ++piece;
     }
   }
+  pdl_launch_dependents();
   tc_fence_before();
   __syncthreads();
   if (warp == ISSUER)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS) : "memory");
+}
+
+// Joins the pieces of the jobs that were cut, one warp per row; a job that lay in one run has been written already.
+// grid = (jobs, rows of a job / 8).
+constexpr int TREE_TC_JOIN_THREADS = 256;
+template <int D, int NT>
+__global__ void __launch_bounds__(TREE_TC_JOIN_THREADS) tova_tree_tc_join_kernel(const __grid_constant__ TreeParams p) {
+  constexpr int ROWS = TREE_TC_ROWS * NT;
+  __shared__ long long sums[2][TREE_TC_JOIN_THREADS / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rb = blockIdx.x % p.row_blocks, bh = blockIdx.x / p.row_blocks, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  const int jobs = p.Hkv * p.row_blocks, tiles = tree_tc_tiles(p, b);
+  long long before, total;
+  if (p.lens) {
+    long long x = 0, y = 0;
+    for (int i = tid; i < p.B; i += TREE_TC_JOIN_THREADS) {
+      const int t = tree_tc_tiles(p, i);
+      y += t;
+      if (i < b) x += t;
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+      x += __shfl_xor_sync(0xffffffffu, x, o);
+      y += __shfl_xor_sync(0xffffffffu, y, o);
+    }
+    if (lane == 0) { sums[0][warp] = x; sums[1][warp] = y; }
+    __syncthreads();
+    before = total = 0;
+    for (int i = 0; i < TREE_TC_JOIN_THREADS / 32; ++i) { before += sums[0][i]; total += sums[1][i]; }
+    before *= jobs;
+    total *= jobs;
+  } else {
+    before = (long long)tiles * jobs * b;
+    total = (long long)tiles * jobs * p.B;
+  }
+  const long long share = tree_tc_share(total, p.blocks, p.least);
+  const long long first_tile = before + (long long)(hk * p.row_blocks + rb) * tiles;
+  const int c0 = (int)(first_tile / share), c1 = (int)((first_tile + tiles - 1) / share);
+  pdl_wait();             // (in every block: the launch must not be over before the one that it depends on)
+  if (c0 == c1) return;
+  constexpr int E = D / 32;
+  const int r = blockIdx.y * (TREE_TC_JOIN_THREADS / 32) + warp, m = rb * ROWS + r;
+  if (m >= p.M) return;
+  // Block c's piece of this job is its first one, unless its run began before the job.
+  auto part_row = [&](int c) { return (long long)(2 * c + (c * share < first_tile ? 1 : 0)) * ROWS + r; };
+  float top = -INFINITY;
+  bool pad = false;
+  for (int c = c0 + lane; c <= c1; c += 32) {
+    const float2 ml = p.part_ml[part_row(c)];
+    top = fmaxf(top, ml.x);
+    if (c == c1) pad = ml.y == TREE_PADDING;
+  }
+  top = warp_max(top);
+  pad = __any_sync(0xffffffffu, pad) != 0;
+  const float base = top == -INFINITY ? 0.f : top;
+  float acc[E], l = 0.f;
+#pragma unroll
+  for (int j = 0; j < E; ++j) acc[j] = 0.f;
+  for (int cc = c0; cc <= c1; cc += 32) {
+    float f = 0.f;                 // this lane's piece: its factor, and its share of the sum
+    if (cc + lane <= c1) {
+      const float2 ml = p.part_ml[part_row(cc + lane)];
+      f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - base);
+      if (f != 0.f) l += f * ml.y;
+    }
+    const int n = min(32, c1 - cc + 1);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float fi = __shfl_sync(0xffffffffu, f, i);
+      const float* a = p.part_acc + part_row(cc + i) * D + lane * E;
+#pragma unroll
+      for (int j = 0; j < E; ++j) acc[j] = fmaf(fi, a[j], acc[j]);
+    }
+  }
+  l = warp_sum(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int n = m / p.G, g = m - n * p.G;
+  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + lane * E;
+#pragma unroll
+  for (int j = 0; j < E; ++j) dst[j] = (__nv_bfloat16)(pad ? 0.f : acc[j] * inv);
 }
 
 }  // namespace tova
