@@ -300,7 +300,7 @@ enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64, TREE_TC_1, TREE_TC
 struct TreePlan {
   int kernel, row_blocks, splits, split_cols;
   int blocks, least;             // tcgen05 kernel
-  size_t ml_bytes, bytes;
+  size_t ml_bytes, acc_bytes, bytes;   // workspace: maxima and sums, weighted sums (and the tcgen05 kernel's list of cuts)
 };
 
 TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count) {
@@ -339,7 +339,8 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     part_rows = t.splits > 1 ? (size_t)t.splits * c.batch * c.n_kv_heads * M : 0;
   }
   t.ml_bytes = (part_rows * sizeof(float2) + 255) / 256 * 256;
-  t.bytes = t.ml_bytes + part_rows * c.head_dim * sizeof(float);
+  t.acc_bytes = part_rows * c.head_dim * sizeof(float);
+  t.bytes = t.ml_bytes + t.acc_bytes + t.blocks * sizeof(tova::TreeTcCut);
   return t;
 }
 
@@ -405,7 +406,7 @@ cudaError_t tree_run_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream
   if (e != cudaSuccess) return e;
   constexpr int JOIN_ROWS = tova::TREE_TC_JOIN_THREADS / 32;
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3((unsigned)(p.B * p.Hkv * t.row_blocks), (unsigned)((std::min(p.M, NT * tova::TREE_TC_ROWS) + JOIN_ROWS - 1) / JOIN_ROWS));
+  lc.gridDim = dim3((unsigned)t.blocks, (unsigned)((std::min(p.M, NT * tova::TREE_TC_ROWS) + JOIN_ROWS - 1) / JOIN_ROWS));
   lc.blockDim = dim3(tova::TREE_TC_JOIN_THREADS);
   lc.stream = st;
   cudaLaunchAttribute at[1];
@@ -475,6 +476,7 @@ extern "C" int tova_tree_attention(const tova_tree_config* cfg, const void* K, c
   p.lens = lens; p.parents = parents; p.out = out;
   p.part_ml = static_cast<float2*>(workspace);
   p.part_acc = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + t.ml_bytes);
+  p.cuts = static_cast<unsigned char*>(workspace) + t.ml_bytes + t.acc_bytes;
   p.N = n_nodes; p.B = cfg->batch; p.H = cfg->n_q_heads; p.Hkv = cfg->n_kv_heads;
   p.G = p.H / p.Hkv; p.M = p.N * p.G; p.cap = cfg->capacity; p.n_live = n_live;
   p.splits = t.splits; p.split_cols = t.split_cols;

@@ -37,6 +37,7 @@ struct TreeParams {
   int N, B, H, Hkv, G, M, cap, n_live;
   int splits, split_cols;      // columns of a run (a multiple of the kernel's tile); the last run also has the drafts
   int row_blocks, blocks, least;   // tcgen05 kernel: jobs per KV head, blocks, fewest tiles of a block's run
+  void* cuts;                  // tcgen05 kernel: one TreeTcCut per block
   int tiled;                   // tcgen05 kernel: there are tensor maps of a bf16 state
   float scale2;                // scale * log2(e)
 };

@@ -70,6 +70,11 @@ __device__ __forceinline__ long long tree_tc_share(long long total, int blocks, 
   return even > least ? even : least;
 }
 
+// A job that starts in one block's run and goes on in the following ones'.
+struct TreeTcCut {
+  int pieces, b, hk, rb, part;     // pieces (0: there is none such), the job, the index of the first piece
+};
+
 // Where a block is in its run.  Every role holds its own copy and steps through the same pieces.
 struct TreeTcRun {
   long long at, end, base;      // next tile, end of the run, first tile of sequence b's jobs
@@ -483,7 +488,18 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
   } else if (warp == HELPER) {
     // ============================== helper warp ==============================
     int done = 0;                                          // pieces with drafts so far
+    // For the second kernel: the job that starts in this run and goes on in another, if there is one.
+    TreeTcCut cut{};
+    const long long share = run.end - run.at;              // (only the last block's may be shorter, and it cuts nothing)
     while (run.next(p, blockIdx.x)) {
+      if (run.i0 == 0 && !run.last) {
+        const long long first_tile = run.at - run.i1;
+        cut.pieces = (int)((first_tile + run.tiles - 1) / share) - (int)blockIdx.x + 1;
+        cut.b = run.b;
+        cut.hk = run.hk;
+        cut.rb = run.rb;
+        cut.part = run.part;
+      }
       if (run.i1 <= run.n_state) continue;
       if (done > 0 && !warp_wait(&bar_af, (uint32_t)((done - 1) & 1))) break;
       for (int i = lane; i < p.N; i += 32) par_s[i] = p.parents ? p.parents[(long long)i * p.B + run.b] : i - 1;
@@ -501,6 +517,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       mbar_arrive(&bar_a);
       ++done;
     }
+    if (lane == 0) static_cast<TreeTcCut*>(p.cuts)[blockIdx.x] = cut;
   } else {
     // ============================== soft-max: two threads per row ==============================
     // Warps 0-3 of a row tile take the first 64 columns of its rows, warps 4-7 the others; a warp reaches the 32 TMEM
@@ -725,49 +742,20 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS) : "memory");
 }
 
-// Joins the pieces of the jobs that were cut, one warp per row; a job that lay in one run has been written already.
-// grid = (jobs, rows of a job / 8).
+// Joins the pieces of the jobs that were cut, one warp per row.  grid = (blocks of the first kernel, rows of a job / 8).
 constexpr int TREE_TC_JOIN_THREADS = 256;
 template <int D, int NT>
 __global__ void __launch_bounds__(TREE_TC_JOIN_THREADS) tova_tree_tc_join_kernel(const __grid_constant__ TreeParams p) {
-  constexpr int ROWS = TREE_TC_ROWS * NT;
-  __shared__ long long sums[2][TREE_TC_JOIN_THREADS / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rb = blockIdx.x % p.row_blocks, bh = blockIdx.x / p.row_blocks, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-  const int jobs = p.Hkv * p.row_blocks, tiles = tree_tc_tiles(p, b);
-  long long before, total;
-  if (p.lens) {
-    long long x = 0, y = 0;
-    for (int i = tid; i < p.B; i += TREE_TC_JOIN_THREADS) {
-      const int t = tree_tc_tiles(p, i);
-      y += t;
-      if (i < b) x += t;
-    }
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) {
-      x += __shfl_xor_sync(0xffffffffu, x, o);
-      y += __shfl_xor_sync(0xffffffffu, y, o);
-    }
-    if (lane == 0) { sums[0][warp] = x; sums[1][warp] = y; }
-    __syncthreads();
-    before = total = 0;
-    for (int i = 0; i < TREE_TC_JOIN_THREADS / 32; ++i) { before += sums[0][i]; total += sums[1][i]; }
-    before *= jobs;
-    total *= jobs;
-  } else {
-    before = (long long)tiles * jobs * b;
-    total = (long long)tiles * jobs * p.B;
-  }
-  const long long share = tree_tc_share(total, p.blocks, p.least);
-  const long long first_tile = before + (long long)(hk * p.row_blocks + rb) * tiles;
-  const int c0 = (int)(first_tile / share), c1 = (int)((first_tile + tiles - 1) / share);
-  pdl_wait();             // (in every block: the launch must not be over before the one that it depends on)
-  if (c0 == c1) return;
-  constexpr int E = D / 32;
-  const int r = blockIdx.y * (TREE_TC_JOIN_THREADS / 32) + warp, m = rb * ROWS + r;
-  if (m >= p.M) return;
-  // Block c's piece of this job is its first one, unless its run began before the job.
-  auto part_row = [&](int c) { return (long long)(2 * c + (c * share < first_tile ? 1 : 0)) * ROWS + r; };
+  constexpr int ROWS = TREE_TC_ROWS * NT, E = D / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = blockIdx.y * (TREE_TC_JOIN_THREADS / 32) + warp;
+  pdl_wait();
+  const TreeTcCut cut = static_cast<const TreeTcCut*>(p.cuts)[blockIdx.x];
+  const int m = cut.rb * ROWS + r;
+  if (cut.pieces == 0 || m >= p.M) return;
+  // The pieces behind the first are the first ones of the blocks that follow.
+  auto part_row = [&](int c) { return (long long)(c == 0 ? cut.part : 2 * ((int)blockIdx.x + c)) * ROWS + r; };
+  const int c0 = 0, c1 = cut.pieces - 1, b = cut.b, hk = cut.hk;
   float top = -INFINITY;
   bool pad = false;
   for (int c = c0 + lane; c <= c1; c += 32) {
