@@ -932,12 +932,10 @@ int check_step_args(const tova_cache* c, const void* q, const void* k, const voi
 
 }  // namespace
 
-// Tiled view of a [B*Hkv*capacity, D] bf16 matrix for the tensor-core split
-// kernel: boxes of 16 rows x 64 columns (128 bytes) with the 128-byte swizzle.
+// Tiled view of a bf16 tensor (up to three dimensions), 128-byte swizzle.
 // The driver's encoder is looked up through the runtime, so the library has no
 // link-time dependency on the driver.
-int encode_state_map(CUtensorMap* map, void* base, const tova_config& cfg, int box_rows = tova::TILE_ROWS,
-                     long long rows_per_head = 0) {
+int encode_map(CUtensorMap* map, void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
   typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -952,15 +950,22 @@ int encode_state_map(CUtensorMap* map, void* base, const tova_config& cfg, int b
     fn = reinterpret_cast<encode_fn>(sym);
     fn_cache.store(fn, std::memory_order_release);
   }
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, base, dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TOVA_OK : TOVA_ERR_CUDA;
+}
+
+// Tiled view of a [B*Hkv*capacity, D] bf16 matrix for the tensor-core split
+// kernel: boxes of 16 rows x 64 columns (128 bytes) with the 128-byte swizzle.
+int encode_state_map(CUtensorMap* map, void* base, const tova_config& cfg, int box_rows = tova::TILE_ROWS,
+                     long long rows_per_head = 0) {
   const cuuint64_t rows = (cuuint64_t)cfg.batch * cfg.n_kv_heads * (rows_per_head ? rows_per_head : cfg.capacity);
   const cuuint64_t dims[2] = {(cuuint64_t)cfg.head_dim, rows};
   const cuuint64_t strides[1] = {(cuuint64_t)cfg.head_dim * 2};
   const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-  const cuuint32_t estr[2] = {1, 1};
-  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? TOVA_OK : TOVA_ERR_CUDA;
+  return encode_map(map, base, 2, dims, strides, box);
 }
 
 // ---------------------------------------------------------------------------

@@ -3,6 +3,8 @@
 // tova_rope.cuh, tova_quant.cuh, tova_tree.cuh and tova_verify.cuh.
 #include "../../include/tova.h"
 
+#include <cuda.h>
+
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -16,7 +18,9 @@
 #include "tova_tree_tc.cuh"
 #include "tova_verify.cuh"
 
-int encode_state_map(CUtensorMap* map, void* base, const tova_config& cfg, int box_rows, long long rows_per_head);   // tova_api.cu
+// tova_api.cu
+int encode_state_map(CUtensorMap* map, void* base, const tova_config& cfg, int box_rows, long long rows_per_head);
+int encode_map(CUtensorMap* map, void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box);
 
 namespace {
 
@@ -393,7 +397,7 @@ cudaError_t tree_run_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream
   using S = tova::TreeTcShape<D, FMT, NT>;
   // Tiled views of a bf16 state in boxes of 128 rows; where they cannot be had (fewer rows, 2^31 or more) the kernel
   // copies every tile as it copies a sequence's last.
-  CUtensorMap map_k{}, map_v{};
+  CUtensorMap map_k{}, map_v{}, map_q{};
   tova::TreeParams q = p;
   const long long rows = (long long)p.B * p.Hkv * p.cap;
   if (FMT == tova::FORMAT_PLAIN && rows >= tova::TREE_TC_COLS && rows < (1LL << 31)) {
@@ -402,7 +406,15 @@ cudaError_t tree_run_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream
     q.tiled = encode_state_map(&map_k, const_cast<void*>(p.K), c, tova::TREE_TC_COLS, 0) == TOVA_OK &&
               encode_state_map(&map_v, const_cast<void*>(p.V), c, tova::TREE_TC_COLS, 0) == TOVA_OK;
   }
-  cudaError_t e = tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, dim3((unsigned)t.blocks), st, q, map_k, map_v);
+  // q as [N, B * H, D] in boxes of 128 / G nodes x one KV head's G query heads, where G divides 128.
+  if (tova::TREE_TC_ROWS % p.G == 0) {
+    const cuuint64_t heads = (cuuint64_t)p.B * p.H;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, heads, (cuuint64_t)p.N};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, heads * D * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)(tova::TREE_TC_ROWS / p.G)};
+    q.q_tiled = encode_map(&map_q, const_cast<void*>(p.q), 3, dims, strides, box) == TOVA_OK;
+  }
+  cudaError_t e = tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, dim3((unsigned)t.blocks), st, q, map_k, map_v, map_q);
   if (e != cudaSuccess) return e;
   constexpr int JOIN_ROWS = tova::TREE_TC_JOIN_THREADS / 32;
   cudaLaunchConfig_t lc{};

@@ -38,7 +38,7 @@ struct TreeParams {
   int splits, split_cols;      // columns of a run (a multiple of the kernel's tile); the last run also has the drafts
   int row_blocks, blocks, least;   // tcgen05 kernel: jobs per KV head, blocks, fewest tiles of a block's run
   void* cuts;                  // tcgen05 kernel: one TreeTcCut per block
-  int tiled;                   // tcgen05 kernel: there are tensor maps of a bf16 state
+  int tiled, q_tiled;          // tcgen05 kernel: there are tensor maps of a bf16 state, of q
   float scale2;                // scale * log2(e)
 };
 

@@ -121,6 +121,13 @@ __device__ __forceinline__ void tma_load_2d_tile(void* dst, const CUtensorMap* m
       : "memory");
 }
 
+__device__ __forceinline__ void tma_load_3d_tile(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
+      : "memory");
+}
+
 // 16 columns of this thread's TMEM lane times f (a power of two or 0: exact).
 __device__ __forceinline__ void tree_tc_scale16(uint32_t taddr, float f) {
   uint32_t v[16];
@@ -133,7 +140,7 @@ __device__ __forceinline__ void tree_tc_scale16(uint32_t taddr, float f) {
 template <int D, int FMT, int NT>
 __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<D, FMT, NT>::BLOCKS)
     tova_tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_k,
-                        const __grid_constant__ CUtensorMap map_v) {
+                        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q) {
   using S = TreeTcShape<D, FMT, NT>;
   constexpr bool PLAIN = S::PLAIN;
   constexpr int C = TREE_TC_COLS, R = TREE_TC_ROWS;
@@ -266,9 +273,23 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       auto load_q = [&]() {
         ok = piece == 0 || mbar_wait_bounded(&bar_qf, (uint32_t)((piece - 1) & 1));
         if (!ok) return;
+        const int m0 = run.rb * (R * NT);
+        if (p.q_tiled) {
+          // (a node's G heads are neighbours: rows (node, head) are boxes of 128 / G nodes, and nodes behind the last zeros)
+          if (pt == 0) {
+            mbar_expect_tx(&bar_q, NT * S::Q_BYTES);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int c = 0; c < D / 64; ++c)
+                tma_load_3d_tile(q_s + t * S::Q_BYTES + c * (R * 128), &map_q, c * 64, run.b * p.H + run.hk * p.G, (m0 + t * R) / p.G, &bar_q);
+          } else {
+            mbar_arrive(&bar_q);
+          }
+          return;
+        }
         const int row_q = pt / QCH, ch = pt % QCH;
         const uint32_t dst = smem_addr(q_s) + (ch >> 3) * (R * 128);
-        const int m0 = run.rb * (R * NT);
 #pragma unroll 8
         for (int k = 0; k < NT * R / QSTEP; ++k) {
           const int r = k * QSTEP + row_q, m = m0 + r, mm = min(m, p.M - 1);
@@ -356,6 +377,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       } else {
         // Raw copies run RAW_SLOTS - 1 ahead of the conversions; raw position rp = 2 (state tiles of the block so far) + x.
         constexpr int AHEAD = S::RAW_SLOTS - 1;
+        const int turn = D == 128 ? (ch_t >> 2) & 1 : row_t & 1;
         const int n_raw = 2 * max(0, min(run.i1, run.n_state) - run.i0);
         auto fetch = [&](int x) {
           if (x >= n_raw || !ok) return;
@@ -402,12 +424,13 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
             for (int k = 0; k < PER; ++k) {
               const int row = k * STEP + row_t;
               const uint4 w = row < valid ? *reinterpret_cast<const uint4*>(raw + k * (PT * 16)) : make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t)) =
-                  make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
-                             tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
-              *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + 1)) =
-                  make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
-                             tree_codes2<FMT>(w.w, w.w, 0, 1), tree_codes2<FMT>(w.w, w.w, 2, 3));
+              const uint4 lo = make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
+                                          tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
+              const uint4 hi = make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
+                                          tree_codes2<FMT>(w.w, w.w, 0, 1), tree_codes2<FMT>(w.w, w.w, 2, 3));
+              // (one half of a row's threads starts with its second chunk: eight of them then meet eight bank groups)
+              *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + turn)) = turn ? hi : lo;
+              *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + (turn ^ 1))) = turn ? lo : hi;
             }
             fence_proxy_async_smem();          // for the tensor cores' reads, and for the next copy into the raw slot
             mbar_arrive(&full[pos % S::SLOTS]);
