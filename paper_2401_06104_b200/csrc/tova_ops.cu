@@ -522,6 +522,7 @@ extern "C" int tova_verify_draft(const tova_verify_config* cfg, const void* targ
   p.n_accepted = n_accepted; p.path = path; p.tokens_out = tokens_out;
   p.row_stride = cfg->row_stride ? cfg->row_stride : cfg->vocab;
   p.B = cfg->batch; p.N = cfg->n_nodes; p.V = cfg->vocab;
+  p.vec = (p.row_stride * dtype_bytes(cfg->dtype)) % 16 == 0;
 
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3(tova::VERIFY_CLUSTER, (unsigned)cfg->batch);

@@ -7,8 +7,10 @@
 // of the inputs alone, not of how they are computed.  a < 2^-100: scale 0, codes 0 (Q / a would leave fp32's range).
 // A row with an infinity or NaN gets scale NaN and codes 0: it reads back as NaN and cannot pass for a finite one.
 //
-// Reading D values and writing D codes does a few operations a value: DRAM bound.  Half a warp (D = 128, bf16) or
-// whatever 16 bytes a lane make holds a row in registers, so that the maximum costs shuffles and no second read.
+// Reading D values and writing D codes does a few operations a value: DRAM bound, if enough loads are in flight and the two
+// correctly rounded quotients of a row, some 20 instructions each, are not formed by all of its lanes.  A group of lanes
+// holds eight rows in registers (16 bytes a lane and row, all loaded before the first is used), reduces their eight maxima
+// in one transposing tree that leaves row j's in lane j, forms each row's quotients once, in that lane, and passes them round.
 #pragma once
 
 #include "tova_device.cuh"
@@ -93,116 +95,142 @@ __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_write_kernel(const _
   const int lane = threadIdx.x % L, r0 = threadIdx.x / L;
   const int total = n_tok * p.Hkv;
   const float qmax = FMT == FORMAT_INT8 ? 127.f : 448.f;
-#pragma unroll 2
-  for (int base = 0; base < total; base += ROWS) {
-    const int i = base + r0;
-    const bool in = i < total;
-    const int ti = in ? i / p.Hkv : 0, h = in ? i - ti * p.Hkv : 0;
-    const int slot = slot_s[ti];
-    const bool ok = in && (unsigned)slot < (unsigned)p.cap;
-    uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    if (ok) {
+  constexpr int U = 4;                           // (token, head) pairs a group holds at a time: U rows of K and U of V
+  for (int base = 0; base < total; base += U * ROWS) {
+    uint4 w[U][2];
+    long long dst[U];                            // row of the state, -1: nothing to write
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = base + u * ROWS + r0;
+      const bool in = i < total;
+      const int ti = in ? i / p.Hkv : 0, h = in ? i - ti * p.Hkv : 0;
+      const int slot = slot_s[ti];
+      const bool ok = in && (unsigned)slot < (unsigned)p.cap;
+      dst[u] = ok ? ((long long)b * p.Hkv + h) * p.cap + slot : -1;
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv)
-        w[kv] = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.x[kv]) +
-                                                ((long long)(t0 + ti) * p.B + b) * p.x_stride[kv] + (long long)h * D + lane * N);
+        w[u][kv] = ok ? __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(p.x[kv]) + ((long long)(t0 + ti) * p.B + b) * p.x_stride[kv] +
+                                                              (long long)h * D + lane * N))
+                      : make_uint4(0, 0, 0, 0);
     }
+    uint32_t top[2 * U];     // bits of |x|: ordered like the values, infinities and NaN on top
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      float f[N];
-      Vec16<T>::unpack(w[kv], f);
-      uint32_t top = 0;      // bits of |x|: ordered like the values, infinities and NaN on top
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+      for (int kv = 0; kv < 2; ++kv) {
+        float f[N];
+        Vec16<T>::unpack(w[u][kv], f);
+        uint32_t t = 0;
 #pragma unroll
-      for (int o = L / 2; o >= 1; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float a = __uint_as_float(top);
-      const bool finite = top < 0x7f800000u;
-      const bool some = finite && a >= 0x1p-100f;
-      const float scale = some ? __fdiv_rn(a, qmax) : (finite ? 0.f : __uint_as_float(0x7fc00000u));
-      const float r = some ? __fdiv_rn(qmax, a) : 0.f;
-      uint32_t c[N / 4];
-#pragma unroll
-      for (int e = 0; e < N / 4; ++e) {
-        float y[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = some ? __fmul_rn(f[4 * e + k], r) : 0.f;
-        c[e] = FMT == FORMAT_INT8 ? quant_pack4_int8(y[0], y[1], y[2], y[3]) : quant_pack4_e4m3(y[0], y[1], y[2], y[3]);
+        for (int e = 0; e < N; ++e) t = max(t, __float_as_uint(f[e]) & 0x7fffffffu);
+        top[2 * u + kv] = t;
       }
-      if (ok) {
-        const long long row = ((long long)b * p.Hkv + h) * p.cap + slot;
-        unsigned char* dst = static_cast<unsigned char*>(p.codes[kv]) + row * D + lane * N;
-        if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(c[0], c[N / 4 - 1]);
-        else *reinterpret_cast<uint32_t*>(dst) = c[0];
-        if (lane == 0) p.scale[kv][row] = scale;
+    // eight maxima over eight lanes: lane j keeps row j's; then over the group's other lanes
+#pragma unroll
+    for (int half = U; half >= 1; half >>= 1) {
+      const bool upper = (lane & half) != 0;
+#pragma unroll
+      for (int i = 0; i < half; ++i) {
+        const uint32_t send = upper ? top[i] : top[i + half], keep = upper ? top[i + half] : top[i];
+        top[i] = max(keep, __shfl_xor_sync(0xffffffffu, send, half));
       }
     }
+#pragma unroll
+    for (int o = 8; o < L; o <<= 1) top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+    const float a = __uint_as_float(top[0]);
+    const bool finite = top[0] < 0x7f800000u, some = finite && a >= 0x1p-100f;
+    const float scale_j = some ? __fdiv_rn(a, qmax) : (finite ? 0.f : __uint_as_float(0x7fc00000u));
+    const float r_j = some ? __fdiv_rn(qmax, a) : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const int j = (threadIdx.x & 31 & ~7) | (2 * u + kv);
+        const float r = __shfl_sync(0xffffffffu, r_j, j), scale = __shfl_sync(0xffffffffu, scale_j, j);
+        float f[N];
+        Vec16<T>::unpack(w[u][kv], f);
+        uint32_t c[N / 4];
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) {
+          float y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = __fmul_rn(f[4 * e + k], r);
+          c[e] = FMT == FORMAT_INT8 ? quant_pack4_int8(y[0], y[1], y[2], y[3]) : quant_pack4_e4m3(y[0], y[1], y[2], y[3]);
+          if (r == 0.f) c[e] = 0;                // (0 times an infinity)
+        }
+        if (dst[u] >= 0) {
+          unsigned char* at = static_cast<unsigned char*>(p.codes[kv]) + dst[u] * D + lane * N;
+          if constexpr (N == 8) *reinterpret_cast<uint2*>(at) = make_uint2(c[0], c[N / 4 - 1]);
+          else *reinterpret_cast<uint32_t*>(at) = c[0];
+          if (lane == 0) p.scale[kv][dst[u]] = scale;
+        }
+      }
   }
 }
 
-// Reading back: value = fp32(code scale), rounded once more where the caller's type is bf16.  Same grid; a slot
-// outside 0..cap-1 gives a row of zeros.
+// Reading back: value = fp32(code scale), rounded once more where the caller's type is bf16.  Same grid; a slot outside
+// 0..cap-1 gives a row of zeros.  16 codes a lane; four rows of K and of V are on their way at a time.
 template <typename T, int D, int FMT>
 __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_read_kernel(const __grid_constant__ QuantParams p) {
-  constexpr int N = Vec16<T>::N;
-  constexpr int L = D / N;
+  constexpr int L = D / 16;
   constexpr int ROWS = QUANT_THREADS / L;
+  constexpr int U = 4;
   const int b = blockIdx.y;
   const int t0 = blockIdx.x * p.tokens_per_block;
   const int n_tok = min(p.tokens_per_block, p.T - t0);
   const int lane = threadIdx.x % L;
   const int total = n_tok * p.Hkv;
-#pragma unroll 2
-  for (int i = threadIdx.x / L; i < total; i += ROWS) {
-    const int ti = i / p.Hkv, h = i - ti * p.Hkv;
-    const long long tb = (long long)(t0 + ti) * p.B + b;
-    const int slot = p.slots ? p.slots[tb] : p.first_slot + t0 + ti;
-    const bool ok = (unsigned)slot < (unsigned)p.cap;
-    const long long row = ((long long)b * p.Hkv + h) * p.cap + slot;
-    uint32_t c[2][N / 4];
-    float s[2];
+  for (int base = threadIdx.x / L; base < total; base += U * ROWS) {
+    uint4 c[U][2];
+    float s[U][2];
+    long long dst[U];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      s[kv] = 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int i = base + u * ROWS;
+      const bool in = i < total;
+      const int ti = in ? i / p.Hkv : 0, h = in ? i - ti * p.Hkv : 0;
+      const long long tb = (long long)(t0 + ti) * p.B + b;
+      const int slot = p.slots ? p.slots[tb] : p.first_slot + t0 + ti;
+      const bool ok = in && (unsigned)slot < (unsigned)p.cap;
+      const long long row = ((long long)b * p.Hkv + h) * p.cap + slot;
+      dst[u] = in ? (tb * p.Hkv + h) * D + lane * 16 : -1;
 #pragma unroll
-      for (int e = 0; e < N / 4; ++e) c[kv][e] = 0;
-      if (ok && p.y[kv]) {
-        const unsigned char* src = static_cast<const unsigned char*>(p.codes[kv]) + row * D + lane * N;
-        if constexpr (N == 8) {
-          const uint2 w = *reinterpret_cast<const uint2*>(src);
-          c[kv][0] = w.x;
-          c[kv][N / 4 - 1] = w.y;
+      for (int kv = 0; kv < 2; ++kv) {
+        const bool get = ok && p.y[kv] != nullptr;
+        c[u][kv] = get ? __ldcs(reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(p.codes[kv]) + row * D + lane * 16))
+                       : make_uint4(0, 0, 0, 0);
+        s[u][kv] = get ? p.scale[kv][row] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        if (dst[u] < 0 || p.y[kv] == nullptr) continue;
+        float f[16];
+        const uint32_t w[4] = {c[u][kv].x, c[u][kv].y, c[u][kv].z, c[u][kv].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float g[4];
+          quant_unpack4<FMT>(w[e], g);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) f[4 * e + k] = g[k] * s[u][kv];
+        }
+        T* at = static_cast<T*>(p.y[kv]) + dst[u];
+        if constexpr (sizeof(T) == 2) {
+          uint32_t x[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const __nv_bfloat162 hh = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+            x[k] = *reinterpret_cast<const uint32_t*>(&hh);
+          }
+          __stcs(reinterpret_cast<uint4*>(at), make_uint4(x[0], x[1], x[2], x[3]));
+          __stcs(reinterpret_cast<uint4*>(at) + 1, make_uint4(x[4], x[5], x[6], x[7]));
         } else {
-          c[kv][0] = *reinterpret_cast<const uint32_t*>(src);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) __stcs(reinterpret_cast<float4*>(at) + k, make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]));
         }
-        s[kv] = p.scale[kv][row];
       }
-    }
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      if (!p.y[kv]) continue;
-      float f[N];
-#pragma unroll
-      for (int e = 0; e < N / 4; ++e) {
-        float g[4];
-        quant_unpack4<FMT>(c[kv][e], g);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[4 * e + k] = g[k] * s[kv];
-      }
-      uint4 w;
-      if constexpr (N == 8) {
-        uint32_t u[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const __nv_bfloat162 hh = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
-          u[k] = *reinterpret_cast<const uint32_t*>(&hh);
-        }
-        w = make_uint4(u[0], u[1], u[2], u[3]);
-      } else {
-        w = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-      }
-      *reinterpret_cast<uint4*>(static_cast<T*>(p.y[kv]) + (tb * p.Hkv + h) * D + lane * N) = w;
-    }
   }
 }
 

@@ -58,71 +58,100 @@ __global__ void __launch_bounds__(ROPE_THREADS) tova_rope_kernel(const __grid_co
   const long long row0 = (long long)blockIdx.x * p.tokens_per_block;
   const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
   const int half = p.rot >> 1;
-  for (int i = threadIdx.x; i < n_tok * half; i += ROPE_THREADS) {
-    const int t = i / half, j = i - t * half;
-    const long long row = row0 + t;
-    const double pos = p.positions ? (double)p.positions[row] : (double)p.first_pos + (double)(row / p.B);
-    double a = pos * p.turns[j];
-    a -= rint(a);
-    float s, c;
-    sincospif((float)(2.0 * a), &s, &c);
-    cs[t][j] = c * p.factor;
-    sn[t][j] = s * p.factor * p.sign;
-  }
-  __syncthreads();
   const int turning = VEC ? (HALF ? half / N : p.rot / N) : half;       // units that turn, per head
   const int passing = VEC ? (p.D - p.rot) / N : p.D - p.rot;            // units that pass through
   const int per_head = turning + passing;
   const int per_tok = (p.heads[0] + p.heads[1]) * per_head;
   const int total = n_tok * per_tok;
-#pragma unroll 2
-  for (int i = threadIdx.x; i < total; i += ROPE_THREADS) {
-    const int t = i / per_tok;
-    int rem = i - t * per_tok;
+  // Where unit i is: its token in the block, its position in the head, its head's place in the input and the output.
+  auto locate = [&](int i, int& t, int& u, const T*& x, T*& y) {
+    t = i / per_tok;
+    const int rem = i - t * per_tok;
     int h = rem / per_head;
-    const int u = rem - h * per_head;
+    u = rem - h * per_head;
     const int which = h >= p.heads[0];
     if (which) h -= p.heads[0];
-    const T* x = static_cast<const T*>(p.x[which]) + (row0 + t) * p.x_stride[which] + (long long)h * p.D;
-    T* y = static_cast<T*>(p.y[which]) + (row0 + t) * p.y_stride[which] + (long long)h * p.D;
-    if constexpr (VEC) {
-      if (u >= turning) {
-        const int d = p.rot + (u - turning) * N;
-        *reinterpret_cast<uint4*>(y + d) = *reinterpret_cast<const uint4*>(x + d);
-      } else if constexpr (HALF) {
-        const int d = u * N;
-        const uint4 wa = *reinterpret_cast<const uint4*>(x + d), wb = *reinterpret_cast<const uint4*>(x + half + d);
-        float a[N], b[N], ya[N], yb[N];
-        Vec16<T>::unpack(wa, a);
-        Vec16<T>::unpack(wb, b);
+    x = static_cast<const T*>(p.x[which]) + (row0 + t) * p.x_stride[which] + (long long)h * p.D;
+    y = static_cast<T*>(p.y[which]) + (row0 + t) * p.y_stride[which] + (long long)h * p.D;
+  };
+  auto angles = [&]() {
+    for (int i = threadIdx.x; i < n_tok * half; i += ROPE_THREADS) {
+      const int t = i / half, j = i - t * half;
+      const long long row = row0 + t;
+      const double pos = p.positions ? (double)p.positions[row] : (double)p.first_pos + (double)(row / p.B);
+      double a = pos * p.turns[j];
+      a -= rint(a);
+      float s, c;
+      sincospif((float)(2.0 * a), &s, &c);
+      cs[t][j] = c * p.factor;
+      sn[t][j] = s * p.factor * p.sign;
+    }
+    __syncthreads();
+  };
+  if constexpr (VEC) {
+    // U units a thread are loaded before any is used, the first ones before the angles are formed.
+    constexpr int U = 4;
+    for (int i0 = threadIdx.x; i0 < total + (int)threadIdx.x; i0 += U * ROPE_THREADS) {
+      uint4 wa[U], wb[U];
+      int t[U], u[U];
+      T* y[U];
 #pragma unroll
-        for (int e = 0; e < N; e += 4) {
-          const float4 c4 = *reinterpret_cast<const float4*>(&cs[t][d + e]);
-          const float4 s4 = *reinterpret_cast<const float4*>(&sn[t][d + e]);
-          const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            ya[e + k] = a[e + k] * c[k] - b[e + k] * s[k];
-            yb[e + k] = b[e + k] * c[k] + a[e + k] * s[k];
-          }
-        }
-        *reinterpret_cast<uint4*>(y + d) = rope_pack<T>(ya);
-        *reinterpret_cast<uint4*>(y + half + d) = rope_pack<T>(yb);
-      } else {
-        const int d = u * N;
-        const uint4 w = *reinterpret_cast<const uint4*>(x + d);
-        float a[N];
-        Vec16<T>::unpack(w, a);
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const float c = cs[t][(d + e) >> 1], s = sn[t][(d + e) >> 1];
-          const float lo = a[e] * c - a[e + 1] * s;
-          a[e + 1] = a[e + 1] * c + a[e] * s;
-          a[e] = lo;
-        }
-        *reinterpret_cast<uint4*>(y + d) = rope_pack<T>(a);
+      for (int k = 0; k < U; ++k) {
+        const int i = i0 + k * ROPE_THREADS;
+        u[k] = -1;
+        if (i >= total) continue;
+        const T* x;
+        locate(i, t[k], u[k], x, y[k]);
+        const int d = u[k] < turning ? u[k] * N : p.rot + (u[k] - turning) * N;
+        wa[k] = __ldcs(reinterpret_cast<const uint4*>(x + d));
+        if (HALF && u[k] < turning) wb[k] = __ldcs(reinterpret_cast<const uint4*>(x + half + d));
       }
-    } else {
+      if (i0 == (int)threadIdx.x) angles();
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (u[k] < 0) continue;
+        if (u[k] >= turning) {
+          __stcs(reinterpret_cast<uint4*>(y[k] + p.rot + (u[k] - turning) * N), wa[k]);
+          continue;
+        }
+        const int d = u[k] * N;
+        float a[N];
+        Vec16<T>::unpack(wa[k], a);
+        if constexpr (HALF) {
+          float b[N], ya[N], yb[N];
+          Vec16<T>::unpack(wb[k], b);
+#pragma unroll
+          for (int e = 0; e < N; e += 4) {
+            const float4 c4 = *reinterpret_cast<const float4*>(&cs[t[k]][d + e]);
+            const float4 s4 = *reinterpret_cast<const float4*>(&sn[t[k]][d + e]);
+            const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              ya[e + x] = a[e + x] * c[x] - b[e + x] * s[x];
+              yb[e + x] = b[e + x] * c[x] + a[e + x] * s[x];
+            }
+          }
+          __stcs(reinterpret_cast<uint4*>(y[k] + d), rope_pack<T>(ya));
+          __stcs(reinterpret_cast<uint4*>(y[k] + half + d), rope_pack<T>(yb));
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const float c = cs[t[k]][(d + e) >> 1], s = sn[t[k]][(d + e) >> 1];
+            const float lo = a[e] * c - a[e + 1] * s;
+            a[e + 1] = a[e + 1] * c + a[e] * s;
+            a[e] = lo;
+          }
+          __stcs(reinterpret_cast<uint4*>(y[k] + d), rope_pack<T>(a));
+        }
+      }
+    }
+  } else {
+    angles();
+    for (int i = threadIdx.x; i < total; i += ROPE_THREADS) {
+      int t, u;
+      const T* x;
+      T* y;
+      locate(i, t, u, x, y);
       if (u >= turning) {
         const int d = p.rot + u - turning;
         y[d] = x[d];

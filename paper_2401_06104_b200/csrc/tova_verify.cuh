@@ -18,7 +18,10 @@
 // the sums.  What has to be read is a few scalars along the walk and the rows where a rejection meets another child
 // or the walk ends: the time is the latency of a chain of small steps.  One cluster of blocks per sequence: the
 // scalars of all nodes are fetched at once at the start, every block walks the same path, and the blocks share out
-// the vocabulary where a row has to be summed; partial sums travel through distributed shared memory.
+// the vocabulary where a row has to be summed; partial sums travel through distributed shared memory.  A lane holds
+// eight neighbouring entries of the row in registers for as long as the walk stays at the node (vocabularies up to
+// 32768 entries), so a second rejection or the final draw there reads nothing, and the draw needs one scan over the
+// lanes of the one warp whose stretch holds the goal.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -27,7 +30,7 @@
 
 namespace tova {
 
-constexpr int VERIFY_THREADS = 512;
+constexpr int VERIFY_THREADS = 256;
 constexpr int VERIFY_WARPS = VERIFY_THREADS / 32;
 constexpr int VERIFY_CLUSTER = 8;
 constexpr int VERIFY_MAX_NODES = 1024;
@@ -44,14 +47,38 @@ struct VerifyParams {
   int32_t* tokens_out;        // [N+1,B]
   long long row_stride;
   int B, N, V;
+  int vec;                    // rows start on 16-byte boundaries
 };
 
-// Dynamic shared memory: per node p(x), q(x), u (floats), token, parent.
-inline size_t verify_smem_bytes(int N) { return (size_t)N * 20; }
+// Dynamic shared memory: per node p(x), q(x), u (floats), token, parent, and a list of tokens.
+inline size_t verify_smem_bytes(int N) { return (size_t)N * 24; }
 
 template <typename T>
 __device__ __forceinline__ float verify_load(const void* p, long long i) {
   return (float)static_cast<const T*>(p)[i];
+}
+
+constexpr int VERIFY_LANE = 8;                     // entries a lane takes at a time
+constexpr int VERIFY_STEP = 32 * VERIFY_LANE;      // ... and a warp
+constexpr int VERIFY_HELD = 2;                     // steps of a warp that are held in registers
+
+// Eight entries i .. i+7 of a row, zeros from `end` on.
+template <typename T>
+__device__ __forceinline__ void verify_load8(const void* p, long long row, int i, int end, bool vec, float (&f)[VERIFY_LANE]) {
+  const T* x = static_cast<const T*>(p) + row + i;
+  if (vec && i + VERIFY_LANE <= end) {
+    constexpr int N = Vec16<T>::N;
+#pragma unroll
+    for (int k = 0; k < VERIFY_LANE / N; ++k) {
+      float g[N];
+      Vec16<T>::unpack(*reinterpret_cast<const uint4*>(x + k * N), g);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[k * N + e] = g[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < VERIFY_LANE; ++e) f[e] = i + e < end ? (float)x[e] : 0.f;
+  }
 }
 
 // The weight that the last token is drawn with, or a term of Z: max(0, p - S q); NaN counts as zero.
@@ -61,7 +88,7 @@ __device__ __forceinline__ double verify_weight(float p, float q, double S) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(VERIFY_THREADS, 2) tova_verify_kernel(const __grid_constant__ VerifyParams p) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   extern __shared__ __align__(16) unsigned char verify_smem[];
@@ -70,9 +97,10 @@ __global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __gri
   float* u_s = qx_s + p.N;
   int* tok_s = reinterpret_cast<int*>(u_s + p.N);
   int* par_s = tok_s + p.N;
+  int* kid_s = par_s + p.N;                       // without q: tokens of the last node's children
   __shared__ double inbox[2][VERIFY_CLUSTER];     // partial sums of the cluster's blocks, double-buffered
   __shared__ double warp_part[VERIFY_WARPS];
-  __shared__ int cmd_s, row_s, node_s, count_s, last_child_s;
+  __shared__ int cmd_s, node_s, count_s, last_child_s, kids_s;
   __shared__ double S_s;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -93,14 +121,47 @@ __global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __gri
     px_s[i] = ok ? verify_load<T>(p.target, row + tok) : 0.f;   // a token outside the vocabulary is never accepted
     qx_s[i] = ok ? (p.draft ? verify_load<T>(p.draft, row + tok) : 1.f) : 0.f;
   }
-  if (tid == 0) { row_s = 0; node_s = -1; count_s = 0; last_child_s = -1; S_s = 0.0; cmd_s = 0; }
+  if (tid == 0) { kids_s = 0; node_s = -1; count_s = 0; last_child_s = -1; S_s = 0.0; cmd_s = 0; }
   cluster.sync();     // every block of the cluster runs before any writes into another's inbox
 
   // This block's share of the vocabulary, and every warp's share of that: contiguous, in order.
-  const int per_block = ((V + nc - 1) / nc + 7) / 8 * 8;
+  const int per_block = ((V + nc - 1) / nc + VERIFY_LANE - 1) / VERIFY_LANE * VERIFY_LANE;
   const int v0 = min(V, rank * per_block), v1 = min(V, v0 + per_block);
-  const int per_warp = ((v1 - v0 + VERIFY_WARPS - 1) / VERIFY_WARPS + 31) / 32 * 32;
+  const int per_warp = ((per_block + VERIFY_WARPS - 1) / VERIFY_WARPS + VERIFY_STEP - 1) / VERIFY_STEP * VERIFY_STEP;
   const int w0 = min(v1, v0 + warp * per_warp), w1 = min(v1, w0 + per_warp);
+  const int steps = per_warp / VERIFY_STEP;
+  const bool held = steps <= VERIFY_HELD;
+  float pr[VERIFY_HELD][VERIFY_LANE], qr[VERIFY_HELD][VERIFY_LANE];     // this lane's entries of the node's row
+  int held_node = -2;
+  // This lane's entries of step k: from registers, or fetched.
+  auto fetch = [&](long long row, int k, bool with_q, float (&a)[VERIFY_LANE], float (&b)[VERIFY_LANE]) {
+    const int i = w0 + k * VERIFY_STEP + lane * VERIFY_LANE;
+    verify_load8<T>(p.target, row, i, w1, p.vec, a);
+    if (with_q) verify_load8<T>(p.draft, row, i, w1, p.vec, b);
+  };
+  auto hold = [&](int node, bool with_q) {
+    if (!held || held_node == node) return;
+    const long long row = ((long long)(node + 1) * p.B + b) * p.row_stride;
+#pragma unroll
+    for (int k = 0; k < VERIFY_HELD; ++k)
+      if (k < steps) fetch(row, k, with_q, pr[k], qr[k]);
+    held_node = node;
+  };
+  // f(k, p entries, q entries) for every step of the warp.
+  auto each_step = [&](int node, bool with_q, auto f) {
+    if (held) {
+      hold(node, with_q);
+#pragma unroll
+      for (int k = 0; k < VERIFY_HELD; ++k)
+        if (k < steps) f(k, pr[k], qr[k]);
+    } else {
+      const long long row = ((long long)(node + 1) * p.B + b) * p.row_stride;
+      for (int k = 0; k < steps; ++k) {
+        fetch(row, k, with_q, pr[0], qr[0]);
+        f(k, pr[0], qr[0]);
+      }
+    }
+  };
 
   int turn = 0;                       // exchanges so far
   // The sum over the cluster of one value per thread, in a fixed order; the block's prefix before this warp and the
@@ -183,11 +244,12 @@ __global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __gri
     }
     __syncthreads();
     if (cmd_s == 2) break;
-    const long long row = ((long long)(node_s + 1) * p.B + b) * p.row_stride;
     const double S = S_s;
     double sum = 0.0, bb, bw;
-    for (int i = w0 + lane; i < w1; i += 32)
-      sum += verify_weight(verify_load<T>(p.target, row + i), verify_load<T>(p.draft, row + i), S);
+    each_step(node_s, true, [&](int, const float (&a)[VERIFY_LANE], const float (&q)[VERIFY_LANE]) {
+#pragma unroll
+      for (int e = 0; e < VERIFY_LANE; ++e) sum += verify_weight(a[e], q[e], S);
+    });
     Z = cluster_sum(sum, bb, bw);
     __syncthreads();
   }
@@ -195,23 +257,33 @@ __global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __gri
   // The last token.
   const int node = node_s, count = count_s;
   const double S = S_s;
-  const long long row = ((long long)(node + 1) * p.B + b) * p.row_stride;
-  auto struck = [&](int x) {     // without q: tokens of the node's children, all rejected
-    for (int i = node + 1; i < N; ++i)
-      if (par_s[i] == node && tok_s[i] == x) return true;
-    return false;
-  };
+  const bool with_q = p.draft != nullptr && S > 0.0;     // (nothing rejected here: r is p)
+  if (!p.draft) {                // tokens of the node's children, all rejected: struck out
+    for (int i = node + 1 + tid; i < N; i += VERIFY_THREADS)
+      if (par_s[i] == node) kid_s[atomicAdd(&kids_s, 1)] = tok_s[i];      // (in any order: they are only compared with)
+    __syncthreads();
+  }
+  const int kids = kids_s;
   bool plain = false;            // r was zero everywhere: drawn from p
   double before_block = 0.0, before_warp = 0.0, all = 0.0, mine = 0.0;
-  auto weight = [&](int i) -> double {
-    const float pr = verify_load<T>(p.target, row + i);
-    if (plain) return pr > 0.f ? (double)pr : 0.0;
-    if (p.draft) return S > 0.0 ? verify_weight(pr, verify_load<T>(p.draft, row + i), S) : (pr > 0.f ? (double)pr : 0.0);
-    return pr > 0.f && !struck(i) ? (double)pr : 0.0;
+  auto weights = [&](int k, const float (&a)[VERIFY_LANE], const float (&q)[VERIFY_LANE], double (&w)[VERIFY_LANE]) {
+    const int i = w0 + k * VERIFY_STEP + lane * VERIFY_LANE;
+#pragma unroll
+    for (int e = 0; e < VERIFY_LANE; ++e) {
+      w[e] = with_q && !plain ? verify_weight(a[e], q[e], S) : (a[e] > 0.f ? (double)a[e] : 0.0);
+      if (!plain)
+        for (int j = 0; j < kids; ++j)
+          if (kid_s[j] == i + e) w[e] = 0.0;
+    }
   };
-  for (int attempt = 0; attempt < 2; ++attempt) {
+  for (;;) {
     double sum = 0.0;
-    for (int i = w0 + lane; i < w1; i += 32) sum += weight(i);
+    each_step(node, with_q, [&](int k, const float (&a)[VERIFY_LANE], const float (&q)[VERIFY_LANE]) {
+      double w[VERIFY_LANE];
+      weights(k, a, q, w);
+#pragma unroll
+      for (int e = 0; e < VERIFY_LANE; ++e) sum += w[e];
+    });
     mine = sum;
     all = cluster_sum(sum, before_block, before_warp);
     if (all > 0.0 || plain) break;
@@ -220,31 +292,45 @@ __global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __gri
   }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  // The warp whose stretch of the running sum holds the target: at or before it below or equal, after it above.  The
-  // prefixes are added up the same way in every warp, so exactly one warp finds it (the target lies below the whole).
+  // The warp whose stretch of the running sum holds the goal: the running sum before it is not above, the one after it
+  // is.  The prefixes are added up the same way in every warp, so exactly one warp finds it (the goal lies below the
+  // whole).
   float us = p.u_sample[b];
   us = us >= 0.f ? fminf(us, 0x1.fffffep-1f) : 0.f;
   const double goal = (double)us * all;
   const double lo = before_block + before_warp, hi = before_block + (before_warp + mine);
-  int found = -1;
   if (mine > 0.0 && lo <= goal && goal < hi) {
     double run = lo;
-    int last_some = -1;
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-      const int i = i0 + lane;
-      const double w = i < w1 ? weight(i) : 0.0;
-      double inc = w;
+    int found = -1, last_some = -1;
+    each_step(node, with_q, [&](int k, const float (&a)[VERIFY_LANE], const float (&q)[VERIFY_LANE]) {
+      if (found >= 0) return;
+      double w[VERIFY_LANE], own = 0.0;
+      weights(k, a, q, w);
+#pragma unroll
+      for (int e = 0; e < VERIFY_LANE; ++e) own += w[e];
+      double inc = own;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const double t = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += t;
       }
-      const unsigned m = __ballot_sync(0xffffffffu, w > 0.0 && run + inc > goal);
-      if (m) { found = i0 + __ffs(m) - 1; break; }
-      const unsigned some = __ballot_sync(0xffffffffu, w > 0.0);
-      if (some) last_some = i0 + 31 - __clz(some);
+      // this lane's entry at which the running sum passes the goal, and its last one that has any weight
+      int at = -1, some = -1;
+      double x = run + (inc - own);
+#pragma unroll
+      for (int e = 0; e < VERIFY_LANE; ++e) {
+        x += w[e];
+        if (w[e] > 0.0) {
+          some = e;
+          if (at < 0 && x > goal) at = e;
+        }
+      }
+      const int i = w0 + k * VERIFY_STEP + lane * VERIFY_LANE;
+      const unsigned m = __ballot_sync(0xffffffffu, at >= 0), n = __ballot_sync(0xffffffffu, some >= 0);
+      if (m) found = __shfl_sync(0xffffffffu, i + at, __ffs(m) - 1);
+      if (n) last_some = __shfl_sync(0xffffffffu, i + some, 31 - __clz(n));
       run += __shfl_sync(0xffffffffu, inc, 31);
-    }
+    });
     if (found < 0) found = last_some;     // the stretch's sum in another order fell short of the goal
     if (lane == 0) p.tokens_out[(long long)count * p.B + b] = found;
   }
@@ -258,7 +344,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) tova_verify_kernel(const __gri
       p.tokens_out[(long long)(i + 1) * p.B + b] = -1;
     }
   }
-  cluster.sync();     // no block leaves while another may still write into its inbox
+  // (No block writes into another's inbox behind the last exchange, so none has to wait for the others to leave.)
 }
 
 }  // namespace tova
