@@ -23,6 +23,9 @@
 #include "tova_shard.cuh"
 #include "tova_poscomp.cuh"
 
+// tova_ops.cu: device bytes that tova_tree_attention needs at whatever length the state has.
+size_t tree_workspace_any_length(const tova_tree_config& cfg, int32_t n_nodes);
+
 namespace {
 
 constexpr size_t ALIGN = 256;
@@ -1496,15 +1499,7 @@ tova_tree_config tree_config_of(const tova_cache& c) {
 
 size_t tova_cache_tree_workspace_bytes(const tova_cache* c, int32_t n_nodes) {
   if (!c) return (size_t)-1;
-  const tova_tree_config t = tree_config_of(*c);
-  // (enough for every length that the state goes through)
-  size_t most = 0;
-  for (int64_t n = 1; n < 2 * (int64_t)t.capacity; n *= 2) {
-    const size_t bytes = tova_tree_workspace_bytes(&t, (int32_t)std::min<int64_t>(n, t.capacity), n_nodes);
-    if (bytes == (size_t)-1) return bytes;
-    most = std::max(most, bytes);
-  }
-  return most;
+  return tree_workspace_any_length(tree_config_of(*c), n_nodes);
 }
 
 int tova_cache_tree_attention(tova_cache* c, const void* q, const void* k, const void* v, int32_t n_nodes,

@@ -304,10 +304,12 @@ enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64, TREE_TC_1, TREE_TC
 struct TreePlan {
   int kernel, row_blocks, splits, split_cols;
   int blocks, least;             // tcgen05 kernel
+  bool cluster;                  // the runs' blocks join by themselves
   size_t ml_bytes, acc_bytes, bytes;   // workspace: maxima and sums, weighted sums (and the tcgen05 kernel's list of cuts)
 };
 
-TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count) {
+// any_length: the workspace is to do for every n_live up to the capacity.
+TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count, bool any_length = false) {
   TreePlan t{};
   const int M = n_nodes * (c.n_q_heads / c.n_kv_heads);
   size_t part_rows;
@@ -335,12 +337,21 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     // would stay half empty.
     const int resident = 2 * sm_count, shortest = whole * (tiles / 2) < resident ? 1 : 2;
     long long want = (2LL * resident + whole - 1) / whole;
+    const long long most = want;
     want = std::max(1LL, std::min<long long>(want, tiles / shortest));
+    // Up to eight runs join in a cluster.  A call with more runs gets eight, too, where they are then at most four tiles
+    // long: that is less time than the second kernel takes.
+    if (t.kernel != TREE_ALU && want > 1 && (want <= tova::TREE_CLUSTER_MAX || tiles <= 4 * tova::TREE_CLUSTER_MAX)) {
+      t.cluster = true;
+      want = std::min<long long>(want, tova::TREE_CLUSTER_MAX);
+    }
     const int per = (int)((tiles + want - 1) / want);
     t.split_cols = per * cols;
     t.splits = (tiles + per - 1) / per;
-    if (t.splits > 1) t.splits += 1;               // a run of its own for the drafts: it does not wait for a run of rows
-    part_rows = t.splits > 1 ? (size_t)t.splits * c.batch * c.n_kv_heads * M : 0;
+    t.cluster = t.cluster && t.splits > 1;
+    if (t.splits > 1 && !t.cluster) t.splits += 1;      // a run of its own for the drafts: it does not wait for a run of rows
+    const long long runs = any_length ? most + 1 : t.splits > 1 && !t.cluster ? t.splits : 0;
+    part_rows = (size_t)runs * c.batch * c.n_kv_heads * M;
   }
   t.ml_bytes = (part_rows * sizeof(float2) + 255) / 256 * 256;
   t.acc_bytes = part_rows * c.head_dim * sizeof(float);
@@ -353,8 +364,8 @@ inline dim3 tree_grid(const tova::TreeParams& p, const TreePlan& t) {
 }
 
 template <typename... Args>
-cudaError_t tree_start(void (*kern)(Args...), std::atomic<bool>* configured, size_t smem, int threads, dim3 grid, cudaStream_t st,
-                       const Args&... args) {
+cudaError_t tree_start(void (*kern)(Args...), std::atomic<bool>* configured, size_t smem, int threads, dim3 grid, int cluster_y,
+                       cudaStream_t st, const Args&... args) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -364,8 +375,19 @@ cudaError_t tree_start(void (*kern)(Args...), std::atomic<bool>* configured, siz
     if (e != cudaSuccess) return e;
     configured[dev & 63] = true;
   }
-  kern<<<grid, threads, smem, st>>>(args...);
-  return cudaGetLastError();
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = grid;
+  lc.blockDim = dim3((unsigned)threads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 1;
+  at[0].val.clusterDim.y = (unsigned)cluster_y;
+  at[0].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = cluster_y > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&lc, kern, args...);
 }
 
 template <typename T, int D>
@@ -384,11 +406,15 @@ cudaError_t tree_merge(const tova::TreeParams& p, cudaStream_t st) {
   return cudaLaunchKernelEx(&lc, tova::tova_tree_merge_kernel<T, D>, p);
 }
 
+template <int D, int FMT, int MT, int WR, bool CLUSTER>
+cudaError_t tree_start_mma_c(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
+  static std::atomic<bool> configured[64];
+  return tree_start(tova::tova_tree_mma_kernel<D, FMT, MT, WR, CLUSTER>, configured, tova::TreeMmaShape<D, FMT, MT, WR>::SMEM,
+                    tova::TREE_MMA_THREADS, tree_grid(p, t), CLUSTER ? t.splits : 1, st, p);
+}
 template <int D, int FMT, int MT, int WR>
 cudaError_t tree_start_mma(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
-  static std::atomic<bool> configured[64];
-  return tree_start(tova::tova_tree_mma_kernel<D, FMT, MT, WR>, configured, tova::TreeMmaShape<D, FMT, MT, WR>::SMEM,
-                    tova::TREE_MMA_THREADS, tree_grid(p, t), st, p);
+  return t.cluster ? tree_start_mma_c<D, FMT, MT, WR, true>(p, t, st) : tree_start_mma_c<D, FMT, MT, WR, false>(p, t, st);
 }
 
 template <int D, int FMT, int NT>
@@ -414,7 +440,7 @@ cudaError_t tree_run_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream
     const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)(tova::TREE_TC_ROWS / p.G)};
     q.q_tiled = encode_map(&map_q, const_cast<void*>(p.q), 3, dims, strides, box) == TOVA_OK;
   }
-  cudaError_t e = tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, dim3((unsigned)t.blocks), st, q, map_k, map_v, map_q);
+  cudaError_t e = tree_start(tova::tova_tree_tc_kernel<D, FMT, NT>, configured, S::SMEM, S::THREADS, dim3((unsigned)t.blocks), 1, st, q, map_k, map_v, map_q);
   if (e != cudaSuccess) return e;
   constexpr int JOIN_ROWS = tova::TREE_TC_JOIN_THREADS / 32;
   cudaLaunchConfig_t lc{};
@@ -435,7 +461,7 @@ cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream
   if constexpr (std::is_same<T, float>::value) {
     static std::atomic<bool> configured[64];
     e = tree_start(tova::tova_tree_alu_kernel<T, D, FMT>, configured, tova::tree_alu_smem_bytes<D>(), tova::TREE_ALU_THREADS,
-                   tree_grid(p, t), st, p);
+                   tree_grid(p, t), 1, st, p);
   } else {
     switch (t.kernel) {
       case TREE_MMA_16: e = tree_start_mma<D, FMT, 1, 1>(p, t, st); break;
@@ -445,7 +471,7 @@ cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream
       default: return tree_run_tc<D, FMT, 2>(p, t, st);
     }
   }
-  if (e != cudaSuccess || t.splits == 1) return e;
+  if (e != cudaSuccess || t.splits == 1 || t.cluster) return e;
   return tree_merge<T, D>(p, st);
 }
 template <typename T, int D>
@@ -463,6 +489,12 @@ extern "C" size_t tova_tree_workspace_bytes(const tova_tree_config* cfg, int32_t
   DeviceInfo dev;
   if (tree_check(cfg, n_live, n_nodes) != TOVA_OK || !device_info(&dev)) return (size_t)-1;
   return n_nodes ? tree_plan(*cfg, n_live, n_nodes, dev.sm_count).bytes : 0;
+}
+
+size_t tree_workspace_any_length(const tova_tree_config& cfg, int32_t n_nodes) {
+  DeviceInfo dev;
+  if (tree_check(&cfg, 0, n_nodes) != TOVA_OK || !device_info(&dev)) return (size_t)-1;
+  return n_nodes ? tree_plan(cfg, cfg.capacity, n_nodes, dev.sm_count, true).bytes : 0;
 }
 
 extern "C" int tova_tree_attention(const tova_tree_config* cfg, const void* K, const void* V, const float* k_scale,

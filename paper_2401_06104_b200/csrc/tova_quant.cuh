@@ -18,7 +18,7 @@
 namespace tova {
 
 constexpr int QUANT_THREADS = 256;
-constexpr int QUANT_MAX_TOKENS = 16;   // tokens per block
+constexpr int QUANT_MAX_TOKENS = 8;   // tokens per block
 
 enum : int { FORMAT_PLAIN = 0, FORMAT_INT8 = 1, FORMAT_E4M3 = 2 };
 
@@ -169,10 +169,12 @@ __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_write_kernel(const _
 }
 
 // Reading back: value = fp32(code scale), rounded once more where the caller's type is bf16.  Same grid; a slot outside
-// 0..cap-1 gives a row of zeros.  16 codes a lane; four rows of K and of V are on their way at a time.
+// 0..cap-1 gives a row of zeros.  A lane writes 16 bytes, so that a warp's stores are whole lines; U rows of K and of V are
+// on their way at a time.
 template <typename T, int D, int FMT>
 __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_read_kernel(const __grid_constant__ QuantParams p) {
-  constexpr int L = D / 16;
+  constexpr int N = Vec16<T>::N;
+  constexpr int L = D / N;
   constexpr int ROWS = QUANT_THREADS / L;
   constexpr int U = 4;
   const int b = blockIdx.y;
@@ -181,7 +183,7 @@ __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_read_kernel(const __
   const int lane = threadIdx.x % L;
   const int total = n_tok * p.Hkv;
   for (int base = threadIdx.x / L; base < total; base += U * ROWS) {
-    uint4 c[U][2];
+    uint2 c[U][2];               // (fp32: the first word)
     float s[U][2];
     long long dst[U];
 #pragma unroll
@@ -193,13 +195,17 @@ __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_read_kernel(const __
       const int slot = p.slots ? p.slots[tb] : p.first_slot + t0 + ti;
       const bool ok = in && (unsigned)slot < (unsigned)p.cap;
       const long long row = ((long long)b * p.Hkv + h) * p.cap + slot;
-      dst[u] = in ? (tb * p.Hkv + h) * D + lane * 16 : -1;
+      dst[u] = in ? (tb * p.Hkv + h) * D + lane * N : -1;
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
-        const bool get = ok && p.y[kv] != nullptr;
-        c[u][kv] = get ? __ldcs(reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(p.codes[kv]) + row * D + lane * 16))
-                       : make_uint4(0, 0, 0, 0);
-        s[u][kv] = get ? p.scale[kv][row] : 0.f;
+        c[u][kv] = make_uint2(0, 0);
+        s[u][kv] = 0.f;
+        if (ok && p.y[kv]) {
+          const unsigned char* src = static_cast<const unsigned char*>(p.codes[kv]) + row * D + lane * N;
+          if constexpr (N == 8) c[u][kv] = *reinterpret_cast<const uint2*>(src);
+          else c[u][kv].x = *reinterpret_cast<const uint32_t*>(src);
+          s[u][kv] = p.scale[kv][row];
+        }
       }
     }
 #pragma unroll
@@ -207,29 +213,26 @@ __global__ void __launch_bounds__(QUANT_THREADS) tova_quant_read_kernel(const __
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         if (dst[u] < 0 || p.y[kv] == nullptr) continue;
-        float f[16];
-        const uint32_t w[4] = {c[u][kv].x, c[u][kv].y, c[u][kv].z, c[u][kv].w};
+        const uint32_t w[2] = {c[u][kv].x, c[u][kv].y};
+        uint32_t x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < N / 4; ++e) {
           float g[4];
           quant_unpack4<FMT>(w[e], g);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) f[4 * e + k] = g[k] * s[u][kv];
-        }
-        T* at = static_cast<T*>(p.y[kv]) + dst[u];
-        if constexpr (sizeof(T) == 2) {
-          uint32_t x[8];
+          for (int k = 0; k < 4; ++k) g[k] *= s[u][kv];
+          if constexpr (N == 8) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const __nv_bfloat162 hh = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
-            x[k] = *reinterpret_cast<const uint32_t*>(&hh);
+            for (int k = 0; k < 2; ++k) {
+              const __nv_bfloat162 hh = __floats2bfloat162_rn(g[2 * k], g[2 * k + 1]);
+              x[2 * e + k] = *reinterpret_cast<const uint32_t*>(&hh);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = __float_as_uint(g[k]);
           }
-          __stcs(reinterpret_cast<uint4*>(at), make_uint4(x[0], x[1], x[2], x[3]));
-          __stcs(reinterpret_cast<uint4*>(at) + 1, make_uint4(x[4], x[5], x[6], x[7]));
-        } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) __stcs(reinterpret_cast<float4*>(at) + k, make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]));
         }
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.y[kv]) + dst[u]) = make_uint4(x[0], x[1], x[2], x[3]);
       }
   }
 }

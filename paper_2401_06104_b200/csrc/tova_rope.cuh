@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) tova_rope_kernel(const __grid_co
   };
   if constexpr (VEC) {
     // U units a thread are loaded before any is used, the first ones before the angles are formed.
-    constexpr int U = 4;
+    constexpr int U = HALF ? 2 : 4;
     for (int i0 = threadIdx.x; i0 < total + (int)threadIdx.x; i0 += U * ROPE_THREADS) {
       uint4 wa[U], wb[U];
       int t[U], u[U];

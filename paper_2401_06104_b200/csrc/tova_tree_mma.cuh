@@ -5,7 +5,9 @@
 // block of four warps runs down its columns in tiles of 64, copied ahead (cp.async, several stages) into swizzled
 // shared memory.  WR groups of warps share out the rows, the 4 / WR warps of a group the tile's columns; every warp
 // keeps a running maximum, sum and O of its own over the columns it has seen, and the warps are joined once, at the
-// end, through shared memory.  O is rescaled only when some row's maximum moved.  The drafts are one more tile, copied
+// end, through shared memory.  Where the columns of a (sequence, KV head) are cut into at most eight runs, the blocks of the
+// runs form a cluster and join through distributed shared memory: a second kernel would cost a small call as much again.
+// O is rescaled only when some row's maximum moved.  The drafts are one more tile, copied
 // ahead like the others.  The weights are summed as they were rounded to bf16, so that what multiplies V adds up to one.
 //
 // 8-bit states are converted on the way from shared memory to the matrix instructions' operands, each code once per
@@ -15,6 +17,8 @@
 // elements are neighbouring bytes, the order of the contraction index (over D for the logits) and of O's columns is a
 // permutation of the natural one - the sums do not care, the operands of the other side follow it.
 #pragma once
+
+#include <cooperative_groups.h>
 
 #include "tova_mma.cuh"
 #include "tova_tc.cuh"     // ex2_approx
@@ -44,6 +48,7 @@ struct TreeMmaShape {
   static_assert(TREE_MMA_COLS * D * 2 * (FMT == FORMAT_PLAIN ? 2 : 1) <= STAGE && STAGES > DRAFT_STAGES, "drafts fit the ring");
   // the ring's room is taken over by the joining of the warps
   static_assert(WK * ROWS * (D * 4 + 8) <= STAGES * STAGE, "partial results fit the ring");
+  static_assert(ROWS * 8 <= Q_BYTES, "a block's maxima and sums fit Q's room");
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t src_bytes) {
@@ -92,7 +97,9 @@ __device__ __forceinline__ uint32_t tree_off8(int row, int ch) {
   else return (uint32_t)((row >> 1) * 128 + (((((row & 1) << 2) | ch) ^ (((row >> 1) & 3) << 1)) << 4));
 }
 
-template <int D, int FMT, int MT, int WR>
+constexpr int TREE_CLUSTER_MAX = 8;
+
+template <int D, int FMT, int MT, int WR, bool CLUSTER>
 __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(const __grid_constant__ TreeParams p) {
   using S = TreeMmaShape<D, FMT, MT, WR>;
   constexpr int C = TREE_MMA_COLS, KS = S::KS, NB = S::NB, OB = D / 8;
@@ -540,11 +547,10 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
       }
     }
   __syncthreads();
-  for (int e = tid; e < S::ROWS * (D / 4); e += TREE_MMA_THREADS) {
-    const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-    const int m = r;
-    if (m >= p.M) continue;
-    float top = -INFINITY, l = 0.f;
+  // A row's four components d .. d+3 over this block's warps; the row's maximum and sum.
+  auto joined = [&](int r, int d, float& top, float& l) {
+    top = -INFINITY;
+    l = 0.f;
     bool pad = false;
 #pragma unroll
     for (int w = 0; w < S::WK; ++w) top = fmaxf(top, ml_s[w * S::ROWS + r].x);
@@ -557,21 +563,79 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
       const float4 x = *reinterpret_cast<const float4*>(o_s + (w * S::ROWS + r) * D + d);
       acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
     }
-    const int n = m / p.G, g = m - n * p.G;
     if (last && odd_s && !pad) {
       float v[4] = {acc.x, acc.y, acc.z, acc.w};
-      tree_add_odd<2, 4>(p, b, hk, anc_s[n], D, d, v);
+      tree_add_odd<2, 4>(p, b, hk, anc_s[r / p.G], D, d, v);
       acc = make_float4(v[0], v[1], v[2], v[3]);
     }
-    if (p.splits == 1) {
-      const float f = l == 0.f ? 0.f : 1.f / l;
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
-      if (pad) tree_store4<__nv_bfloat16>(dst, 0.f, 0.f, 0.f, 0.f);
-      else tree_store4<__nv_bfloat16>(dst, acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-    } else {
-      const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
-      if (d == 0) p.part_ml[at] = make_float2(top, pad ? TREE_PADDING : l);
-      *reinterpret_cast<float4*>(p.part_acc + at * D + d) = acc;
+    if (pad) l = TREE_PADDING;
+    return acc;
+  };
+  auto write = [&](int m, int d, const float4& acc, float l) {
+    const float f = l == 0.f || l == TREE_PADDING ? 0.f : 1.f / l;
+    const int n = m / p.G, g = m - n * p.G;
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
+    if (l == TREE_PADDING) tree_store4<__nv_bfloat16>(dst, 0.f, 0.f, 0.f, 0.f);
+    else tree_store4<__nv_bfloat16>(dst, acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+  };
+  if constexpr (CLUSTER) {
+    // Every block leaves its row sums over its own first warp's partial result and its (maximum, sum) over Q; then the rows'
+    // components are dealt out over the cluster's threads, and each is added up from all blocks.
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    float2* block_ml = reinterpret_cast<float2*>(q_s);
+    for (int e = tid; e < p.M * (D / 4); e += TREE_MMA_THREADS) {
+      const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+      float top, l;
+      const float4 acc = joined(r, d, top, l);
+      *reinterpret_cast<float4*>(o_s + r * D + d) = acc;       // (read by this thread only, and just now)
+      if (d == 0) block_ml[r] = make_float2(top, l);
+    }
+    cluster.sync();
+    for (int e = split * TREE_MMA_THREADS + tid; e < p.M * (D / 4); e += p.splits * TREE_MMA_THREADS) {
+      const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+      float2 ml[TREE_CLUSTER_MAX];
+      float4 x[TREE_CLUSTER_MAX];
+#pragma unroll
+      for (int c = 0; c < TREE_CLUSTER_MAX; ++c) {
+        ml[c] = make_float2(-INFINITY, 0.f);
+        x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < p.splits) {
+          ml[c] = cluster.map_shared_rank(block_ml, c)[r];
+          x[c] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(o_s, c) + r * D + d);
+        }
+      }
+      float top = -INFINITY, l = 0.f;
+      bool pad = false;
+#pragma unroll
+      for (int c = 0; c < TREE_CLUSTER_MAX; ++c) {
+        top = fmaxf(top, ml[c].x);
+        pad |= ml[c].y == TREE_PADDING;
+      }
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int c = 0; c < TREE_CLUSTER_MAX; ++c) {
+        if (ml[c].x == -INFINITY) continue;
+        const float f = ex2_approx(ml[c].x - top);
+        l += f * ml[c].y;
+        acc.x = fmaf(f, x[c].x, acc.x); acc.y = fmaf(f, x[c].y, acc.y);
+        acc.z = fmaf(f, x[c].z, acc.z); acc.w = fmaf(f, x[c].w, acc.w);
+      }
+      write(r, d, acc, pad ? TREE_PADDING : l);
+    }
+    cluster.sync();      // no block leaves while another reads its shared memory
+  } else {
+    for (int e = tid; e < p.M * (D / 4); e += TREE_MMA_THREADS) {
+      const int m = e / (D / 4), d = (e % (D / 4)) * 4;
+      float top, l;
+      const float4 acc = joined(m, d, top, l);
+      if (p.splits == 1) {
+        write(m, d, acc, l);
+      } else {
+        const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
+        if (d == 0) p.part_ml[at] = make_float2(top, l);
+        *reinterpret_cast<float4*>(p.part_acc + at * D + d) = acc;
+      }
     }
   }
 }
