@@ -328,11 +328,11 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     if (c.dtype == TOVA_DTYPE_BF16) {
       t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : TREE_MMA_64;
       rows = 64;
-      cols = tova::TREE_MMA_COLS;
+      cols = 64;                 // a tile of four warps
     }
     t.row_blocks = (M + rows - 1) / rows;
     const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;
-    const int tiles = std::max(1, (n_live + cols - 1) / cols);
+    int tiles = std::max(1, (n_live + cols - 1) / cols);
     // Runs of columns for two rounds of resident blocks (two per SM), but none shorter than two tiles unless the GPU
     // would stay half empty.
     const int resident = 2 * sm_count, shortest = whole * (tiles / 2) < resident ? 1 : 2;
@@ -343,7 +343,9 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     // long: that is less time than the second kernel takes.
     if (t.kernel != TREE_ALU && want > 1 && (want <= tova::TREE_CLUSTER_MAX || tiles <= 4 * tova::TREE_CLUSTER_MAX)) {
       t.cluster = true;
-      want = std::min<long long>(want, tova::TREE_CLUSTER_MAX);
+      cols *= 2;                 // a tile of eight warps
+      tiles = (tiles + 1) / 2;
+      want = std::min<long long>(std::min<long long>(want, tova::TREE_CLUSTER_MAX), tiles);
     }
     const int per = (int)((tiles + want - 1) / want);
     t.split_cols = per * cols;
@@ -409,12 +411,13 @@ cudaError_t tree_merge(const tova::TreeParams& p, cudaStream_t st) {
 template <int D, int FMT, int MT, int WR, bool CLUSTER>
 cudaError_t tree_start_mma_c(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
   static std::atomic<bool> configured[64];
-  return tree_start(tova::tova_tree_mma_kernel<D, FMT, MT, WR, CLUSTER>, configured, tova::TreeMmaShape<D, FMT, MT, WR>::SMEM,
-                    tova::TREE_MMA_THREADS, tree_grid(p, t), CLUSTER ? t.splits : 1, st, p);
+  using S = tova::TreeMmaShape<D, FMT, MT, WR, CLUSTER ? 8 : 4>;
+  return tree_start(tova::tova_tree_mma_kernel<D, FMT, MT, WR, CLUSTER>, configured, S::SMEM, S::THREADS, tree_grid(p, t),
+                    CLUSTER ? t.splits : 1, st, p);
 }
 template <int D, int FMT, int MT, int WR>
 cudaError_t tree_start_mma(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
-  return t.cluster ? tree_start_mma_c<D, FMT, MT, WR, true>(p, t, st) : tree_start_mma_c<D, FMT, MT, WR, false>(p, t, st);
+  return t.cluster && t.splits > 1 ? tree_start_mma_c<D, FMT, MT, WR, true>(p, t, st) : tree_start_mma_c<D, FMT, MT, WR, false>(p, t, st);
 }
 
 template <int D, int FMT, int NT>

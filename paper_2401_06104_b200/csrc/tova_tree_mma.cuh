@@ -26,26 +26,28 @@
 
 namespace tova {
 
-constexpr int TREE_MMA_THREADS = 128;
-constexpr int TREE_MMA_COLS = 64;      // columns of a tile
 constexpr int TREE_MMA_NODES = 64;     // M <= 64, so there are no more nodes than that: the drafts are one tile
 
-template <int D, int FMT, int MT, int WR>
+// W warps a block, tiles of 16 W columns.  Four warps and two blocks per SM where there are blocks enough to fill the GPU;
+// eight warps a block where there are not, so that fewer tiles follow one another and two warps share a scheduler.
+template <int D, int FMT, int MT, int WR, int W>
 struct TreeMmaShape {
-  static constexpr int WK = 4 / WR;                     // warps that share out a tile's columns
-  static constexpr int KS = TREE_MMA_COLS / WK;         // columns of a warp
+  static constexpr int THREADS = 32 * W;
+  static constexpr int COLS = 16 * W;                   // columns of a tile
+  static constexpr int WK = W / WR;                     // warps that share out a tile's columns
+  static constexpr int KS = COLS / WK;                  // columns of a warp
   static constexpr int NB = KS / 8;
   static constexpr int ROWS = 16 * MT * WR;             // rows of the product per block
   static constexpr int ROW_BYTES = D * (FMT == FORMAT_PLAIN ? 2 : 1);
-  static constexpr int TILE = TREE_MMA_COLS * ROW_BYTES;
-  static constexpr int STAGE = 2 * TILE + (FMT == FORMAT_PLAIN ? 0 : 2 * TREE_MMA_COLS * 4);
-  // 48 to 100 KiB in flight per block, two blocks per SM: about twice what the memory's latency asks for
+  static constexpr int TILE = COLS * ROW_BYTES;
+  static constexpr int STAGE = 2 * TILE + (FMT == FORMAT_PLAIN ? 0 : 2 * COLS * 4);
+  // 48 to 100 KiB a block and two blocks per SM, or twice that and one: about twice what the memory's latency asks for
   static constexpr int STAGES = FMT == FORMAT_PLAIN ? 3 : (D == 128 ? 5 : 8);
   static constexpr int Q_BYTES = ROWS * D * 2;
   static constexpr int SMEM = STAGES * STAGE + Q_BYTES;
   // the drafts take one stage (bf16 states), or one for their keys and one for their values (8-bit states)
   static constexpr int DRAFT_STAGES = FMT == FORMAT_PLAIN ? 1 : 2;
-  static_assert(TREE_MMA_COLS * D * 2 * (FMT == FORMAT_PLAIN ? 2 : 1) <= STAGE && STAGES > DRAFT_STAGES, "drafts fit the ring");
+  static_assert(COLS * D * 2 * (FMT == FORMAT_PLAIN ? 2 : 1) <= STAGE && STAGES > DRAFT_STAGES, "drafts fit the ring");
   // the ring's room is taken over by the joining of the warps
   static_assert(WK * ROWS * (D * 4 + 8) <= STAGES * STAGE, "partial results fit the ring");
   static_assert(ROWS * 8 <= Q_BYTES, "a block's maxima and sums fit Q's room");
@@ -100,9 +102,9 @@ __device__ __forceinline__ uint32_t tree_off8(int row, int ch) {
 constexpr int TREE_CLUSTER_MAX = 8;
 
 template <int D, int FMT, int MT, int WR, bool CLUSTER>
-__global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(const __grid_constant__ TreeParams p) {
-  using S = TreeMmaShape<D, FMT, MT, WR>;
-  constexpr int C = TREE_MMA_COLS, KS = S::KS, NB = S::NB, OB = D / 8;
+__global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tree_mma_kernel(const __grid_constant__ TreeParams p) {
+  using S = TreeMmaShape<D, FMT, MT, WR, CLUSTER ? 8 : 4>;
+  constexpr int THREADS = S::THREADS, C = S::COLS, KS = S::KS, NB = S::NB, OB = D / 8;
   constexpr bool PLAIN = FMT == FORMAT_PLAIN;
   extern __shared__ __align__(128) unsigned char tree_smem[];
   unsigned char* ring = tree_smem;
@@ -137,8 +139,8 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
     if (i >= n_tiles) {
       constexpr int DC = D / 8;
 #pragma unroll
-      for (int x = 0; x < C * DC / TREE_MMA_THREADS; ++x) {
-        const int e = x * TREE_MMA_THREADS + tid;
+      for (int x = 0; x < C * DC / THREADS; ++x) {
+        const int e = x * THREADS + tid;
         const int row = e / DC, ch = e % DC;
         const uint32_t off = tree_off16<2 * D>(row, ch), size = row < p.N ? 16u : 0u;
         if (PLAIN) {
@@ -151,8 +153,8 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
       return;
     }
 #pragma unroll
-    for (int x = 0; x < C * CH / TREE_MMA_THREADS; ++x) {
-      const int e = x * TREE_MMA_THREADS + tid;
+    for (int x = 0; x < C * CH / THREADS; ++x) {
+      const int e = x * THREADS + tid;
       const int row = e / CH, ch = e % CH;
       const bool in = j0 + row < c1;                       // columns behind the run are zeros, whatever lies there
       const long long at = (long long)(in ? j0 + row : c0) * S::ROW_BYTES + ch * 16;
@@ -161,9 +163,10 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
       cp_async16(st + S::TILE + off, Vg + at, in ? 16u : 0u);
     }
     if constexpr (!PLAIN) {
-      const int row = tid & 63;
+      static_assert(THREADS == 2 * C, "one scale a thread");
+      const int row = tid & (C - 1);
       const bool in = j0 + row < c1;
-      cp_async4(st + 2 * S::TILE + tid * 4, (tid < 64 ? ksg : vsg) + (in ? j0 + row : c0), in ? 4u : 0u);
+      cp_async4(st + 2 * S::TILE + tid * 4, (tid < C ? ksg : vsg) + (in ? j0 + row : c0), in ? 4u : 0u);
     }
   };
 #pragma unroll
@@ -183,7 +186,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   }
   // Q in operand order.  Step ks of the contraction: natural order (bf16 states) k = 16 ks + 2 lc + {0,1}, + 8; permuted
   // (8-bit states), with ks = 4 i + w: d = 64 i + 16 lc + 4 w + {0,1}, {2,3}.
-  for (int e = tid; e < (S::ROWS / 16) * (D / 16) * 32; e += TREE_MMA_THREADS) {
+  for (int e = tid; e < (S::ROWS / 16) * (D / 16) * 32; e += THREADS) {
     const int l = e & 31, ks = (e >> 5) % (D / 16), rt = (e >> 5) / (D / 16);
     const int r = l >> 2, c = l & 3;
     uint32_t w[4] = {0, 0, 0, 0};
@@ -401,8 +404,8 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
     // A draft that a row does not see may hold anything, and 0 times an infinity is not 0: values that are not finite
     // are taken out (each thread looks at the chunks it copied) and added at the end to the rows that see them.
 #pragma unroll
-    for (int x = 0; x < C * (D / 8) / TREE_MMA_THREADS; ++x) {
-      const int e = x * TREE_MMA_THREADS + tid;
+    for (int x = 0; x < C * (D / 8) / THREADS; ++x) {
+      const int e = x * THREADS + tid;
       uint4* at = reinterpret_cast<uint4*>(dv + tree_off16<2 * D>(e / (D / 8), e % (D / 8)));
       uint4 w = *at;
       if (tree_drop_odd(w)) {
@@ -515,6 +518,9 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
   __syncthreads();
   float* o_s = reinterpret_cast<float*>(ring);                       // [WK][ROWS][D]
   float2* ml_s = reinterpret_cast<float2*>(ring + S::WK * S::ROWS * D * 4);   // [WK][ROWS]
+  // Float offset of 16-byte chunk q of row r: the chunks turn with the row, and where a thread holds whole chunks also with
+  // their eighth, so that the lanes that store together meet different banks.
+  auto place = [](int r, int q) { return PLAIN ? (q ^ ((r << 1) & 7)) * 4 : (q ^ ((r ^ ((q >> 3) << 1)) & 7)) * 4; };
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -535,14 +541,19 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
 #pragma unroll
       for (int w = 0; w < S::WK; ++w) top = fmaxf(top, ml_s[w * S::ROWS + r].x);
       const float f = top == -INFINITY ? 0.f : ex2_approx(m_run[t][h] - top);
-      float* dst = o_s + (wk * S::ROWS + r) * D;
-#pragma unroll
-      for (int j = 0; j < OB; ++j) {
+      if (r < p.M) {
+        float* dst = o_s + (wk * S::ROWS + r) * D;
         if constexpr (PLAIN) {
-          *reinterpret_cast<float2*>(dst + 8 * j + 2 * lc) = make_float2(o[t][j][2 * h] * f, o[t][j][2 * h + 1] * f);
+#pragma unroll
+          for (int j = 0; j < OB; ++j)
+            *reinterpret_cast<float2*>(dst + place(r, 2 * j + (lc >> 1)) + 2 * (lc & 1)) = make_float2(o[t][j][2 * h] * f, o[t][j][2 * h + 1] * f);
         } else {
-          dst[OB * (2 * lc) + j] = o[t][j][2 * h] * f;
-          dst[OB * (2 * lc + 1) + j] = o[t][j][2 * h + 1] * f;
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int j = 0; j < OB; j += 4)
+              *reinterpret_cast<float4*>(dst + place(r, OB / 4 * (2 * lc + e) + j / 4)) =
+                  make_float4(o[t][j][2 * h + e] * f, o[t][j + 1][2 * h + e] * f, o[t][j + 2][2 * h + e] * f, o[t][j + 3][2 * h + e] * f);
         }
       }
     }
@@ -560,7 +571,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
       const float2 ml = ml_s[w * S::ROWS + r];
       pad |= ml.y == TREE_PADDING;
       if (ml.x != -INFINITY) l += ml.y * ex2_approx(ml.x - top);
-      const float4 x = *reinterpret_cast<const float4*>(o_s + (w * S::ROWS + r) * D + d);
+      const float4 x = *reinterpret_cast<const float4*>(o_s + (w * S::ROWS + r) * D + place(r, d >> 2));
       acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
     }
     if (last && odd_s && !pad) {
@@ -584,15 +595,15 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     float2* block_ml = reinterpret_cast<float2*>(q_s);
-    for (int e = tid; e < p.M * (D / 4); e += TREE_MMA_THREADS) {
+    for (int e = tid; e < p.M * (D / 4); e += THREADS) {
       const int r = e / (D / 4), d = (e % (D / 4)) * 4;
       float top, l;
       const float4 acc = joined(r, d, top, l);
-      *reinterpret_cast<float4*>(o_s + r * D + d) = acc;       // (read by this thread only, and just now)
+      *reinterpret_cast<float4*>(o_s + r * D + place(r, d >> 2)) = acc;       // (read by this thread only, and just now)
       if (d == 0) block_ml[r] = make_float2(top, l);
     }
     cluster.sync();
-    for (int e = split * TREE_MMA_THREADS + tid; e < p.M * (D / 4); e += p.splits * TREE_MMA_THREADS) {
+    for (int e = split * THREADS + tid; e < p.M * (D / 4); e += p.splits * THREADS) {
       const int r = e / (D / 4), d = (e % (D / 4)) * 4;
       float2 ml[TREE_CLUSTER_MAX];
       float4 x[TREE_CLUSTER_MAX];
@@ -602,7 +613,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
         x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (c < p.splits) {
           ml[c] = cluster.map_shared_rank(block_ml, c)[r];
-          x[c] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(o_s, c) + r * D + d);
+          x[c] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(o_s, c) + r * D + place(r, d >> 2));
         }
       }
       float top = -INFINITY, l = 0.f;
@@ -625,7 +636,7 @@ __global__ void __launch_bounds__(TREE_MMA_THREADS, 2) tova_tree_mma_kernel(cons
     }
     cluster.sync();      // no block leaves while another reads its shared memory
   } else {
-    for (int e = tid; e < p.M * (D / 4); e += TREE_MMA_THREADS) {
+    for (int e = tid; e < p.M * (D / 4); e += THREADS) {
       const int m = e / (D / 4), d = (e % (D / 4)) * 4;
       float top, l;
       const float4 acc = joined(m, d, top, l);
