@@ -315,12 +315,13 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
   size_t part_rows;
   if (c.dtype == TOVA_DTYPE_BF16 && M > 64) {
     // More than 64 rows: the contractions, not the state's bytes, set the pace of a warp-level kernel.
-    t.kernel = M <= 128 ? TREE_TC_1 : TREE_TC_2;
-    const int rows = (M <= 128 ? 1 : 2) * tova::TREE_TC_ROWS;
-    const bool two = M <= 128 && c.format == TOVA_FORMAT_PLAIN;
+    // Two row tiles a block from 129 rows on; 8-bit states one (see the kernel).
+    const bool one = M <= 128 || c.format != TOVA_FORMAT_PLAIN, two_blocks = M <= 128 && c.format == TOVA_FORMAT_PLAIN;
+    t.kernel = one ? TREE_TC_1 : TREE_TC_2;
+    const int rows = (one ? 1 : 2) * tova::TREE_TC_ROWS;
     t.row_blocks = (M + rows - 1) / rows;
     t.splits = 1;
-    t.blocks = (two ? 2 : 1) * sm_count;
+    t.blocks = (two_blocks ? 2 : 1) * sm_count;
     t.least = 4;                 // tiles of 128 columns: less than that does not pay for a block's set-up
     part_rows = (size_t)2 * t.blocks * rows;
   } else {
@@ -471,7 +472,9 @@ cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream
       case TREE_MMA_32: e = tree_start_mma<D, FMT, 1, 2>(p, t, st); break;
       case TREE_MMA_64: e = tree_start_mma<D, FMT, 2, 2>(p, t, st); break;
       case TREE_TC_1: return tree_run_tc<D, FMT, 1>(p, t, st);
-      default: return tree_run_tc<D, FMT, 2>(p, t, st);
+      default:
+        if constexpr (FMT == tova::FORMAT_PLAIN) return tree_run_tc<D, FMT, 2>(p, t, st);
+        return cudaErrorInvalidValue;
     }
   }
   if (e != cudaSuccess || t.splits == 1 || t.cluster) return e;

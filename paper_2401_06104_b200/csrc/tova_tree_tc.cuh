@@ -12,11 +12,14 @@
 //   producer warps      Q, then K and V tiles into a ring of shared-memory slots in the 128-byte-swizzled layout the tensor
 //                       cores read: bf16 states by tiled TMA, as far ahead as there are slots (by cp.async the two warps
 //                       could not keep up; values of rows behind a sequence's last are zeroed when they have landed,
-//                       whatever lies there); 8-bit states by bulk copies into a raw ring and an exact conversion (see
+//                       whatever lies there); 8-bit states from a raw ring, with an exact conversion (see
 //                       tova_tree_mma.cuh); drafts by plain loads that take out infinities and NaN.
 //   1 issuing thread    S = Q K^T (128 x 128, fp32 in TMEM) and O += P V in the order PV_0(i) S_0(i+1) PV_1(i) S_1(i+1):
 //                       the tensor cores work on one row tile while the other's soft-max runs (two row tiles in a block,
-//                       or two blocks on an SM)
+//                       or two blocks on an SM); 8-bit states: one row tile a block and SM, two S buffers, S of the next
+//                       tile ahead of O += P V of this one - the conversion needs eight warps, and registers
+//   1 copying thread    (8-bit states) bulk copies into the raw ring: a producer that had to wait for all of them to be done
+//                       with a raw slot before it could ask for the next copy would hold up its own conversions
 //   1 helper warp       ancestor bits of the next job's drafts, and whether one of their values is not finite
 //   8 warps a row tile  two threads a row, 64 columns each: logits from TMEM, weights as bf16 back over them, where they are
 //                       the A operand of O += P V.  The weights' reference is a whole number, set by a job's first tile
@@ -41,21 +44,24 @@ template <int D, int FMT, int NT>
 struct TreeTcShape {
   static constexpr bool PLAIN = FMT == FORMAT_PLAIN;
   static constexpr int SOFT_WARPS = 8 * NT;
-  static constexpr int PRODUCER_WARPS = PLAIN ? 2 : 4;
-  static constexpr int THREADS = 32 * (SOFT_WARPS + PRODUCER_WARPS + 2);
+  static constexpr int PRODUCER_WARPS = PLAIN ? 2 : 8;
+  static constexpr bool DOUBLE = !PLAIN;                           // two S buffers
+  static_assert(PLAIN || NT == 1, "an 8-bit state's second S buffer takes the second row tile's tensor memory");
+  static constexpr int THREADS = 32 * (SOFT_WARPS + PRODUCER_WARPS + (PLAIN ? 2 : 3));
   static constexpr int BLOCKS = PLAIN && NT == 1 ? 2 : 1;          // per SM
   static constexpr int Q_BYTES = TREE_TC_ROWS * D * 2;             // per row tile
   static constexpr int SLOT = TREE_TC_COLS * D * 2;
-  static constexpr int SLOTS = (PLAIN ? (NT == 1 ? 2 : 4) : 3) * (128 / D);
+  static constexpr int SLOTS = (PLAIN && NT == 1 ? 2 : 4) * (128 / D);
   static constexpr int RAW = PLAIN ? 0 : TREE_TC_COLS * D;
-  static constexpr int RAW_SLOTS = PLAIN ? 0 : (NT == 1 ? 4 : 3) * (128 / D);
+  static constexpr int RAW_SLOTS = PLAIN ? 0 : 3 * (128 / D);
   // Tiles whose scales are kept.  K of tile i takes the slot of a copy SLOTS positions back; when that has been consumed,
   // the soft-max of tile i - SLOTS/2 - 1 has passed.
   static constexpr int SCALE_TILES = SLOTS / 2 + 2;
   static constexpr int SCALES = PLAIN ? 0 : SCALE_TILES * 2 * TREE_TC_COLS * 4;
   static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + RAW_SLOTS * RAW + SCALES + 1024;
-  static constexpr int TMEM_COLS = 256 * NT;
-  static constexpr int NODES = NT == 1 ? TREE_TC_ROWS : TREE_MAX_NODES;   // one row tile: M <= 128, so N <= 128
+  static constexpr int TMEM_COLS = DOUBLE ? 512 : 256 * NT;
+  static constexpr int BUFFERS = DOUBLE ? 2 : NT;                  // S buffers (and barriers for them)
+  static constexpr int NODES = BLOCKS == 2 ? TREE_TC_ROWS : TREE_MAX_NODES;   // (taken for M <= 128 only, so N <= 128)
   static constexpr int WORDS = NODES / 32;
 };
 
@@ -137,6 +143,13 @@ __device__ __forceinline__ void tree_tc_scale16(uint32_t taddr, float f) {
   tmem_st16(taddr, v);
 }
 
+// One arrival for a whole warp: an arrival is an atomic operation on shared memory, and 32 of them on one word take as long
+// as a tile's worth of copies.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+
 template <int D, int FMT, int NT>
 __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<D, FMT, NT>::BLOCKS)
     tova_tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_k,
@@ -144,8 +157,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
   using S = TreeTcShape<D, FMT, NT>;
   constexpr bool PLAIN = S::PLAIN;
   constexpr int C = TREE_TC_COLS, R = TREE_TC_ROWS;
-  constexpr int PRODUCER = S::SOFT_WARPS, ISSUER = PRODUCER + S::PRODUCER_WARPS, HELPER = ISSUER + 1;      // first warp of each role
-  constexpr int PT = 32 * S::PRODUCER_WARPS, SOFT = 32 * S::SOFT_WARPS;
+  constexpr int PRODUCER = S::SOFT_WARPS, ISSUER = PRODUCER + S::PRODUCER_WARPS, HELPER = ISSUER + 1, COPIER = HELPER + 1;      // first warp of each role
+  constexpr int PT = 32 * S::PRODUCER_WARPS;
   extern __shared__ unsigned char tree_tc_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(tree_tc_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* q_s = smem;                               // per row tile: boxes of [128 rows][128 bytes]
@@ -154,9 +167,10 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
   float* scale_s = reinterpret_cast<float*>(raw_s + S::RAW_SLOTS * S::RAW);   // [tile % SCALE_TILES][k times the logits' scale, v][128]
   __shared__ __align__(8) uint64_t full[S::SLOTS], empty[S::SLOTS], bar_sc[S::SCALE_TILES];
   __shared__ __align__(8) uint64_t raw_full[PLAIN ? 1 : S::RAW_SLOTS], raw_empty[PLAIN ? 1 : S::RAW_SLOTS];
-  // Q landed, Q free again, S computed, weights written, O complete, ancestor bits there, ancestor bits free again, the
+  // Q landed, Q free again, S computed, weights written, O complete, (two S buffers) a tile's O += P V
+  // complete, ancestor bits there, ancestor bits free again, the
   // two warps of 32 rows meet, a tile that has to be trimmed landed
-  __shared__ __align__(8) uint64_t bar_q, bar_qf, bar_s[NT], bar_p[NT], bar_o[NT], bar_a, bar_af, bar_pair[NT * 4], bar_trim;
+  __shared__ __align__(8) uint64_t bar_q, bar_qf, bar_s[S::BUFFERS], bar_p[S::BUFFERS], bar_o[NT], bar_v, bar_a, bar_af, bar_pair[NT * 4], bar_trim;
   __shared__ uint32_t tmem_base_s;
   __shared__ int odd_s;                                    // some draft's value is not finite
   __shared__ TreeTcRun run_s, soft_run_s[S::SOFT_WARPS];   // (the soft-max warps' registers are for the rows)
@@ -169,25 +183,26 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
 
   if (tid == 0) {
     for (int i = 0; i < S::SLOTS; ++i) {
-      mbar_init(&full[i], PT);
+      mbar_init(&full[i], S::PRODUCER_WARPS);
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < S::RAW_SLOTS; ++i) {
       mbar_init(&raw_full[i], 1);
-      mbar_init(&raw_empty[i], PT);
+      mbar_init(&raw_empty[i], S::PRODUCER_WARPS);
     }
-    mbar_init(&bar_q, PT);
+    mbar_init(&bar_q, S::PRODUCER_WARPS);
     mbar_init(&bar_trim, 1);
     mbar_init(&bar_qf, 1);
-    for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < S::BUFFERS; ++t) {
       mbar_init(&bar_s[t], 1);
-      mbar_init(&bar_p[t], 2 * R);
-      mbar_init(&bar_o[t], 1);
+      mbar_init(&bar_p[t], 2 * R / 32);
     }
-    for (int i = 0; i < S::SCALE_TILES; ++i) mbar_init(&bar_sc[i], PT);
-    mbar_init(&bar_a, 32);
-    mbar_init(&bar_af, SOFT);
-    for (int i = 0; i < NT * 4; ++i) mbar_init(&bar_pair[i], 64);
+    for (int t = 0; t < NT; ++t) mbar_init(&bar_o[t], 1);
+    mbar_init(&bar_v, 1);
+    for (int i = 0; i < S::SCALE_TILES; ++i) mbar_init(&bar_sc[i], S::PRODUCER_WARPS);
+    mbar_init(&bar_a, 1);
+    mbar_init(&bar_af, S::SOFT_WARPS);
+    for (int i = 0; i < NT * 4; ++i) mbar_init(&bar_pair[i], 2);
     mbar_fence_init();
   }
   if (tid < NT * 4) flag_s[tid] = -1;
@@ -251,6 +266,10 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
   const uint32_t tmem = tmem_base_s;
   TreeTcRun run = run_s;
   bool ok = true;
+  // S of row tile t, tile g: its buffer, the buffer's columns, and the phase of the buffer's barriers.
+  auto s_buf = [](int t, int g) { return S::DOUBLE ? g & 1 : t; };
+  auto s_col = [&](int t, int g) { return tmem + 256 * s_buf(t, g); };
+  auto s_phase = [](int g) { return (uint32_t)((S::DOUBLE ? g >> 1 : g) & 1); };
   // Copies are made and consumed in the order Q K0 V0 K1 V1 ...; the counters go on from piece to piece.  Tile g (of the
   // block's run) has K at ring position 2 g and V at 2 g + 1.
 
@@ -283,7 +302,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
 #pragma unroll
               for (int c = 0; c < D / 64; ++c)
                 tma_load_3d_tile(q_s + t * S::Q_BYTES + c * (R * 128), &map_q, c * 64, run.b * p.H + run.hk * p.G, (m0 + t * R) / p.G, &bar_q);
-          } else {
+          } else if (lane == 0) {
             mbar_arrive(&bar_q);
           }
           return;
@@ -300,7 +319,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
         cp_async_commit();
         cp_async_wait<0>();
         fence_proxy_async_smem();
-        mbar_arrive(&bar_q);
+        warp_arrive(&bar_q, lane);
       };
       const unsigned char* src[2] = {static_cast<const unsigned char*>(p.K) + (long long)bh * p.cap * (PLAIN ? 2 * D : D),
                                      static_cast<const unsigned char*>(p.V) + (long long)bh * p.cap * (PLAIN ? 2 * D : D)};
@@ -328,7 +347,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
           }
         }
         fence_proxy_async_smem();
-        mbar_arrive(&full[pos % S::SLOTS]);
+        warp_arrive(&full[pos % S::SLOTS], lane);
       };
       if constexpr (PLAIN) {
         for (int x = 0; x < 2 * n && ok; ++x) {
@@ -356,8 +375,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
               for (int e = valid * QCH + pt; e < C * QCH; e += PT)
                 *reinterpret_cast<uint4*>(dst + place(e / QCH, e % QCH)) = make_uint4(0, 0, 0, 0);
               fence_proxy_async_smem();
-              mbar_arrive(&full[pos % S::SLOTS]);
-            } else if (pt != 0) {
+              warp_arrive(&full[pos % S::SLOTS], lane);
+            } else if (pt != 0 && lane == 0) {
               mbar_arrive(&full[pos % S::SLOTS]);
             }
           } else {
@@ -370,46 +389,34 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
             cp_async_commit();
             cp_async_wait<0>();
             fence_proxy_async_smem();
-            mbar_arrive(&full[pos % S::SLOTS]);
+            warp_arrive(&full[pos % S::SLOTS], lane);
           }
           if (x == 1) load_q();
         }
       } else {
-        // Raw copies run RAW_SLOTS - 1 ahead of the conversions; raw position rp = 2 (state tiles of the block so far) + x.
-        constexpr int AHEAD = S::RAW_SLOTS - 1;
+        const int n_raw = 2 * max(0, min(run.i1, run.n_state) - run.i0);     // raw copies of this piece
         const int turn = D == 128 ? (ch_t >> 2) & 1 : row_t & 1;
-        const int n_raw = 2 * max(0, min(run.i1, run.n_state) - run.i0);
-        auto fetch = [&](int x) {
-          if (x >= n_raw || !ok) return;
-          const int rp = raw0 + x, j = (run.i0 + x / 2) * C;
-          if (rp >= S::RAW_SLOTS) ok = mbar_wait_bounded(&raw_empty[rp % S::RAW_SLOTS], (uint32_t)((rp / S::RAW_SLOTS - 1) & 1));
-          if (!ok) return;
-          const uint32_t bytes = (uint32_t)min(C, run.len - j) * D;
-          mbar_expect_tx(&raw_full[rp % S::RAW_SLOTS], bytes);
-          bulk_g2s(raw_s + (rp % S::RAW_SLOTS) * S::RAW, ((x & 1) ? src[1] : src[0]) + (long long)j * D, bytes, &raw_full[rp % S::RAW_SLOTS]);
-        };
         // Two scales a thread and tile (columns behind the sequence's last get finite, positive ones: a masked logit is
         // minus infinity), fetched a tile early and stored with the tile's K.
-        float next_k, next_v;
+        float next_k, next_v;                    // (as loaded: a product with one would wait for it here)
         auto fetch_scales = [&](int tile) {
-          const int j = tile * C + pt;
+          const int j = tile * C + (pt & (C - 1));           // (of 256 threads two fetch the same)
           const bool in = tile < run.n_state && j < run.len;
-          next_k = p.scale2 * (in ? p.k_scale[(long long)bh * p.cap + j] : 1.f);
+          next_k = in ? p.k_scale[(long long)bh * p.cap + j] : 1.f;
           next_v = in ? p.v_scale[(long long)bh * p.cap + j] : 1.f;
         };
         fetch_scales(run.i0);
-        if (pt == 0)
-          for (int x = 0; x < AHEAD; ++x) fetch(x);
         for (int x = 0; x < 2 * n && ok; ++x) {
           const int pos = 2 * g0 + x, tile = run.i0 + x / 2, g = g0 + x / 2;
-          if (pt == 0) fetch(x + AHEAD);
-          ok = ok && slot_free(pos);
+          ok = slot_free(pos);
           if (!ok) break;
           if (!(x & 1)) {
             float* sc = scale_s + (g % S::SCALE_TILES) * 2 * C;
-            sc[pt] = next_k;
-            sc[C + pt] = next_v;
-            mbar_arrive(&bar_sc[g % S::SCALE_TILES]);
+            if (pt < C) {
+              sc[pt] = p.scale2 * next_k;
+              sc[C + pt] = next_v;
+            }
+            warp_arrive(&bar_sc[g % S::SCALE_TILES], lane);
             fetch_scales(tile + 1);
           }
           if (tile >= run.n_state) {
@@ -433,8 +440,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
               *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + (turn ^ 1))) = turn ? lo : hi;
             }
             fence_proxy_async_smem();          // for the tensor cores' reads, and for the next copy into the raw slot
-            mbar_arrive(&full[pos % S::SLOTS]);
-            mbar_arrive(&raw_empty[rp % S::RAW_SLOTS]);
+            warp_arrive(&full[pos % S::SLOTS], lane);
+            if (lane == 0) mbar_arrive(&raw_empty[rp % S::RAW_SLOTS]);
           }
           if (x == 1) load_q();
         }
@@ -443,7 +450,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       g0 += n;
       ++piece;
     }
-    // (Bulk copies: where a wait ran out it took two seconds, and whatever was on its way has landed since.)
+    // (TMA: where a wait ran out it took two seconds, and whatever was on its way has landed since.)
   } else if (warp == ISSUER) {
     // ============================== issuing thread ==============================
     if (lane == 0) {
@@ -466,9 +473,9 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
           const uint64_t k_t = at(k_d, (pos % S::SLOTS) * S::SLOT);
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
-            umma_bf16(tmem + 256 * t, at(q_d, t * S::Q_BYTES + (ks >> 2) * (R * 128) + (ks & 3) * 32),
+            umma_bf16(s_col(t, g0 + x), at(q_d, t * S::Q_BYTES + (ks >> 2) * (R * 128) + (ks & 3) * 32),
                       at(k_t, (ks >> 2) * (C * 128) + (ks & 3) * 32), idesc_s, ks > 0 ? 1u : 0u);
-          umma_commit(&bar_s[t]);
+          umma_commit(&bar_s[s_buf(t, g0 + x)]);
           if (t == NT - 1) {
             umma_commit(&empty[pos % S::SLOTS]);
             if (x == n - 1) umma_commit(&bar_qf);
@@ -484,29 +491,55 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
           const uint64_t v_t = at(v_d, (pos % S::SLOTS) * S::SLOT);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
+            if (S::DOUBLE && x + 1 < n) {
+              ok = landed(pos + 1);
+              if (!ok) break;
+              tc_fence_after();
+              issue_s(t, x + 1);
+            }
             if (t == 0) ok = landed(pos);
-            ok = ok && mbar_wait_bounded(&bar_p[t], (uint32_t)(g & 1));
+            ok = ok && mbar_wait_bounded(&bar_p[s_buf(t, g)], s_phase(g));
             if (!ok) break;
             tc_fence_after();
             // (the weights of columns 64.. lie 64 TMEM columns up: each half of a row overwrites its own logits only)
 #pragma unroll
             for (int kk = 0; kk < C / 16; ++kk)
-              umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + (kk >> 2) * 64 + (kk & 3) * 8,
+              umma_bf16_a_tmem(tmem + 256 * t + 128, s_col(t, g) + (kk >> 2) * 64 + (kk & 3) * 8,
                                at(v_t, kk * 2048), idesc_o, (x > 0 || kk > 0) ? 1u : 0u);
             if (t == NT - 1) umma_commit(&empty[pos % S::SLOTS]);
-            if (x + 1 < n) {
+            if (S::DOUBLE) umma_commit(&bar_v);
+            if (x + 1 == n) {
+              umma_commit(&bar_o[t]);
+            } else if (!S::DOUBLE) {
               if (t == 0) ok = landed(pos + 1);
               if (!ok) break;
               tc_fence_after();
               issue_s(t, x + 1);
-            } else {
-              umma_commit(&bar_o[t]);
             }
           }
         }
         g0 += n;
         ++piece;
       }
+    }
+  } else if (!PLAIN && warp == COPIER) {
+    // ============================== copying thread ==============================
+    if (lane == 0) {
+      int raw0 = 0;                              // raw copies before this piece
+      while (ok && run.next(p, blockIdx.x)) {
+        const long long row0 = (long long)(run.b * p.Hkv + run.hk) * p.cap;
+        const int n_raw = 2 * max(0, min(run.i1, run.n_state) - run.i0);
+        for (int x = 0; x < n_raw && ok; ++x) {
+          const int rp = raw0 + x, j = (run.i0 + x / 2) * C, slot = rp % max(1, S::RAW_SLOTS);
+          if (rp >= S::RAW_SLOTS) ok = mbar_wait_bounded(&raw_empty[slot], (uint32_t)((rp / max(1, S::RAW_SLOTS) - 1) & 1));
+          if (!ok) break;
+          const uint32_t bytes = (uint32_t)min(C, run.len - j) * D;
+          mbar_expect_tx(&raw_full[slot], bytes);
+          bulk_g2s(raw_s + slot * S::RAW, static_cast<const unsigned char*>((x & 1) ? p.V : p.K) + (row0 + j) * D, bytes, &raw_full[slot]);
+        }
+        raw0 += n_raw;
+      }
+      // (Where a wait ran out it took two seconds, and whatever was on its way has landed since.)
     }
   } else if (warp == HELPER) {
     // ============================== helper warp ==============================
@@ -537,7 +570,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       }
       odd = __any_sync(0xffffffffu, odd) != 0;
       if (lane == 0) odd_s = odd;
-      mbar_arrive(&bar_a);
+      warp_arrive(&bar_a, lane);
       ++done;
     }
     if (lane == 0) static_cast<TreeTcCut*>(p.cuts)[blockIdx.x] = cut;
@@ -547,15 +580,15 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
     // lanes of its quarter (warp mod 4).
     const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;
     const int pair = t * 4 + quarter, row = t * R + quarter * 32 + lane;
-    const uint32_t base = tmem + 256 * t + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t mine = base + 64 * half;                // this thread's logits, and its weights
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t base = tmem + 256 * t + lanes;
     const uint64_t scale_2 = pack_f2(p.scale2, p.scale2);
     volatile TreeTcRun& mr = soft_run_s[warp];
     int g0 = 0, piece = 0, done = 0;
     uint32_t met = 0;                    // phase of the pair's barrier
     // The two warps that share 32 rows meet: what either wrote to shared memory before is there for both.
     auto meet = [&]() {
-      mbar_arrive(&bar_pair[pair]);
+      warp_arrive(&bar_pair[pair], lane);
       ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bar_pair[pair], met)) != 0;
       met ^= 1u;
     };
@@ -585,7 +618,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       for (int x = 0; x < n && ok; ++x) {
         const int i = mr.i0 + x, g = g0 + x;
         const float* sc = scale_s + (g % S::SCALE_TILES) * 2 * C + 64 * half;
-        ok = mbar_wait_bounded(&bar_s[t], (uint32_t)(g & 1));
+        const uint32_t mine = s_col(t, g) + lanes + 64 * half;                  // this thread's logits, and its weights
+        ok = mbar_wait_bounded(&bar_s[s_buf(t, g)], s_phase(g));
         if constexpr (!PLAIN) ok = ok && mbar_wait_bounded(&bar_sc[g % S::SCALE_TILES], (uint32_t)((g / S::SCALE_TILES) & 1));
         ok = __all_sync(0xffffffffu, ok) != 0;
         if (ok && i >= mr.n_state && !looked) look();
@@ -683,8 +717,13 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
           m_ref = m_new;
           l *= corr;
           if (x > 0) {
-            // O of the tiles so far, half the columns a thread.  (The last of them is complete: S of this tile was issued
-            // behind it.)
+            // O of the tiles so far, half the columns a thread.  (The last of them is complete where S of this tile was
+            // issued behind it.)
+            if (S::DOUBLE) {
+              ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bar_v, (uint32_t)((g - 1) & 1))) != 0;
+              if (!ok) break;
+              tc_fence_after();
+            }
 #pragma unroll
             for (int c = 0; c < D / 2; c += 16) tree_tc_scale16(base + 128 + half * (D / 2) + c, corr);
           }
@@ -700,7 +739,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&bar_p[t]);
+        warp_arrive(&bar_p[s_buf(t, g)], lane);
       }
       if (drafts && ok && !looked) look();
       if (ok) {
@@ -751,7 +790,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
       }
       tc_fence_before();                 // O has been read: the next piece's first weights are reported behind this
       if (drafts) {
-        mbar_arrive(&bar_af);
+        warp_arrive(&bar_af, lane);
         ++done;
       }
       g0 += n;
