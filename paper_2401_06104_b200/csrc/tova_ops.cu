@@ -303,7 +303,7 @@ int tree_check(const tova_tree_config* c, int32_t n_live, int32_t n_nodes) {
 enum : int { TREE_ALU, TREE_MMA_16, TREE_MMA_32, TREE_MMA_64, TREE_TC_1, TREE_TC_2 };
 struct TreePlan {
   int kernel, row_blocks, splits, split_cols;
-  int blocks, least;             // tcgen05 kernel
+  int blocks, group, row_rounds, least;      // tcgen05 kernel
   bool cluster;                  // the runs' blocks join by themselves
   size_t ml_bytes, acc_bytes, bytes;   // workspace: maxima and sums, weighted sums (and the tcgen05 kernel's list of cuts)
 };
@@ -316,12 +316,13 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
   if (c.dtype == TOVA_DTYPE_BF16 && M > 64) {
     // More than 64 rows: the contractions, not the state's bytes, set the pace of a warp-level kernel.
     // Two row tiles a block from 129 rows on; 8-bit states one (see the kernel).
-    const bool one = M <= 128 || c.format != TOVA_FORMAT_PLAIN, two_blocks = M <= 128 && c.format == TOVA_FORMAT_PLAIN;
+    const bool one = M <= 128 || c.format != TOVA_FORMAT_PLAIN;
     t.kernel = one ? TREE_TC_1 : TREE_TC_2;
-    const int rows = (one ? 1 : 2) * tova::TREE_TC_ROWS;
-    t.row_blocks = (M + rows - 1) / rows;
     t.splits = 1;
-    t.blocks = (two_blocks ? 2 : 1) * sm_count;
+    const int rows = (one ? 1 : 2) * tova::TREE_TC_ROWS, row_blocks = (M + rows - 1) / rows;
+    t.row_rounds = (row_blocks + sm_count - 1) / sm_count;
+    t.group = (row_blocks + t.row_rounds - 1) / t.row_rounds;
+    t.blocks = sm_count / t.group * t.group;
     t.least = 4;                 // tiles of 128 columns: less than that does not pay for a block's set-up
     part_rows = (size_t)2 * t.blocks * rows;
   } else {
@@ -530,7 +531,7 @@ extern "C" int tova_tree_attention(const tova_tree_config* cfg, const void* K, c
   p.N = n_nodes; p.B = cfg->batch; p.H = cfg->n_q_heads; p.Hkv = cfg->n_kv_heads;
   p.G = p.H / p.Hkv; p.M = p.N * p.G; p.cap = cfg->capacity; p.n_live = n_live;
   p.splits = t.splits; p.split_cols = t.split_cols;
-  p.row_blocks = t.row_blocks; p.blocks = t.blocks; p.least = t.least;
+  p.group = t.group; p.row_rounds = t.row_rounds; p.least = t.least;
   const float scale = cfg->sm_scale == 0.f ? 1.f / std::sqrt((float)cfg->head_dim) : cfg->sm_scale;
   p.scale2 = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -36,7 +36,7 @@ struct TreeParams {
   float* part_acc;             // [splits][B,Hkv,M][D]
   int N, B, H, Hkv, G, M, cap, n_live;
   int splits, split_cols;      // columns of a run (a multiple of the kernel's tile); the last run also has the drafts
-  int row_blocks, blocks, least;   // tcgen05 kernel: jobs per KV head, blocks, fewest tiles of a block's run
+  int group, row_rounds, least;    // tcgen05 kernel: blocks side by side, rounds of their rows per KV head, fewest tiles of a run
   void* cuts;                  // tcgen05 kernel: one TreeTcCut per block
   int tiled, q_tiled;          // tcgen05 kernel: there are tensor maps of a bf16 state, of q
   float scale2;                // scale * log2(e)

@@ -2,10 +2,12 @@
 // bf16 queries, more than 64 rows of the product (nodes x query heads of a KV head).
 //
 // Work.  A job is up to NT x 128 rows of one KV head of one sequence against all their columns, in tiles of 128; the
-// drafts are its last tiles.  The tiles of all jobs, one behind the other, are dealt out evenly: every block (as many as fit
-// the GPU at a time) takes a run of `share` tiles and walks through the jobs in it.  A job that lies in one run is written
-// out; one cut by the end of a run leaves (reference, sum, weighted sum) of its pieces in the workspace, at most two a
-// block, and a second kernel joins them.  So lengths that differ cost nobody idle time, and hardly any job is cut.
+// drafts are its last tiles.  More rows than that are other jobs over the same columns: as many blocks as there are such
+// jobs form a group and walk side by side, so that what one reads the others find in L2.  The tiles of all (sequence, KV
+// head) pairs, one behind the other, are dealt out evenly to the groups (as many as fit the GPU at a time): each takes a
+// run of `share` tiles and walks through the pairs in it.  A job that lies in one run is written out; one cut by the end of
+// a run leaves (reference, sum, weighted sum) of its pieces in the workspace, at most two a block, and a second kernel joins
+// them.  So lengths that differ cost nobody idle time, and hardly any job is cut.
 //
 // Roles in a block.  They meet through mbarriers only and run ahead of one another across jobs: while the rows of one job
 // are written out, the next one's Q, K and V are on their way and its first logits computed.
@@ -14,10 +16,10 @@
 //                       could not keep up; values of rows behind a sequence's last are zeroed when they have landed,
 //                       whatever lies there); 8-bit states from a raw ring, with an exact conversion (see
 //                       tova_tree_mma.cuh); drafts by plain loads that take out infinities and NaN.
-//   1 issuing thread    S = Q K^T (128 x 128, fp32 in TMEM) and O += P V in the order PV_0(i) S_0(i+1) PV_1(i) S_1(i+1):
-//                       the tensor cores work on one row tile while the other's soft-max runs (two row tiles in a block,
-//                       or two blocks on an SM); 8-bit states: one row tile a block and SM, two S buffers, S of the next
-//                       tile ahead of O += P V of this one - the conversion needs eight warps, and registers
+//   1 issuing thread    S = Q K^T (128 x 128, fp32 in TMEM) and O += P V.  Two row tiles (more than 128 rows of a bf16 state)
+//                       fill the tensor memory, 256 columns each (S, O); their contractions take turns, PV_0(i) S_0(i+1)
+//                       PV_1(i) S_1(i+1), so that one's run while the other's soft-max does.  One row tile has room for a
+//                       second S: the next tile's logits are computed ahead of O += P V of this one.
 //   1 copying thread    (8-bit states) bulk copies into the raw ring: a producer that had to wait for all of them to be done
 //                       with a raw slot before it could ask for the next copy would hold up its own conversions
 //   1 helper warp       ancestor bits of the next job's drafts, and whether one of their values is not finite
@@ -45,13 +47,12 @@ struct TreeTcShape {
   static constexpr bool PLAIN = FMT == FORMAT_PLAIN;
   static constexpr int SOFT_WARPS = 8 * NT;
   static constexpr int PRODUCER_WARPS = PLAIN ? 2 : 8;
-  static constexpr bool DOUBLE = !PLAIN;                           // two S buffers
-  static_assert(PLAIN || NT == 1, "an 8-bit state's second S buffer takes the second row tile's tensor memory");
+  static constexpr bool DOUBLE = NT == 1;                          // two S buffers
+  static_assert(PLAIN || NT == 1, "an 8-bit state's conversion takes eight warps and their registers: one row tile");
   static constexpr int THREADS = 32 * (SOFT_WARPS + PRODUCER_WARPS + (PLAIN ? 2 : 3));
-  static constexpr int BLOCKS = PLAIN && NT == 1 ? 2 : 1;          // per SM
   static constexpr int Q_BYTES = TREE_TC_ROWS * D * 2;             // per row tile
   static constexpr int SLOT = TREE_TC_COLS * D * 2;
-  static constexpr int SLOTS = (PLAIN && NT == 1 ? 2 : 4) * (128 / D);
+  static constexpr int SLOTS = (PLAIN && NT == 1 ? 5 : 4) * (128 / D);
   static constexpr int RAW = PLAIN ? 0 : TREE_TC_COLS * D;
   static constexpr int RAW_SLOTS = PLAIN ? 0 : 3 * (128 / D);
   // Tiles whose scales are kept.  K of tile i takes the slot of a copy SLOTS positions back; when that has been consumed,
@@ -61,8 +62,7 @@ struct TreeTcShape {
   static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + RAW_SLOTS * RAW + SCALES + 1024;
   static constexpr int TMEM_COLS = DOUBLE ? 512 : 256 * NT;
   static constexpr int BUFFERS = DOUBLE ? 2 : NT;                  // S buffers (and barriers for them)
-  static constexpr int NODES = BLOCKS == 2 ? TREE_TC_ROWS : TREE_MAX_NODES;   // (taken for M <= 128 only, so N <= 128)
-  static constexpr int WORDS = NODES / 32;
+  static constexpr int NODES = TREE_MAX_NODES, WORDS = TREE_ANC_WORDS;
 };
 
 // --- how the work is dealt out -----------------------------------------------------------------------------------
@@ -70,9 +70,9 @@ struct TreeTcShape {
 __device__ __forceinline__ int tree_tc_tiles(const TreeParams& p, int b) {
   return (tree_len(p, b) + TREE_TC_COLS - 1) / TREE_TC_COLS + (p.N + TREE_TC_COLS - 1) / TREE_TC_COLS;
 }
-// Tiles a block takes: an even share of all, but no fewer than `least`.
-__device__ __forceinline__ long long tree_tc_share(long long total, int blocks, int least) {
-  const long long even = (total + blocks - 1) / blocks;
+// Tiles a group takes: an even share of all, but no fewer than `least`.
+__device__ __forceinline__ long long tree_tc_share(long long total, int groups, int least) {
+  const long long even = (total + groups - 1) / groups;
   return even > least ? even : least;
 }
 
@@ -92,7 +92,7 @@ struct TreeTcRun {
 
   __device__ __forceinline__ bool next(const TreeParams& p, int block) {
     if (at >= end) return false;
-    const int jobs = p.Hkv * p.row_blocks;        // of a sequence
+    const int jobs = p.Hkv * p.row_rounds;        // of a sequence, for this block
     while (at >= base + (long long)tiles * jobs) {
       base += (long long)tiles * jobs;
       ++b;
@@ -102,8 +102,8 @@ struct TreeTcRun {
     const int job = (int)(r / tiles);
     i0 = (int)(r - (long long)job * tiles);
     i1 = (int)min((long long)tiles, i0 + (end - at));
-    hk = job / p.row_blocks;
-    rb = job - hk * p.row_blocks;
+    hk = job / p.row_rounds;
+    rb = (job - hk * p.row_rounds) * p.group + block % p.group;
     len = tree_len(p, b);
     n_state = (len + TREE_TC_COLS - 1) / TREE_TC_COLS;
     last = i1 == tiles;
@@ -151,7 +151,7 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
 }
 
 template <int D, int FMT, int NT>
-__global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<D, FMT, NT>::BLOCKS)
+__global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
     tova_tree_tc_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap map_k,
                         const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q) {
   using S = TreeTcShape<D, FMT, NT>;
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
   }
   if (warp == HELPER) {
     // The block's run: all tiles, its share of them, and the sequence that the share starts in.
-    const int jobs = p.Hkv * p.row_blocks;
+    const int jobs = p.Hkv * p.row_rounds;
     TreeTcRun r;
     long long total;
     if (p.lens) {
@@ -226,8 +226,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
     } else {
       total = (long long)tree_tc_tiles(p, 0) * jobs * p.B;
     }
-    const long long share = tree_tc_share(total, gridDim.x, p.least);
-    r.at = min(total, blockIdx.x * share);
+    const long long share = tree_tc_share(total, gridDim.x / p.group, p.least);
+    r.at = min(total, blockIdx.x / p.group * share);
     r.end = min(total, r.at + share);
     r.base = 0;
     r.b = 0;
@@ -332,7 +332,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
         const int j0 = (run.i0 + x / 2 - run.n_state) * C;
         const int row_q = pt / QCH, ch = pt % QCH;
         const __nv_bfloat16* at = from + (((long long)j0 * p.B + run.b) * p.Hkv + run.hk) * D + ch * 8;
-        constexpr int BATCH = 8;                           // loads in flight per thread
+        constexpr int BATCH = C / QSTEP < 8 ? C / QSTEP : 8;     // loads in flight per thread
+        static_assert(C % (BATCH * QSTEP) == 0, "the batches end with the tile");
         for (int k = 0; k < C / QSTEP; k += BATCH) {
           uint4 w[BATCH];
 #pragma unroll
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, TreeTcShape<
     while (run.next(p, blockIdx.x)) {
       if (run.i0 == 0 && !run.last) {
         const long long first_tile = run.at - run.i1;
-        cut.pieces = (int)((first_tile + run.tiles - 1) / share) - (int)blockIdx.x + 1;
+        cut.pieces = (int)((first_tile + run.tiles - 1) / share) - (int)blockIdx.x / p.group + 1;
         cut.b = run.b;
         cut.hk = run.hk;
         cut.rb = run.rb;
@@ -815,8 +816,8 @@ __global__ void __launch_bounds__(TREE_TC_JOIN_THREADS) tova_tree_tc_join_kernel
   const TreeTcCut cut = static_cast<const TreeTcCut*>(p.cuts)[blockIdx.x];
   const int m = cut.rb * ROWS + r;
   if (cut.pieces == 0 || m >= p.M) return;
-  // The pieces behind the first are the first ones of the blocks that follow.
-  auto part_row = [&](int c) { return (long long)(c == 0 ? cut.part : 2 * ((int)blockIdx.x + c)) * ROWS + r; };
+  // The pieces behind the first are the first ones of the blocks that follow, group by group.
+  auto part_row = [&](int c) { return (long long)(c == 0 ? cut.part : 2 * ((int)blockIdx.x + c * p.group)) * ROWS + r; };
   const int c0 = 0, c1 = cut.pieces - 1, b = cut.b, hk = cut.hk;
   float top = -INFINITY;
   bool pad = false;
