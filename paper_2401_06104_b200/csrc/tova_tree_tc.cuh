@@ -62,6 +62,10 @@ struct TreeTcShape {
   static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + RAW_SLOTS * RAW + SCALES + 1024;
   static constexpr int TMEM_COLS = DOUBLE ? 512 : 256 * NT;
   static constexpr int BUFFERS = DOUBLE ? 2 : NT;                  // S buffers (and barriers for them)
+  // Trimmed tiles lie at least four ring positions apart (a job's last V, its drafts' K and V, the next job's K and V), and
+  // no producer is more than SLOTS positions ahead of another: with this many barriers none can come round to one that
+  // another still waits on.
+  static constexpr int TRIMS = SLOTS / 4 + 2;
   static constexpr int NODES = TREE_MAX_NODES, WORDS = TREE_ANC_WORDS;
 };
 
@@ -170,7 +174,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
   // Q landed, Q free again, S computed, weights written, O complete, (two S buffers) a tile's O += P V
   // complete, ancestor bits there, ancestor bits free again, the
   // two warps of 32 rows meet, a tile that has to be trimmed landed
-  __shared__ __align__(8) uint64_t bar_q, bar_qf, bar_s[S::BUFFERS], bar_p[S::BUFFERS], bar_o[NT], bar_v, bar_a, bar_af, bar_pair[NT * 4], bar_trim;
+  __shared__ __align__(8) uint64_t bar_q, bar_qf, bar_s[S::BUFFERS], bar_p[S::BUFFERS], bar_o[NT], bar_v, bar_a, bar_af, bar_pair[NT * 4], bar_trim[S::TRIMS];
   __shared__ uint32_t tmem_base_s;
   __shared__ int odd_s;                                    // some draft's value is not finite
   __shared__ TreeTcRun run_s, soft_run_s[S::SOFT_WARPS];   // (the soft-max warps' registers are for the rows)
@@ -191,7 +195,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
       mbar_init(&raw_empty[i], S::PRODUCER_WARPS);
     }
     mbar_init(&bar_q, S::PRODUCER_WARPS);
-    mbar_init(&bar_trim, 1);
+    for (int i = 0; i < S::TRIMS; ++i) mbar_init(&bar_trim[i], 1);
     mbar_init(&bar_qf, 1);
     for (int t = 0; t < S::BUFFERS; ++t) {
       mbar_init(&bar_s[t], 1);
@@ -362,7 +366,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
             // Rows behind the sequence's last come along: of K they give logits that are masked, of V they must be zeros.
             const int valid = run.len - tile * C;
             const bool trim = (x & 1) && valid < C;
-            uint64_t* bar = trim ? &bar_trim : &full[pos % S::SLOTS];
+            uint64_t* bar = trim ? &bar_trim[trims % S::TRIMS] : &full[pos % S::SLOTS];
             if (pt == 0) {
               const int y = bh * p.cap + tile * C;
               mbar_expect_tx(bar, S::SLOT);
@@ -370,7 +374,7 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
               for (int c = 0; c < D / 64; ++c) tma_load_2d_tile(dst + c * (C * 128), (x & 1) ? &map_v : &map_k, c * 64, y, bar);
             }
             if (trim) {
-              ok = mbar_wait_bounded(&bar_trim, trims & 1u);
+              ok = mbar_wait_bounded(bar, (trims / S::TRIMS) & 1u);
               ++trims;
               if (!ok) break;
               for (int e = valid * QCH + pt; e < C * QCH; e += PT)

@@ -420,6 +420,51 @@ def test_tree_chain_over_a_long_state(dtype, N, lens):
     run_tree(dtype, "plain", N, 1, 8, 2, 128, lens, lens[0], None, seed=N, gain=2.0)
 
 
+@pytest.mark.parametrize("fmt", ["plain", "int8", "e4m3"])
+@pytest.mark.parametrize("D, N, H, Hkv", [(128, 20, 8, 2), (64, 20, 8, 2), (128, 40, 8, 2), (64, 150, 4, 2), (128, 25, 6, 2), (64, 30, 12, 4)])
+def test_tree_many_short_sequences(fmt, D, N, H, Hkv):
+    """More than 64 rows of the product over many sequences of a tile or two: a block walks through many jobs, most of
+    them ending inside a tile, some empty, some cut by the end of its run; query groups that do not divide 128 too."""
+    B = 41
+    g = torch.Generator().manual_seed(N)
+    lens = [int(x) for x in torch.randint(0, 300, (B,), generator=g)]
+    lens[3], lens[4], lens[5], lens[6] = 0, 128, 256, 1
+    run_tree("bf16", fmt, N, B, H, Hkv, D, lens, 301, random_parents(N, B, N), seed=N)
+
+
+@pytest.mark.parametrize("fmt", ["plain", "int8"])
+@pytest.mark.parametrize("N, H", [(3, 4096), (16, 4096), (2, 1000)])
+def test_tree_more_rows_than_the_gpu_has_blocks_for(fmt, N, H):
+    """One KV head under thousands of query heads: more row blocks than SMs, groups larger than a row tile."""
+    run_tree("bf16", fmt, N, 1, H, 1, 64, [70], 80, random_parents(N, 1, N), seed=N)
+
+
+@pytest.mark.parametrize("dtype, fmt, N", [("bf16", "plain", 4), ("bf16", "plain", 24), ("bf16", "plain", 50), ("bf16", "int8", 50), ("fp32", "plain", 5)])
+def test_tree_logits_that_grow_along_the_state(dtype, fmt, N):
+    """Later columns outweigh earlier ones by far more than any slack in the running reference: keys grow along the state."""
+    g = gen(N)
+    B, H, Hkv, D, L = 1, 8, 2, 128, 1500
+    t = TT[dtype]
+    q, k, v = (randn(g, N, B, n, D).to(t) for n in (H, Hkv, Hkv))
+    grow = torch.linspace(0.01, 60.0, L, device=DEV)[None, None, :, None]
+    Kf, Vf = randn(g, B, Hkv, L, D) * grow, randn(g, B, Hkv, L, D)
+    ks = vs = None
+    if fmt == "plain":
+        K, V = Kf.to(t), Vf.to(t)
+        Kd, Vd = K.double(), V.double()
+    else:
+        (K, V), (ks, vs) = new_state(B, Hkv, L, D, fmt)
+        tova.tova_quant_write(tova.tova_quant_config(B, Hkv, D, L, tova.TOVA_DTYPE_FP32, FMT[fmt]), Kf.permute(2, 0, 1, 3).contiguous(),
+                              Vf.permute(2, 0, 1, 3).contiguous(), L, K, ks, V, vs)
+        Kd, Vd = codes_as_floats(K, fmt).double() * ks.double()[..., None], codes_as_floats(V, fmt).double() * vs.double()[..., None]
+    cfg = tova.tova_tree_config(B, H, Hkv, D, L, TD[dtype], FMT[fmt], 0.0)
+    ws = torch.empty(max(16, tova.tova_tree_workspace_bytes(cfg, L, N)), dtype=torch.uint8, device=DEV)
+    out = torch.empty(N, B, H, D, dtype=t, device=DEV)
+    tova.tova_tree_attention(cfg, K, V, L, q, k, v, N, out, ws, k_scale=ks, v_scale=vs)
+    want, wv, reach, _ = tree_reference(q, k, v, Kd, Vd, [L], None)
+    assert bool(((out.double() - want).abs() <= tree_tolerance(dtype, D, L + N, want, wv, reach)).all())
+
+
 def test_tree_scale_and_live_bound():
     """A scale of the caller's; n_live above every length (the launch is cut for it, the lengths decide)."""
     run_tree("bf16", "plain", 7, 2, 8, 2, 64, [40, 0], 3000, random_parents(7, 2, 1), sm_scale=0.31, n_live=3000)
