@@ -255,7 +255,8 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
     }
   };
   // Two neighbouring weights as operand elements, times the columns' value scales f (8-bit states); added to the running
-  // sum as rounded.  (The sum is this thread's; a row's four threads add up at the end.)
+  // sum as rounded, the scales' reciprocals r taken out again; where those would leave fp32's range (a row of zeros, or one
+  // written with hardly more), as it was.  (The sum is this thread's; a row's four threads add up at the end.)
   auto weight2 = [&](float w0, float w1, float f0, float f1, float r0, float r1, float& sum) -> uint32_t {
     if constexpr (PLAIN) {
       const uint32_t u = pack_bf16(w0, w1);
@@ -263,7 +264,8 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
       return u;
     } else {
       const uint32_t u = pack_bf16(w0 * f0, w1 * f1);
-      sum += (f0 != 0.f ? __uint_as_float(u << 16) * r0 : w0) + (f1 != 0.f ? __uint_as_float(u & 0xffff0000u) * r1 : w1);
+      sum += (fabsf(f0) >= 0x1p-100f ? __uint_as_float(u << 16) * r0 : w0) +
+             (fabsf(f1) >= 0x1p-100f ? __uint_as_float(u & 0xffff0000u) * r1 : w1);
       return u;
     }
   };

@@ -465,6 +465,30 @@ def test_tree_logits_that_grow_along_the_state(dtype, fmt, N):
     assert bool(((out.double() - want).abs() <= tree_tolerance(dtype, D, L + N, want, wv, reach)).all())
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype, N", [("bf16", 3), ("bf16", 12), ("bf16", 50), ("fp32", 3), ("fp32", 12)])
+def test_tree_value_scales_of_any_size(dtype, fmt, N):
+    """Value scales from zero and below the normal numbers up to 2^60, each row's its own, under codes that are not zero."""
+    g = gen(N)
+    B, H, Hkv, D, L = 2, 8, 2, 128, 330
+    t = TT[dtype]
+    q, k, v = (randn(g, N, B, n, D).to(t) for n in (H, Hkv, Hkv))
+    (K, V), (ks, vs) = new_state(B, Hkv, L, D, fmt)
+    Kf, Vf = randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+    tova.tova_quant_write(tova.tova_quant_config(B, Hkv, D, L, tova.TOVA_DTYPE_FP32, FMT[fmt]), Kf, Vf, L, K, ks, V, vs)
+    sizes = torch.tensor([0.0, 2.0 ** -140, 2.0 ** -126, 2.0 ** -101, 2.0 ** -90, 2.0 ** -20, 2.0 ** -6, -2.0 ** -7], device=DEV)
+    vs.copy_(sizes[torch.arange(L, device=DEV) % 8].expand(B, Hkv, L))
+    vs[1, :, 77] = 2.0 ** 60
+    Kd, Vd = codes_as_floats(K, fmt).double() * ks.double()[..., None], codes_as_floats(V, fmt).double() * vs.double()[..., None]
+    cfg = tova.tova_tree_config(B, H, Hkv, D, L, TD[dtype], FMT[fmt], 0.0)
+    ws = torch.empty(max(16, tova.tova_tree_workspace_bytes(cfg, L, N)), dtype=torch.uint8, device=DEV)
+    out = torch.empty(N, B, H, D, dtype=t, device=DEV)
+    par = random_parents(N, B, N)
+    tova.tova_tree_attention(cfg, K, V, L, q, k, v, N, out, ws, parents=par, k_scale=ks, v_scale=vs)
+    want, wv, reach, _ = tree_reference(q, k, v, Kd, Vd, [L] * B, par.cpu())
+    assert bool(((out.double() - want).abs() <= tree_tolerance(dtype, D, L + N, want, wv, reach)).all())
+
+
 def test_tree_scale_and_live_bound():
     """A scale of the caller's; n_live above every length (the launch is cut for it, the lengths decide)."""
     run_tree("bf16", "plain", 7, 2, 8, 2, 64, [40, 0], 3000, random_parents(7, 2, 1), sm_scale=0.31, n_live=3000)
