@@ -122,29 +122,36 @@ __device__ __forceinline__ void tree_store4<__nv_bfloat16>(__nv_bfloat16* dst, f
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Plain-ALU kernel: every product in fp32.  Serves fp32 queries, whose results the tensor cores' bf16 operands could
-// not give.  A block takes 32 rows of the product and a run of columns in tiles of 32: logits with 2 x 4 outputs a
-// thread, the weighted sum with 8 rows x (D/32) columns a thread... both from shared memory in fp32.
-// grid = (ceil(M / 32), splits, B * Hkv).
+// Plain-ALU kernel: every product in fp32.  Serves fp32 queries, whose results the tensor cores' bf16 operands could not
+// give (three bf16 terms a factor would take six contractions, as long as this).  A block takes R rows of the product (64,
+// or 16 where there are no more) and a run of columns in tiles of 32, all in shared memory as fp32.  Bound by the FMA pipes as
+// long as a thread does enough with what it reads: 4 x 4 logits from eight 16-byte reads (64 FMA), the weighted sum in 8 rows
+// x 8 components from four (64 FMA; the weights lie transposed); with 2 x 4 and 8 x 4 it was bound by shared memory, at a
+// third of that.  grid = (ceil(M / R), splits, B * Hkv).
 constexpr int TREE_ALU_THREADS = 128;
-constexpr int TREE_ALU_ROWS = 32;
 constexpr int TREE_ALU_COLS = 32;
 
-template <int D>
+template <int D, int R>
 inline size_t tree_alu_smem_bytes() {
-  return sizeof(float) * (2 * TREE_ALU_ROWS * (D + 4) + TREE_ALU_COLS * D + TREE_ALU_ROWS * (TREE_ALU_COLS + 4));
+  return sizeof(float) * (R * (D + 4) + TREE_ALU_COLS * (2 * D + 4) + TREE_ALU_COLS * (R + 4));
 }
 
-template <typename T, int D, int FMT>
+template <typename T, int D, int FMT, int R>
 __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const __grid_constant__ TreeParams p) {
-  constexpr int R = TREE_ALU_ROWS, C = TREE_ALU_COLS;
+  constexpr int C = TREE_ALU_COLS, TH = TREE_ALU_THREADS;
   constexpr int LD = D + 4;                      // row stride of Q and K in shared memory: rows 4 banks apart
-  constexpr int LP = C + 4;
+  constexpr int LP = R + 4;                      // ... of the weights, a column's R rows
+  constexpr int QR = R == 64 ? 4 : 2, QC = R == 64 ? 4 : 2;     // logits of a thread
+  constexpr int CG = C / QC;                                    // threads of a row: neighbouring lanes
+  constexpr int PR = R == 64 ? 8 : 4;                           // weighted sum of a thread: PR rows x PC components
+  constexpr int XG = TH / (R / PR), PC = D / XG;
+  constexpr int PV = PC < 4 ? PC : 4;                           // ... in pieces of PV neighbours, XG * PV apart
+  static_assert(CG * (R / QR) == TH && XG * (R / PR) == TH, "every thread has a share");
   extern __shared__ __align__(16) float tree_alu_smem[];
   float* q_s = tree_alu_smem;                    // [R][LD]
   float* k_s = q_s + R * LD;                     // [C][LD]
   float* v_s = k_s + C * LD;                     // [C][D]
-  float* p_s = v_s + C * D;                      // [R][LP]
+  float* p_s = v_s + C * D;                      // [C][LP]
   __shared__ int par_s[TREE_MAX_NODES];
   __shared__ uint32_t anc_s[TREE_MAX_NODES][TREE_ANC_WORDS];
   __shared__ float m_s[R], corr_s[R];
@@ -160,38 +167,39 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
   const int n_draft = last ? (p.N + C - 1) / C : 0;
 
   if (last) {
-    for (int i = tid; i < p.N; i += TREE_ALU_THREADS) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
+    for (int i = tid; i < p.N; i += TH) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
     __syncthreads();
-    for (int i = tid; i < p.N; i += TREE_ALU_THREADS) tree_ancestor_bits<TREE_ANC_WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
+    for (int i = tid; i < p.N; i += TH) tree_ancestor_bits<TREE_ANC_WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
   }
   // Q rows, scaled into the base-2 domain
-  for (int i = tid; i < R * (D / 4); i += TREE_ALU_THREADS) {
+  for (int i = tid; i < R * (D / 4); i += TH) {
     const int r = i / (D / 4), d = (i % (D / 4)) * 4;
     const int m = row0 + r;
     float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
     if (m < p.M) {
       const int n = m / p.G, g = m - n * p.G;
-      const T* src = static_cast<const T*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
-      w = tree_load4(src);
+      w = tree_load4(static_cast<const T*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d);
     }
     *reinterpret_cast<float4*>(q_s + r * LD + d) = make_float4(w.x * p.scale2, w.y * p.scale2, w.z * p.scale2, w.w * p.scale2);
   }
-  // logits: thread -> rows 2 (tid / 8), +1; columns tid % 8 + 8 k.  Weighted sum: rows 8 (tid / 32) ..+7, D/32 columns.
-  const int lr = (tid >> 3) * 2, lc = tid & 7;
-  const int orow = (tid >> 5) * 8, oc = (tid & 31) * (D / 32);
-  float acc[8][D / 32];
+  const int lr = (tid / CG) * QR, lc = tid % CG;         // logits: rows lr.., columns lc + CG k
+  const int orow = (tid / XG) * PR, ox = (tid % XG) * PV; // weighted sum: rows orow.., components ox + XG PV j + 0..PV-1
+  float acc[PR][PC];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < PR; ++i)
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) acc[i][j] = 0.f;
-  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+    for (int j = 0; j < PC; ++j) acc[i][j] = 0.f;
+  float m_run[QR], l_run[QR];
+#pragma unroll
+  for (int i = 0; i < QR; ++i) { m_run[i] = -INFINITY; l_run[i] = 0.f; }
 
   for (int tile = 0; tile < n_state + n_draft; ++tile) {
     const bool draft = tile >= n_state;
     const int j0 = draft ? (tile - n_state) * C : c0 + tile * C;      // first column of the tile, in its own numbering
     const int jn = draft ? p.N : c1;
     __syncthreads();
-    for (int i = tid; i < C * (D / 4); i += TREE_ALU_THREADS) {
+#pragma unroll 4
+    for (int i = tid; i < C * (D / 4); i += TH) {
       const int r = i / (D / 4), d = (i % (D / 4)) * 4;
       const int j = j0 + r;
       float4 kf = make_float4(0.f, 0.f, 0.f, 0.f), vf = kf;
@@ -199,10 +207,8 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
         if (draft || FMT == FORMAT_PLAIN) {
           const long long at = draft ? (((long long)j * p.B + b) * p.Hkv + hk) * D + d
                                      : ((long long)blockIdx.z * p.cap + j) * D + d;
-          const T* kp = static_cast<const T*>(draft ? p.k_new : p.K) + at;
-          const T* vp = static_cast<const T*>(draft ? p.v_new : p.V) + at;
-          kf = tree_load4(kp);
-          vf = tree_load4(vp);
+          kf = tree_load4(static_cast<const T*>(draft ? p.k_new : p.K) + at);
+          vf = tree_load4(static_cast<const T*>(draft ? p.v_new : p.V) + at);
         } else if constexpr (FMT != FORMAT_PLAIN) {
           const long long row = (long long)blockIdx.z * p.cap + j;
           float a[4];
@@ -217,86 +223,113 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
       *reinterpret_cast<float4*>(v_s + r * D + d) = vf;
     }
     __syncthreads();
-    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    float s[QR][QC];
+#pragma unroll
+    for (int i = 0; i < QR; ++i)
+#pragma unroll
+      for (int k = 0; k < QC; ++k) s[i][k] = 0.f;
 #pragma unroll 4
     for (int d = 0; d < D; d += 4) {
-      const float4 q0 = *reinterpret_cast<const float4*>(q_s + lr * LD + d);
-      const float4 q1 = *reinterpret_cast<const float4*>(q_s + (lr + 1) * LD + d);
+      float4 q[QR];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float4 kk = *reinterpret_cast<const float4*>(k_s + (lc + 8 * k) * LD + d);
-        s[0][k] = fmaf(q0.x, kk.x, fmaf(q0.y, kk.y, fmaf(q0.z, kk.z, fmaf(q0.w, kk.w, s[0][k]))));
-        s[1][k] = fmaf(q1.x, kk.x, fmaf(q1.y, kk.y, fmaf(q1.z, kk.z, fmaf(q1.w, kk.w, s[1][k]))));
+      for (int i = 0; i < QR; ++i) q[i] = *reinterpret_cast<const float4*>(q_s + (lr + i) * LD + d);
+#pragma unroll
+      for (int k = 0; k < QC; ++k) {
+        const float4 kk = *reinterpret_cast<const float4*>(k_s + (lc + CG * k) * LD + d);
+#pragma unroll
+        for (int i = 0; i < QR; ++i)
+          s[i][k] = fmaf(q[i].x, kk.x, fmaf(q[i].y, kk.y, fmaf(q[i].z, kk.z, fmaf(q[i].w, kk.w, s[i][k]))));
       }
     }
+    float e[QC][QR];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < QR; ++i) {
       const int m = row0 + lr + i;
       const uint32_t see = draft ? (m < p.M ? anc_s[m / p.G][j0 >> 5] : 0u) : 0u;
       float top = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = lc + 8 * k;
+      for (int k = 0; k < QC; ++k) {
+        const int c = lc + CG * k;
         const bool vis = draft ? ((see >> c) & 1u) != 0 : j0 + c < jn;
         if (!vis) s[i][k] = -INFINITY;
         top = fmaxf(top, s[i][k]);
       }
 #pragma unroll
-      for (int o = 4; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int o = CG / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       const float m_new = fmaxf(m_run[i], top);
       const float base = m_new == -INFINITY ? 0.f : m_new;
       const float corr = exp2f(m_run[i] - base);       // 0 while nothing has been seen
       float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float e = exp2f(s[i][k] - base);
-        sum += e;
-        p_s[(lr + i) * LP + lc + 8 * k] = e;
+      for (int k = 0; k < QC; ++k) {
+        e[k][i] = exp2f(s[i][k] - base);
+        sum += e[k][i];
       }
 #pragma unroll
-      for (int o = 4; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      for (int o = CG / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       l_run[i] = l_run[i] * corr + sum;
       m_run[i] = m_new;
       if (lc == 0) corr_s[lr + i] = corr;
     }
+#pragma unroll
+    for (int k = 0; k < QC; ++k) {
+      float* dst = p_s + (lc + CG * k) * LP + lr;
+      if constexpr (QR == 4) *reinterpret_cast<float4*>(dst) = make_float4(e[k][0], e[k][1], e[k][2], e[k][3]);
+      else *reinterpret_cast<float2*>(dst) = make_float2(e[k][0], e[k][1]);
+    }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < PR; ++i) {
       const float corr = corr_s[orow + i];
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) acc[i][j] *= corr;
+      for (int j = 0; j < PC; ++j) acc[i][j] *= corr;
     }
-    if (!draft) {
-#pragma unroll 4
-      for (int c = 0; c < C; ++c) {
-        float v[D / 32];
+    auto column = [&](int c, float (&w)[PR], float (&v)[PC]) {
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) v[j] = v_s[c * D + oc + j];
+      for (int i = 0; i < PR; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(p_s + c * LP + orow + i);
+        w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
+      }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float w = p_s[(orow + i) * LP + c];
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) acc[i][j] = fmaf(w, v[j], acc[i][j]);
+      for (int j = 0; j < PC; j += PV) {
+        const float* src = v_s + c * D + ox + XG * j;
+        if constexpr (PV == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(src);
+          v[j] = x.x; v[j + 1] = x.y; v[j + 2] = x.z; v[j + 3] = x.w;
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(src);
+          v[j] = x.x; v[j + 1] = x.y;
         }
+      }
+    };
+    if (!draft) {
+#pragma unroll 2
+      for (int c = 0; c < C; ++c) {
+        float w[PR], v[PC];
+        column(c, w, v);
+#pragma unroll
+        for (int i = 0; i < PR; ++i)
+#pragma unroll
+          for (int j = 0; j < PC; ++j) acc[i][j] = fmaf(w[i], v[j], acc[i][j]);
       }
     } else {
       // Drafts that a row does not see may hold anything: 0 times an infinity must not reach the sum.
       for (int c = 0; c < C; ++c) {
+        float w[PR], v[PC];
+        column(c, w, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float w = p_s[(orow + i) * LP + c];
-          if (w != 0.f) {
+        for (int i = 0; i < PR; ++i)
+          if (w[i] != 0.f) {
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) acc[i][j] = fmaf(w, v_s[c * D + oc + j], acc[i][j]);
+            for (int j = 0; j < PC; ++j) acc[i][j] = fmaf(w[i], v[j], acc[i][j]);
           }
-        }
       }
     }
   }
   __syncthreads();
   if (lc == 0) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < QR; ++i) {
       const int m = row0 + lr + i;
       float l = l_run[i];
       if (last && m < p.M) {
@@ -309,21 +342,20 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < PR; ++i) {
     const int m = row0 + orow + i;
     if (m >= p.M) continue;
     const float l = corr_s[orow + i];
-    if (p.splits == 1) {
-      const float r = l == 0.f ? 0.f : 1.f / l;
-      const int n = m / p.G, g = m - n * p.G;
-      T* dst = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + oc;
+    const float r = l == 0.f || l == TREE_PADDING ? 0.f : 1.f / l;
+    const int n = m / p.G, g = m - n * p.G;
+    const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
+    T* out = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D;
+    if (p.splits > 1 && ox == 0) p.part_ml[at] = make_float2(m_s[orow + i], l);
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) dst[j] = (T)(l == TREE_PADDING ? 0.f : acc[i][j] * r);
-    } else {
-      const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
-      if ((tid & 31) == 0) p.part_ml[at] = make_float2(m_s[orow + i], l);
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) p.part_acc[at * D + oc + j] = acc[i][j];
+    for (int j = 0; j < PC; ++j) {
+      const int d = ox + XG * (j / PV * PV) + j % PV;
+      if (p.splits == 1) out[d] = (T)(l == TREE_PADDING ? 0.f : acc[i][j] * r);
+      else p.part_acc[at * D + d] = acc[i][j];
     }
   }
 }
