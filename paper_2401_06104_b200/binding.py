@@ -443,9 +443,9 @@ def _rows(t, n_tokens: int, batch: int, heads: int, dim: int, dtype, device: int
     if t.dtype is not dtype or t.get_device() != device or device < 0:
         _misfit(t, 0, dtype, device)
     T, B, H, D = t.shape
+    s0, s1, s2, s3 = t.stride()
     if T < n_tokens or B != batch or H != heads or D != dim:
         raise ValueError(f"expected [{n_tokens},{batch},{heads},{dim}], got {tuple(t.shape)}")
-    s0, s1, s2, s3 = t.stride()
     if batch == 1:
         s1 = s0 if n_tokens > 1 else heads * dim
     elif n_tokens > 1 and s0 != s1 * batch:
@@ -455,21 +455,25 @@ def _rows(t, n_tokens: int, batch: int, heads: int, dim: int, dtype, device: int
     return s1
 
 
-_raw_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
-    lambda device: torch.cuda.current_stream(device).cuda_stream)
+def _shortcut(name, plain):
+    """torch's own internal form of a call where it has one (a fifth of the time; a small call is as short as its checks)."""
+    return getattr(torch._C, name, plain)
+
+
+_raw_current_stream = _shortcut("_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = _shortcut("_cuda_getDevice", lambda: torch.cuda.current_device())
 
 
 def _call(fn, what: str, device: int, stream, *args) -> None:
     """fn(*args, stream) with `device` current (switched to where it is not already); the stream is the caller's, or the
     current one of that device."""
-    was = torch.cuda.current_device()
-    if was != device:
-        torch.cuda.set_device(device)
-    try:
-        rc = fn(*args, _raw_current_stream(device) if stream is None else stream.cuda_stream)
-    finally:
-        if was != device:
-            torch.cuda.set_device(was)
+    st = _raw_current_stream(device) if stream is None else stream.cuda_stream
+    was = _current_device()
+    if was == device:
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, st)
     if rc != 0:
         raise TovaError(rc, what)
 
