@@ -326,7 +326,7 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     t.least = 4;                 // tiles of 128 columns: less than that does not pay for a block's set-up
     part_rows = (size_t)2 * t.blocks * rows;
   } else {
-    int rows = M <= 16 ? 16 : 64, cols = tova::TREE_ALU_COLS;       // fp32: the plain-ALU kernel
+    int rows = M <= 4 ? 4 : M <= 16 ? 16 : 64, cols = tova::TREE_ALU_COLS;       // fp32: the plain-ALU kernel
     if (c.dtype == TOVA_DTYPE_BF16) {
       t.kernel = M <= 16 ? TREE_MMA_16 : M <= 32 ? TREE_MMA_32 : TREE_MMA_64;
       rows = 64;
@@ -460,10 +460,10 @@ cudaError_t tree_run_tc(const tova::TreeParams& p, const TreePlan& t, cudaStream
   return cudaLaunchKernelEx(&lc, tova::tova_tree_tc_join_kernel<D, NT>, p);
 }
 
-template <typename T, int D, int FMT, int R>
+template <int D, int FMT, int R>
 cudaError_t tree_start_alu(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
   static std::atomic<bool> configured[64];
-  return tree_start(tova::tova_tree_alu_kernel<T, D, FMT, R>, configured, tova::tree_alu_smem_bytes<D, R>(), tova::TREE_ALU_THREADS,
+  return tree_start(tova::tova_tree_alu_kernel<D, FMT, R>, configured, tova::tree_alu_smem_bytes<D, R>(), tova::TREE_ALU_THREADS,
                     tree_grid(p, t), 1, st, p);
 }
 
@@ -471,7 +471,9 @@ template <typename T, int D, int FMT>
 cudaError_t tree_launch(const tova::TreeParams& p, const TreePlan& t, cudaStream_t st) {
   cudaError_t e;
   if constexpr (std::is_same<T, float>::value) {
-    e = p.M <= 16 ? tree_start_alu<T, D, FMT, 16>(p, t, st) : tree_start_alu<T, D, FMT, 64>(p, t, st);
+    e = p.M <= 4    ? tree_start_alu<D, FMT, 4>(p, t, st)
+        : p.M <= 16 ? tree_start_alu<D, FMT, 16>(p, t, st)
+                    : tree_start_alu<D, FMT, 64>(p, t, st);
   } else {
     switch (t.kernel) {
       case TREE_MMA_16: e = tree_start_mma<D, FMT, 1, 1>(p, t, st); break;

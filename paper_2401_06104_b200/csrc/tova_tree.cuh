@@ -82,14 +82,6 @@ __device__ __forceinline__ bool tree_drop_odd(uint4& w) {
   return odd;
 }
 
-// Four consecutive values (aligned to four) as floats.
-__device__ __forceinline__ float4 tree_load4(const float* x) { return *reinterpret_cast<const float4*>(x); }
-__device__ __forceinline__ float4 tree_load4(const __nv_bfloat16* x) {
-  const uint2 w = *reinterpret_cast<const uint2*>(x);
-  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                     __uint_as_float(w.y & 0xffff0000u));
-}
-
 // Adds the values that tree_drop_odd took out, of the drafts whose bits are set, to a row's components d0..d0+E-1 before
 // normalisation: a positive weight times an infinity or NaN is that again.
 template <int WORDS, int E>
@@ -122,12 +114,26 @@ __device__ __forceinline__ void tree_store4<__nv_bfloat16>(__nv_bfloat16* dst, f
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// Copies to shared memory that run on; bytes past src_bytes become zeros.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Plain-ALU kernel: every product in fp32.  Serves fp32 queries, whose results the tensor cores' bf16 operands could not
 // give (three bf16 terms a factor would take six contractions, as long as this).  A block takes R rows of the product (64,
-// or 16 where there are no more) and a run of columns in tiles of 32, all in shared memory as fp32.  Bound by the FMA pipes as
-// long as a thread does enough with what it reads: 4 x 4 logits from eight 16-byte reads (64 FMA), the weighted sum in 8 rows
-// x 8 components from four (64 FMA; the weights lie transposed); with 2 x 4 and 8 x 4 it was bound by shared memory, at a
-// third of that.  grid = (ceil(M / R), splits, B * Hkv).
+// or 16 or 4 where there are no more) and a run of columns in tiles of 32, all in shared memory as fp32.  Bound by shared
+// memory and the FMA pipes together, so a thread does as much as it can with what it reads: 4 x 4 logits from eight 16-byte
+// reads (64 FMA), the weighted sum in 8 rows x 8 components from four (64 FMA; the weights lie transposed).  Keys of the next
+// tile are on their way while the weighted sum runs, values while the logits are formed: each has one buffer, free at just
+// that time.  8-bit codes wait in registers.  Measured (D 128, 8 sequences x 4096 rows, 32 query heads): a single step over 32 KV
+// heads 265 us (4.1 TB/s of state), 64 chained drafts over 8 KV heads 1140 us (30.6 TFLOP/s).  Without the early copies 793 and
+// 1463 us.  grid = (ceil(M / R), splits, B * Hkv).
 constexpr int TREE_ALU_THREADS = 128;
 constexpr int TREE_ALU_COLS = 32;
 
@@ -136,14 +142,14 @@ inline size_t tree_alu_smem_bytes() {
   return sizeof(float) * (R * (D + 4) + TREE_ALU_COLS * (2 * D + 4) + TREE_ALU_COLS * (R + 4));
 }
 
-template <typename T, int D, int FMT, int R>
+template <int D, int FMT, int R>
 __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const __grid_constant__ TreeParams p) {
   constexpr int C = TREE_ALU_COLS, TH = TREE_ALU_THREADS;
   constexpr int LD = D + 4;                      // row stride of Q and K in shared memory: rows 4 banks apart
   constexpr int LP = R + 4;                      // ... of the weights, a column's R rows
-  constexpr int QR = R == 64 ? 4 : 2, QC = R == 64 ? 4 : 2;     // logits of a thread
+  constexpr int QR = R == 64 ? 4 : R == 16 ? 2 : 1, QC = QR;    // logits of a thread
   constexpr int CG = C / QC;                                    // threads of a row: neighbouring lanes
-  constexpr int PR = R == 64 ? 8 : 4;                           // weighted sum of a thread: PR rows x PC components
+  constexpr int PR = R == 64 ? 8 : R == 16 ? 4 : D / 32;        // weighted sum of a thread: PR rows x PC components
   constexpr int XG = TH / (R / PR), PC = D / XG;
   constexpr int PV = PC < 4 ? PC : 4;                           // ... in pieces of PV neighbours, XG * PV apart
   static_assert(CG * (R / QR) == TH && XG * (R / PR) == TH, "every thread has a share");
@@ -166,6 +172,54 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
   const int n_state = c1 > c0 ? (c1 - c0 + C - 1) / C : 0;
   const int n_draft = last ? (p.N + C - 1) / C : 0;
 
+  // One tile's rows of keys (x = 0) or values (1) on their way: 16 bytes of floats go straight to shared memory, codes and
+  // their scales to registers, from where landed() converts them.  Rows past the end: zeros.
+  constexpr int CHUNKS = C * D / 4 / TH;
+  constexpr bool CODES = FMT != FORMAT_PLAIN;
+  uint32_t code[CODES ? CHUNKS : 1];
+  float code_scale[CODES ? CHUNKS : 1];
+  auto fetch = [&](int tile, int x) {
+    const bool draft = tile >= n_state;
+    const int j0 = draft ? (tile - n_state) * C : c0 + tile * C, jn = draft ? p.N : c1;
+    float* dst = x ? v_s : k_s;
+    const int ld = x ? D : LD;
+#pragma unroll
+    for (int u = 0; u < CHUNKS; ++u) {
+      const int i = u * TH + tid, r = i / (D / 4), d = (i % (D / 4)) * 4;
+      const bool in = j0 + r < jn;
+      const int j = in ? j0 + r : j0;          // (a tile has at least one row)
+      if (!CODES || draft) {
+        const float* src = draft ? static_cast<const float*>(x ? p.v_new : p.k_new) + (((long long)j * p.B + b) * p.Hkv + hk) * D + d
+                                 : static_cast<const float*>(x ? p.V : p.K) + ((long long)blockIdx.z * p.cap + j) * D + d;
+        cp_async16(smem_addr(dst + r * ld + d), src, in ? 16 : 0);
+      } else if constexpr (CODES) {
+        const long long row = (long long)blockIdx.z * p.cap + j;
+        code[u] = in ? *reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(x ? p.V : p.K) + row * D + d) : 0u;
+        code_scale[u] = in ? (x ? p.v_scale : p.k_scale)[row] : 0.f;
+      }
+    }
+    cp_async_commit();
+  };
+  auto landed = [&](int tile, int x) {
+    if (CODES && tile < n_state) {
+      float* dst = x ? v_s : k_s;
+      const int ld = x ? D : LD;
+#pragma unroll
+      for (int u = 0; u < CHUNKS; ++u) {
+        const int i = u * TH + tid, r = i / (D / 4), d = (i % (D / 4)) * 4;
+        float a[4];
+        if constexpr (CODES) {
+          quant_unpack4<FMT>(code[u], a);
+          const float f = code_scale[u];
+          *reinterpret_cast<float4*>(dst + r * ld + d) = make_float4(a[0] * f, a[1] * f, a[2] * f, a[3] * f);
+        }
+      }
+    }
+    cp_async_wait<0>();
+    __syncthreads();
+  };
+  if (n_state + n_draft > 0) fetch(0, 0);
+
   if (last) {
     for (int i = tid; i < p.N; i += TH) par_s[i] = p.parents ? p.parents[(long long)i * p.B + b] : i - 1;
     __syncthreads();
@@ -178,12 +232,14 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
     float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
     if (m < p.M) {
       const int n = m / p.G, g = m - n * p.G;
-      w = tree_load4(static_cast<const T*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d);
+      w = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d);
     }
     *reinterpret_cast<float4*>(q_s + r * LD + d) = make_float4(w.x * p.scale2, w.y * p.scale2, w.z * p.scale2, w.w * p.scale2);
   }
   const int lr = (tid / CG) * QR, lc = tid % CG;         // logits: rows lr.., columns lc + CG k
   const int orow = (tid / XG) * PR, ox = (tid % XG) * PV; // weighted sum: rows orow.., components ox + XG PV j + 0..PV-1
+  // Warps whose rows all lie behind the last have nothing to do (129 rows are two blocks and a warp); what they hold is not used.
+  const bool has_logits = row0 + (tid & ~31) / CG * QR < p.M, has_sums = row0 + (tid & ~31) / XG * PR < p.M;
   float acc[PR][PC];
 #pragma unroll
   for (int i = 0; i < PR; ++i)
@@ -197,87 +253,68 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
     const bool draft = tile >= n_state;
     const int j0 = draft ? (tile - n_state) * C : c0 + tile * C;      // first column of the tile, in its own numbering
     const int jn = draft ? p.N : c1;
-    __syncthreads();
+    landed(tile, 0);            // (and every thread has done with the values and weights of the last tile)
+    fetch(tile, 1);
+    if (has_logits) {
+      float s[QR][QC];
+#pragma unroll
+      for (int i = 0; i < QR; ++i)
+#pragma unroll
+        for (int k = 0; k < QC; ++k) s[i][k] = 0.f;
 #pragma unroll 4
-    for (int i = tid; i < C * (D / 4); i += TH) {
-      const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-      const int j = j0 + r;
-      float4 kf = make_float4(0.f, 0.f, 0.f, 0.f), vf = kf;
-      if (j < jn) {
-        if (draft || FMT == FORMAT_PLAIN) {
-          const long long at = draft ? (((long long)j * p.B + b) * p.Hkv + hk) * D + d
-                                     : ((long long)blockIdx.z * p.cap + j) * D + d;
-          kf = tree_load4(static_cast<const T*>(draft ? p.k_new : p.K) + at);
-          vf = tree_load4(static_cast<const T*>(draft ? p.v_new : p.V) + at);
-        } else if constexpr (FMT != FORMAT_PLAIN) {
-          const long long row = (long long)blockIdx.z * p.cap + j;
-          float a[4];
-          const float ks = p.k_scale[row], vs = p.v_scale[row];
-          quant_unpack4<FMT>(*reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.K) + row * D + d), a);
-          kf = make_float4(a[0] * ks, a[1] * ks, a[2] * ks, a[3] * ks);
-          quant_unpack4<FMT>(*reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(p.V) + row * D + d), a);
-          vf = make_float4(a[0] * vs, a[1] * vs, a[2] * vs, a[3] * vs);
+      for (int d = 0; d < D; d += 4) {
+        float4 q[QR];
+#pragma unroll
+        for (int i = 0; i < QR; ++i) q[i] = *reinterpret_cast<const float4*>(q_s + (lr + i) * LD + d);
+#pragma unroll
+        for (int k = 0; k < QC; ++k) {
+          const float4 kk = *reinterpret_cast<const float4*>(k_s + (lc + CG * k) * LD + d);
+#pragma unroll
+          for (int i = 0; i < QR; ++i)
+            s[i][k] = fmaf(q[i].x, kk.x, fmaf(q[i].y, kk.y, fmaf(q[i].z, kk.z, fmaf(q[i].w, kk.w, s[i][k]))));
         }
       }
-      *reinterpret_cast<float4*>(k_s + r * LD + d) = kf;
-      *reinterpret_cast<float4*>(v_s + r * D + d) = vf;
-    }
-    __syncthreads();
-    float s[QR][QC];
+      float e[QC][QR];
 #pragma unroll
-    for (int i = 0; i < QR; ++i)
+      for (int i = 0; i < QR; ++i) {
+        const int m = row0 + lr + i;
+        const uint32_t see = draft ? (m < p.M ? anc_s[m / p.G][j0 >> 5] : 0u) : 0u;
+        float top = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < QC; ++k) s[i][k] = 0.f;
-#pragma unroll 4
-    for (int d = 0; d < D; d += 4) {
-      float4 q[QR];
+        for (int k = 0; k < QC; ++k) {
+          const int c = lc + CG * k;
+          const bool vis = draft ? ((see >> c) & 1u) != 0 : j0 + c < jn;
+          if (!vis) s[i][k] = -INFINITY;
+          top = fmaxf(top, s[i][k]);
+        }
 #pragma unroll
-      for (int i = 0; i < QR; ++i) q[i] = *reinterpret_cast<const float4*>(q_s + (lr + i) * LD + d);
+        for (int o = CG / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float m_new = fmaxf(m_run[i], top);
+        const float base = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = exp2f(m_run[i] - base);       // 0 while nothing has been seen
+        float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < QC; ++k) {
-        const float4 kk = *reinterpret_cast<const float4*>(k_s + (lc + CG * k) * LD + d);
+        for (int k = 0; k < QC; ++k) {
+          e[k][i] = exp2f(s[i][k] - base);
+          sum += e[k][i];
+        }
 #pragma unroll
-        for (int i = 0; i < QR; ++i)
-          s[i][k] = fmaf(q[i].x, kk.x, fmaf(q[i].y, kk.y, fmaf(q[i].z, kk.z, fmaf(q[i].w, kk.w, s[i][k]))));
-      }
-    }
-    float e[QC][QR];
-#pragma unroll
-    for (int i = 0; i < QR; ++i) {
-      const int m = row0 + lr + i;
-      const uint32_t see = draft ? (m < p.M ? anc_s[m / p.G][j0 >> 5] : 0u) : 0u;
-      float top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < QC; ++k) {
-        const int c = lc + CG * k;
-        const bool vis = draft ? ((see >> c) & 1u) != 0 : j0 + c < jn;
-        if (!vis) s[i][k] = -INFINITY;
-        top = fmaxf(top, s[i][k]);
+        for (int o = CG / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        l_run[i] = l_run[i] * corr + sum;
+        m_run[i] = m_new;
+        if (lc == 0) corr_s[lr + i] = corr;
       }
 #pragma unroll
-      for (int o = CG / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float m_new = fmaxf(m_run[i], top);
-      const float base = m_new == -INFINITY ? 0.f : m_new;
-      const float corr = exp2f(m_run[i] - base);       // 0 while nothing has been seen
-      float sum = 0.f;
-#pragma unroll
       for (int k = 0; k < QC; ++k) {
-        e[k][i] = exp2f(s[i][k] - base);
-        sum += e[k][i];
+        float* dst = p_s + (lc + CG * k) * LP + lr;
+        if constexpr (QR == 4) *reinterpret_cast<float4*>(dst) = make_float4(e[k][0], e[k][1], e[k][2], e[k][3]);
+        else if constexpr (QR == 2) *reinterpret_cast<float2*>(dst) = make_float2(e[k][0], e[k][1]);
+        else *dst = e[k][0];
       }
-#pragma unroll
-      for (int o = CG / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      l_run[i] = l_run[i] * corr + sum;
-      m_run[i] = m_new;
-      if (lc == 0) corr_s[lr + i] = corr;
     }
-#pragma unroll
-    for (int k = 0; k < QC; ++k) {
-      float* dst = p_s + (lc + CG * k) * LP + lr;
-      if constexpr (QR == 4) *reinterpret_cast<float4*>(dst) = make_float4(e[k][0], e[k][1], e[k][2], e[k][3]);
-      else *reinterpret_cast<float2*>(dst) = make_float2(e[k][0], e[k][1]);
-    }
-    __syncthreads();
+    landed(tile, 1);            // (and every thread has done with the keys)
+    if (tile + 1 < n_state + n_draft) fetch(tile + 1, 0);
+    if (!has_sums) continue;
 #pragma unroll
     for (int i = 0; i < PR; ++i) {
       const float corr = corr_s[orow + i];
@@ -285,10 +322,15 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
       for (int j = 0; j < PC; ++j) acc[i][j] *= corr;
     }
     auto column = [&](int c, float (&w)[PR], float (&v)[PC]) {
+      if constexpr (PR % 4 == 0) {
 #pragma unroll
-      for (int i = 0; i < PR; i += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(p_s + c * LP + orow + i);
-        w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
+        for (int i = 0; i < PR; i += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(p_s + c * LP + orow + i);
+          w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < PR; ++i) w[i] = p_s[c * LP + orow + i];
       }
 #pragma unroll
       for (int j = 0; j < PC; j += PV) {
@@ -296,9 +338,11 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
         if constexpr (PV == 4) {
           const float4 x = *reinterpret_cast<const float4*>(src);
           v[j] = x.x; v[j + 1] = x.y; v[j + 2] = x.z; v[j + 3] = x.w;
-        } else {
+        } else if constexpr (PV == 2) {
           const float2 x = *reinterpret_cast<const float2*>(src);
           v[j] = x.x; v[j + 1] = x.y;
+        } else {
+          v[j] = *src;
         }
       }
     };
@@ -349,12 +393,12 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
     const float r = l == 0.f || l == TREE_PADDING ? 0.f : 1.f / l;
     const int n = m / p.G, g = m - n * p.G;
     const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
-    T* out = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D;
+    float* out = static_cast<float*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D;
     if (p.splits > 1 && ox == 0) p.part_ml[at] = make_float2(m_s[orow + i], l);
 #pragma unroll
     for (int j = 0; j < PC; ++j) {
       const int d = ox + XG * (j / PV * PV) + j % PV;
-      if (p.splits == 1) out[d] = (T)(l == TREE_PADDING ? 0.f : acc[i][j] * r);
+      if (p.splits == 1) out[d] = l == TREE_PADDING ? 0.f : acc[i][j] * r;
       else p.part_acc[at * D + d] = acc[i][j];
     }
   }
