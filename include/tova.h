@@ -537,9 +537,11 @@ int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const flo
  * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the
  * result is.  The result does not depend on n_live, lens, other sequences or the
  * GPU beyond the order of fp32 sums, and is the same bits every time.
- *   tova_tree_workspace_bytes   device bytes that a call with this shape needs
- *          for partial results (0 is possible: none; an invalid configuration
- *          gives (size_t)-1).  It asks the current device for its SM count.
+ *   tova_tree_workspace_bytes   device bytes that calls of this configuration and
+ *          N need for partial results, for every length up to n_live (0 is
+ *          possible: none; an invalid configuration gives (size_t)-1).  It asks
+ *          the current device for its SM count.  Calls that may run at the same
+ *          time, captured ones among them, need a workspace each.
  *   tova_cache_tree_attention   the same over the live rows of a cache (format
  *          and geometry are the cache's).  Waits for a pending deferred eviction.
  *          Refused (TOVA_ERR_UNSUPPORTED) under position compression, whose keys

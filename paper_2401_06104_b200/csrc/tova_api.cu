@@ -24,7 +24,6 @@
 #include "tova_poscomp.cuh"
 
 // tova_ops.cu: device bytes that tova_tree_attention needs at whatever length the state has.
-size_t tree_workspace_any_length(const tova_tree_config& cfg, int32_t n_nodes);
 
 namespace {
 
@@ -1499,7 +1498,8 @@ tova_tree_config tree_config_of(const tova_cache& c) {
 
 size_t tova_cache_tree_workspace_bytes(const tova_cache* c, int32_t n_nodes) {
   if (!c) return (size_t)-1;
-  return tree_workspace_any_length(tree_config_of(*c), n_nodes);
+  const tova_tree_config t = tree_config_of(*c);
+  return tova_tree_workspace_bytes(&t, t.capacity, n_nodes);
 }
 
 int tova_cache_tree_attention(tova_cache* c, const void* q, const void* k, const void* v, int32_t n_nodes,

@@ -308,8 +308,9 @@ struct TreePlan {
   size_t ml_bytes, acc_bytes, bytes;   // workspace: maxima and sums, weighted sums (and the tcgen05 kernel's list of cuts)
 };
 
-// any_length: the workspace is to do for every n_live up to the capacity.
-TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count, bool any_length = false) {
+// up_to: the workspace is to do for every length up to n_live (fewer tiles can make more runs: 150 tiles for at most 148 runs
+// are 75 of two, 148 are 148 of one).
+TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, int sm_count, bool up_to = false) {
   TreePlan t{};
   const int M = n_nodes * (c.n_q_heads / c.n_kv_heads);
   size_t part_rows;
@@ -334,7 +335,8 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     }
     t.row_blocks = (M + rows - 1) / rows;
     const long long whole = (long long)t.row_blocks * c.batch * c.n_kv_heads;
-    int tiles = std::max(1, (n_live + cols - 1) / cols);
+    const int all_tiles = std::max(1, (n_live + cols - 1) / cols);
+    int tiles = all_tiles;
     // Runs of columns for two rounds of resident blocks (two per SM), but none shorter than two tiles unless the GPU
     // would stay half empty.
     const int resident = 2 * sm_count, shortest = whole * (tiles / 2) < resident ? 1 : 2;
@@ -354,7 +356,9 @@ TreePlan tree_plan(const tova_tree_config& c, int32_t n_live, int32_t n_nodes, i
     t.splits = (tiles + per - 1) / per;
     t.cluster = t.cluster && t.splits > 1;
     if (t.splits > 1 && !t.cluster) t.splits += 1;      // a run of its own for the drafts: it does not wait for a run of rows
-    const long long runs = any_length ? most + 1 : t.splits > 1 && !t.cluster ? t.splits : 0;
+    // A shorter state makes at most as many runs as it has tiles, and joins them in a cluster where it has few.
+    const bool merges = most > 1 && all_tiles > 1 && (t.kernel == TREE_ALU || (most > tova::TREE_CLUSTER_MAX && all_tiles > 4 * tova::TREE_CLUSTER_MAX));
+    const long long runs = up_to ? (merges ? std::min<long long>(most, all_tiles) + 1 : 0) : t.splits > 1 && !t.cluster ? t.splits : 0;
     part_rows = (size_t)runs * c.batch * c.n_kv_heads * M;
   }
   t.ml_bytes = (part_rows * sizeof(float2) + 255) / 256 * 256;
@@ -502,13 +506,7 @@ cudaError_t tree_launch_f(int format, const tova::TreeParams& p, const TreePlan&
 extern "C" size_t tova_tree_workspace_bytes(const tova_tree_config* cfg, int32_t n_live, int32_t n_nodes) {
   DeviceInfo dev;
   if (tree_check(cfg, n_live, n_nodes) != TOVA_OK || !device_info(&dev)) return (size_t)-1;
-  return n_nodes ? tree_plan(*cfg, n_live, n_nodes, dev.sm_count).bytes : 0;
-}
-
-size_t tree_workspace_any_length(const tova_tree_config& cfg, int32_t n_nodes) {
-  DeviceInfo dev;
-  if (tree_check(&cfg, 0, n_nodes) != TOVA_OK || !device_info(&dev)) return (size_t)-1;
-  return n_nodes ? tree_plan(cfg, cfg.capacity, n_nodes, dev.sm_count, true).bytes : 0;
+  return n_nodes ? tree_plan(*cfg, n_live, n_nodes, dev.sm_count, true).bytes : 0;
 }
 
 extern "C" int tova_tree_attention(const tova_tree_config* cfg, const void* K, const void* V, const float* k_scale,

@@ -618,6 +618,23 @@ def test_tree_workspace_is_checked():
         assert e.value.code == code
 
 
+@pytest.mark.parametrize("dtype, B, H, N, D", [("bf16", 1, 4, 2, 128), ("bf16", 2, 3, 5, 64), ("bf16", 1, 1, 40, 64), ("bf16", 7, 4, 2, 64), ("bf16", 50, 4, 1, 64),
+                                                ("bf16", 1, 2, 70, 64), ("fp32", 1, 2, 3, 64), ("fp32", 3, 4, 20, 64), ("fp32", 80, 4, 1, 64)])
+def test_tree_workspace_does_for_every_length_up_to_the_bound(dtype, B, H, N, D):
+    """A state that grows: one workspace, sized for the most rows it will hold."""
+    t = TT[dtype]
+    top = 24000 // B
+    cfg = tova.tova_tree_config(B, H, H, D, top, TD[dtype], tova.TOVA_FORMAT_PLAIN, 0.0)
+    K = torch.zeros(B, H, top, D, dtype=t, device=DEV)
+    x = torch.zeros(N, B, H, D, dtype=t, device=DEV)
+    out = torch.empty_like(x)
+    for most in (top, top // 2 + 1, top // 3):
+        ws = torch.empty(tova.tova_tree_workspace_bytes(cfg, most, N), dtype=torch.uint8, device=DEV)
+        for n in list(range(most, 0, -max(1, most // 150))) + [1, 0]:
+            tova.tova_tree_attention(cfg, K, K, n, x, x, x, N, out, ws)
+    torch.cuda.synchronize()
+
+
 # -------------------------------------------------------------------------------------------- verification
 
 def verify_reference(p, q, tokens, parents, u, us):
