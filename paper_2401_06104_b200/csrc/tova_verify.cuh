@@ -21,8 +21,8 @@
 // the vocabulary where a row has to be summed; partial sums travel through distributed shared memory.  A lane holds
 // eight neighbouring entries of the row in registers for as long as the walk stays at the node (vocabularies up to
 // 32768 entries), so a second rejection or the final draw there reads nothing, and the draw needs one scan over the
-// lanes of the one warp whose stretch holds the goal.  Measured: trees of 63 drafts, 32 sequences, 32000 tokens 12 us, about
-// 2.5 us for each row sum along the longest walk; a chain of five 7.1 us.
+// lanes of the one warp whose stretch holds the goal.  Measured: trees of 63 drafts, 32 sequences, 32000 tokens 14 to 16 us,
+// about 2.5 us for each row sum along the longest walk; a chain of five 6.6 us.
 #pragma once
 
 #include <cooperative_groups.h>
