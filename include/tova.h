@@ -544,6 +544,8 @@ int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const flo
  *          time, captured ones among them, need a workspace each.
  *   tova_cache_tree_attention   the same over the live rows of a cache (format
  *          and geometry are the cache's).  Waits for a pending deferred eviction.
+ *          The number of rows held is the host's at the call: a captured call
+ *          keeps it (fixed anyway once the state is full).
  *          Refused (TOVA_ERR_UNSUPPORTED) under position compression, whose keys
  *          are not rotated. */
 typedef struct {

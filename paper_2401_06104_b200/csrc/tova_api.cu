@@ -23,8 +23,6 @@
 #include "tova_shard.cuh"
 #include "tova_poscomp.cuh"
 
-// tova_ops.cu: device bytes that tova_tree_attention needs at whatever length the state has.
-
 namespace {
 
 constexpr size_t ALIGN = 256;
