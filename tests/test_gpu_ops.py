@@ -538,6 +538,38 @@ def test_tree_values_of_unseen_drafts_do_not_leak(dtype, H, Hkv, N):
             assert torch.equal(out[:, b][sees][..., keep], clean[:, b][sees][..., keep])
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype, H, Hkv, N", [("bf16", 4, 4, 6), ("bf16", 8, 2, 40), ("fp32", 8, 2, 40)])
+def test_tree_values_of_unseen_drafts_do_not_leak_over_an_8_bit_state(dtype, fmt, H, Hkv, N):
+    """The same over codes: a NaN key and infinite values of one draft reach the nodes that see it and no others."""
+    g = gen(16)
+    B, D, L = 2, 128, 270
+    t = TT[dtype]
+    q, k, v = (randn(g, N, B, n, D).to(t) for n in (H, Hkv, Hkv))
+    (K, V), (ks, vs) = new_state(B, Hkv, L, D, fmt)
+    tova.tova_quant_write(tova.tova_quant_config(B, Hkv, D, L, tova.TOVA_DTYPE_FP32, FMT[fmt]), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D),
+                          L, K, ks, V, vs)
+    par = random_parents(N, B, 3, padding=False)
+    cfg = tova.tova_tree_config(B, H, Hkv, D, L, TD[dtype], FMT[fmt], 0.0)
+    ws = torch.empty(max(16, tova.tova_tree_workspace_bytes(cfg, L, N)), dtype=torch.uint8, device=DEV)
+    clean, out = torch.empty(N, B, H, D, dtype=t, device=DEV), torch.empty(N, B, H, D, dtype=t, device=DEV)
+    tova.tova_tree_attention(cfg, K, V, L, q, k, v, N, clean, ws, parents=par, k_scale=ks, v_scale=vs)
+    bad = 2
+    k2, v2 = k.clone(), v.clone()
+    k2[bad, 0] = math.nan
+    v2[bad, 1, :, 5] = -math.inf
+    tova.tova_tree_attention(cfg, K, V, L, q, k2, v2, N, out, ws, parents=par, k_scale=ks, v_scale=vs)
+    for b in range(B):
+        sees = torch.tensor([bad in c for c in ancestors(par[:, b].tolist())], device=DEV)
+        assert torch.equal(out[:, b][~sees], clean[:, b][~sees])
+        if b == 0:
+            assert bool(out[:, b][sees].isnan().all())
+        else:
+            assert bool((out[:, b][sees][..., 5] == -math.inf).all())
+            keep = [d for d in range(D) if d != 5]
+            assert torch.equal(out[:, b][sees][..., keep], clean[:, b][sees][..., keep])
+
+
 def test_tree_offsets_beyond_32_bits():
     """A state of more than 2^31 elements: the last sequence's rows lie behind that."""
     B, H, Hkv, D, cap, L = 2, 4, 2, 128, 4300000, 300
