@@ -620,9 +620,10 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int c = 0; c < TREE_CLUSTER_MAX; ++c) {
-        if (ml[c].x == -INFINITY) continue;
-        const float f = ex2_approx(ml[c].x - top);
-        l += f * ml[c].y;
+        // A run without a finite logit has the factor 0, and adds its sums all the same: where its logits are NaN, so are
+        // they, and the row's result.  (Its l may be NaN beside finite ones: it is left out, and the sums carry the NaN.)
+        const float f = ml[c].x == -INFINITY ? 0.f : ex2_approx(ml[c].x - top);
+        if (f != 0.f) l += f * ml[c].y;
         acc.x = fmaf(f, x[c].x, acc.x); acc.y = fmaf(f, x[c].y, acc.y);
         acc.z = fmaf(f, x[c].z, acc.z); acc.w = fmaf(f, x[c].w, acc.w);
       }

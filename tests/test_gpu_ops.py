@@ -946,3 +946,77 @@ def test_operators_take_an_explicit_stream():
     r.tova_rope_apply(x, None, T, b, None)
     torch.cuda.synchronize()
     assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------- drafted tokens: values that are not finite
+
+# One shape for each way that a call is cut: one run of columns; runs joined in a cluster, few rows and many; runs joined by
+# the second kernel; the tcgen05 kernel, with whole jobs and with cut ones.  N, B, H, Hkv, L.
+CUTS = {"one run": (3, 2, 8, 2, 50), "cluster": (3, 2, 8, 2, 1000), "cluster, one token": (1, 1, 32, 8, 1000),
+        "cluster, 48 rows": (12, 2, 8, 2, 500), "second kernel": (5, 1, 8, 2, 9000), "tcgen05": (40, 2, 8, 2, 300),
+        "tcgen05, cut jobs": (40, 1, 8, 2, 9000)}
+
+
+def cut_inputs(cut, dtype, fmt, seed):
+    """Inputs of a call cut that way, the function that makes the call on given q, k, v and state, and its tree's parents
+    (a padding node in every other sequence, where there are more than three nodes)."""
+    N, B, H, Hkv, L = CUTS[cut]
+    D, g, t = 128, gen(seed), TT[dtype]
+    q, k, v = (randn(g, N, B, n, D).to(t) for n in (H, Hkv, Hkv))
+    ks = vs = None
+    if fmt == "plain":
+        K, V = randn(g, B, Hkv, L, D).to(t), randn(g, B, Hkv, L, D).to(t)
+    else:
+        (K, V), (ks, vs) = new_state(B, Hkv, L, D, fmt)
+        tova.tova_quant_write(tova.tova_quant_config(B, Hkv, D, L, tova.TOVA_DTYPE_FP32, FMT[fmt]), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D),
+                              L, K, ks, V, vs)
+    par = random_parents(N, B, seed)
+    cfg = tova.tova_tree_config(B, H, Hkv, D, L, TD[dtype], FMT[fmt], 0.0)
+    ws = torch.empty(max(16, tova.tova_tree_workspace_bytes(cfg, L, N)), dtype=torch.uint8, device=DEV)
+
+    def call(q, k, v, K, V, ks, vs):
+        out = torch.full((N, B, H, D), 7.0, dtype=t, device=DEV)
+        tova.tova_tree_attention(cfg, K, V, L, q, k, v, N, out, ws, parents=par, k_scale=ks, v_scale=vs)
+        return out
+    real = torch.tensor([[bool(ancestors(par[:, b].tolist())[i]) for b in range(B)] for i in range(N)], device=DEV)
+    return (q, k, v, K, V, ks, vs), call, real
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("dtype, fmt", [("bf16", "plain"), ("bf16", "int8"), ("bf16", "e4m3"), ("fp32", "plain"), ("fp32", "e4m3")])
+def test_tree_queries_that_are_not_numbers(dtype, fmt, cut):
+    """A NaN in a query makes that row NaN, whichever way the call is cut; every other row keeps its bits, padding its zeros."""
+    (q, k, v, *state), call, real = cut_inputs(cut, dtype, fmt, 31)
+    N, B, H, D = q.shape
+    clean = call(q, k, v, *state)
+    assert bool(clean.isfinite().all())
+    bad = torch.zeros(N, B, H, dtype=torch.bool, device=DEV)
+    bad.view(-1)[::5] = True
+    q2 = q.clone()
+    q2[..., 77] = torch.where(bad, torch.full_like(q[..., 77], math.nan), q[..., 77])
+    out = call(q2, k, v, *state)
+    nan = bad & real[..., None]
+    assert bool(out[nan].isnan().all())
+    assert torch.equal(out[~nan], clean[~nan])
+    assert bool((out[~real] == 0).all())
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("dtype, fmt", [("bf16", "plain"), ("bf16", "int8"), ("fp32", "plain"), ("fp32", "int8")])
+def test_tree_keys_of_the_state_that_are_not_numbers(dtype, fmt, cut):
+    """Every key of a stretch of the state is NaN: all that see it come back NaN.  The whole state of a KV head, so that only the
+    drafts have finite logits; a stretch that is all that one run of columns has; one that begins and ends within runs."""
+    (q, k, v, K, V, ks, vs), call, real = cut_inputs(cut, dtype, fmt, 32)
+    L, G = K.shape[2], q.shape[2] // K.shape[1]
+    clean = call(q, k, v, K, V, ks, vs)
+    for a, b in ((0, L), (min(128, L // 2), min(256, L)), (L // 8, L // 2), (L - 1, L)):
+        K2, ks2 = K.clone(), None if ks is None else ks.clone()
+        if ks is None:
+            K2[0, 0, a:b] = math.nan
+        else:
+            ks2[0, 0, a:b] = math.nan
+        out = call(q, k, v, K2, V, ks2, vs)
+        hit = real[..., None].expand(out.shape[:3]).clone()
+        hit[:, 1:], hit[:, :, G:] = False, False
+        assert bool(out[hit].isnan().all()), (a, b)
+        assert torch.equal(out[~hit], clean[~hit])
