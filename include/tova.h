@@ -531,7 +531,8 @@ int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const flo
  *   parents [N,B] int32       -1 (hangs below the last settled token) or an
  *                             earlier node's index; NULL: a chain, parent i-1.
  *                             Any other value makes the node, and those below
- *                             it, padding: output 0
+ *                             it, padding: output 0.  Padding only: a node whose
+ *                             logits are NaN, or all minus infinity, gets NaN
  *   q [N,B,H,D], k, v [N,B,Hkv,D], out [N,B,H,D]   all in cfg->dtype
  * Logits, soft-max and sums are fp32; fp32 configurations form every product in
  * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the

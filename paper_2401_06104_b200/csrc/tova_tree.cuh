@@ -4,6 +4,7 @@
 // A node sees the state's live rows, its ancestors and itself:
 //   o_i = sum_j p_ij v_j,  p_ij = softmax_j(scale q_i k_j)  over j in state rows + {i, parent(i), parent(parent(i)), ...}
 // A node whose parent is neither -1 nor an earlier node, and every node below it, is padding: it sees nothing, o = 0.
+// Any other node sees itself; where all its logits are minus infinity it has no soft-max, and 0 / 0 makes the row NaN.
 // The state is only read.  N = 1 is a plain step without eviction.
 //
 // The rows of the product are the M = N G pairs (node, query head) that share a KV head; its columns the state's rows,
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(TREE_ALU_THREADS) tova_tree_alu_kernel(const _
     const int m = row0 + orow + i;
     if (m >= p.M) continue;
     const float l = corr_s[orow + i];
-    const float r = l == 0.f || l == TREE_PADDING ? 0.f : 1.f / l;
+    const float r = 1.f / l;
     const int n = m / p.G, g = m - n * p.G;
     const long long at = ((long long)split * gridDim.z + blockIdx.z) * p.M + m;
     float* out = static_cast<float*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D;
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(TREE_MERGE_THREADS) tova_tree_merge_kernel(con
   const int bh = (int)(row / p.M), mm = (int)(row - (long long)bh * p.M);
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv, n = mm / p.G, g = mm - n * p.G;
   T* dst = static_cast<T*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + lane * E;
-  const float r = l == 0.f ? 0.f : 1.f / l;
+  const float r = 1.f / l;
 #pragma unroll
   for (int j = 0; j < E; ++j) dst[j] = (T)(pad ? 0.f : acc[j] * r);
 }

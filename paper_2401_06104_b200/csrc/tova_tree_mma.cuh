@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
     return acc;
   };
   auto write = [&](int m, int d, const float4& acc, float l) {
-    const float f = l == 0.f || l == TREE_PADDING ? 0.f : 1.f / l;
+    const float f = 1.f / l;      // (l = 0: every logit is minus infinity, and the result NaN)
     const int n = m / p.G, g = m - n * p.G;
     __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + d;
     if (l == TREE_PADDING) tree_store4<__nv_bfloat16>(dst, 0.f, 0.f, 0.f, 0.f);

@@ -768,8 +768,8 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
       }
       if (mr.last && !real) l = TREE_PADDING;
       if (!ok) l = __uint_as_float(0x7fc00000u);
-      const bool zero = l == TREE_PADDING || l == 0.f;
-      const float r = mr.part >= 0 ? 1.f : (zero ? 0.f : 1.f / l);
+      const bool zero = l == TREE_PADDING;
+      const float r = mr.part >= 0 ? 1.f : 1.f / l;
       const long long at = (long long)mr.part * (R * NT) + row;
       if (mr.part >= 0 && half == 0) p.part_ml[at] = make_float2(m_ref, l);
       const int gq = max(node, 0);
@@ -861,7 +861,7 @@ __global__ void __launch_bounds__(TREE_TC_JOIN_THREADS) tova_tree_tc_join_kernel
     }
   }
   l = warp_sum(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = 1.f / l;
   const int n = m / p.G, g = m - n * p.G;
   __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((long long)n * p.B + b) * p.H + hk * p.G + g) * D + lane * E;
 #pragma unroll

@@ -1020,3 +1020,27 @@ def test_tree_keys_of_the_state_that_are_not_numbers(dtype, fmt, cut):
         hit[:, 1:], hit[:, :, G:] = False, False
         assert bool(out[hit].isnan().all()), (a, b)
         assert torch.equal(out[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("dtype, fmt", [("bf16", "plain"), ("bf16", "int8"), ("fp32", "plain"), ("fp32", "e4m3")])
+def test_tree_logits_that_are_all_minus_infinity(dtype, fmt, cut):
+    """A row that sees columns, all of them with the logit minus infinity, has no soft-max: NaN by the formula, not the zeros
+    of a row that sees nothing."""
+    (q, k, v, K, V, ks, vs), call, real = cut_inputs(cut, dtype, fmt, 33)
+    N, B, H, D = q.shape
+    # component 5 of every key is negative, and an infinite query there makes every logit of its row minus infinity
+    k[..., 5] = -1.0
+    K[..., 5] = -1
+    if fmt == "e4m3":
+        K[..., 5] = -72                               # 0xb8: -1
+    clean = call(q, k, v, K, V, ks, vs)
+    bad = torch.zeros(N, B, H, dtype=torch.bool, device=DEV)
+    bad.view(-1)[::3] = True
+    q2 = q.clone()
+    q2[..., 5] = torch.where(bad, torch.full_like(q[..., 5], math.inf), q[..., 5])
+    out = call(q2, k, v, K, V, ks, vs)
+    nan = bad & real[..., None]
+    assert bool(out[nan].isnan().all())
+    assert torch.equal(out[~nan], clean[~nan])
+    assert bool((out[~real] == 0).all())
