@@ -584,7 +584,9 @@ int tova_cache_tree_attention(tova_cache* c, const void* q, const void* k, const
  * Comparisons and sums are in 64 bits.
  *   n_accepted [B]; path [N,B] (may be NULL): the accepted nodes, then -1;
  *   tokens_out [N+1,B]: their tokens, then the last token, then -1.  A row of p
- *   without any positive entry gives the last token -1.
+ *   without any positive finite entry gives the last token -1.
+ * Entries of p that are infinite or NaN count as zeros; a token whose q(x) is not
+ * finite is not accepted, and has no weight in r once a draft was rejected there.
  * A token outside 0..V-1 is never accepted.  N = 0 draws one token. */
 typedef struct {
   int32_t batch, n_nodes, vocab; /* n_nodes 0..1024                                    */

@@ -82,10 +82,14 @@ __device__ __forceinline__ void verify_load8(const void* p, long long row, int i
   }
 }
 
-// The weight that the last token is drawn with, or a term of Z: max(0, p - S q); NaN counts as zero.
+// A probability that counts: an entry of p that is an infinity or NaN is none, and negative ones are none either.
+__device__ __forceinline__ double verify_prob(float p) { return p > 0.f && p < INFINITY ? (double)p : 0.0; }
+
+// The weight that the last token is drawn with, or a term of Z: max(0, p - S q).  Where p or q is not finite it is zero, so
+// that every sum is finite and the draw always finds a token where there is one.
 __device__ __forceinline__ double verify_weight(float p, float q, double S) {
   const double w = (double)p - S * (double)q;
-  return w > 0.0 ? w : 0.0;
+  return w > 0.0 && w < (double)INFINITY ? w : 0.0;
 }
 
 template <typename T>
@@ -209,16 +213,16 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) tova_verify_kernel(const __
       int c = next_child(from);
       while (cmd == 0) {
         if (c < 0) { cmd = 2; break; }
-        const double pr = (double)px_s[c], qr = (double)qx_s[c];
+        const double qr = (double)qx_s[c];
         double r;
         if (p.draft) {
           r = verify_weight(px_s[c], qx_s[c], S);
         } else {                                 // struck out if an earlier child carried the same token
           bool again = false;
           for (int i = node + 1 + lane; i < c; i += 32) again |= par_s[i] == node && tok_s[i] == tok_s[c];
-          r = __any_sync(0xffffffffu, again) ? 0.0 : (pr > 0.0 ? pr : 0.0);
+          r = __any_sync(0xffffffffu, again) ? 0.0 : verify_prob(px_s[c]);
         }
-        if ((double)u_s[c] * qr * Z < r) {
+        if (r > 0.0 && (double)u_s[c] * qr * Z < r) {      // (a negative q must not pass a token without probability)
           if (rank == 0 && lane == 0) {
             if (p.path) p.path[(long long)count * p.B + b] = c;
             p.tokens_out[(long long)count * p.B + b] = tok_s[c];
@@ -271,7 +275,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) tova_verify_kernel(const __
     const int i = w0 + k * VERIFY_STEP + lane * VERIFY_LANE;
 #pragma unroll
     for (int e = 0; e < VERIFY_LANE; ++e) {
-      w[e] = with_q && !plain ? verify_weight(a[e], q[e], S) : (a[e] > 0.f ? (double)a[e] : 0.0);
+      w[e] = with_q && !plain ? verify_weight(a[e], q[e], S) : verify_prob(a[e]);
       if (!plain)
         for (int j = 0; j < kids; ++j)
           if (kid_s[j] == i + e) w[e] = 0.0;

@@ -1044,3 +1044,42 @@ def test_tree_logits_that_are_all_minus_infinity(dtype, fmt, cut):
     assert bool(out[nan].isnan().all())
     assert torch.equal(out[~nan], clean[~nan])
     assert bool((out[~real] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("V", [300, 40000])
+def test_verify_probabilities_that_are_not_finite(dtype, draft, V):
+    """An entry that is an infinity or NaN counts as nothing, for its own token and in every sum: the results are those of
+    the same rows with zeros there, and every output is written."""
+    B, N = 6, 4
+    g = gen(41)
+    p = (torch.softmax(randn(g, N + 1, B, V), -1)).to(TT[dtype])
+    q = (torch.softmax(randn(g, N + 1, B, V), -1)).to(TT[dtype])
+    tok = torch.randint(0, V, (N, B), generator=g, device=DEV, dtype=torch.int32)
+    tok[1, 4] = tok[0, 4]
+    par = torch.tensor([-1, -1, 0, -1], device=DEV, dtype=torch.int32)[:, None].expand(N, B).contiguous()
+    u, us = torch.rand(N, B, generator=g, device=DEV), torch.rand(B, generator=g, device=DEV)
+    us[0], us[1] = 0.0, 1.0 - 2.0 ** -24
+    u[:, 5] = 0.0
+    bad_p, bad_q = p.clone(), q.clone()
+    bad_p[:, :, 17], bad_p[:, 1, 3], bad_p[:, 2, V - 1], bad_p[:, 3, ::7] = math.inf, -math.inf, math.nan, math.inf
+    for i in range(N):                               # tokens of the drafts among them
+        bad_p[0, 4, tok[i, 4].long()] = math.inf
+        bad_p[:, 5, tok[i, 5].long()] = math.inf
+    p = torch.where(bad_p.isfinite(), bad_p, torch.zeros_like(p))
+    got, want = run_verify(bad_p, q if draft else None, tok, par, u, us, dtype), run_verify(p, q if draft else None, tok, par, u, us, dtype)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    n, path, out = got
+    assert int(n[5]) == 0 and bool((out != 99).all()) and bool((path != 99).all())
+    pc, b = [-1, -1, 0, -1], 4
+    assert (int(n[b]), path[:, b].tolist(), out[:, b].tolist()) == verify_reference(
+        p[:, b].double().tolist(), q[:, b].double().tolist() if draft else None, tok[:, b].tolist(), pc, u[:, b].double().tolist(), float(us[b].double()))
+    all_bad = torch.full_like(p, math.inf)           # nothing to draw from
+    n, path, out = run_verify(all_bad, q if draft else None, tok, par, u, us, dtype)
+    assert bool((n == 0).all()) and bool((out == -1).all()) and bool((path == -1).all())
+    if draft:                                        # a draft's entries: the token is not accepted, the rest is the target's
+        bad_q[0, :, 17], bad_q[0, :, 20], bad_q[0, :, 23] = math.inf, -math.inf, math.nan
+        tok[0], tok[1], tok[3] = 17, 20, 23
+        n, path, out = run_verify(p, bad_q, tok, par, u, us, dtype)
+        assert bool((n == 0).all()) and bool(((out[0] >= 0) & (out[0] < V)).all()) and bool((out[1:] == -1).all())
