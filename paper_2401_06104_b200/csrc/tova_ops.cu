@@ -99,8 +99,14 @@ extern "C" int tova_rope_init(tova_rope** out, const tova_rope_config* cfg) {
   double ramp_lo = 0.0, ramp_hi = 0.0;
   if (c.scaling == TOVA_ROPE_YARN) {
     auto pair_of = [&](double turns) { return rot * std::log(c.original_context / (turns * two_pi)) / (2.0 * std::log(base)); };
-    ramp_lo = std::max(std::floor(pair_of(high)), 0.0);
-    ramp_hi = std::min(std::ceil(pair_of(low)), rot - 1.0);
+    ramp_lo = std::floor(pair_of(high));
+    ramp_hi = std::ceil(pair_of(low));
+    // The bounds are held to the pairs' indices, unless the whole ramp lies before the first pair (then all pairs turn less
+    // than `low` times) or behind: held there too, it would run backwards.
+    if (ramp_hi >= 0.0 && ramp_lo <= rot - 1.0) {
+      ramp_lo = std::max(ramp_lo, 0.0);
+      ramp_hi = std::min(ramp_hi, rot - 1.0);
+    }
     if (ramp_hi == ramp_lo) ramp_hi += 0.001;
     m = c.factor > 1.0 ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
   }

@@ -1083,3 +1083,22 @@ def test_verify_probabilities_that_are_not_finite(dtype, draft, V):
         tok[0], tok[1], tok[3] = 17, 20, 23
         n, path, out = run_verify(p, bad_q, tok, par, u, us, dtype)
         assert bool((n == 0).all()) and bool(((out[0] >= 0) & (out[0] < V)).all()) and bool((out[1:] == -1).all())
+
+
+@pytest.mark.parametrize("base, rot, orig", [(10000.0, 128, 1), (10000.0, 128, 4), (10000.0, 64, 4), (1.5, 64, 2 ** 31 - 1), (1.01, 128, 100000)])
+def test_rope_yarn_where_all_pairs_turn_less_or_more_than_the_blend(base, rot, orig):
+    """Contexts so short that even the first pair turns less than once are divided by the factor throughout; with
+    frequencies so close together that the last pair still turns more than 32 times nothing is."""
+    g = gen(51)
+    T, B, H, D, factor = 40, 2, 2, 128, 4.0
+    x = randn(g, T, B, H, D)
+    r = tova.TovaRope(B, H, H, D, dtype=tova.TOVA_DTYPE_FP32, rotary_dim=rot, base=base, scaling=tova.TOVA_ROPE_YARN, factor=factor, original_context=orig)
+    w = base ** (-2.0 * torch.arange(rot // 2, dtype=torch.float64) / rot)
+    turns = orig * w / (2 * math.pi)
+    assert bool((turns < 1).all()) or bool((turns > 32).all())
+    if bool((turns < 1).all()):
+        w = w / factor
+    y = torch.empty_like(x)
+    r.tova_rope_apply(x, None, T, y, None, first_pos=1000)
+    pos = 1000 + torch.arange(T, device=DEV)[:, None].expand(T, B)
+    check_rope(y, *rope_reference(x, pos, w.to(DEV), 0.1 * math.log(factor) + 1, rot, 0), "fp32")
