@@ -493,6 +493,8 @@ int tova_rope_destroy(tova_rope* r);
  *   code_d = nearest(fp32(x_d * fp32(Q / a))), ties to even,  value = code_d * scale.
  * Rows with a < 2^-100 store zeros; rows with an infinity or NaN store scale NaN
  * and read back as NaN.  Codes and scales are a function of the rows alone.
+ * Codes from elsewhere are taken as they are: int8 -128..127; e4m3 with NaN for 0x7f
+ * and 0xff, wherever the state is read.
  *   tova_quant_write   rows k, v [T,B,Hkv,D] (strides as for tova_rope_apply)
  *          go to slots [T,B] int32, or NULL: first_slot + token, which must lie
  *          in the state.  A listed slot outside 0..capacity-1 skips the row;

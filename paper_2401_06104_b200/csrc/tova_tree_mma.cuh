@@ -15,6 +15,7 @@
 // 8-bit states are converted on the way from shared memory to the matrix instructions' operands, each code once per
 // row group: int8 by pasting its 7 low bits and its sign bit behind the exponent of 128 (two bf16 numbers whose
 // difference is the code), e4m3 by shifting exponent and mantissa into bf16's and multiplying by 2^120; both exact.
+// A key with one of e4m3's two NaN codes gets the scale NaN where it lies, a value's component is noted and made NaN at the end.
 // The row's scale goes onto the logit and onto the weight, never onto a converted operand.  So that a thread's operand
 // elements are neighbouring bytes, the order of the contraction index (over D for the logits) and of O's columns is a
 // permutation of the natural one - the sums do not care, the operands of the other side follow it.
@@ -76,6 +77,31 @@ __device__ __forceinline__ uint32_t tree_codes2(uint32_t a, uint32_t b, int ia, 
     const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&up));
     return *reinterpret_cast<const uint32_t*>(&d);
   }
+}
+
+// e4m3 has no infinities, and NaN for the codes 0x7f and 0xff, which tree_codes2 turns into 480 and -480.  A state may hold them
+// (tova_quant_write stores none, but codes converted elsewhere can), so all that is converted is looked at: adding one to a
+// byte changes its top bit only where the seven others are ones.  (A carry out of 0xff reaches the next byte, beside a
+// code that has been found.)  Two instructions for four codes, beside ten that convert them: single steps over 64 x 32 heads x
+// 1024 rows take 206 us where 191 without, trees of 25 over 4 x 16001 rows (tcgen05 kernel) 93 where 90.
+// Here: the top bits of w's NaN codes | what has been found before.
+__device__ __forceinline__ uint32_t tree_nan_codes(uint32_t w, uint32_t found) { return found | (w ^ (w + 0x01010101u)); }
+__device__ __forceinline__ uint32_t tree_nan_codes(const uint4& w, uint32_t found) {
+  return tree_nan_codes(w.w, tree_nan_codes(w.z, tree_nan_codes(w.y, tree_nan_codes(w.x, found))));
+}
+constexpr uint32_t TREE_NAN_FOUND = 0x80808080u;
+// The bytes of four codes that are NaN, as bits 0..3.
+__device__ __forceinline__ uint32_t tree_which_nan(uint32_t w) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m |= (uint32_t)(((w >> (8 * i)) & 0x7fu) == 0x7fu) << i;
+  return m;
+}
+// tree_codes2's results where a NaN may be among the codes: nothing else gives 480.
+__device__ __forceinline__ uint32_t tree_mark_nan(uint32_t d) {
+  if ((d & 0x00007fffu) == 0x000043f0u) d |= 0x00007fffu;
+  if ((d & 0x7fff0000u) == 0x43f00000u) d |= 0x7fff0000u;
+  return d;
 }
 
 // Byte offset of 16-byte chunk `ch` of row `row` in a tile.  bf16 rows: the low three chunk bits turn with the row, so
@@ -170,6 +196,9 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
   __shared__ int par_s[TREE_MMA_NODES];
   __shared__ uint32_t anc_s[TREE_MMA_NODES][2];      // ancestor bits of every node
   __shared__ int odd_s;                              // some draft's value is not finite
+  constexpr bool NAN_CODES = FMT == FORMAT_E4M3;
+  __shared__ uint32_t nan_s[NAN_CODES ? D / 32 : 1]; // components with a NaN code in some row of V
+  if (NAN_CODES && tid < D / 32) nan_s[tid] = 0;     // (the tiles' first barrier lies between this and its first use)
   if (last) {
     if (tid < p.N) par_s[tid] = p.parents ? p.parents[(long long)tid * p.B + b] : tid - 1;
     if (tid == 0) odd_s = 0;
@@ -274,6 +303,7 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
     cp_async_commit();
     const unsigned char* stp = ring + (i % S::STAGES) * S::STAGE;
     const uint32_t st = smem_addr(stp);
+    uint32_t nan_k = 0, nan_v = 0;                       // NaN codes among the tile's, as tree_nan_codes finds them
     float s[MT][NB][4];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -303,7 +333,10 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
       for (int hf = 0; hf < D / 64; ++hf) {
         uint4 kw[NB];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) kw[n] = *reinterpret_cast<const uint4*>(stp + tree_off8<D>(kb + n * 8 + lr, 4 * hf + lc));
+        for (int n = 0; n < NB; ++n) {
+          kw[n] = *reinterpret_cast<const uint4*>(stp + tree_off8<D>(kb + n * 8 + lr, 4 * hf + lc));
+          if (NAN_CODES) nan_k = tree_nan_codes(kw[n], nan_k);
+        }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           uint32_t a[MT][4];
@@ -319,7 +352,18 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
         }
       }
     }
-    const float* ks_s = reinterpret_cast<const float*>(stp + 2 * S::TILE);
+    float* ks_s = reinterpret_cast<float*>(ring + (i % S::STAGES) * S::STAGE + 2 * S::TILE);
+    if constexpr (NAN_CODES) {
+      if (__any_sync(0xffffffffu, (nan_k & TREE_NAN_FOUND) != 0)) {      // (every warp that reads the column finds it itself)
+#pragma unroll 1
+        for (int n = 0; n < NB; ++n)
+#pragma unroll 1
+          for (int hf = 0; hf < D / 64; ++hf)
+            if (tree_nan_codes(*reinterpret_cast<const uint4*>(stp + tree_off8<D>(kb + n * 8 + lr, 4 * hf + lc)), 0u) & TREE_NAN_FOUND)
+              ks_s[kb + n * 8 + lr] = __uint_as_float(0x7fc00000u);
+        __syncwarp();
+      }
+    }
     const int left = c1 - (c0 + i * C) - kb;             // columns of this warp's share that exist
 #pragma unroll
     for (int n = 0; n < NB; ++n)
@@ -377,6 +421,10 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
             const uint2 x = *reinterpret_cast<const uint2*>(stp + S::TILE + tree_off8<D>(row, lr >> 1) + (lr & 1) * 8);
             vw[r][0] = x.x; vw[r][1] = x.y;
           }
+          if (NAN_CODES) {
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) nan_v = tree_nan_codes(vw[r][x], nan_v);
+          }
         }
 #pragma unroll
         for (int j = 0; j < OB; ++j) {
@@ -384,6 +432,16 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
           const uint32_t b1 = tree_codes2<FMT>(vw[2][j >> 2], vw[3][j >> 2], j & 3, 4 + (j & 3));
 #pragma unroll
           for (int t = 0; t < MT; ++t) mma_bf16(o[t][j], a[t], b0, b1);
+        }
+      }
+    }
+    if constexpr (NAN_CODES) {
+      if ((nan_v & TREE_NAN_FOUND) != 0) {               // every real row sees the state's rows: only the components count
+#pragma unroll 1
+        for (int x = 0; x < KS / 4 * (D / 32); ++x) {
+          const int r = x / (D / 32), row = kb + (r >> 2) * 16 + 2 * lc + (r & 1) + 8 * ((r >> 1) & 1), byte = OB * lr + 4 * (x % (D / 32));
+          const uint32_t m = tree_which_nan(*reinterpret_cast<const uint32_t*>(stp + S::TILE + tree_off8<D>(row, byte >> 4) + (byte & 15)));
+          if (m) atomicOr(&nan_s[byte >> 5], m << (byte & 31));
         }
       }
     }
@@ -572,6 +630,14 @@ __global__ void __launch_bounds__(CLUSTER ? 256 : 128, CLUSTER ? 1 : 2) tova_tre
       float v[4] = {acc.x, acc.y, acc.z, acc.w};
       tree_add_odd<2, 4>(p, b, hk, anc_s[r / p.G], D, d, v);
       acc = make_float4(v[0], v[1], v[2], v[3]);
+    }
+    if constexpr (NAN_CODES) {
+      const uint32_t m = nan_s[d >> 5] >> (d & 31);
+      const float nan = __uint_as_float(0x7fc00000u);
+      if (m & 1u) acc.x = nan;
+      if (m & 2u) acc.y = nan;
+      if (m & 4u) acc.z = nan;
+      if (m & 8u) acc.w = nan;
     }
     if (pad) l = TREE_PADDING;
     return acc;

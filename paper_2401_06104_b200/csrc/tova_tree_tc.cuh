@@ -439,10 +439,12 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
             if (!ok) break;
             unsigned char* dst = slot_s + (pos % S::SLOTS) * S::SLOT;
             const unsigned char* raw = raw_s + (rp % S::RAW_SLOTS) * S::RAW + pt * 16;
+            uint32_t nan = 0;                    // e4m3: NaN codes among this thread's
 #pragma unroll 4
             for (int k = 0; k < PER; ++k) {
               const int row = k * STEP + row_t;
               const uint4 w = row < valid ? *reinterpret_cast<const uint4*>(raw + k * (PT * 16)) : make_uint4(0, 0, 0, 0);
+              if (FMT == FORMAT_E4M3) nan = tree_nan_codes(w, nan);
               const uint4 lo = make_uint4(tree_codes2<FMT>(w.x, w.x, 0, 1), tree_codes2<FMT>(w.x, w.x, 2, 3),
                                           tree_codes2<FMT>(w.y, w.y, 0, 1), tree_codes2<FMT>(w.y, w.y, 2, 3));
               const uint4 hi = make_uint4(tree_codes2<FMT>(w.z, w.z, 0, 1), tree_codes2<FMT>(w.z, w.z, 2, 3),
@@ -450,6 +452,14 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
               // (one half of a row's threads starts with its second chunk: eight of them then meet eight bank groups)
               *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + turn)) = turn ? hi : lo;
               *reinterpret_cast<uint4*>(dst + place(row, 2 * ch_t + (turn ^ 1))) = turn ? lo : hi;
+            }
+            if (FMT == FORMAT_E4M3 && (nan & TREE_NAN_FOUND) != 0) {
+#pragma unroll 1
+              for (int k = 0; k < 2 * PER; ++k) {          // once more over what this thread has written
+                uint4* at = reinterpret_cast<uint4*>(dst + place((k >> 1) * STEP + row_t, 2 * ch_t + (k & 1)));
+                const uint4 w = *at;
+                *at = make_uint4(tree_mark_nan(w.x), tree_mark_nan(w.y), tree_mark_nan(w.z), tree_mark_nan(w.w));
+              }
             }
             fence_proxy_async_smem();          // for the tensor cores' reads, and for the next copy into the raw slot
             warp_arrive(&full[pos % S::SLOTS], lane);

@@ -1102,3 +1102,38 @@ def test_rope_yarn_where_all_pairs_turn_less_or_more_than_the_blend(base, rot, o
     r.tova_rope_apply(x, None, T, y, None, first_pos=1000)
     pos = 1000 + torch.arange(T, device=DEV)[:, None].expand(T, B)
     check_rope(y, *rope_reference(x, pos, w.to(DEV), 0.1 * math.log(factor) + 1, rot, 0), "fp32")
+
+
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_tree_e4m3_codes_that_are_not_numbers(dtype, cut):
+    """0x7f and 0xff are NaN wherever codes are read: a key that holds one makes every row that sees it NaN, a value the one
+    component.  (The library's own writer stores neither; codes converted elsewhere may hold them.)"""
+    (q, k, v, K, V, ks, vs), call, real = cut_inputs(cut, dtype, "e4m3", 34)
+    B, Hkv, L, D = K.shape
+    G = q.shape[2] // Hkv
+    K[K.view(torch.uint8) % 128 == 127] = 0
+    K[0, 0, L // 2], V[0, 0, L // 2] = 126, -2                 # the largest numbers, 0x7e and 0xfe, are none
+    clean = call(q, k, v, K, V, ks, vs)
+    assert bool(clean.isfinite().all())
+    for row, d, code in ((0, 0, 127), (L - 1, 127, -1), (L // 2, 63, 127), (L // 3, 70, -1)):
+        K2, V2 = K.clone(), V.clone()
+        K2[0, Hkv - 1, row, d] = code
+        V2[0, 0, row, d] = code
+        V2[B - 1, Hkv - 1, row, (d + 9) % D] = code
+        out = call(q, k, v, K2, V, ks, vs)
+        hit = real[..., None].expand(out.shape[:3]).clone()
+        hit[:, 1:], hit[:, :, :(Hkv - 1) * G] = False, False
+        assert bool(out[hit].isnan().all())
+        assert torch.equal(out[~hit], clean[~hit])
+        out = call(q, k, v, K, V2, ks, vs)
+        want = clean.clone()
+        want[:, 0, :G, d] = torch.where(real[:, 0, None], torch.full_like(want[:, 0, :G, d], math.nan), want[:, 0, :G, d])
+        x = want[:, B - 1, (Hkv - 1) * G:]
+        x[..., (d + 9) % D] = torch.where(real[:, B - 1, None], torch.full_like(x[..., 0], math.nan), x[..., (d + 9) % D])
+        assert torch.equal(out.isnan(), want.isnan())
+        assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want))
+    back = torch.empty(L, B, Hkv, D, device=DEV)
+    cfg = tova.tova_quant_config(B, Hkv, D, L, tova.TOVA_DTYPE_FP32, tova.TOVA_FORMAT_E4M3)
+    tova.tova_quant_read(cfg, K2, ks, V2, vs, L, back, None)
+    assert int(back.isnan().sum()) == 1 and bool(back[row, 0, Hkv - 1, d].isnan())
