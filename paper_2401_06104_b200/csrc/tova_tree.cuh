@@ -43,7 +43,7 @@ struct TreeParams {
   float scale2;                // scale * log2(e)
 };
 
-__device__ __forceinline__ int tree_len(const TreeParams& p, int b) {
+__host__ __device__ __forceinline__ int tree_len(const TreeParams& p, int b) {
   return p.lens ? max(0, min(p.lens[b], p.n_live)) : p.n_live;
 }
 

@@ -73,12 +73,13 @@ struct TreeTcShape {
 };
 
 // --- how the work is dealt out -----------------------------------------------------------------------------------
+// (On the host, too: a CPU test walks through every block's run.)
 // Tiles of a job of sequence b.
-__device__ __forceinline__ int tree_tc_tiles(const TreeParams& p, int b) {
+__host__ __device__ __forceinline__ int tree_tc_tiles(const TreeParams& p, int b) {
   return (tree_len(p, b) + TREE_TC_COLS - 1) / TREE_TC_COLS + (p.N + TREE_TC_COLS - 1) / TREE_TC_COLS;
 }
 // Tiles a group takes: an even share of all, but no fewer than `least`.
-__device__ __forceinline__ long long tree_tc_share(long long total, int groups, int least) {
+__host__ __device__ __forceinline__ long long tree_tc_share(long long total, int groups, int least) {
   const long long even = (total + groups - 1) / groups;
   return even > least ? even : least;
 }
@@ -97,7 +98,7 @@ struct TreeTcRun {
   int hk, rb, i0, i1, len, n_state, part;
   bool last;                    // has the job's last tile
 
-  __device__ __forceinline__ bool next(const TreeParams& p, int block) {
+  __host__ __device__ __forceinline__ bool next(const TreeParams& p, int block) {
     if (at >= end) return false;
     const int jobs = p.Hkv * p.row_rounds;        // of a sequence, for this block
     while (at >= base + (long long)tiles * jobs) {
@@ -120,6 +121,28 @@ struct TreeTcRun {
     return true;
   }
 };
+
+// Walks through a block's run; drafts(piece) is called for every piece that has drafts, until it returns false (a wait ran
+// out).  The job that starts in the run and goes on in another, if there is one, is found all the same: its pieces hold NaN
+// then, and must reach the result.
+template <typename F>
+__host__ __device__ __forceinline__ TreeTcCut tree_tc_walk(TreeTcRun run, const TreeParams& p, int block, F drafts) {
+  TreeTcCut cut{};
+  const long long share = run.end - run.at;              // (only the last block's may be shorter, and it cuts nothing)
+  bool ok = true;
+  while (run.next(p, block)) {
+    if (run.i0 == 0 && !run.last) {
+      const long long first_tile = run.at - run.i1;
+      cut.pieces = (int)((first_tile + run.tiles - 1) / share) - block / p.group + 1;
+      cut.b = run.b;
+      cut.hk = run.hk;
+      cut.rb = run.rb;
+      cut.part = run.part;
+    }
+    if (ok && run.i1 > run.n_state) ok = drafts(run);
+  }
+  return cut;
+}
 
 // Four floats of shared memory as two pairs.  (Volatile: read again where they are needed again, instead of being kept in
 // registers that the rows need.)
@@ -566,35 +589,25 @@ __global__ void __launch_bounds__(TreeTcShape<D, FMT, NT>::THREADS, 1)
   } else if (warp == HELPER) {
     // ============================== helper warp ==============================
     int done = 0;                                          // pieces with drafts so far
-    // For the second kernel: the job that starts in this run and goes on in another, if there is one.
-    TreeTcCut cut{};
-    const long long share = run.end - run.at;              // (only the last block's may be shorter, and it cuts nothing)
-    while (run.next(p, blockIdx.x)) {
-      if (run.i0 == 0 && !run.last) {
-        const long long first_tile = run.at - run.i1;
-        cut.pieces = (int)((first_tile + run.tiles - 1) / share) - (int)blockIdx.x / p.group + 1;
-        cut.b = run.b;
-        cut.hk = run.hk;
-        cut.rb = run.rb;
-        cut.part = run.part;
-      }
-      if (run.i1 <= run.n_state) continue;
-      if (done > 0 && !warp_wait(&bar_af, (uint32_t)((done - 1) & 1))) break;
-      for (int i = lane; i < p.N; i += 32) par_s[i] = p.parents ? p.parents[(long long)i * p.B + run.b] : i - 1;
+    // (The list is for the second kernel.)
+    const TreeTcCut cut = tree_tc_walk(run, p, blockIdx.x, [&](const TreeTcRun& r) {
+      if (done > 0 && !warp_wait(&bar_af, (uint32_t)((done - 1) & 1))) return false;
+      for (int i = lane; i < p.N; i += 32) par_s[i] = p.parents ? p.parents[(long long)i * p.B + r.b] : i - 1;
       __syncwarp();
       for (int i = lane; i < p.N; i += 32) tree_ancestor_bits<S::WORDS>(i, p.parents == nullptr, par_s, anc_s[i]);
       bool odd = false;
 #pragma unroll 4
       for (int e = lane; e < p.N * (D / 8); e += 32) {
         uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.v_new) +
-                                                  (((long long)(e / (D / 8)) * p.B + run.b) * p.Hkv + run.hk) * D + (e % (D / 8)) * 8);
+                                                  (((long long)(e / (D / 8)) * p.B + r.b) * p.Hkv + r.hk) * D + (e % (D / 8)) * 8);
         odd |= tree_drop_odd(w);
       }
       odd = __any_sync(0xffffffffu, odd) != 0;
       if (lane == 0) odd_s = odd;
       warp_arrive(&bar_a, lane);
       ++done;
-    }
+      return true;
+    });
     if (lane == 0) static_cast<TreeTcCut*>(p.cuts)[blockIdx.x] = cut;
   } else {
     // ============================== soft-max: two threads per row ==============================

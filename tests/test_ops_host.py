@@ -1,11 +1,15 @@
 """Host-side checks of the operators around the decode step (rotary positions, 8-bit state, drafted tokens): every
 refusal comes before anything is launched, so none of them needs a GPU."""
 import ctypes
+import os
+import random
+import subprocess
 
 import pytest
 import torch
 
 import paper_2401_06104_b200 as tova
+from paper_2401_06104_b200 import build as tbuild
 
 NULL, UNSUPPORTED, SHAPE, ALIGN, CUDA = -1, -3, -2, -4, -7
 A = ctypes.c_void_p(4096)          # never dereferenced: the calls below are refused
@@ -173,3 +177,35 @@ def test_valid_calls_fail_loudly_without_a_device():
     assert L.tova_tree_attention(ctypes.byref(tree_cfg()), A, A, None, None, None, 1, A, A, A, 1, None, A, A, 1 << 40, None) == CUDA
     c = tova.tova_verify_config(1, 1, 8, tova.TOVA_DTYPE_FP32, 0)
     assert L.tova_verify_draft(ctypes.byref(c), A, A, A, None, A, A, A, A, A, None) == CUDA
+
+
+@pytest.fixture(scope="module")
+def tree_runs(tmp_path_factory):
+    src = os.path.join(os.path.dirname(os.path.abspath(__file__)), "tree_runs_host.cu")
+    so = str(tmp_path_factory.mktemp("tree_runs") / "tree_runs.so")
+    flags = [f for f in tbuild.NVCC_FLAGS if f not in ("-O3", "-lineinfo")]
+    subprocess.run([tbuild._nvcc(), *flags, "-O1", "-o", so, src], check=True, capture_output=True, text=True)
+    f = ctypes.CDLL(so).check_tree_runs
+    f.argtypes = [ctypes.c_int] * 5 + [ctypes.c_void_p] + [ctypes.c_int] * 6
+    return f
+
+
+def test_tree_runs_cover_every_job_whatever_wait_runs_out(tree_runs):
+    """More than 64 rows of drafts: the tiles of all jobs are dealt out to the blocks exactly once, and the list for the joining
+    kernel holds every job that was cut - also where a wait of the block ran out before it came to that job, since the NaN
+    that its pieces then hold must reach the result.  (The wait is the host's stand-in: none runs out on a GPU here.)"""
+    rng = random.Random(5)
+    for case in range(400):
+        B, Hkv, G = rng.choice([1, 2, 7, 41]), rng.choice([1, 2, 8]), rng.choice([1, 4, 8, 32])
+        N = rng.randint(1, 256)
+        cap = rng.choice([1, 130, 700, 5000, 70000])
+        n_live = rng.randint(0, cap)
+        lens = (ctypes.c_int * B)(*[rng.choice([0, 1, 128, n_live, rng.randint(0, cap)]) for _ in range(B)]) if rng.random() < 0.7 else None
+        sm = rng.choice([1, 5, 100, 148])
+        row_blocks = -(-N * G // rng.choice([128, 256]))
+        rounds = -(-row_blocks // sm)
+        group = -(-row_blocks // rounds)
+        blocks = sm // group * group
+        for fail_at in (-1, 0, 1, 5):
+            rc = tree_runs(B, Hkv, G, N, cap, lens, n_live, blocks, group, rounds, rng.choice([1, 4]), fail_at)
+            assert rc == 0, (rc, B, Hkv, G, N, cap, lens and list(lens), n_live, blocks, group, rounds, fail_at)
