@@ -538,8 +538,10 @@ int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const flo
  *   q [N,B,H,D], k, v [N,B,Hkv,D], out [N,B,H,D]   all in cfg->dtype
  * Logits, soft-max and sums are fp32; fp32 configurations form every product in
  * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the
- * result is.  The result does not depend on n_live, lens, other sequences or the
- * GPU beyond the order of fp32 sums, and is the same bits every time.
+ * result is (an answer for one token is so less exact than tova_decode_step's).
+ * n_live, lens, the other sequences and the GPU's size decide how the columns are
+ * cut: they change the order of fp32 sums and, in bf16, the maximum against which a
+ * weight is rounded, and nothing else.  The same call gives the same bits every time.
  *   tova_tree_workspace_bytes   device bytes that calls of this configuration and
  *          N need for partial results, for every length up to n_live (0 is
  *          possible: none; an invalid configuration gives (size_t)-1).  It asks

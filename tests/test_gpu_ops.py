@@ -1137,3 +1137,41 @@ def test_tree_e4m3_codes_that_are_not_numbers(dtype, cut):
     cfg = tova.tova_quant_config(B, Hkv, D, L, tova.TOVA_DTYPE_FP32, tova.TOVA_FORMAT_E4M3)
     tova.tova_quant_read(cfg, K2, ks, V2, vs, L, back, None)
     assert int(back.isnan().sum()) == 1 and bool(back[row, 0, Hkv - 1, d].isnan())
+
+
+@pytest.mark.parametrize("fmt", ["plain", "int8"])
+@pytest.mark.parametrize("N", [1, 6, 14, 30])
+def test_tree_results_under_other_cuts(fmt, N):
+    """The same sequence under other bounds on the length, and beside other sequences: the columns are cut differently, so
+    fp32 sums come in another order and a weight may be rounded to bf16 against another reference, and that is all."""
+    H, Hkv, D, L, cap = 8, 2, 128, 777, 20000
+    g = gen(61)
+    one = [randn(g, N, 1, n, D).bfloat16() for n in (H, Hkv, Hkv)]
+    Kf, Vf = randn(g, L, 1, Hkv, D).bfloat16(), randn(g, L, 1, Hkv, D).bfloat16()
+    got, ref = [], None
+    for B, n_live in ((1, L), (1, 3000), (1, cap), (2, cap), (9, 5000), (150, 1000)):
+        c = min(cap, n_live)
+        q, k, v = (torch.cat([x, randn(g, N, B - 1, x.shape[2], D).bfloat16()], 1).contiguous() for x in one)
+        Kb, Vb = (torch.cat([x, randn(g, L, B - 1, Hkv, D).bfloat16()], 1) for x in (Kf, Vf))
+        ks = vs = None
+        if fmt == "plain":
+            K, V = (torch.zeros(B, Hkv, c, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            K[:, :, :L], V[:, :, :L] = Kb.permute(1, 2, 0, 3), Vb.permute(1, 2, 0, 3)
+            Kd, Vd = K[:1, :, :L].double(), V[:1, :, :L].double()
+        else:
+            (K, V), (ks, vs) = new_state(B, Hkv, c, D, fmt)
+            tova.tova_quant_write(tova.tova_quant_config(B, Hkv, D, c, tova.TOVA_DTYPE_BF16, FMT[fmt]), Kb.contiguous(), Vb.contiguous(), L, K, ks, V, vs)
+            Kd, Vd = K[:1, :, :L].double() * ks[:1, :, :L, None].double(), V[:1, :, :L].double() * vs[:1, :, :L, None].double()
+        lens = torch.tensor([L] + [max(1, (L * b) // B) for b in range(1, B)], dtype=torch.int32, device=DEV)
+        cfg = tova.tova_tree_config(B, H, Hkv, D, c, tova.TOVA_DTYPE_BF16, FMT[fmt], 0.0)
+        ws = torch.empty(max(16, tova.tova_tree_workspace_bytes(cfg, c, N)), dtype=torch.uint8, device=DEV)
+        out = torch.empty_like(q)
+        tova.tova_tree_attention(cfg, K, V, c, q, k, v, N, out, ws, lens=lens, k_scale=ks, v_scale=vs)
+        got.append(out[:, :1].double())
+        ref = ref or tree_reference(*one, Kd, Vd, [L], None)
+    want, wv, reach, _ = ref
+    # either result is within the tolerance of the exact one, apart from each result's own rounding
+    tol = 2 * tree_tolerance("bf16", D, L + N, want, wv, reach)
+    for x in got:
+        assert bool(((x - want).abs() <= tol / 2).all())
+        assert bool(((x - got[0]).abs() <= tol).all())
