@@ -1175,3 +1175,16 @@ def test_tree_results_under_other_cuts(fmt, N):
     for x in got:
         assert bool(((x - want).abs() <= tol / 2).all())
         assert bool(((x - got[0]).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("N, B, V, chain", [(6, 2, 32769, False), (9, 2, 50001, False), (3, 1, 128256, True), (20, 2, 131072, False)])
+def test_verify_large_vocabularies(dtype, draft, N, B, V, chain):
+    """Rows longer than the registers of a cluster hold are read again for every sum."""
+    p, q, tok, par, pc, u, us = verify_inputs(N, B, V, dtype, N + V, chain, draft)
+    n, path, out = run_verify(p, q, tok, par, u, us, dtype)
+    for b in range(B):
+        want = verify_reference(p[:, b].double().tolist(), None if q is None else q[:, b].double().tolist(), tok[:, b].tolist(),
+                                pc[:, b].tolist(), u[:, b].double().tolist(), float(us[b].double()))
+        assert (int(n[b]), path[:, b].tolist(), out[:, b].tolist()) == want, b
