@@ -82,14 +82,16 @@ __device__ __forceinline__ void verify_load8(const void* p, long long row, int i
   }
 }
 
-// A probability that counts: an entry of p that is an infinity or NaN is none, and negative ones are none either.
-__device__ __forceinline__ double verify_prob(float p) { return p > 0.f && p < INFINITY ? (double)p : 0.0; }
+// A probability that counts: an entry of p that is an infinity or NaN is none, and negative ones are none either.  (The bits
+// of positive finite numbers, and of 0, are the smallest.)
+__device__ __forceinline__ double verify_prob(float p) { return __float_as_uint(p) < 0x7f800000u ? (double)p : 0.0; }
 
 // The weight that the last token is drawn with, or a term of Z: max(0, p - S q).  Where p or q is not finite it is zero, so
-// that every sum is finite and the draw always finds a token where there is one.
+// that every sum is finite and the draw always finds a token where there is one.  (One integer comparison of the high word, in
+// place of two of 64 bits.)
 __device__ __forceinline__ double verify_weight(float p, float q, double S) {
   const double w = (double)p - S * (double)q;
-  return w > 0.0 && w < (double)INFINITY ? w : 0.0;
+  return (uint32_t)__double2hiint(w) < 0x7ff00000u ? w : 0.0;
 }
 
 template <typename T>
