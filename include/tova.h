@@ -486,7 +486,9 @@ int tova_rope_apply(const tova_rope* r, const void* q, int64_t q_stride, const v
                     int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* cuda_stream);
 int tova_rope_destroy(tova_rope* r);
 
-/* A state in 8 bits: half the bytes of a bf16 state per step and per sequence.
+/* A state in 8 bits: half the bytes of a bf16 state per sequence.  Attention over it
+ * takes no less time than over a bf16 state (its codes are converted on the way).
+ * It is the caller's: a tova_cache holds none, and no call chooses a row to drop.
  * codes k, v [B,Hkv,capacity,D] one byte each, scales [B,Hkv,capacity] fp32, one
  * for each row of K and of V:
  *   a = max |x_d|,  Q = 127 (int8) or 448 (e4m3),  scale = fp32(a / Q),
@@ -499,7 +501,9 @@ int tova_rope_destroy(tova_rope* r);
  *          go to slots [T,B] int32, or NULL: first_slot + token, which must lie
  *          in the state.  A listed slot outside 0..capacity-1 skips the row;
  *          where a call lists a slot of a sequence twice, the later token's row
- *          stands.  All other rows stay as they are.
+ *          stands.  All other rows stay as they are.  The call looks, for its rows,
+ *          through the slots of all later tokens, so that the time of long listed
+ *          prompts grows with the square of n_tokens.
  *   tova_quant_read    the rows of those slots as k, v [T,B,Hkv,D] in cfg->dtype,
  *          fp32(code * scale) rounded to it; a slot outside the state gives
  *          zeros.  k or v may be NULL. */
@@ -554,7 +558,7 @@ int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const flo
  *          Refused (TOVA_ERR_UNSUPPORTED) under position compression, whose keys
  *          are not rotated. */
 typedef struct {
-  int32_t batch, n_q_heads, n_kv_heads, head_dim, capacity; /* as in tova_config               */
+  int32_t batch, n_q_heads, n_kv_heads, head_dim, capacity; /* as in tova_config; batch * n_kv_heads <= 65535 */
   int32_t dtype;                                            /* of q, k, v, out, and plain states */
   int32_t format;                                           /* TOVA_FORMAT_* of K and V          */
   float sm_scale;                                           /* 0 selects 1/sqrt(head_dim)        */

@@ -11,8 +11,10 @@
 // correctly rounded quotients of a row, some 20 instructions each, are not formed by all of its lanes.  A group of lanes
 // holds eight rows in registers (16 bytes a lane and row, all loaded before the first is used), reduces their eight maxima
 // in one transposing tree that leaves row j's in lane j, forms each row's quotients once, in that lane, and passes them round.
-// Measured: 8 x 4096 tokens of 8 heads x 128 from bf16 to int8 (203 MB) 41 us, 4.9 TB/s; a state of 4 x 4001 rows of 32 heads
-// back from e4m3 to bf16 (397 MB) 68 us, 5.8 TB/s; one step's rows of 32 sequences 2.6 us.
+// Measured (GPU time, in a captured graph): 8 x 4096 tokens of 8 heads x 128 from bf16 to int8 (203 MB) 41 us, 4.9 TB/s; a state
+// of 4 x 4001 rows of 32 heads back from e4m3 to bf16 (397 MB) 68 us, 5.8 TB/s; one step's rows of 32 sequences 2.7 us.
+// Listed slots are another matter: every block looks through those of all later tokens, T^2 / 16 reads a sequence.  The first
+// case with its slots listed takes 59 us, 32768 tokens of one sequence 181 (contiguous 41), 65536 of 4 heads 631 (61).
 #pragma once
 
 #include "tova_device.cuh"

@@ -10,7 +10,10 @@
 // The map reads and writes every component once and does three operations on it: DRAM bound.  A block takes a few
 // tokens; their cosines and sines are formed once - the angle as a fraction of a turn in 64 bits, since p w_i in 32
 // bits is off by whole degrees at far positions, then sincospi in 32 - and serve all H + Hkv heads from shared memory.
-// Measured: 4 x 4096 tokens of 32 + 8 heads x 128 in bf16 (335 MB) 54 us, 6.2 TB/s; one step's 64 tokens 2.9 us.
+// Measured (GPU time, in a captured graph): 4 x 4096 tokens of 32 + 8 heads x 128 in bf16 (335 MB) 54 us, 6.2 TB/s; one step's
+// 64 tokens 2.8 us.  Four tokens a block are few bytes where heads are few or small, and half the bytes in flight where half a
+// head passes through: 4 x 16384 tokens of 8 + 2 heads x 64 (168 MB) 47 us, 3.6 TB/s; the first case with 64 of 128
+// components turning 67 us.
 #pragma once
 
 #include "tova_device.cuh"

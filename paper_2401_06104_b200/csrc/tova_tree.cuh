@@ -127,7 +127,7 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Plain-ALU kernel: every product in fp32.  Serves fp32 queries, whose results the tensor cores' bf16 operands could not
-// give (three bf16 terms a factor would take six contractions, as long as this).  A block takes R rows of the product (64,
+// give one contraction at a time (three bf16 terms a factor, six contractions, could; not built).  A block takes R rows of the product (64,
 // or 16 or 4 where there are no more) and a run of columns in tiles of 32, all in shared memory as fp32.  Bound by shared
 // memory and the FMA pipes together, so a thread does as much as it can with what it reads: 4 x 4 logits from eight 16-byte
 // reads (64 FMA), the weighted sum in 8 rows x 8 components from four (64 FMA; the weights lie transposed).  Keys of the next

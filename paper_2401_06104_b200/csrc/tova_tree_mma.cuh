@@ -9,8 +9,10 @@
 // runs form a cluster and join through distributed shared memory: a second kernel would cost a small call as much again.
 // O is rescaled only when some row's maximum moved.  The drafts are one more tile, copied
 // ahead like the others.  The weights are summed as they were rounded to bf16, so that what multiplies V adds up to one.
-// Measured: 8 chained drafts of 64 sequences over up to 1024 rows of 32 heads x 128 (738 MB) 138 us, 5.3 TB/s, DRAM bound; one
-// token over 1000 int8 rows of 8 KV heads 7.9 us, the latency of one cluster.
+// Measured (GPU time, in a captured graph): 8 chained drafts of 64 sequences over up to 1024 rows of 32 heads x 128 (738 MB) 139
+// us, 5.3 TB/s, DRAM bound; one token over 1000 int8 rows of 8 KV heads 8.2 us, the latency of one cluster.  Single steps of 64
+// sequences over 1024 rows of 32 heads: bf16 168 us (6.4 TB/s), int8 203, e4m3 206; over 32 x 4096 rows of 8 heads 108, 138,
+// 139: an 8-bit state's bytes would take half, the conversion of its codes takes longer.
 //
 // 8-bit states are converted on the way from shared memory to the matrix instructions' operands, each code once per
 // row group: int8 by pasting its 7 low bits and its sign bit behind the exponent of 128 (two bf16 numbers whose

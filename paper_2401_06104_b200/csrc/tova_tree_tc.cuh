@@ -32,9 +32,10 @@
 // A tile of 128 columns, not 64, because S = Q K^T reads both operands from shared memory: 8 KiB per 64 cycles of math
 // (128 x 128 x 16) are what shared memory delivers, 6 KiB per 32 cycles (128 x 64 x 16) are not.  TMEM: 256 columns per row
 // tile (S 128, O 128).  Every wait is bounded; one that runs out leaves NaN in the rows that the block had yet to write.
-// Measured: trees of 63 drafts, 32 sequences x up to 4000 bf16 rows, 32 query over 8 KV heads x 128 (89.5 GFLOP) 147 us, 610
-// TFLOP/s, bound by the round trips between contraction and soft-max; trees of 25, 4 x 16001 e4m3 rows, 8 query heads a KV head
-// (26.2 GFLOP) 90 us, 290 TFLOP/s, bound by the instructions of the conversion and the soft-max.
+// Measured (GPU time, in a captured graph; a call among others takes 162 and 96 us): trees of 63 drafts, 32 sequences x up to 4000
+// bf16 rows, 32 query over 8 KV heads x 128 (89.5 GFLOP) 146 us, 610 TFLOP/s, bound by the round trips between contraction and
+// soft-max; trees of 25, 4 x 16001 e4m3 rows, 8 query heads a KV head (26.2 GFLOP) 93 us, 280 TFLOP/s, bound by the
+// instructions of the conversion and the soft-max.
 #pragma once
 
 #include "tova_tree_mma.cuh"
@@ -58,9 +59,12 @@ struct TreeTcShape {
   static constexpr int SLOTS = (PLAIN && NT == 1 ? 5 : 4) * (128 / D);
   static constexpr int RAW = PLAIN ? 0 : TREE_TC_COLS * D;
   static constexpr int RAW_SLOTS = PLAIN ? 0 : 3 * (128 / D);
-  // Tiles whose scales are kept.  K of tile i takes the slot of a copy SLOTS positions back; when that has been consumed,
-  // the soft-max of tile i - SLOTS/2 - 1 has passed.
+  // Tiles whose scales are kept.  K of tile i takes the slot of a copy SLOTS positions back, K of tile j = i - SLOTS/2.  When
+  // that has been consumed, S of tile j is complete; with two S buffers it was issued behind the weights of tile j - 2, not
+  // of tile j - 1, so the soft-max of tile i - SLOTS/2 - 2 has passed and that tile's scales may be written over, and no later
+  // one's.
   static constexpr int SCALE_TILES = SLOTS / 2 + 2;
+  static_assert(PLAIN || (DOUBLE && SLOTS % 2 == 0 && SCALE_TILES >= SLOTS / 2 + 2), "a tile's scales outlast its soft-max");
   static constexpr int SCALES = PLAIN ? 0 : SCALE_TILES * 3 * TREE_TC_COLS * 4;
   static constexpr int SMEM = NT * Q_BYTES + SLOTS * SLOT + RAW_SLOTS * RAW + SCALES + 1024;
   static constexpr int TMEM_COLS = DOUBLE ? 512 : 256 * NT;
