@@ -605,6 +605,147 @@ int tova_verify_draft(const tova_verify_config* cfg, const void* target, const v
                       const int32_t* parents, const float* u, const float* u_sample, int32_t* n_accepted,
                       int32_t* path, int32_t* tokens_out, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Sequences of different lengths over an unbounded state.
+ *
+ * A tova_cache holds sequences that advance in lock step in a state of fixed
+ * capacity.  The calls below serve the arm that drops nothing (the state that
+ * the policies are compared with) to sequences that come and go: the projections
+ * become queries and keys (tova_norm_rope_apply), whole prompts one behind the
+ * other are attended to (tova_packed_attention) and their rows kept in pages of
+ * a pool (tova_paged_write), new tokens attend over the pages
+ * (tova_paged_attention), and the model's logits give the tokens' probabilities
+ * (tova_token_logprobs), with which a text's perplexity is formed.  The
+ * conventions are those of the section above: plain tensors, caller-owned memory,
+ * nothing kept between calls, any stream, argument errors found on the host
+ * before anything is launched.  Two calls that may run at the same time, captured
+ * ones among them, need a workspace each.  Packed tokens: [N,...], the tokens of
+ * sequence b are offsets[b] .. offsets[b+1] - 1, rows behind offsets[S] are left
+ * alone.  Lengths, offsets and page tables are read on the device at the time of
+ * the call's execution, so that a captured call follows them.
+ * ------------------------------------------------------------------------- */
+
+/* Norms of queries and keys, each head by itself, with the rotation of
+ * tova_rope_apply in the same pass: a head's row x becomes
+ *   R_p (x r w),  r = (mean of x^2 + eps)^(-1/2),
+ * w the weights q_weight or k_weight [D] (the handle's dtype; NULL: ones), the
+ * same for all heads; all D components are normed, the handle's rotary_dim of
+ * them turn.  Arguments, strides and aliasing as for tova_rope_apply.
+ * fp32 arithmetic (a sum of squares beyond its range gives zeros).
+ *   tova_norm_rope_backward   from the inputs q, k of that call and the gradients
+ *          dq_out, dk_out of its results: the gradients dq, dk of its inputs and,
+ *          where asked for, dq_weight, dk_weight [D] fp32 of the weights, summed
+ *          over all rows in an order of their own that is the same every time
+ *          (zeros where there are no tokens).  k, dk_out and dk come together or
+ *          are all NULL (then dk_weight is zeros).  dq may be dq_out, dk dk_out.
+ *          Every sum is overwritten, none added to.
+ *   tova_norm_rope_workspace_bytes   device bytes that the backward call needs for
+ *          any number of tokens up to n_tokens; (size_t)-1 for a NULL handle or
+ *          negative n_tokens. */
+int tova_norm_rope_apply(const tova_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* q_weight, const void* k_weight, float eps, int32_t n_tokens,
+                         const int32_t* positions, int32_t first_pos, void* q_out, int64_t q_out_stride, void* k_out,
+                         int64_t k_out_stride, void* cuda_stream);
+size_t tova_norm_rope_workspace_bytes(const tova_rope* r, int32_t n_tokens);
+int tova_norm_rope_backward(const tova_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* q_weight, const void* k_weight, float eps, int32_t n_tokens,
+                            const int32_t* positions, int32_t first_pos, const void* dq_out, int64_t dq_out_stride,
+                            const void* dk_out, int64_t dk_out_stride, void* dq, int64_t dq_stride, void* dk,
+                            int64_t dk_stride, float* dq_weight, float* dk_weight, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+
+/* A state in pages.  K and V are pools of n_pages small states
+ * [n_pages,Hkv,page_rows,D]; row j of sequence b lies in page
+ * page_table[b][j / page_rows], at row j mod page_rows of it.  Pages may lie in
+ * any order and be shared by sequences (of their common beginning).  Entries of
+ * the table [B,max_pages] that no row needs are not looked at; an entry outside
+ * 0..n_pages-1 holds no rows: what would be written there is dropped, what would
+ * be read there has no weight.
+ *   tova_paged_write   rows k, v [N,Hkv,D] (strides as for tova_rope_apply) of
+ *          packed tokens: token i of sequence b goes to row first_rows[b] +
+ *          i - offsets[b] (first_rows [B] int32, NULL: 0).  offsets NULL: one token
+ *          a sequence, N <= B of them.  Rows that the table has no entry for are
+ *          dropped.  Where two tokens of a call go to the same place (pages that
+ *          sequences share) each 16 bytes there are one of theirs.
+ *   tova_paged_attention   one new token of every sequence over rows
+ *          0..lens[b]-1 (its own among them, if it has been written): q [B,H,D]
+ *          (q_stride elements between sequences, 0 = contiguous), out [B,H,D] in
+ *          cfg->dtype.  lens [B] are taken as 0..n_live, n_live <= max_pages *
+ *          page_rows being the most rows that any sequence has.  No rows: zeros.
+ *          A row of logits that are NaN, or all minus infinity, gives NaN.  Rows
+ *          behind the last, and pages that no row needs, may hold anything; a value
+ *          that is not finite in a row that is attended to makes its component of
+ *          the result not finite, NaN or infinite.
+ *          fp32: every product in fp32; bf16: weights as two bf16 terms.  How the
+ *          rows are cut (n_live, lens, the GPU's size) changes the order of fp32
+ *          sums, nothing else; the same call gives the same bits every time.
+ *   tova_paged_workspace_bytes   device bytes, for every n_live up to this one;
+ *          (size_t)-1 for an invalid configuration.  It asks the current device
+ *          for its SM count. */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim; /* as in tova_config                         */
+  int32_t n_pages;                                /* pages of the pool                         */
+  int32_t page_rows;                              /* a power of two, 1..32768                  */
+  int32_t max_pages;                              /* entries of the table per sequence         */
+  int32_t dtype;                                  /* of q, k, v, the pages and out             */
+  float sm_scale;                                 /* 0 selects 1/sqrt(head_dim)                */
+} tova_paged_config;
+int tova_paged_write(const tova_paged_config* cfg, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     int32_t n_tokens, const int32_t* offsets, const int32_t* first_rows, const int32_t* page_table,
+                     void* K, void* V, void* cuda_stream);
+size_t tova_paged_workspace_bytes(const tova_paged_config* cfg, int32_t n_live);
+int tova_paged_attention(const tova_paged_config* cfg, const void* K, const void* V, const int32_t* page_table,
+                         const int32_t* lens, int32_t n_live, const void* q, int64_t q_stride, void* out,
+                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Causal attention of packed prompts: token i of a sequence attends to itself and
+ * to the earlier tokens of its sequence (Eq. 4 and 7 while nothing is dropped).
+ *   q [N,H,D], k, v [N,Hkv,D]   strides as for tova_rope_apply (v may be a slice of
+ *          the projection), out [N,H,D], all in cfg->dtype
+ *   offsets [S+1] int32         rising; values outside 0..N are taken as the
+ *          nearest of them, a sequence that would end before it starts is empty.
+ *          Rows that belong to no sequence are not written
+ * Logits, soft-max and sums are fp32; fp32 configurations form every product in
+ * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the
+ * result is.  A token's result does not depend on later tokens or on other
+ * sequences, whatever they hold.  A token whose logits are NaN, or all minus
+ * infinity, gets NaN.  The same call gives the same bits every time.
+ *   tova_packed_workspace_bytes   device bytes for n_tokens tokens (0 is possible:
+ *          none; (size_t)-1 for an invalid configuration).  It asks the current
+ *          device for its SM count. */
+typedef struct {
+  int32_t n_seqs;                                 /* S, 1..65535                               */
+  int32_t n_q_heads, n_kv_heads, head_dim;        /* as in tova_config                         */
+  int32_t dtype;
+  float sm_scale;                                 /* 0 selects 1/sqrt(head_dim)                */
+} tova_packed_config;
+size_t tova_packed_workspace_bytes(const tova_packed_config* cfg, int32_t n_tokens);
+int tova_packed_attention(const tova_packed_config* cfg, const void* q, int64_t q_stride, const void* k,
+                          int64_t k_stride, const void* v, int64_t v_stride, int32_t n_tokens,
+                          const int32_t* offsets, void* out, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream);
+
+/* Log probabilities of given tokens under rows of logits [T,V] (natural
+ * logarithms; exp of minus their mean is a text's perplexity):
+ *   logprobs [T]      log softmax(logits)[tokens[t]]; minus infinity for a token
+ *                     outside 0..V-1
+ *   entropy [T]       -sum_x p(x) log p(x) (a logit of minus infinity adds
+ *                     nothing), or NULL
+ *   top_ids, top_logprobs [T,n_top]   the n_top largest logits, in order; equal
+ *                     ones in the order of their tokens (-0 equals 0); NULL where
+ *                     n_top is 0
+ * Statistics are fp32.  A row with a NaN, with +infinity, or with nothing but minus
+ * infinity has NaN for numbers; its top_ids are still the order of its logits, NaN
+ * before everything else. */
+typedef struct {
+  int32_t vocab;        /* V, 1..2^24                                                          */
+  int32_t dtype;        /* of the logits                                                       */
+  int32_t n_top;        /* 0..32, at most V                                                    */
+  int64_t row_stride;   /* elements between rows; 0 = V                                        */
+} tova_logprobs_config;
+int tova_token_logprobs(const tova_logprobs_config* cfg, const void* logits, int32_t n_tokens, const int32_t* tokens,
+                        float* logprobs, float* entropy, int32_t* top_ids, float* top_logprobs, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

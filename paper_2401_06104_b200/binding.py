@@ -64,6 +64,22 @@ class tova_verify_config(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
 
 
+class tova_paged_config(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
+
+
+class tova_packed_config(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
+
+
+class tova_logprobs_config(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_top", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -157,6 +173,27 @@ def lib() -> ctypes.CDLL:
         L.tova_cache_tree_workspace_bytes.argtypes = [vp, i32]
         L.tova_cache_tree_attention.restype = ctypes.c_int
         L.tova_cache_tree_attention.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        szt, f32 = ctypes.c_size_t, ctypes.c_float
+        L.tova_norm_rope_apply.restype = ctypes.c_int
+        L.tova_norm_rope_apply.argtypes = [vp, vp, i64, vp, i64, vp, vp, f32, i32, vp, i32, vp, i64, vp, i64, vp]
+        L.tova_norm_rope_workspace_bytes.restype = szt
+        L.tova_norm_rope_workspace_bytes.argtypes = [vp, i32]
+        L.tova_norm_rope_backward.restype = ctypes.c_int
+        L.tova_norm_rope_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, f32, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp,
+                                              i64, vp, vp, vp, szt, vp]
+        L.tova_paged_write.restype = ctypes.c_int
+        L.tova_paged_write.argtypes = [ctypes.POINTER(tova_paged_config), vp, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp]
+        L.tova_paged_workspace_bytes.restype = szt
+        L.tova_paged_workspace_bytes.argtypes = [ctypes.POINTER(tova_paged_config), i32]
+        L.tova_paged_attention.restype = ctypes.c_int
+        L.tova_paged_attention.argtypes = [ctypes.POINTER(tova_paged_config), vp, vp, vp, vp, i32, vp, i64, vp, vp, szt, vp]
+        L.tova_packed_workspace_bytes.restype = szt
+        L.tova_packed_workspace_bytes.argtypes = [ctypes.POINTER(tova_packed_config), i32]
+        L.tova_packed_attention.restype = ctypes.c_int
+        L.tova_packed_attention.argtypes = [ctypes.POINTER(tova_packed_config), vp, i64, vp, i64, vp, i64, i32, vp, vp, vp,
+                                            szt, vp]
+        L.tova_token_logprobs.restype = ctypes.c_int
+        L.tova_token_logprobs.argtypes = [ctypes.POINTER(tova_logprobs_config), vp, i32, vp, vp, vp, vp, vp, vp]
         L.tova_verify_draft.restype = ctypes.c_int
         L.tova_verify_draft.argtypes = [ctypes.POINTER(tova_verify_config), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.tova_strerror.restype = ctypes.c_char_p
@@ -508,6 +545,54 @@ class TovaRope:
         _call(lib().tova_rope_apply, "tova_rope_apply", dev, stream, self._h, _a(q), qs, _a(k), ks, n_tokens, _a(positions),
               first_pos, 1 if inverse else 0, _a(q_out), qos, _a(k_out), kos)
 
+    def _pairs(self, n_tokens: int, *pairs):
+        """Strides of (q-shaped, k-shaped) pairs of tensors, whose keys are all there or all None."""
+        B, H, Hkv, D, t = self._dims
+        dev = pairs[0][0].get_device()
+        got = []
+        for a, b in pairs:
+            if (b is None) != (pairs[0][1] is None):
+                raise ValueError("the keys' tensors come together")
+            got.append(_rows(a, n_tokens, B, H, D, t, dev))
+            got.append(0 if b is None else _rows(b, n_tokens, B, Hkv, D, t, dev))
+        return dev, got
+
+    def tova_norm_rope_apply(self, q, k, n_tokens: int, q_out, k_out, q_weight=None, k_weight=None, eps: float = 1e-6,
+                             positions=None, first_pos: int = 0, stream=None) -> None:
+        """Each head of q [T,B,H,D] and k [T,B,Hkv,D] (or None) normed, times its weights [D] (None: ones), and rotated,
+        into q_out, k_out; all may be evenly strided over (T, B)."""
+        dev, (qs, ks, qos, kos) = self._pairs(n_tokens, (q, k), (q_out, k_out))
+        B, H, Hkv, D, t = self._dims
+        _need(q_weight, D, t, dev)
+        _need(k_weight, D, t, dev)
+        _need(positions, n_tokens * B, torch.int32, dev)
+        _call(lib().tova_norm_rope_apply, "tova_norm_rope_apply", dev, stream, self._h, _a(q), qs, _a(k), ks, _a(q_weight),
+              _a(k_weight), eps, n_tokens, _a(positions), first_pos, _a(q_out), qos, _a(k_out), kos)
+
+    def tova_norm_rope_workspace_bytes(self, n_tokens: int) -> int:
+        n = int(lib().tova_norm_rope_workspace_bytes(self._h, int(n_tokens)))
+        if n == _NO_SIZE:
+            raise TovaError(-2, "tova_norm_rope_workspace_bytes rejected the size")
+        return n
+
+    def tova_norm_rope_backward(self, q, k, dq_out, dk_out, n_tokens: int, dq, dk, workspace, q_weight=None, k_weight=None,
+                                dq_weight=None, dk_weight=None, eps: float = 1e-6, positions=None, first_pos: int = 0,
+                                stream=None) -> None:
+        """The gradients dq, dk of tova_norm_rope_apply's inputs q, k, and dq_weight, dk_weight [D] fp32 (None: not asked
+        for) of its weights, from the gradients dq_out, dk_out of its results; workspace of
+        tova_norm_rope_workspace_bytes(n_tokens) bytes."""
+        dev, (qs, ks, gqs, gks, dqs, dks) = self._pairs(n_tokens, (q, k), (dq_out, dk_out), (dq, dk))
+        B, H, Hkv, D, t = self._dims
+        _need(q_weight, D, t, dev)
+        _need(k_weight, D, t, dev)
+        _need(dq_weight, D, torch.float32, dev)
+        _need(dk_weight, D, torch.float32, dev)
+        _need(positions, n_tokens * B, torch.int32, dev)
+        _need_workspace(workspace, dev)
+        _call(lib().tova_norm_rope_backward, "tova_norm_rope_backward", dev, stream, self._h, _a(q), qs, _a(k), ks, _a(q_weight),
+              _a(k_weight), eps, n_tokens, _a(positions), first_pos, _a(dq_out), gqs, _a(dk_out), gks, _a(dq), dqs, _a(dk), dks,
+              _a(dq_weight), _a(dk_weight), _a(workspace), _bytes(workspace))
+
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
             lib().tova_rope_destroy(self._h)
@@ -601,6 +686,97 @@ def tova_verify_draft(cfg: tova_verify_config, target, draft, tokens, u, u_sampl
     _need(tokens_out, (N + 1) * B, torch.int32, dev)
     _call(lib().tova_verify_draft, "tova_verify_draft", dev, stream, _byref(cfg), _a(target), _a(draft), _a(tokens),
           _a(parents), _a(u), _a(u_sample), _a(n_accepted), _a(path), _a(tokens_out))
+
+
+# -- sequences of different lengths over an unbounded state --------------------------------------------------------
+
+def _packed_rows(t, n_tokens: int, heads: int, dim: int, dtype, device: int) -> int:
+    """Checks [N,heads,dim] with contiguous heads and evenly spaced rows; their element stride."""
+    if t.dtype is not dtype or t.get_device() != device or device < 0:
+        _misfit(t, 0, dtype, device)
+    if t.dim() != 3 or t.shape[0] < n_tokens or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"expected [{n_tokens},{heads},{dim}], got {tuple(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if n_tokens <= 1:
+        s0 = heads * dim
+    if s0 < heads * dim or (s1 != dim and heads > 1) or s2 != 1:
+        raise ValueError(f"rows of {tuple(t.shape)} with strides {t.stride()} are not evenly spaced with contiguous heads")
+    return s0
+
+
+def _need_pages(cfg, K, V, page_table, dtype, device: int) -> None:
+    n = cfg.n_pages * cfg.n_kv_heads * cfg.page_rows * cfg.head_dim
+    _need(K, n, dtype, device)
+    _need(V, n, dtype, device)
+    _need(page_table, cfg.batch * cfg.max_pages, torch.int32, device)
+
+
+def tova_paged_write(cfg: tova_paged_config, k, v, n_tokens: int, page_table, K, V, first_rows=None, offsets=None,
+                     stream=None) -> None:
+    """Rows k, v [N,Hkv,D] (evenly strided) of packed tokens into the pages K, V [pages,Hkv,rows,D]: token i of sequence b
+    to its row first_rows[b] + i - offsets[b]; offsets [B+1] None: one token a sequence."""
+    t, dev, H, D = _TORCH_TYPE.get(cfg.dtype), k.get_device(), cfg.n_kv_heads, cfg.head_dim
+    ks, vs = _packed_rows(k, n_tokens, H, D, t, dev), _packed_rows(v, n_tokens, H, D, t, dev)
+    _need_pages(cfg, K, V, page_table, t, dev)
+    _need(first_rows, cfg.batch, torch.int32, dev)
+    _need(offsets, cfg.batch + 1, torch.int32, dev)
+    _call(lib().tova_paged_write, "tova_paged_write", dev, stream, _byref(cfg), _a(k), ks, _a(v), vs, n_tokens, _a(offsets),
+          _a(first_rows), _a(page_table), _a(K), _a(V))
+
+
+def tova_paged_workspace_bytes(cfg: tova_paged_config, n_live: int) -> int:
+    n = int(lib().tova_paged_workspace_bytes(_byref(cfg), int(n_live)))
+    if n == _NO_SIZE:
+        raise TovaError(-2, "tova_paged_workspace_bytes rejected the shape")
+    return n
+
+
+def tova_paged_attention(cfg: tova_paged_config, K, V, page_table, lens, n_live: int, q, out, workspace=None,
+                         stream=None) -> None:
+    """Attention of one new token of every sequence, q [B,H,D] (evenly strided), over the lens[b] <= n_live rows that it
+    has in the pages; out [B,H,D] in the type of q."""
+    t, dev, B, H, D = _TORCH_TYPE.get(cfg.dtype), q.get_device(), cfg.batch, cfg.n_q_heads, cfg.head_dim
+    qs = _packed_rows(q, B, H, D, t, dev)
+    _need_pages(cfg, K, V, page_table, t, dev)
+    _need(lens, B, torch.int32, dev)
+    _need(out, B * H * D, t, dev)
+    _need_workspace(workspace, dev)
+    _call(lib().tova_paged_attention, "tova_paged_attention", dev, stream, _byref(cfg), _a(K), _a(V), _a(page_table), _a(lens),
+          n_live, _a(q), qs, _a(out), _a(workspace), _bytes(workspace))
+
+
+def tova_packed_workspace_bytes(cfg: tova_packed_config, n_tokens: int) -> int:
+    n = int(lib().tova_packed_workspace_bytes(_byref(cfg), int(n_tokens)))
+    if n == _NO_SIZE:
+        raise TovaError(-2, "tova_packed_workspace_bytes rejected the shape")
+    return n
+
+
+def tova_packed_attention(cfg: tova_packed_config, q, k, v, n_tokens: int, offsets, out, workspace=None, stream=None) -> None:
+    """Causal attention of packed sequences q [N,H,D], k, v [N,Hkv,D] (each evenly strided), sequence b being the tokens
+    offsets[b] .. offsets[b+1] - 1 (int32, on the GPU); out [N,H,D] in the type of q."""
+    t, dev, H, Hkv, D = _TORCH_TYPE.get(cfg.dtype), q.get_device(), cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    qs, ks, vs = (_packed_rows(x, n_tokens, h, D, t, dev) for x, h in ((q, H), (k, Hkv), (v, Hkv)))
+    _need(offsets, cfg.n_seqs + 1, torch.int32, dev)
+    _need(out, n_tokens * H * D, t, dev)
+    _need_workspace(workspace, dev)
+    _call(lib().tova_packed_attention, "tova_packed_attention", dev, stream, _byref(cfg), _a(q), qs, _a(k), ks, _a(v), vs,
+          n_tokens, _a(offsets), _a(out), _a(workspace), _bytes(workspace))
+
+
+def tova_token_logprobs(cfg: tova_logprobs_config, logits, n_tokens: int, tokens, logprobs, entropy=None, top_ids=None,
+                        top_logprobs=None, stream=None) -> None:
+    """Log probabilities [T] of tokens [T] int32 under logits [T,V] (rows cfg.row_stride elements apart), fp32; entropy [T]
+    or None; top_ids [T,n_top] int32 and top_logprobs [T,n_top] (None where cfg.n_top is 0)."""
+    t, dev, T = _TORCH_TYPE.get(cfg.dtype), logits.get_device(), n_tokens
+    _need(logits, (T - 1) * (cfg.row_stride or cfg.vocab) + cfg.vocab if T > 0 else 0, t, dev)
+    _need(tokens, T, torch.int32, dev)
+    _need(logprobs, T, torch.float32, dev)
+    _need(entropy, T, torch.float32, dev)
+    _need(top_ids, T * cfg.n_top, torch.int32, dev)
+    _need(top_logprobs, T * cfg.n_top, torch.float32, dev)
+    _call(lib().tova_token_logprobs, "tova_token_logprobs", dev, stream, _byref(cfg), _a(logits), T, _a(tokens), _a(logprobs),
+          _a(entropy), _a(top_ids), _a(top_logprobs))
 
 
 def to_device(x, dtype: int, device="cuda:0") -> torch.Tensor:

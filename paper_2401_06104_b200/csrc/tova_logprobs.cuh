@@ -1,0 +1,326 @@
+// Log probabilities of given tokens, entropy, the most probable alternatives (sm_100a).
+//
+// A row x of V logits:  m = max x,  S = sum exp(x - m),  E = sum exp(x - m) (x - m);
+//   log p(t) = (x_t - m) - log S,   entropy = log S - E / S,   and the n largest logits, equal ones in the tokens' order.
+//
+// One pass over the row, in which every thread keeps a maximum, S and E against it, rescaled when the maximum moves; joined at
+// the end.  DRAM bound for many rows.  The n largest need no second pass over the row: they lie in the shares of the n threads
+// whose maxima are the largest (equal maxima: whose first such element comes first), since every other thread's elements have
+// n ahead of them.  Those n shares, V / threads elements each, are read again, one by a warp; what is no less than the n-th of
+// the maxima is collected and ordered by counting.  Where more is collected than there is room for (rows of equal logits), n
+// passes over the shares find one after the other.
+//
+// A block per row; a cluster of eight blocks where rows are few, each with an eighth of the row, which join in the first
+// block's shared memory.
+#pragma once
+
+#include "tova_tc.cuh"
+
+namespace tova {
+
+constexpr int LOGPROBS_THREADS = 512, LOGPROBS_WARPS = LOGPROBS_THREADS / 32;
+constexpr int LOGPROBS_MAX_TOP = 32;
+constexpr int LOGPROBS_ROOM = 1024;          // elements collected at most
+constexpr int LOGPROBS_CLUSTER = 8;
+
+struct LogprobsParams {
+  const void* x;               // [T, V]
+  const int32_t* tokens;       // [T]
+  float *lp, *entropy;         // [T]; entropy may be NULL
+  int32_t* ids;                // [T, top]
+  float* top_lp;               // [T, top]
+  long long row_stride;
+  int T, V, top;
+};
+
+// A key that orders logits: larger is earlier.  -0 counts as 0; a NaN comes before everything.
+__device__ __forceinline__ uint32_t logit_key(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// ... with the token: distinct for all elements of a row, and never 0.
+__device__ __forceinline__ unsigned long long logit_order(uint32_t key, int token) {
+  return ((unsigned long long)key << 32) | (0xffffffffu - (uint32_t)token);
+}
+
+template <typename T>
+__device__ __forceinline__ float logit_at(const T* row, int i) { return (float)row[i]; }
+
+// N neighbouring elements that start at element i (a multiple of N behind the first 16-byte boundary, so i may be negative);
+// those outside lo .. hi - 1 are minus infinity.
+template <typename T>
+__device__ __forceinline__ void logits_load(const T* row, int i, int lo, int hi, float (&f)[Vec16<T>::N]) {
+  constexpr int N = Vec16<T>::N;
+  if (i >= lo && i + N <= hi) {
+    Vec16<T>::unpack(__ldg(reinterpret_cast<const uint4*>(row + i)), f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = i + e >= lo && i + e < hi ? logit_at(row, i + e) : -INFINITY;
+  }
+}
+
+template <typename T, bool CLUSTER>
+__global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const __grid_constant__ LogprobsParams p) {
+  constexpr int N = Vec16<T>::N, U = 4, TH = LOGPROBS_THREADS;
+  __shared__ float red_s[LOGPROBS_WARPS][3];
+  __shared__ uint32_t key_s[TH];
+  __shared__ int first_s[TH], win_s[LOGPROBS_MAX_TOP];
+  __shared__ unsigned long long pool_s[LOGPROBS_ROOM];
+  __shared__ unsigned long long best_s[LOGPROBS_MAX_TOP], warp_best_s[LOGPROBS_WARPS];
+  __shared__ uint32_t bar_s;
+  __shared__ int n_pool, n_win, n_tie, n_put;
+  // what the blocks of a cluster leave in the first one's memory
+  __shared__ float peer_red[CLUSTER ? LOGPROBS_CLUSTER : 1][3];
+  __shared__ unsigned long long peer_best[CLUSTER ? LOGPROBS_CLUSTER : 1][LOGPROBS_MAX_TOP];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = CLUSTER ? blockIdx.x % LOGPROBS_CLUSTER : 0;
+  const int t = CLUSTER ? blockIdx.x / LOGPROBS_CLUSTER : blockIdx.x;
+  const T* row = static_cast<const T*>(p.x) + t * p.row_stride;
+  const int shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));      // elements behind a 16-byte boundary
+  // This block's elements lo .. hi - 1; vector k starts at element base + k N.
+  int lo = 0, hi = p.V;
+  if constexpr (CLUSTER) {
+    cluster_arrive_release();                 // (waited for before the first store into another block's memory)
+    const int share = ((p.V + shift + N - 1) / N + LOGPROBS_CLUSTER - 1) / LOGPROBS_CLUSTER * N;
+    lo = min(p.V, max(0, rank * share - shift));
+    hi = min(p.V, max(lo, (rank + 1) * share - shift));
+  }
+  const int base = lo == 0 ? -shift : lo, n_vec = hi > lo ? (hi - base + N - 1) / N : 0;
+  const int top = min(p.top, hi - lo);        // of this block
+  constexpr float L2E = 1.4426950408889634f;
+
+  // --- the pass
+  float m = -INFINITY, s = 0.f, e = 0.f;
+  bool nan = false;
+  for (int k0 = tid; k0 < n_vec; k0 += U * TH) {
+    float f[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * TH;
+      if (k < n_vec) {
+        logits_load<T>(row, base + k * N, lo, hi, f[u]);
+      } else {
+#pragma unroll
+        for (int x = 0; x < N; ++x) f[u][x] = -INFINITY;
+      }
+    }
+    float most = f[0][0];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int x = 0; x < N; ++x) most = fmaxf(most, f[u][x]);
+    if (most > m) {
+      const float d = m - most;               // minus infinity at first
+      const float r = ex2_approx(d * L2E);
+      e = r * fmaf(fmaxf(d, -1e30f), s, e);
+      s *= r;
+      m = most;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        const float d = f[u][x] - ref, w = ex2_approx(d * L2E);
+        s += w;
+        e = fmaf(w, fmaxf(d, -1e30f), e);     // (a logit of minus infinity: 0 times something finite)
+        nan |= f[u][x] != f[u][x];
+      }
+  }
+  // --- maxima, sums of the block
+  const float mine = m;
+  {
+    const float wm = warp_max(m);
+    const float d = m - (wm == -INFINITY ? 0.f : wm), r = ex2_approx(d * L2E);
+    e = warp_sum(r * fmaf(fmaxf(d, -1e30f), s, e));
+    s = warp_sum(r * s);
+    if (lane == 0) {
+      red_s[warp][0] = wm;
+      red_s[warp][1] = s;
+      red_s[warp][2] = e;
+    }
+  }
+  key_s[tid] = nan ? 0xffffffffu : logit_key(mine);
+  if (tid == 0) n_pool = n_win = n_tie = n_put = 0;
+  __syncthreads();
+  // Joins n triples (m, S, E).
+  auto join = [&](const float (*red)[3], int n, float& gm, float& gs, float& ge) {
+    gm = -INFINITY;
+    for (int w = 0; w < n; ++w) gm = fmaxf(gm, red[w][0]);
+    gs = ge = 0.f;
+    const float ref = gm == -INFINITY ? 0.f : gm;
+    for (int w = 0; w < n; ++w) {
+      const float d = red[w][0] - ref, r = ex2_approx(d * L2E);
+      ge += r * fmaf(fmaxf(d, -1e30f), red[w][1], red[w][2]);
+      gs += r * red[w][1];
+    }
+  };
+  float gm, gs, ge;
+  join(red_s, LOGPROBS_WARPS, gm, gs, ge);
+
+  // --- the n largest of the block, best_s, in order
+  if (top > 0) {
+    const int active = min(TH, n_vec);        // threads with elements
+    // The n-th largest of the maxima (of all of them where there are fewer): the largest key that `want` maxima reach.
+    const int want = min(top, active);
+    if (warp == 0) {
+      uint32_t k[TH / 32];
+#pragma unroll
+      for (int i = 0; i < TH / 32; ++i) k[i] = lane + 32 * i < active ? key_s[lane + 32 * i] : 0u;
+      uint32_t at = 0;
+      for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t test = at | (1u << bit);
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < TH / 32; ++i) c += k[i] >= test;
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (c >= want) {
+          at = test;
+          if (c == want) {                    // the smallest of those that reach it is what is looked for
+            uint32_t low = 0xffffffffu;
+#pragma unroll
+            for (int i = 0; i < TH / 32; ++i)
+              if (k[i] >= test) low = min(low, k[i]);
+            at = __reduce_min_sync(0xffffffffu, low);
+            break;
+          }
+        }
+      }
+      if (lane == 0) bar_s = at;
+    }
+    __syncthreads();
+    const uint32_t bar = bar_s;
+    const bool above = tid < active && key_s[tid] > bar, equal = tid < active && key_s[tid] == bar;
+    if (above) win_s[atomicAdd(&n_win, 1)] = tid;      // (in any order: what comes of it is put in order below)
+    if (equal) atomicAdd(&n_tie, 1);
+    __syncthreads();
+    const int n_above = n_win, ties = n_tie;
+    if (n_above + ties <= want) {
+      if (equal) win_s[n_above + atomicAdd(&n_put, 1)] = tid;
+    } else {
+      // Of the threads whose maxima are equal those whose first such element comes first.
+      int first = 0x7fffffff;
+      if (equal) {
+        for (int k = tid; k < n_vec && first == 0x7fffffff; k += TH) {
+          float f[N];
+          logits_load<T>(row, base + k * N, lo, hi, f);
+#pragma unroll
+          for (int x = N - 1; x >= 0; --x) {
+            const int i = base + k * N + x;
+            if (i >= lo && i < hi && logit_key(f[x]) == bar) first = i;
+          }
+        }
+      }
+      first_s[tid] = first;
+      __syncthreads();
+      if (equal) {
+        int before = 0;
+        for (int x = 0; x < active; ++x) before += first_s[x] < first;
+        if (before < want - n_above) win_s[n_above + before] = tid;
+      }
+    }
+    __syncthreads();
+    // Their shares once more, one by a warp.
+    const int per = (n_vec + TH - 1) / TH;              // vectors a thread, at most
+    auto each = [&](auto&& use) {                       // use(order) for the elements of the winners' shares that reach the bar
+      for (int w = warp; w < want; w += LOGPROBS_WARPS) {
+        for (int j = lane; j < per; j += 32) {
+          const int k = win_s[w] + j * TH;
+          if (k >= n_vec) break;
+          float f[N];
+          logits_load<T>(row, base + k * N, lo, hi, f);
+#pragma unroll
+          for (int x = 0; x < N; ++x) {
+            const int i = base + k * N + x;
+            const uint32_t key = logit_key(f[x]);
+            if (i >= lo && i < hi && (key >= bar || want < top)) use(logit_order(key, i));
+          }
+        }
+      }
+    };
+    each([&](unsigned long long o) {
+      const int at = atomicAdd(&n_pool, 1);
+      if (at < LOGPROBS_ROOM) pool_s[at] = o;
+    });
+    __syncthreads();
+    const int n = n_pool;
+    if (n <= LOGPROBS_ROOM) {
+      for (int c = tid; c < n; c += TH) {
+        const unsigned long long o = pool_s[c];
+        int before = 0;
+        for (int x = 0; x < n; ++x) before += pool_s[x] > o;
+        if (before < top) best_s[before] = o;
+      }
+    } else {
+      unsigned long long last = ~0ull;
+      for (int r = 0; r < top; ++r) {
+        unsigned long long o = 0;
+        each([&](unsigned long long x) {
+          if (x < last && x > o) o = x;
+        });
+#pragma unroll
+        for (int x = 16; x >= 1; x >>= 1) {
+          const unsigned long long y = __shfl_xor_sync(0xffffffffu, o, x);
+          if (y > o) o = y;
+        }
+        if (lane == 0) warp_best_s[warp] = o;
+        __syncthreads();
+        o = 0;
+#pragma unroll
+        for (int x = 0; x < LOGPROBS_WARPS; ++x)
+          if (warp_best_s[x] > o) o = warp_best_s[x];
+        if (tid == 0) best_s[r] = o;
+        last = o;
+        __syncthreads();
+      }
+    }
+    __syncthreads();
+  }
+
+  // --- results
+  const unsigned long long* best = best_s;
+  if constexpr (CLUSTER) {
+    cluster_wait_acquire();                   // all blocks have started
+    auto first_block = [](const void* x) {
+      uint32_t a;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(x)), "r"(0));
+      return a;
+    };
+    if (tid < p.top) {
+      const unsigned long long o = tid < top ? best_s[tid] : 0ull;
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(first_block(&peer_best[rank][tid])), "l"(o) : "memory");
+    }
+    if (tid == 0) {
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][0])), "f"(gm) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][1])), "f"(gs) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][2])), "f"(ge) : "memory");
+    }
+    cluster_arrive_release();
+    if (rank != 0) return;
+    cluster_wait_acquire();
+    join(peer_red, LOGPROBS_CLUSTER, gm, gs, ge);
+    if (tid < LOGPROBS_CLUSTER * p.top) {
+      const unsigned long long o = peer_best[tid / p.top][tid % p.top];
+      int before = 0;
+      for (int r = 0; r < LOGPROBS_CLUSTER; ++r)
+        for (int x = 0; x < p.top; ++x) before += peer_best[r][x] > o;
+      if (o != 0 && before < p.top) best_s[before] = o;
+    }
+    __syncthreads();
+  }
+  const float ls = logf(gs);
+  if (tid == 0) {
+    const int tok = p.tokens[t];
+    const float x = tok >= 0 && tok < p.V ? logit_at(row, tok) : -INFINITY;
+    p.lp[t] = (x - gm) - ls;
+    if (p.entropy) p.entropy[t] = ls - ge / gs;
+  }
+  if (tid < p.top) {
+    const int id = (int)(0xffffffffu - (uint32_t)best[tid]);
+    p.ids[(long long)t * p.top + tid] = id;
+    p.top_lp[(long long)t * p.top + tid] = (logit_at(row, id) - gm) - ls;
+  }
+}
+
+}  // namespace tova

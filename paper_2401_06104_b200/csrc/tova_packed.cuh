@@ -1,0 +1,269 @@
+// Causal attention of packed prompts (sm_100a): sequences of different lengths, one behind the other, every token of which
+// attends to itself and the earlier tokens of its sequence,
+//   o_i[h] = sum_{j <= i} softmax_j(scale q_i[h] k_j[hk]) v_j[hk],   hk = h / (H / Hkv).
+//
+// Here: how the work is dealt out, and the kernel on the plain ALUs (fp32, every product in fp32).
+#pragma once
+
+#include "tova_mma.cuh"
+#include "tova_tc.cuh"
+
+namespace tova {
+
+struct PackedParams {
+  const void *q, *k, *v;       // [N, heads * D], rows q_stride, k_stride, v_stride elements apart
+  void* out;                   // [N,H,D]
+  const int32_t* offsets;      // [S + 1]
+  const int2* list;            // (sequence, tile), those with the most columns first; NULL: found by every block itself
+  const int* n_list;
+  long long q_stride, k_stride, v_stride;
+  int S, N, H, Hkv, G, pairs;  // (pairs: see the tcgen05 kernel)
+  float scale2;                // scale * log2(e)
+};
+
+// First and last token of sequence b; offsets that fall, or lie outside the tokens, give sequences without tokens.
+__device__ __forceinline__ void packed_bounds(const PackedParams& p, int b, int& t0, int& t1) {
+  t0 = min(max(p.offsets[b], 0), p.N);
+  t1 = min(max(p.offsets[b + 1], t0), p.N);
+}
+
+// Sequence and tile number x of `rows` tokens, counted through the sequences, by a whole warp; false behind the last.
+__device__ __forceinline__ bool packed_find(const PackedParams& p, int rows, int x, int lane, int& b, int& tile) {
+  int base = 0;
+  for (int b0 = 0; b0 < p.S; b0 += 32) {
+    int mine = 0;
+    if (b0 + lane < p.S) {
+      int t0, t1;
+      packed_bounds(p, b0 + lane, t0, t1);
+      mine = (t1 - t0 + rows - 1) / rows;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, base + upto > x);
+    if (hit) {
+      const int k = __ffs(hit) - 1;
+      b = b0 + k;
+      tile = x - base - __shfl_sync(0xffffffffu, upto - mine, k);
+      return true;
+    }
+    base += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return false;
+}
+
+// The list of all tiles, in order of falling work (to a 1024th of the longest; which of equal ones comes first changes no
+// result).  One block.  `room`: entries there are (offsets that overlap could make more tiles than tokens allow).
+constexpr int PACKED_PLAN_THREADS = 1024, PACKED_BUCKETS = 1024;
+__global__ void __launch_bounds__(PACKED_PLAN_THREADS) tova_packed_plan_kernel(const __grid_constant__ PackedParams p, int rows, int2* list,
+                                                                              int* n_list, int room) {
+  __shared__ int count[PACKED_BUCKETS], most_s, warp_s[32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  count[tid] = 0;
+  if (tid == 0) most_s = 1;
+  __syncthreads();
+  auto tiles_of = [&](int b) {
+    int t0, t1;
+    packed_bounds(p, b, t0, t1);
+    return (t1 - t0 + rows - 1) / rows;
+  };
+  for (int b = tid; b < p.S; b += PACKED_PLAN_THREADS) atomicMax(&most_s, tiles_of(b));
+  __syncthreads();
+  const int most = most_s;
+  auto bucket = [&](int tile) { return PACKED_BUCKETS - 1 - (int)((long long)tile * PACKED_BUCKETS / most); };
+  for (int b = warp; b < p.S; b += 32) {
+    const int n = tiles_of(b);
+    for (int i = lane; i < n; i += 32) atomicAdd(&count[bucket(i)], 1);
+  }
+  __syncthreads();
+  const int mine = count[tid];
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 31) warp_s[warp] = upto;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < warp; ++w) before += warp_s[w];
+  count[tid] = before + upto - mine;
+  if (tid == PACKED_PLAN_THREADS - 1) *n_list = min(room, before + upto);
+  __syncthreads();
+  for (int b = warp; b < p.S; b += 32) {
+    const int n = tiles_of(b);
+    for (int i = lane; i < n; i += 32) {
+      const int at = atomicAdd(&count[bucket(i)], 1);
+      if (at < room) list[at] = make_int2(b, i);
+    }
+  }
+  pdl_launch_dependents();
+}
+
+// Plain ALUs: 64 tokens of one head a block, 64 columns at a time through shared memory; a thread has 4 x 4 logits and 4 x D/16
+// components of the result, a row's 16 threads are neighbouring lanes.  grid = (tiles, H).
+constexpr int PACKED_ALU_ROWS = 64, PACKED_ALU_THREADS = 256;
+template <int D>
+constexpr int packed_alu_smem() { return (3 * 64 * (D + 4) + 64 * 68) * 4; }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PACKED_ALU_THREADS) tova_packed_alu_kernel(const __grid_constant__ PackedParams p) {
+  constexpr int R = PACKED_ALU_ROWS, LD = D + 4, LP = 68, N = Vec16<T>::N;
+  extern __shared__ __align__(16) float packed_alu_raw[];
+  float *q_s = packed_alu_raw, *k_s = q_s + R * LD, *v_s = k_s + R * LD, *p_s = v_s + R * LD;
+  __shared__ int found_s[3];
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  pdl_wait();
+  if (tid < 32) {
+    int b = 0, tile = 0;
+    bool have;
+    if (p.list) {
+      have = (int)blockIdx.x < *p.n_list;
+      if (have) {
+        const int2 e = p.list[blockIdx.x];
+        b = e.x;
+        tile = e.y;
+      }
+    } else {
+      have = packed_find(p, R, blockIdx.x, tid, b, tile);
+    }
+    if (tid == 0) {
+      found_s[0] = have;
+      found_s[1] = b;
+      found_s[2] = tile;
+    }
+  }
+  __syncthreads();
+  if (!found_s[0]) return;
+  const int tile = found_s[2], h = blockIdx.y, hk = h / p.G;
+  int t0, t1;
+  packed_bounds(p, found_s[1], t0, t1);
+  const int row0 = t0 + tile * R, rows = min(R, t1 - row0);          // first token of the tile
+  // 64 rows of one head, those behind `n` zeros.
+  auto load = [&](float* to, const void* from, long long stride, int first, int head, int n) {
+#pragma unroll 4
+    for (int e = tid; e < R * (D / N); e += PACKED_ALU_THREADS) {
+      const int r = e / (D / N), c = (e - r * (D / N)) * N;
+      float f[N];
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (r < n) w = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(from) + (first + r) * stride + (long long)head * D + c));
+      Vec16<T>::unpack(w, f);
+#pragma unroll
+      for (int x = 0; x < N; x += 4) *reinterpret_cast<float4*>(to + r * LD + c + x) = make_float4(f[x], f[x + 1], f[x + 2], f[x + 3]);
+    }
+  };
+  load(q_s, p.q, p.q_stride, row0, h, rows);
+  float o[4][D / 16], m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+  }
+  for (int j = 0; j <= tile; ++j) {
+    __syncthreads();
+    const int n = min(R, t1 - (t0 + j * R));
+    load(k_s, p.k, p.k_stride, t0 + j * R, hk, n);
+    load(v_s, p.v, p.v_stride, t0 + j * R, hk, n);
+    __syncthreads();
+    float s[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < D; d += 4) {
+      float4 a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(q_s + (ty * 4 + i) * LD + d);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const float4*>(k_s + (tx + 16 * c) * LD + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          s[i][c] = fmaf(a[i].w, b[c].w, fmaf(a[i].z, b[c].z, fmaf(a[i].y, b[c].y, fmaf(a[i].x, b[c].x, s[i][c]))));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = ty * 4 + i;
+      float top = m[i];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[i][c] = j < tile || tx + 16 * c <= r ? s[i][c] * p.scale2 : -INFINITY;
+        top = fmaxf(top, s[i][c]);
+      }
+#pragma unroll
+      for (int x = 8; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+      const float base = top == -INFINITY ? 0.f : top, f = m[i] == -INFINITY ? 0.f : exp2f(m[i] - base);
+      m[i] = top;
+      l[i] *= f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float w = exp2f(s[i][c] - base);
+        l[i] += w;
+        p_s[r * LP + tx + 16 * c] = w;
+      }
+    }
+    __syncwarp();               // a row's weights are written and read by the same half warp
+    // A masked weight is 0, and 0 times a value that is not finite would be NaN: on the diagonal the columns end with the row.
+    if (j < tile) {
+#pragma unroll 4
+      for (int k = 0; k < R; k += 4) {
+        float4 a[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(p_s + (ty * 4 + i) * LP + k);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) {
+            const float4 b = *reinterpret_cast<const float4*>(v_s + (k + x) * LD + c * 64 + tx * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float w = x == 0 ? a[i].x : x == 1 ? a[i].y : x == 2 ? a[i].z : a[i].w;
+              o[i][4 * c] = fmaf(w, b.x, o[i][4 * c]);
+              o[i][4 * c + 1] = fmaf(w, b.y, o[i][4 * c + 1]);
+              o[i][4 * c + 2] = fmaf(w, b.z, o[i][4 * c + 2]);
+              o[i][4 * c + 3] = fmaf(w, b.w, o[i][4 * c + 3]);
+            }
+          }
+      }
+    } else {
+      for (int k = 0; k < min(rows, ty * 4 + 4); ++k) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          const float4 b = *reinterpret_cast<const float4*>(v_s + k * LD + c * 64 + tx * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (k > ty * 4 + i) continue;
+            const float w = p_s[(ty * 4 + i) * LP + k];
+            o[i][4 * c] = fmaf(w, b.x, o[i][4 * c]);
+            o[i][4 * c + 1] = fmaf(w, b.y, o[i][4 * c + 1]);
+            o[i][4 * c + 2] = fmaf(w, b.z, o[i][4 * c + 2]);
+            o[i][4 * c + 3] = fmaf(w, b.w, o[i][4 * c + 3]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int x = 8; x >= 1; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+    const int r = ty * 4 + i;
+    if (r >= rows) continue;
+    T* out = static_cast<T*>(p.out) + ((long long)(row0 + r) * p.H + h) * D + tx * 4;
+    const float inv = 1.f / l[i];
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) out[(c >> 2) * 64 + (c & 3)] = (T)(o[i][c] * inv);
+  }
+}
+
+}  // namespace tova
