@@ -14,10 +14,12 @@ struct PackedParams {
   const void *q, *k, *v;       // [N, heads * D], rows q_stride, k_stride, v_stride elements apart
   void* out;                   // [N,H,D]
   const int32_t* offsets;      // [S + 1]
-  const int2* list;            // (sequence, tile), those with the most columns first; NULL: found by every block itself
+  const int4* list;            // (first token of the sequence, the first behind it, tile, 0), those with the most columns first;
+                               // NULL: found by every block itself
   const int* n_list;
   long long q_stride, k_stride, v_stride;
-  int S, N, H, Hkv, G, pairs;  // (pairs: see the tcgen05 kernel)
+  int S, N, H, Hkv, G;
+  int pairs;                   // tcgen05 kernel: two heads an item
   float scale2;                // scale * log2(e)
 };
 
@@ -58,7 +60,7 @@ __device__ __forceinline__ bool packed_find(const PackedParams& p, int rows, int
 // The list of all tiles, in order of falling work (to a 1024th of the longest; which of equal ones comes first changes no
 // result).  One block.  `room`: entries there are (offsets that overlap could make more tiles than tokens allow).
 constexpr int PACKED_PLAN_THREADS = 1024, PACKED_BUCKETS = 1024;
-__global__ void __launch_bounds__(PACKED_PLAN_THREADS) tova_packed_plan_kernel(const __grid_constant__ PackedParams p, int rows, int2* list,
+__global__ void __launch_bounds__(PACKED_PLAN_THREADS) tova_packed_plan_kernel(const __grid_constant__ PackedParams p, int rows, int4* list,
                                                                               int* n_list, int room) {
   __shared__ int count[PACKED_BUCKETS], most_s, warp_s[32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -94,10 +96,12 @@ __global__ void __launch_bounds__(PACKED_PLAN_THREADS) tova_packed_plan_kernel(c
   if (tid == PACKED_PLAN_THREADS - 1) *n_list = min(room, before + upto);
   __syncthreads();
   for (int b = warp; b < p.S; b += 32) {
-    const int n = tiles_of(b);
+    int t0, t1;
+    packed_bounds(p, b, t0, t1);
+    const int n = (t1 - t0 + rows - 1) / rows;
     for (int i = lane; i < n; i += 32) {
       const int at = atomicAdd(&count[bucket(i)], 1);
-      if (at < room) list[at] = make_int2(b, i);
+      if (at < room) list[at] = make_int4(t0, t1, i, 0);
     }
   }
   pdl_launch_dependents();
@@ -114,33 +118,23 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS) tova_packed_alu_kernel(con
   constexpr int R = PACKED_ALU_ROWS, LD = D + 4, LP = 68, N = Vec16<T>::N;
   extern __shared__ __align__(16) float packed_alu_raw[];
   float *q_s = packed_alu_raw, *k_s = q_s + R * LD, *v_s = k_s + R * LD, *p_s = v_s + R * LD;
-  __shared__ int found_s[3];
+  __shared__ int4 found_s;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   pdl_wait();
   if (tid < 32) {
     int b = 0, tile = 0;
-    bool have;
+    int4 e = make_int4(0, 0, 0, 0);
     if (p.list) {
-      have = (int)blockIdx.x < *p.n_list;
-      if (have) {
-        const int2 e = p.list[blockIdx.x];
-        b = e.x;
-        tile = e.y;
-      }
-    } else {
-      have = packed_find(p, R, blockIdx.x, tid, b, tile);
+      if ((int)blockIdx.x < *p.n_list) e = p.list[blockIdx.x];
+    } else if (packed_find(p, R, blockIdx.x, tid, b, tile)) {
+      packed_bounds(p, b, e.x, e.y);
+      e.z = tile;
     }
-    if (tid == 0) {
-      found_s[0] = have;
-      found_s[1] = b;
-      found_s[2] = tile;
-    }
+    if (tid == 0) found_s = e;
   }
   __syncthreads();
-  if (!found_s[0]) return;
-  const int tile = found_s[2], h = blockIdx.y, hk = h / p.G;
-  int t0, t1;
-  packed_bounds(p, found_s[1], t0, t1);
+  const int t0 = found_s.x, t1 = found_s.y, tile = found_s.z, h = blockIdx.y, hk = h / p.G;
+  if (t0 == t1) return;                  // (no tile lies in a sequence without tokens)
   const int row0 = t0 + tile * R, rows = min(R, t1 - row0);          // first token of the tile
   // 64 rows of one head, those behind `n` zeros.
   auto load = [&](float* to, const void* from, long long stride, int first, int head, int n) {

@@ -13,6 +13,7 @@
 #include "tova_logprobs.cuh"
 #include "tova_norm_rope.cuh"
 #include "tova_packed.cuh"
+#include "tova_packed_tc.cuh"
 #include "tova_paged.cuh"
 
 namespace {
@@ -338,26 +339,51 @@ int packed_check(const tova_packed_config* c, int32_t n_tokens) {
 }
 
 struct PackedPlan {
-  int rows, room;              // tokens of a tile, the most tiles there can be
-  bool list;                   // tiles in order of their work
+  bool pairs;                  // bf16: an item is two heads, not two tiles of tokens
+  int rows, room, heads;       // tokens of a list's entry, the most entries there can be, items (fp32: blocks) of each
+  bool list;                   // entries in order of their work
   size_t bytes;
 };
 PackedPlan packed_plan(const tova_packed_config& c, int32_t n_tokens, int sm_count) {
   PackedPlan t{};
-  t.rows = tova::PACKED_ALU_ROWS;
+  const bool bf16 = c.dtype == TOVA_DTYPE_BF16;
+  t.pairs = bf16 && (c.n_q_heads / c.n_kv_heads) % 2 == 0;
+  t.rows = !bf16 ? tova::PACKED_ALU_ROWS : t.pairs ? 128 : 256;
   t.room = n_tokens / t.rows + std::min(c.n_seqs, n_tokens);
-  t.list = (long long)t.room * c.n_q_heads > sm_count;
-  t.bytes = t.list ? 16 + round_up((size_t)t.room * sizeof(int2), 16) : 0;
+  t.heads = t.pairs ? c.n_q_heads / 2 : c.n_q_heads;
+  t.list = (long long)t.room * t.heads > sm_count;
+  t.bytes = t.list ? 16 + (size_t)t.room * sizeof(int4) : 0;
   return t;
 }
 
-template <typename T, int D>
-cudaError_t packed_launch(const tova::PackedParams& p, const PackedPlan& t, cudaStream_t st) {
+template <int D>
+cudaError_t packed_launch_alu(const tova::PackedParams& p, const PackedPlan& t, cudaStream_t st) {
   static std::atomic<bool> done[64];
   constexpr int smem = tova::packed_alu_smem<D>();
-  const cudaError_t e = allow_smem(tova::tova_packed_alu_kernel<T, D>, done, smem);
+  const cudaError_t e = allow_smem(tova::tova_packed_alu_kernel<float, D>, done, smem);
   if (e != cudaSuccess) return e;
-  return start(tova::tova_packed_alu_kernel<T, D>, dim3((unsigned)t.room, (unsigned)p.H), tova::PACKED_ALU_THREADS, smem, 1, t.list, st, p);
+  return start(tova::tova_packed_alu_kernel<float, D>, dim3((unsigned)t.room, (unsigned)p.H), tova::PACKED_ALU_THREADS, smem, 1, t.list, st, p);
+}
+
+template <int D>
+cudaError_t packed_launch_tc(const tova::PackedParams& p, const PackedPlan& t, int sm_count, cudaStream_t st) {
+  static std::atomic<bool> done[64];
+  using S = tova::PackedTcShape<D>;
+  const cudaError_t e = allow_smem(tova::tova_packed_tc_kernel<D>, done, S::SMEM);
+  if (e != cudaSuccess) return e;
+  // q, k, v as [N, heads, D] in boxes of 128 tokens of one head x 64 components.
+  CUtensorMap map[3];
+  const void* base[3] = {p.q, p.k, p.v};
+  const int64_t stride[3] = {p.q_stride, p.k_stride, p.v_stride};
+  for (int i = 0; i < 3; ++i) {
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)(i == 0 ? p.H : p.Hkv), (cuuint64_t)p.N};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride[i] * 2};
+    const cuuint32_t box[3] = {64, 1, 128};
+    if (encode_map(&map[i], const_cast<void*>(base[i]), 3, dims, strides, box) != TOVA_OK) return cudaErrorInvalidValue;
+  }
+  const long long items = (long long)t.room * t.heads;
+  const unsigned grid = (unsigned)(t.list ? std::min<long long>(items, sm_count) : items);
+  return start(tova::tova_packed_tc_kernel<D>, dim3(grid), S::THREADS, S::SMEM, 1, t.list, st, p, map[0], map[1], map[2]);
 }
 
 }  // namespace
@@ -391,17 +417,19 @@ extern "C" int tova_packed_attention(const tova_packed_config* cfg, const void* 
   const float scale = cfg->sm_scale == 0.f ? 1.f / std::sqrt((float)cfg->head_dim) : cfg->sm_scale;
   p.scale2 = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  p.pairs = t.pairs;
+  if (n_tokens == 1) p.q_stride = qr, p.k_stride = kr, p.v_stride = kr;      // (no second row: any stride will do)
   if (t.list) {
     int* n_list = static_cast<int*>(workspace);
-    int2* list = reinterpret_cast<int2*>(static_cast<unsigned char*>(workspace) + 16);
+    int4* list = reinterpret_cast<int4*>(static_cast<unsigned char*>(workspace) + 16);
     tova::tova_packed_plan_kernel<<<1, tova::PACKED_PLAN_THREADS, 0, st>>>(p, t.rows, list, n_list, t.room);
     if (int rc = launched(cudaGetLastError())) return rc;
     p.list = list;
     p.n_list = n_list;
   }
   if (cfg->dtype == TOVA_DTYPE_BF16)
-    return launched(cfg->head_dim == 128 ? packed_launch<__nv_bfloat16, 128>(p, t, st) : packed_launch<__nv_bfloat16, 64>(p, t, st));
-  return launched(cfg->head_dim == 128 ? packed_launch<float, 128>(p, t, st) : packed_launch<float, 64>(p, t, st));
+    return launched(cfg->head_dim == 128 ? packed_launch_tc<128>(p, t, dev.sm_count, st) : packed_launch_tc<64>(p, t, dev.sm_count, st));
+  return launched(cfg->head_dim == 128 ? packed_launch_alu<128>(p, t, st) : packed_launch_alu<64>(p, t, st));
 }
 
 // ---------------------------------------------------------------------------

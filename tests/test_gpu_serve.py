@@ -287,12 +287,15 @@ def paged_reference(q, K, V, table, lens, rows, scale=None):
 def attention_tolerance(dtype, D, cols, want, wv, reach, weights_rounded):
     """A logit is off by delta <= 2 (D + 4) 2^-24 reach (products and sums in fp32, truncating adders), a weight by
     e^delta - 1 relative, in numerator and denominator; fp32 sums over the columns add 2 cols 2^-24 at the very most of
-    sum p|v|; exp2's own error is 2^-22.  Weights as two bf16 terms are off by 2^-16, as one by 2^-8; the result's rounding."""
+    sum p|v|; exp2's own error is 2^-22.  Weights as two bf16 terms are off by 2^-16.  As one they are p (1 + d), |d| <= 2^-8,
+    and summed as they are: sum p (1 + d) v / sum p (1 + d) is off from o = sum p v by sum p d (v - o) / sum p (1 + d), that
+    is by 2^-8 (sum p|v| + |o|) / (1 - 2^-8).  Then the result's rounding."""
     delta = 2 * (D + 4) * U * reach
     rel = 2 * torch.expm1(delta) + (2 * cols + 16) * U
     if dtype == "bf16":
         rel = rel + (2.0 ** -8 if weights_rounded else 2.0 ** -16)
-    return rel * wv * 1.01 + HALF[dtype] * want.abs() + 1e-30
+    sum_rounded = 2.0 ** -8 * want.abs() if dtype == "bf16" and weights_rounded else 0.0
+    return (rel * wv + sum_rounded) * 1.01 + HALF[dtype] * want.abs() + 1e-30
 
 
 def run_paged(dtype, B, H, Hkv, D, lens, rows, seed=0, n_live=None, gain=1.3, sm_scale=0.0, extra=0, bad=()):
