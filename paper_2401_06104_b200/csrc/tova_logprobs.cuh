@@ -14,11 +14,12 @@
 // block's shared memory.
 #pragma once
 
+#include "tova_rope.cuh"
 #include "tova_tc.cuh"
 
 namespace tova {
 
-constexpr int LOGPROBS_THREADS = 512, LOGPROBS_WARPS = LOGPROBS_THREADS / 32;
+constexpr int LOGPROBS_THREADS = 256, LOGPROBS_BLOCKS = 6, LOGPROBS_WARPS = LOGPROBS_THREADS / 32;
 constexpr int LOGPROBS_MAX_TOP = 32;
 constexpr int LOGPROBS_ROOM = 1024;          // elements collected at most
 constexpr int LOGPROBS_CLUSTER = 8;
@@ -39,6 +40,8 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+// The logit of a key (of a NaN: a NaN).
+__device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 // ... with the token: distinct for all elements of a row, and never 0.
 __device__ __forceinline__ unsigned long long logit_order(uint32_t key, int token) {
   return ((unsigned long long)key << 32) | (0xffffffffu - (uint32_t)token);
@@ -48,20 +51,55 @@ template <typename T>
 __device__ __forceinline__ float logit_at(const T* row, int i) { return (float)row[i]; }
 
 // N neighbouring elements that start at element i (a multiple of N behind the first 16-byte boundary, so i may be negative);
-// those outside lo .. hi - 1 are minus infinity.
+// those outside lo .. hi - 1 are `other`.
 template <typename T>
-__device__ __forceinline__ void logits_load(const T* row, int i, int lo, int hi, float (&f)[Vec16<T>::N]) {
+__device__ __forceinline__ void logits_load(const T* row, int i, int lo, int hi, float other, float (&f)[Vec16<T>::N]) {
   constexpr int N = Vec16<T>::N;
   if (i >= lo && i + N <= hi) {
     Vec16<T>::unpack(__ldg(reinterpret_cast<const uint4*>(row + i)), f);
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = i + e >= lo && i + e < hi ? logit_at(row, i + e) : -INFINITY;
+    for (int e = 0; e < N; ++e) f[e] = i + e >= lo && i + e < hi ? logit_at(row, i + e) : other;
   }
 }
 
+// A 16-byte vector as it lies: two logits as a packed pair of fp32, the largest logit.
+__device__ __forceinline__ uint64_t logits_pair(const float*, const uint4& w, int k) {
+  return k == 0 ? (uint64_t)w.y << 32 | w.x : (uint64_t)w.w << 32 | w.z;
+}
+__device__ __forceinline__ uint64_t logits_pair(const __nv_bfloat16*, const uint4& w, int k) {
+  const uint32_t x = k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w;
+  return (uint64_t)(x & 0xffff0000u) << 32 | x << 16;
+}
+template <int U>
+__device__ __forceinline__ float logits_most(const float*, const uint4 (&w)[U]) {
+  float m = __uint_as_float(w[0].x);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(w[u].x)), fmaxf(__uint_as_float(w[u].y), __uint_as_float(w[u].z))), __uint_as_float(w[u].w));
+  return m;
+}
+template <int U>
+__device__ __forceinline__ float logits_most(const __nv_bfloat16*, const uint4 (&w)[U]) {
+  auto h = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
+  __nv_bfloat162 m = h(w[0].x);
+#pragma unroll
+  for (int u = 0; u < U; ++u) m = __hmax2(m, __hmax2(__hmax2(h(w[u].x), h(w[u].y)), __hmax2(h(w[u].z), h(w[u].w))));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+template <typename T>
+struct LogitLowest;            // the lowest finite logit, as it lies in a vector
+template <>
+struct LogitLowest<float> {
+  static constexpr uint32_t word = 0xff7fffffu, value = 0xff7fffffu;
+};
+template <>
+struct LogitLowest<__nv_bfloat16> {
+  static constexpr uint32_t word = 0xff7fff7fu, value = 0xff7f0000u;
+};
+
 template <typename T, bool CLUSTER>
-__global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const __grid_constant__ LogprobsParams p) {
+__global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logprobs_kernel(const __grid_constant__ LogprobsParams p) {
   constexpr int N = Vec16<T>::N, U = 4, TH = LOGPROBS_THREADS;
   __shared__ float red_s[LOGPROBS_WARPS][3];
   __shared__ uint32_t key_s[TH];
@@ -89,44 +127,83 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const _
   const int base = lo == 0 ? -shift : lo, n_vec = hi > lo ? (hi - base + N - 1) / N : 0;
   const int top = min(p.top, hi - lo);        // of this block
   constexpr float L2E = 1.4426950408889634f;
+  const int tok = p.tokens[t];
+  const bool known = tok >= 0 && tok < p.V;
+  float chosen = -INFINITY;
+  if (tid == 0 && rank == 0 && known) chosen = logit_at(row, tok);
 
-  // --- the pass
+  // --- the pass.  Places that hold no element count as the lowest finite logit, whose weight is 0 unless nothing else is there.
   float m = -INFINITY, s = 0.f, e = 0.f;
   bool nan = false;
-  for (int k0 = tid; k0 < n_vec; k0 += U * TH) {
-    float f[U][N];
+  {
+    const float lowest = __uint_as_float(LogitLowest<T>::value);
+    const T* kind = nullptr;
+    const uint64_t l2e_2 = pack_f2(L2E, L2E);
+    uint64_t s2 = pack_f2(0.f, 0.f), e2 = s2;
+    for (int k0 = tid; k0 < n_vec; k0 += U * TH) {
+      uint4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + u * TH;
-      if (k < n_vec) {
-        logits_load<T>(row, base + k * N, lo, hi, f[u]);
-      } else {
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * TH, i = base + k * N;
+        constexpr uint32_t low = LogitLowest<T>::word;
+        w[u] = make_uint4(low, low, low, low);
+        if (i >= lo && i + N <= hi) {
+          w[u] = __ldg(reinterpret_cast<const uint4*>(row + i));
+        } else if (k < n_vec) {
+          float f[N];
+          logits_load<T>(row, i, lo, hi, lowest, f);
+          w[u] = rope_pack<T>(f);
+        }
+      }
+      const float most = logits_most(kind, w);
+      if (most > m) {
+        if (m != -INFINITY) {
+          const float d = m - most, r = ex2_approx(d * L2E);
+          e2 = mul_f2(fma_f2(pack_f2(d, d), s2, e2), pack_f2(r, r));
+          s2 = mul_f2(s2, pack_f2(r, r));
+        }
+        m = most;
+      }
+      const uint64_t neg_2 = pack_f2(-m, -m);
 #pragma unroll
-        for (int x = 0; x < N; ++x) f[u][x] = -INFINITY;
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int x = 0; x < N / 2; ++x) {
+          const uint64_t d = add_f2(logits_pair(kind, w[u], x), neg_2);
+          float x0, x1;
+          unpack_f2(mul_f2(d, l2e_2), x0, x1);
+          const uint64_t wt = pack_f2(ex2_approx(x0), ex2_approx(x1));
+          s2 = add_f2(s2, wt);
+          e2 = fma_f2(wt, d, e2);
+        }
+    }
+    float a, b;
+    unpack_f2(s2, a, b);
+    s = a + b;
+    unpack_f2(e2, a, b);
+    e = a + b;
+    // Infinities, NaN and nothing but the lowest logit: once more, one by one.
+    if (tid < n_vec && (!(fabsf(e) < INFINITY) || s != s || !(m > lowest))) {
+      m = -INFINITY;
+      s = e = 0.f;
+      for (int pass = 0; pass < 2; ++pass) {
+        const float ref = m == -INFINITY ? 0.f : m;
+        for (int k = tid; k < n_vec; k += TH) {
+          float f[N];
+          logits_load<T>(row, base + k * N, lo, hi, -INFINITY, f);
+          for (int x = 0; x < N; ++x) {
+            if (pass == 0) {
+              nan |= f[x] != f[x];
+              m = fmaxf(m, f[x]);
+            } else {
+              const float d = f[x] - ref, w = ex2_approx(d * L2E);
+              s += w;
+              if (w != 0.f) e = fmaf(w, d, e);
+            }
+          }
+        }
       }
     }
-    float most = f[0][0];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int x = 0; x < N; ++x) most = fmaxf(most, f[u][x]);
-    if (most > m) {
-      const float d = m - most;               // minus infinity at first
-      const float r = ex2_approx(d * L2E);
-      e = r * fmaf(fmaxf(d, -1e30f), s, e);
-      s *= r;
-      m = most;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int x = 0; x < N; ++x) {
-        const float d = f[u][x] - ref, w = ex2_approx(d * L2E);
-        s += w;
-        e = fmaf(w, fmaxf(d, -1e30f), e);     // (a logit of minus infinity: 0 times something finite)
-        nan |= f[u][x] != f[u][x];
-      }
   }
   // --- maxima, sums of the block
   const float mine = m;
@@ -204,7 +281,7 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const _
       if (equal) {
         for (int k = tid; k < n_vec && first == 0x7fffffff; k += TH) {
           float f[N];
-          logits_load<T>(row, base + k * N, lo, hi, f);
+          logits_load<T>(row, base + k * N, lo, hi, 0.f, f);
 #pragma unroll
           for (int x = N - 1; x >= 0; --x) {
             const int i = base + k * N + x;
@@ -229,7 +306,7 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const _
           const int k = win_s[w] + j * TH;
           if (k >= n_vec) break;
           float f[N];
-          logits_load<T>(row, base + k * N, lo, hi, f);
+          logits_load<T>(row, base + k * N, lo, hi, 0.f, f);
 #pragma unroll
           for (int x = 0; x < N; ++x) {
             const int i = base + k * N + x;
@@ -279,7 +356,6 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const _
   }
 
   // --- results
-  const unsigned long long* best = best_s;
   if constexpr (CLUSTER) {
     cluster_wait_acquire();                   // all blocks have started
     auto first_block = [](const void* x) {
@@ -311,15 +387,13 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS) tova_logprobs_kernel(const _
   }
   const float ls = logf(gs);
   if (tid == 0) {
-    const int tok = p.tokens[t];
-    const float x = tok >= 0 && tok < p.V ? logit_at(row, tok) : -INFINITY;
-    p.lp[t] = (x - gm) - ls;
+    p.lp[t] = (chosen - gm) - ls;
     if (p.entropy) p.entropy[t] = ls - ge / gs;
   }
   if (tid < p.top) {
-    const int id = (int)(0xffffffffu - (uint32_t)best[tid]);
-    p.ids[(long long)t * p.top + tid] = id;
-    p.top_lp[(long long)t * p.top + tid] = (logit_at(row, id) - gm) - ls;
+    const unsigned long long o = best_s[tid];
+    p.ids[(long long)t * p.top + tid] = (int)(0xffffffffu - (uint32_t)o);
+    p.top_lp[(long long)t * p.top + tid] = (key_logit((uint32_t)(o >> 32)) - gm) - ls;
   }
 }
 

@@ -8,10 +8,10 @@
 // The statistics are formed again from x, which the gradient has to read anyway: nothing is kept from the forward pass.
 //
 // Every component is read once and written once (gradient: two reads, one write) with about ten operations on it: DRAM
-// bound.  A row lies in a group of D / N neighbouring lanes, 16 bytes each, so that a lane meets the same components in every
-// row: its weights stay in registers, and so do its shares of dw.  The sum of squares takes log2(D / N) shuffles, the other
-// half of a pair one shuffle a component (the half layout with whole vectors), none (interleaved), or a trip through the
-// warp's own shared memory (other sizes of the rotated part).  Cosines and sines are formed once per token and serve all heads.
+// bound.  A row lies in a group of D / 2N neighbouring lanes, two vectors of 16 bytes each, so chosen that both components of a
+// pair meet in one lane; N pairs a lane, the same ones in every row.  The sum of squares takes log2(D / 2N) shuffles.  Cosines
+// and sines are formed once per token and serve all heads; they, and the weights, lie in shared memory in the lanes' order, so
+// that a lane reads them 16 bytes at a time without bank conflicts.
 #pragma once
 
 #include "tova_rope.cuh"
@@ -37,104 +37,139 @@ struct NormRopeParams {
   double turns[ROPE_MAX_PAIRS];
 };
 
-template <typename T, int D>
+// A row's D / 2 pairs: N in each of LANES lanes.  Behind the rot / 2 pairs that turn, neighbouring components that pass through
+// are pairs that turn by nothing.
+template <typename T, int D, int MODE>
 struct NormShape {
-  static constexpr int N = Vec16<T>::N, LANES = D / N, GROUPS = NORM_THREADS / LANES;     // lanes a row, rows at a time
+  static constexpr int N = Vec16<T>::N, LANES = D / (2 * N), GROUPS = NORM_THREADS / LANES;     // rows at a time
+  // Pair k of lane c, and its two components.
+  __device__ __forceinline__ static int pair(int c, int k) { return MODE == NORM_HALF_ODD ? k * LANES + c : c * N + k; }
+  __device__ __forceinline__ static void components(int i, int half, int& a, int& b) {
+    if (MODE == NORM_INTERLEAVED || i >= half) {
+      a = 2 * i;                // (of the half layout's passing ones: 2 half + 2 (i - half))
+      b = a + 1;
+    } else {
+      a = i;
+      b = i + half;
+    }
+  }
+  // Where pair k of lane c lies in a table in the lanes' order.
+  __device__ __forceinline__ static int place(int c, int k) { return ((k >> 2) * LANES + c) * 4 + (k & 3); }
+
+  struct Raw {
+    uint4 v[2];
+  };
+  // A lane's components of a row, as they lie; split: the pairs' first and second components in order.
+  __device__ __forceinline__ static void load(const T* row, int c, int half, Raw& r) {
+    if constexpr (MODE == NORM_HALF_ODD) {
+      T* x = reinterpret_cast<T*>(r.v);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        int a, b;
+        components(pair(c, k), half, a, b);
+        x[k] = row[a];
+        x[N + k] = row[b];
+      }
+    } else {
+      int a, b;
+      vectors(c, half, a, b);
+      r.v[0] = __ldcs(reinterpret_cast<const uint4*>(row + a));
+      r.v[1] = __ldcs(reinterpret_cast<const uint4*>(row + b));
+    }
+  }
+  __device__ __forceinline__ static void store(T* row, int c, int half, const float (&f)[2][N]) {
+    if constexpr (MODE == NORM_HALF_ODD) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        int a, b;
+        components(pair(c, k), half, a, b);
+        row[a] = (T)f[0][k];
+        row[b] = (T)f[1][k];
+      }
+    } else {
+      int a, b;
+      vectors(c, half, a, b);
+      float u[2][N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (apart(c, half)) {
+          u[0][k] = f[0][k];
+          u[1][k] = f[1][k];
+        } else {
+          u[(2 * k) / N][(2 * k) % N] = f[0][k];
+          u[(2 * k) / N][(2 * k) % N + 1] = f[1][k];
+        }
+      }
+      __stcs(reinterpret_cast<uint4*>(row + a), rope_pack<T>(u[0]));
+      __stcs(reinterpret_cast<uint4*>(row + b), rope_pack<T>(u[1]));
+    }
+  }
+  // The lane's pairs are (a + k, b + k) for its two vectors; else they are neighbours in both.
+  __device__ __forceinline__ static bool apart(int c, int half) { return MODE == NORM_HALF && c * N < half; }
+  __device__ __forceinline__ static void vectors(int c, int half, int& a, int& b) {
+    a = apart(c, half) ? c * N : 2 * c * N;
+    b = apart(c, half) ? c * N + half : 2 * c * N + N;
+  }
+  __device__ __forceinline__ static void split(const Raw& r, int c, int half, float (&f)[2][N]) {
+    float u[2][N];
+    Vec16<T>::unpack(r.v[0], u[0]);
+    Vec16<T>::unpack(r.v[1], u[1]);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (MODE == NORM_HALF_ODD || apart(c, half)) {
+        f[0][k] = u[0][k];
+        f[1][k] = u[1][k];
+      } else {
+        f[0][k] = u[(2 * k) / N][(2 * k) % N];
+        f[1][k] = u[(2 * k) / N][(2 * k) % N + 1];
+      }
+    }
+  }
+  __device__ __forceinline__ static void table(const float* t, int c, float (&f)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; k += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(t + place(c, k));
+      f[k] = x.x; f[k + 1] = x.y; f[k + 2] = x.z; f[k + 3] = x.w;
+    }
+  }
+  __device__ __forceinline__ static float sum(float x) {
+#pragma unroll
+    for (int o = LANES / 2; o >= 1; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+  }
+  // Angles of the block's tokens.
+  __device__ __forceinline__ static void angles(const NormRopeParams& p, long long row0, int n_tok, float (*cs)[D / 2], float (*sn)[D / 2]) {
+    const int half = p.rot >> 1;
+    for (int i = threadIdx.x; i < n_tok * (D / 2); i += NORM_THREADS) {
+      const int t = i / (D / 2), at = i - t * (D / 2), k = at / LANES, c = at - k * LANES, j = pair(c, k);
+      float s = 0.f, co = 1.f;
+      if (j < half) {
+        const long long row = row0 + t;
+        const double pos = p.positions ? (double)p.positions[row] : (double)p.first_pos + (double)(row / p.B);
+        double a = pos * p.turns[j];
+        a -= rint(a);
+        sincospif((float)(2.0 * a), &s, &co);
+        co *= p.factor;
+        s *= p.factor;
+      }
+      cs[t][place(c, k)] = co;
+      sn[t][place(c, k)] = s;
+    }
+  }
 };
-
-// The row's part of a pair that other lanes hold, for each of this lane's components; f: this lane's.  half: rot / 2.
-template <typename T, int D, int MODE>
-__device__ __forceinline__ void norm_partner(const float (&f)[Vec16<T>::N], float (&o)[Vec16<T>::N], int c, int half, float* stage) {
-  constexpr int N = Vec16<T>::N, LANES = D / N;
-  if constexpr (MODE == NORM_HALF) {
-    const int mate = c * N < half ? c + half / N : c * N < 2 * half ? c - half / N : c;
-#pragma unroll
-    for (int e = 0; e < N; ++e) o[e] = __shfl_sync(0xffffffffu, f[e], mate, LANES);
-  } else if constexpr (MODE == NORM_INTERLEAVED) {
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      o[e] = f[e + 1];
-      o[e + 1] = f[e];
-    }
-  } else {
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < N; ++e) stage[c * N + e] = f[e];
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int d = c * N + e;
-      o[e] = stage[d < half ? d + half : d < 2 * half ? d - half : d];
-    }
-  }
-}
-
-// f turned by the token's angles (by their negatives where dir is -1).
-template <typename T, int D, int MODE>
-__device__ __forceinline__ void norm_turn(float (&f)[Vec16<T>::N], int c, int half, const float* cs, const float* sn, float dir, float* stage) {
-  constexpr int N = Vec16<T>::N;
-  float o[N];
-  norm_partner<T, D, MODE>(f, o, c, half, stage);
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int d = c * N + e;
-    if (d < 2 * half) {
-      const int pair = MODE == NORM_INTERLEAVED ? d >> 1 : d < half ? d : d - half;
-      const bool first = MODE == NORM_INTERLEAVED ? !(e & 1) : d < half;
-      const float s = sn[pair] * dir;
-      f[e] = f[e] * cs[pair] + o[e] * (first ? -s : s);
-    }
-  }
-}
-
-template <int LANES>
-__device__ __forceinline__ float norm_group_sum(float x) {
-#pragma unroll
-  for (int o = LANES / 2; o >= 1; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
-}
-
-// Angles of the block's tokens.
-__device__ __forceinline__ void norm_angles(const NormRopeParams& p, long long row0, int n_tok, float (*cs)[ROPE_MAX_PAIRS],
-                                            float (*sn)[ROPE_MAX_PAIRS]) {
-  const int half = p.rot >> 1;
-  for (int i = threadIdx.x; i < n_tok * half; i += NORM_THREADS) {
-    const int t = i / half, j = i - t * half;
-    const long long row = row0 + t;
-    const double pos = p.positions ? (double)p.positions[row] : (double)p.first_pos + (double)(row / p.B);
-    double a = pos * p.turns[j];
-    a -= rint(a);
-    float s, c;
-    sincospif((float)(2.0 * a), &s, &c);
-    cs[t][j] = c * p.factor;
-    sn[t][j] = s * p.factor;
-  }
-}
 
 // Forward.  grid = ceil(rows / tokens_per_block).
 template <typename T, int D, int MODE>
-__global__ void __launch_bounds__(NORM_THREADS) tova_norm_rope_kernel(const __grid_constant__ NormRopeParams p) {
-  using S = NormShape<T, D>;
-  constexpr int N = S::N, U = 4;
-  __shared__ __align__(16) float cs[NORM_MAX_TOKENS][ROPE_MAX_PAIRS], sn[NORM_MAX_TOKENS][ROPE_MAX_PAIRS];
-  __shared__ float stage_s[MODE == NORM_HALF_ODD ? S::GROUPS : 1][D + 1];
+__global__ void __launch_bounds__(NORM_THREADS, 4) tova_norm_rope_kernel(const __grid_constant__ NormRopeParams p) {
+  using S = NormShape<T, D, MODE>;
+  constexpr int N = S::N, U = 2;
+  __shared__ __align__(16) float cs[NORM_MAX_TOKENS][D / 2], sn[NORM_MAX_TOKENS][D / 2], w_s[2][2][D / 2];
   const int group = threadIdx.x / S::LANES, c = threadIdx.x % S::LANES, half = p.rot >> 1;
-  float* stage = stage_s[MODE == NORM_HALF_ODD ? group : 0];
   const long long row0 = (long long)blockIdx.x * p.tokens_per_block;
   const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
   const int per_tok = p.heads[0] + p.heads[1], total = n_tok * per_tok;
-  float w[2][N];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    if (p.w[k]) {
-      Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.w[k]) + c * N), w[k]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e) w[k][e] = 1.f;
-    }
-  }
   for (int i0 = 0; i0 < total; i0 += U * S::GROUPS) {
-    uint4 raw[U];
+    typename S::Raw raw[U];
     int tok[U], which[U], head[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -143,114 +178,138 @@ __global__ void __launch_bounds__(NORM_THREADS) tova_norm_rope_kernel(const __gr
       head[u] = i - tok[u] * per_tok;
       which[u] = head[u] >= p.heads[0];
       if (which[u]) head[u] -= p.heads[0];
-      raw[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(p.x[which[u]]) + (row0 + tok[u]) * p.x_stride[which[u]] +
-                                                     (long long)head[u] * D + c * N));
+      S::load(static_cast<const T*>(p.x[which[u]]) + (row0 + tok[u]) * p.x_stride[which[u]] + (long long)head[u] * D, c, half, raw[u]);
     }
     if (i0 == 0) {
-      norm_angles(p, row0, n_tok, cs, sn);
+      for (int i = threadIdx.x; i < 2 * (D / 2); i += NORM_THREADS) {
+        const int k = i / (D / 2), j = i - k * (D / 2), kk = j / S::LANES, cc = j - kk * S::LANES;
+        int a, b;
+        S::components(S::pair(cc, kk), half, a, b);
+        w_s[k][0][S::place(cc, kk)] = p.w[k] ? (float)static_cast<const T*>(p.w[k])[a] : 1.f;
+        w_s[k][1][S::place(cc, kk)] = p.w[k] ? (float)static_cast<const T*>(p.w[k])[b] : 1.f;
+      }
+      S::angles(p, row0, n_tok, cs, sn);
       __syncthreads();
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u * S::GROUPS >= total) break;
-      float f[N], sum = 0.f;
-      Vec16<T>::unpack(raw[u], f);
+      float x[2][N], co[N], si[N], w[2][N], sum = 0.f;
+      S::split(raw[u], c, half, x);
 #pragma unroll
-      for (int e = 0; e < N; ++e) sum = fmaf(f[e], f[e], sum);
-      const float r = rsqrtf(norm_group_sum<S::LANES>(sum) * (1.f / D) + p.eps);
+      for (int k = 0; k < N; ++k) sum = fmaf(x[0][k], x[0][k], fmaf(x[1][k], x[1][k], sum));
+      const float r = rsqrtf(S::sum(sum) * (1.f / D) + p.eps);
+      S::table(cs[tok[u]], c, co);
+      S::table(sn[tok[u]], c, si);
+      S::table(w_s[which[u]][0], c, w[0]);
+      S::table(w_s[which[u]][1], c, w[1]);
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = f[e] * r * (which[u] ? w[1][e] : w[0][e]);
-      norm_turn<T, D, MODE>(f, c, half, cs[tok[u]], sn[tok[u]], 1.f, stage);
+      for (int k = 0; k < N; ++k) {
+        const float a = x[0][k] * r * w[0][k], b = x[1][k] * r * w[1][k];
+        x[0][k] = a * co[k] - b * si[k];
+        x[1][k] = b * co[k] + a * si[k];
+      }
       if (i0 + u * S::GROUPS + group < total)
-        __stcs(reinterpret_cast<uint4*>(static_cast<T*>(p.y[which[u]]) + (row0 + tok[u]) * p.y_stride[which[u]] + (long long)head[u] * D + c * N),
-               rope_pack<T>(f));
+        S::store(static_cast<T*>(p.y[which[u]]) + (row0 + tok[u]) * p.y_stride[which[u]] + (long long)head[u] * D, c, half, x);
     }
   }
 }
 
-// Backward.  Blocks walk over the tokens; dw_part[block] is what the block's rows add to the weights' gradients.
+// Backward.  Blocks walk over the tokens, once for q and once for k, whose weights and weights' gradients a lane then holds in
+// registers; dw_part[block] is what the block's rows add to the weights' gradients.
 template <typename T, int D, int MODE>
-__global__ void __launch_bounds__(NORM_THREADS) tova_norm_rope_back_kernel(const __grid_constant__ NormRopeParams p) {
-  using S = NormShape<T, D>;
+__global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(const __grid_constant__ NormRopeParams p) {
+  using S = NormShape<T, D, MODE>;
   constexpr int N = S::N, U = 2;
-  __shared__ __align__(16) float cs[NORM_MAX_TOKENS][ROPE_MAX_PAIRS], sn[NORM_MAX_TOKENS][ROPE_MAX_PAIRS];
-  __shared__ float stage_s[MODE == NORM_HALF_ODD ? S::GROUPS : 1][D + 1];
-  __shared__ float sum_s[S::GROUPS][D];
+  __shared__ __align__(16) float cs[NORM_MAX_TOKENS][D / 2], sn[NORM_MAX_TOKENS][D / 2];
+  __shared__ float sum_s[NORM_THREADS / 32][D];
   const int group = threadIdx.x / S::LANES, c = threadIdx.x % S::LANES, half = p.rot >> 1;
-  float* stage = stage_s[MODE == NORM_HALF_ODD ? group : 0];
-  const int per_tok = p.heads[0] + p.heads[1];
-  float w[2][N], dw[2][N];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int which = 0; which < 2; ++which) {
+    const int heads = p.heads[which];
+    float w[2][N], dw[2][N];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      w[k][e] = 1.f;
-      dw[k][e] = 0.f;
+    for (int k = 0; k < N; ++k) {
+      int a, b;
+      S::components(S::pair(c, k), half, a, b);
+      w[0][k] = p.w[which] ? (float)static_cast<const T*>(p.w[which])[a] : 1.f;
+      w[1][k] = p.w[which] ? (float)static_cast<const T*>(p.w[which])[b] : 1.f;
+      dw[0][k] = dw[1][k] = 0.f;
     }
-    if (p.w[k]) Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.w[k]) + c * N), w[k]);
-  }
-  for (long long row0 = (long long)blockIdx.x * p.tokens_per_block; row0 < p.rows; row0 += (long long)gridDim.x * p.tokens_per_block) {
-    const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
-    const int total = n_tok * per_tok;
-    for (int i0 = 0; i0 < total; i0 += U * S::GROUPS) {
-      uint4 raw[U], graw[U];
-      int tok[U], which[U], head[U];
+    for (long long row0 = (long long)blockIdx.x * p.tokens_per_block; row0 < p.rows && heads > 0; row0 += (long long)gridDim.x * p.tokens_per_block) {
+      const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
+      const int total = n_tok * heads;
+      for (int i0 = 0; i0 < total; i0 += U * S::GROUPS) {
+        typename S::Raw raw[U], graw[U];
+        int tok[U], head[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = min(i0 + u * S::GROUPS + group, total - 1);
-        tok[u] = i / per_tok;
-        head[u] = i - tok[u] * per_tok;
-        which[u] = head[u] >= p.heads[0];
-        if (which[u]) head[u] -= p.heads[0];
-        const long long at = (long long)head[u] * D + c * N;
-        raw[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(p.x[which[u]]) + (row0 + tok[u]) * p.x_stride[which[u]] + at));
-        graw[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(p.dy[which[u]]) + (row0 + tok[u]) * p.dy_stride[which[u]] + at));
-      }
-      if (i0 == 0) {
-        __syncthreads();               // (the tokens before have been turned)
-        norm_angles(p, row0, n_tok, cs, sn);
-        __syncthreads();
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i0 + u * S::GROUPS >= total) break;
-        const bool in = i0 + u * S::GROUPS + group < total;
-        float x[N], g[N], sum = 0.f;
-        Vec16<T>::unpack(raw[u], x);
-        Vec16<T>::unpack(graw[u], g);
-        norm_turn<T, D, MODE>(g, c, half, cs[tok[u]], sn[tok[u]], -1.f, stage);
-#pragma unroll
-        for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], sum);
-        const float r = rsqrtf(norm_group_sum<S::LANES>(sum) * (1.f / D) + p.eps);
-        float along = 0.f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          x[e] *= r;
-          const float add = in ? g[e] * x[e] : 0.f;
-          if (which[u]) dw[1][e] += add;
-          else dw[0][e] += add;
-          g[e] *= which[u] ? w[1][e] : w[0][e];
-          along = fmaf(g[e], x[e], along);
+        for (int u = 0; u < U; ++u) {
+          const int i = min(i0 + u * S::GROUPS + group, total - 1);
+          tok[u] = i / heads;
+          head[u] = i - tok[u] * heads;
+          S::load(static_cast<const T*>(p.x[which]) + (row0 + tok[u]) * p.x_stride[which] + (long long)head[u] * D, c, half, raw[u]);
+          S::load(static_cast<const T*>(p.dy[which]) + (row0 + tok[u]) * p.dy_stride[which] + (long long)head[u] * D, c, half, graw[u]);
         }
-        along = norm_group_sum<S::LANES>(along) * (1.f / D);
+        if (i0 == 0) {
+          __syncthreads();               // (the tokens before have been turned)
+          S::angles(p, row0, n_tok, cs, sn);
+          __syncthreads();
+        }
 #pragma unroll
-        for (int e = 0; e < N; ++e) g[e] = r * (g[e] - x[e] * along);
-        if (in)
-          __stcs(reinterpret_cast<uint4*>(static_cast<T*>(p.y[which[u]]) + (row0 + tok[u]) * p.y_stride[which[u]] + (long long)head[u] * D + c * N),
-                 rope_pack<T>(g));
+        for (int u = 0; u < U; ++u) {
+          if (i0 + u * S::GROUPS >= total) break;
+          const bool in = i0 + u * S::GROUPS + group < total;
+          float x[2][N], g[2][N], co[N], si[N], sum = 0.f;
+          S::split(raw[u], c, half, x);
+#pragma unroll
+          for (int k = 0; k < N; ++k) sum = fmaf(x[0][k], x[0][k], fmaf(x[1][k], x[1][k], sum));
+          const float r = rsqrtf(S::sum(sum) * (1.f / D) + p.eps);
+          S::split(graw[u], c, half, g);
+          S::table(cs[tok[u]], c, co);
+          S::table(sn[tok[u]], c, si);
+          float along = 0.f;
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            const float a = g[0][k] * co[k] + g[1][k] * si[k], b = g[1][k] * co[k] - g[0][k] * si[k];
+            x[0][k] *= r;
+            x[1][k] *= r;
+            if (in) {
+              dw[0][k] = fmaf(a, x[0][k], dw[0][k]);
+              dw[1][k] = fmaf(b, x[1][k], dw[1][k]);
+            }
+            g[0][k] = a * w[0][k];
+            g[1][k] = b * w[1][k];
+            along = fmaf(g[0][k], x[0][k], fmaf(g[1][k], x[1][k], along));
+          }
+          along = S::sum(along) * (1.f / D);
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            g[0][k] = r * (g[0][k] - x[0][k] * along);
+            g[1][k] = r * (g[1][k] - x[1][k] * along);
+          }
+          if (in) S::store(static_cast<T*>(p.y[which]) + (row0 + tok[u]) * p.y_stride[which] + (long long)head[u] * D, c, half, g);
+        }
       }
     }
-  }
-  for (int k = 0; k < 2; ++k) {
+    // The groups of a warp, the warps, and out.
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum_s[group][c * N + e] = dw[k][e];
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        float t = dw[x][k];
+#pragma unroll
+        for (int o = S::LANES; o <= 16; o <<= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        int a, b;
+        S::components(S::pair(c, k), half, a, b);
+        if (lane < S::LANES) sum_s[warp][x ? b : a] = t;
+      }
     __syncthreads();
     for (int d = threadIdx.x; d < D; d += NORM_THREADS) {
       float t = 0.f;
 #pragma unroll
-      for (int x = 0; x < S::GROUPS; ++x) t += sum_s[x][d];
-      p.dw_part[((long long)blockIdx.x * 2 + k) * D + d] = t;
+      for (int x = 0; x < NORM_THREADS / 32; ++x) t += sum_s[x][d];
+      p.dw_part[((long long)blockIdx.x * 2 + which) * D + d] = t;
     }
   }
   pdl_launch_dependents();
