@@ -7,12 +7,12 @@
 //
 // Roles in a block.  They meet through mbarriers only and run ahead of one another across items.
 //   1 copying thread    Q, then K and V tiles of 128 tokens by tiled TMA into a ring of slots (128-byte swizzle)
-//   1 issuing thread    S_t = Q_t K^T (128 x 128, fp32 in TMEM) and O_t += P_t V of the two tiles in turn, PV_0(j) S_0(j+1)
+//   1 issuing warp      S_t = Q_t K^T (128 x 128, fp32 in TMEM) and O_t += P_t V of the two tiles in turn, PV_0(j) S_0(j+1)
 //                       PV_1(j) S_1(j+1): one tile's contractions run while the other's soft-max does
 //   4 warps a tile      a thread per row: logits from TMEM, weights as bf16 back over them, where they are the A operand of
-//                       O += P V.  The weights' reference is a whole number, set by the row's first tile and hardly ever moved
-//                       again (see tova_tree_tc.cuh): a later tile needs no maximum, only where its weights sum to more than
-//                       2^32 is it done over.  The sum is over the rounded weights, so that the weights that multiply V add up
+//                       O += P V.  The weights' reference is a whole number, 0 at first and hardly ever moved (see tova_tree_tc.cuh): a
+//                       tile needs no maximum, only where its weights sum to more than 2^32, or a row's first ones to less than
+//                       2^-32, is it done over.  The sum is over the rounded weights, so that the weights that multiply V add up
 //                       to one.  At the end the row of O, divided by its sum.
 //   2 checking warps    V tiles on the diagonal hold values of later tokens, and of other sequences, under weights of 0; where
 //                       one is not finite it becomes 0, and the rows that do see it get it added in the end.
@@ -43,46 +43,48 @@ struct PackedItem {
   int checked;                 // the first column tile with masked columns
 };
 
-template <int D>
+// The items of a block: every grid-th of the list, up and down in turn, so that no block has the longer one each time.  (The
+// list's next entry is fetched an item early.)
 struct PackedWalk {
-  int at, round, total, heads;
-  // Items of this block: every grid-th, up and down in turn, so that no block has the longer one each time.
-  __device__ __forceinline__ void start(const PackedParams& p) {
+  int round, total, heads, x;
+  int4 e;
+  __device__ __forceinline__ int place() const { return round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+  __device__ __forceinline__ void start(const PackedParams& p, const int4& own) {
     heads = p.pairs ? p.H / 2 : p.H;
-    total = p.list ? *p.n_list * heads : 0;
     round = 0;
+    if (p.list) {
+      total = *p.n_list * heads;
+      x = blockIdx.x;
+      if (x < total) e = __ldg(p.list + x / heads);
+    } else {                               // the one item that the block has found itself
+      total = own.w ? 1 : 0;
+      x = 0;
+      e = own;
+    }
   }
-  __device__ __forceinline__ void fill(const PackedParams& p, int4 e, int hd, PackedItem& it) {
+  __device__ __forceinline__ bool next(const PackedParams& p, PackedItem& it) {
+    if (x >= total) return false;
+    const int hd = (p.list ? x : blockIdx.x) % heads, tile = e.z;
     it.t0 = e.x;
     it.t1 = e.y;
-    const int len = e.y - e.x;
     if (p.pairs) {
-      it.q0[0] = it.q0[1] = e.z * 128;
+      it.q0[0] = it.q0[1] = tile * 128;
       it.head[0] = 2 * hd;
       it.head[1] = 2 * hd + 1;
-      it.n[0] = it.n[1] = it.most = e.z + 1;
-      it.checked = e.z;
+      it.n[0] = it.n[1] = it.most = tile + 1;
+      it.checked = tile;
     } else {
-      it.q0[0] = e.z * 256;
+      it.q0[0] = tile * 256;
       it.q0[1] = it.q0[0] + 128;
       it.head[0] = it.head[1] = hd;
-      it.n[0] = 2 * e.z + 1;
-      it.n[1] = it.q0[1] < len ? 2 * e.z + 2 : 0;
+      it.n[0] = 2 * tile + 1;
+      it.n[1] = it.q0[1] < e.y - e.x ? 2 * tile + 2 : 0;
       it.most = max(it.n[0], it.n[1]);
-      it.checked = 2 * e.z;
-    }
-  }
-  __device__ __forceinline__ bool next(const PackedParams& p, const int4& own, PackedItem& it) {
-    int x;
-    if (p.list) {
-      x = round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-      if (x >= total) return false;
-      fill(p, __ldg(p.list + x / heads), x % heads, it);
-    } else {
-      if (round > 0 || own.w == 0) return false;
-      fill(p, own, blockIdx.x % heads, it);
+      it.checked = 2 * tile;
     }
     ++round;
+    x = p.list ? place() : 1;
+    if (x < total) e = __ldg(p.list + x / heads);
     return true;
   }
 };
@@ -139,8 +141,8 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
   const uint32_t tmem = tmem_base_s;
   const int4 own = own_s;
   bool ok = true;
-  PackedWalk<D> walk;
-  walk.start(p);
+  PackedWalk walk;
+  walk.start(p, own);
   PackedItem it;
   // Copies are made and consumed in the order K0 V0 K1 V1 ...; the ring's positions go on from item to item.
   int ring = 0;
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) tma_load_3d_tile(dst + c * (R * 128), map, c * 64, head, token, bar);
       };
-      while (ok && walk.next(p, own, it)) {
+      while (ok && walk.next(p, it)) {
         const int hk = it.head[0] / p.G;
         for (int x = 0; x < 2 * it.most && ok; ++x) {
           const int pos = ring + x, slot = pos % S::SLOTS;
@@ -177,73 +179,91 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
       // (Where a wait ran out it took two seconds, and whatever was on its way has landed since.)
     }
   } else if (warp == S::ISSUER) {
-    // ============================== issuing thread ==============================
-    if (lane == 0) {
-      const uint32_t idesc_s = umma_idesc_bf16(R, C, false), idesc_o = umma_idesc_bf16(R, D, true);
-      const uint64_t q_d = umma_desc_sw128(smem_addr(q_s), 16, 1024);
-      const uint64_t k_d = umma_desc_sw128(smem_addr(slot_s), 16, 1024), v_d = umma_desc_sw128(smem_addr(slot_s), C * 128, 1024);
-      auto at = [](uint64_t d, uint32_t bytes) { return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4)); };
-      auto landed = [&](int pos) { return mbar_wait_bounded(&full[pos % S::SLOTS], (uint32_t)((pos / S::SLOTS) & 1)); };
-      uint32_t used[2] = {0, 0}, weights[2] = {0, 0};
-      for (int item = 0; ok && walk.next(p, own, it); ++item) {
-        auto issue_s = [&](int t, int j) {
-          const uint64_t k_t = at(k_d, ((ring + 2 * j) % S::SLOTS) * S::TILE);
+    // ============================== issuing warp ==============================
+    // The whole warp walks through the items, so that descriptors are formed in the warp's own registers; one lane of it
+    // issues.  (By a single thread the address arithmetic between the contractions left the tensor cores idle.)
+    uint32_t leader;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(leader));
+    const uint32_t idesc_s = umma_idesc_bf16(R, C, false), idesc_o = umma_idesc_bf16(R, D, true);
+    const uint64_t q_d = umma_desc_sw128(smem_addr(q_s), 16, 1024);
+    const uint64_t k_d = umma_desc_sw128(smem_addr(slot_s), 16, 1024), v_d = umma_desc_sw128(smem_addr(slot_s), C * 128, 1024);
+    auto at = [](uint64_t d, uint32_t bytes) { return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4)); };
+    // Positions in the ring: where K and V of the next columns are, as (slot, phase).
+    int k_slot = 0, v_slot = 1;
+    uint32_t k_phase = 0, v_phase = 0;
+    auto step2 = [](int& slot, uint32_t& phase) {
+      slot += 2;
+      if (slot >= S::SLOTS) {
+        slot -= S::SLOTS;
+        phase ^= 1u;
+      }
+    };
+    uint32_t used[2] = {0, 0}, weights[2] = {0, 0};
+    for (int item = 0; ok && walk.next(p, it); ++item) {
+      // S of tile t over the columns in slot k_slot.
+      auto issue_s = [&](int t, bool last) {
+        const uint64_t k_t = at(k_d, k_slot * S::TILE);
+        if (leader) {
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
             umma_bf16(tmem + 256 * t, at(q_d, t * S::TILE + (ks >> 2) * (R * 128) + (ks & 3) * 32), at(k_t, (ks >> 2) * (C * 128) + (ks & 3) * 32),
                       idesc_s, ks > 0 ? 1u : 0u);
           umma_commit(&bar_s[t]);
-          if (j == it.n[t] - 1) umma_commit(&q_free[t]);
-        };
-        ok = landed(ring);
+          if (last) umma_commit(&q_free[t]);
+        }
+        __syncwarp();
+      };
+      ok = warp_wait(&full[k_slot], k_phase);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (it.n[t] == 0) continue;
+        ok = ok && warp_wait(&q_full[t], used[t] & 1);
+        if (!ok) break;
+        ++used[t];
+        tc_fence_after();
+        issue_s(t, it.n[t] == 1);
+      }
+      if (!ok) break;
+      if (leader) umma_commit(&empty[k_slot]);
+      __syncwarp();
+      step2(k_slot, k_phase);
+      for (int j = 0; j < it.most && ok; ++j) {
+        const uint64_t v_t = at(v_d, v_slot * S::TILE);
+        ok = warp_wait(&full[v_slot], v_phase);
+        if (j + 1 < it.most) ok = ok && warp_wait(&full[k_slot], k_phase);
+        if (j == it.checked) ok = ok && warp_wait(&bar_odd[item & 1], (uint32_t)((item >> 1) & 1));
+        if (!ok) break;
+        const int last = j < it.n[1] ? 1 : 0;                  // the last tile that takes these columns
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (it.n[t] == 0) continue;
-          ok = ok && mbar_wait_bounded(&q_full[t], used[t] & 1);
+          if (j >= it.n[t]) continue;
+          ok = warp_wait(&bar_p[t], weights[t] & 1);
           if (!ok) break;
-          ++used[t];
+          ++weights[t];
           tc_fence_after();
-          issue_s(t, 0);
-        }
-        if (!ok) break;
-        umma_commit(&empty[ring % S::SLOTS]);
-        for (int j = 0; j < it.most && ok; ++j) {
-          const int pos = ring + 2 * j + 1;
-          const uint64_t v_t = at(v_d, (pos % S::SLOTS) * S::TILE);
-          ok = landed(pos);
-          if (j == it.checked) ok = ok && mbar_wait_bounded(&bar_odd[item & 1], (uint32_t)((item >> 1) & 1));
-          if (!ok) break;
-          const int last = j < it.n[1] ? 1 : 0;                // the last tile that takes these columns
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (j >= it.n[t]) continue;
-            ok = mbar_wait_bounded(&bar_p[t], weights[t] & 1);
-            if (!ok) break;
-            ++weights[t];
-            tc_fence_after();
+          if (leader) {
 #pragma unroll
             for (int kk = 0; kk < C / 16; ++kk)
               umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + kk * 8, at(v_t, kk * 2048), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
-            if (t == last) umma_commit(&empty[pos % S::SLOTS]);
-            if (j + 1 == it.n[t]) {
-              umma_commit(&bar_o[t]);
-            } else {
-              ok = landed(pos + 1);
-              if (!ok) break;
-              tc_fence_after();
-              issue_s(t, j + 1);
-            }
+            if (j + 1 == it.n[t]) umma_commit(&bar_o[t]);
+            if (t == last) umma_commit(&empty[v_slot]);
           }
-          // (the last tile of all to take the next columns has been issued: all have)
-          if (ok && j + 1 < it.most) umma_commit(&empty[(pos + 1) % S::SLOTS]);
+          __syncwarp();
+          if (j + 1 < it.n[t]) issue_s(t, j + 2 == it.n[t]);
         }
-        ring += 2 * it.most;
+        if (!ok) break;
+        step2(v_slot, v_phase);
+        if (j + 1 < it.most) {             // (the last tile of all to take the next columns has been issued: all have)
+          if (leader) umma_commit(&empty[k_slot]);
+          __syncwarp();
+          step2(k_slot, k_phase);
+        }
       }
     }
   } else if (warp >= S::CHECKER) {
     // ============================== checking warps ==============================
     const int w = warp - S::CHECKER;
-    for (int item = 0; ok && walk.next(p, own, it); ++item) {
+    for (int item = 0; ok && walk.next(p, it); ++item) {
       if (item >= 2) ok = warp_wait(&bar_done[item & 1], (uint32_t)(((item >> 1) - 1) & 1));     // its flag has been read
       bool odd = false;
       // They follow every copy, and a slot is free again only when they have seen what was in it: a wait by parity must be
@@ -254,16 +274,30 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
         if (!ok) break;
         if ((x & 1) && (x >> 1) >= it.checked) {
           unsigned char* v_t = slot_s + slot * S::TILE;
+          // Zero times a value is a NaN where it is not finite.
+          const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+          __nv_bfloat162 found[2] = {zero, zero};
+          auto h = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
           for (int r = w * 32 + lane; r < C; r += 32 * S::CHECK_WARPS) {
 #pragma unroll
             for (int ch = 0; ch < D / 8; ++ch) {
-              uint4* at = reinterpret_cast<uint4*>(v_t + (ch >> 3) * (C * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
-              uint4 v = *at;
-              if (tree_drop_odd(v)) {
-                *at = v;
-                odd = true;
-              }
+              const uint4 v = *reinterpret_cast<const uint4*>(v_t + (ch >> 3) * (C * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+              found[0] = __hfma2(h(v.x), zero, found[0]);
+              found[1] = __hfma2(h(v.y), zero, found[1]);
+              found[0] = __hfma2(h(v.z), zero, found[0]);
+              found[1] = __hfma2(h(v.w), zero, found[1]);
             }
+          }
+          found[0] = __hadd2(found[0], found[1]);
+          if (__low2float(found[0]) != 0.f || __high2float(found[0]) != 0.f) {        // (NaN)
+            for (int r = w * 32 + lane; r < C; r += 32 * S::CHECK_WARPS)
+#pragma unroll 1
+              for (int ch = 0; ch < D / 8; ++ch) {
+                uint4* at = reinterpret_cast<uint4*>(v_t + (ch >> 3) * (C * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+                uint4 v = *at;
+                if (tree_drop_odd(v)) *at = v;
+              }
+            odd = true;
           }
         }
         warp_arrive(&empty[slot], lane);
@@ -280,9 +314,9 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
     const uint32_t base = tmem + 256 * t + ((uint32_t)((warp & 3) * 32) << 16);
     const uint64_t scale_2 = pack_f2(p.scale2, p.scale2);
     uint32_t tiles = 0, outs = 0;
-    for (int item = 0; walk.next(p, own, it); ++item) {
+    for (int item = 0; walk.next(p, it); ++item) {
       const int n = t ? it.n[1] : it.n[0], q0 = t ? it.q0[1] : it.q0[0], head = t ? it.head[1] : it.head[0];
-      float m_ref = -INFINITY, l = 0.f;
+      float m_ref = 0.f, l = 0.f;
       for (int j = 0; j < n && ok; ++j) {
         ok = warp_wait(&bar_s[t], tiles & 1);
         if (!ok) break;
@@ -322,12 +356,10 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
           unpack_f2(add_f2(sum2[0], sum2[1]), s0, s1);
           sum = s0 + s1;
         };
-        bool over = j == 0;                                    // the reference has to be found or moved
-        if (j > 0) {
-          weights();
-          over = __any_sync(0xffffffffu, !(sum <= TREE_TC_MOST) || m_ref == -INFINITY) != 0;
-        }
-        if (over) {
+        weights();
+        // The reference is moved where weights grow too large, or where a row's first ones are all very small (below 2^-32 of a
+        // weight of 1: later ones might lose their smallest).
+        if (__any_sync(0xffffffffu, !(sum <= TREE_TC_MOST) || m_ref == -INFINITY || (j == 0 && sum < 1.f / TREE_TC_MOST))) {
           float top = -INFINITY;
 #pragma unroll
           for (int c = 0; c < C / 32; ++c) {
@@ -340,9 +372,9 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
           }
           top *= p.scale2;
           // (a reference that is right already stays: another row of the warp asked)
-          const bool beyond = top > m_ref + 16.f || (m_ref == -INFINITY && top > -INFINITY);
+          const bool beyond = top > m_ref + 16.f || j == 0 || (m_ref == -INFINITY && top > -INFINITY);
           const float m_new = beyond ? ceilf(top) : m_ref;
-          const float corr = beyond ? ex2_approx(m_ref - m_new) : 1.f;       // a power of two, or 0
+          const float corr = beyond && j > 0 ? ex2_approx(m_ref - m_new) : 1.f;       // a power of two, or 0
           m_ref = m_new;
           l *= corr;
           // (S of this tile was issued behind O of the one before, which is complete therefore)
@@ -371,7 +403,8 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
         const int tok = it.t0 + q0 + row;
         const bool in = tok < it.t1;
         const float r = 1.f / l;
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + ((long long)tok * p.H + head) * D;
+        const int first = tok - (lane & 3);                    // of the four rows whose pieces this lane stores
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + ((long long)first * p.H + head) * D;
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
           float o[32];
@@ -395,12 +428,28 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
               }
             }
           }
-          if (in) {
+          // Four lanes transpose their four 16-byte pieces, so that each store writes 64 bytes of a row: eight rows an
+          // instruction, not 32.
+          uint4 w[4];
 #pragma unroll
-            for (int k = 0; k < 32; k += 8)
-              *reinterpret_cast<uint4*>(out + c + k) = make_uint4(pack_bf16(o[k] * r, o[k + 1] * r), pack_bf16(o[k + 2] * r, o[k + 3] * r),
-                                                                  pack_bf16(o[k + 4] * r, o[k + 5] * r), pack_bf16(o[k + 6] * r, o[k + 7] * r));
-          }
+          for (int k = 0; k < 4; ++k)
+            w[k] = make_uint4(pack_bf16(o[8 * k] * r, o[8 * k + 1] * r), pack_bf16(o[8 * k + 2] * r, o[8 * k + 3] * r),
+                              pack_bf16(o[8 * k + 4] * r, o[8 * k + 5] * r), pack_bf16(o[8 * k + 6] * r, o[8 * k + 7] * r));
+#pragma unroll
+          for (int bit = 1; bit <= 2; bit <<= 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (k & bit) continue;
+              const bool up = (lane & bit) != 0;
+              const uint4 send = up ? w[k] : w[k | bit], keep = up ? w[k | bit] : w[k];
+              const uint4 got = make_uint4(__shfl_xor_sync(0xffffffffu, send.x, bit), __shfl_xor_sync(0xffffffffu, send.y, bit),
+                                           __shfl_xor_sync(0xffffffffu, send.z, bit), __shfl_xor_sync(0xffffffffu, send.w, bit));
+              w[k] = up ? got : keep;
+              w[k | bit] = up ? keep : got;
+            }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (first + k < it.t1) *reinterpret_cast<uint4*>(out + (long long)k * p.H * D + c + (lane & 3) * 8) = w[k];
           __syncwarp();
         }
         tc_fence_before();                 // O has been read: the next item's first weights are reported behind this
