@@ -5,9 +5,9 @@
 //
 // One pass over the row, in which every thread keeps a maximum, S and E against it, rescaled when the maximum moves; joined at
 // the end.  DRAM bound for many rows.  The n largest need no second pass over the row: they lie in the shares of the n threads
-// whose maxima are the largest (equal maxima: whose first such element comes first), since every other thread's elements have
-// n ahead of them.  Those n shares, V / threads elements each, are read again, one by a warp; what is no less than the n-th of
-// the maxima is collected and ordered by counting.  Where more is collected than there is room for (rows of equal logits), n
+// whose maxima are the largest (of equal ones all, or those whose first such element comes first where they are many), since
+// every other thread's elements have n ahead of them.  Those shares, V / threads elements each, are read again by the warps; what
+// is no less than the n-th of the maxima is collected and ordered by counting.  Where more is collected than there is room for (rows of equal logits), n
 // passes over the shares find one after the other.
 //
 // A block per row; a cluster of eight blocks where rows are few, each with an eighth of the row, which join in the first
@@ -19,9 +19,10 @@
 
 namespace tova {
 
-constexpr int LOGPROBS_THREADS = 256, LOGPROBS_BLOCKS = 6, LOGPROBS_WARPS = LOGPROBS_THREADS / 32;
+constexpr int LOGPROBS_THREADS = 256, LOGPROBS_BLOCKS = 4, LOGPROBS_WARPS = LOGPROBS_THREADS / 32;
 constexpr int LOGPROBS_MAX_TOP = 32;
 constexpr int LOGPROBS_ROOM = 1024;          // elements collected at most
+constexpr int LOGPROBS_SHARES = 64;          // threads' shares read again at most
 constexpr int LOGPROBS_CLUSTER = 8;
 
 struct LogprobsParams {
@@ -103,11 +104,12 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
   constexpr int N = Vec16<T>::N, U = 4, TH = LOGPROBS_THREADS;
   __shared__ float red_s[LOGPROBS_WARPS][3];
   __shared__ uint32_t key_s[TH];
-  __shared__ int first_s[TH], win_s[LOGPROBS_MAX_TOP];
+  __shared__ int first_s[TH], win_s[LOGPROBS_SHARES];
   __shared__ unsigned long long pool_s[LOGPROBS_ROOM];
   __shared__ unsigned long long best_s[LOGPROBS_MAX_TOP], warp_best_s[LOGPROBS_WARPS];
   __shared__ uint32_t bar_s;
-  __shared__ int n_pool, n_win, n_tie, n_put;
+  __shared__ int n_pool, n_above_s, n_win_s;
+  __shared__ float all_s[3];
   // what the blocks of a cluster leave in the first one's memory
   __shared__ float peer_red[CLUSTER ? LOGPROBS_CLUSTER : 1][3];
   __shared__ unsigned long long peer_best[CLUSTER ? LOGPROBS_CLUSTER : 1][LOGPROBS_MAX_TOP];
@@ -140,22 +142,8 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
     const T* kind = nullptr;
     const uint64_t l2e_2 = pack_f2(L2E, L2E);
     uint64_t s2 = pack_f2(0.f, 0.f), e2 = s2;
-    for (int k0 = tid; k0 < n_vec; k0 += U * TH) {
-      uint4 w[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = k0 + u * TH, i = base + k * N;
-        constexpr uint32_t low = LogitLowest<T>::word;
-        w[u] = make_uint4(low, low, low, low);
-        if (i >= lo && i + N <= hi) {
-          w[u] = __ldg(reinterpret_cast<const uint4*>(row + i));
-        } else if (k < n_vec) {
-          float f[N];
-          logits_load<T>(row, i, lo, hi, lowest, f);
-          w[u] = rope_pack<T>(f);
-        }
-      }
-      const float most = logits_most(kind, w);
+    // A larger maximum: what was summed against the one before is scaled.
+    auto raise = [&](float most) {
       if (most > m) {
         if (m != -INFINITY) {
           const float d = m - most, r = ex2_approx(d * L2E);
@@ -164,6 +152,18 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
         }
         m = most;
       }
+    };
+    const int whole0 = base < lo ? 1 : 0, whole1 = (hi - base) / N;        // vectors that lie in the row
+    auto fetch = [&](int k, uint4 (&w)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u, k += TH) {
+        constexpr uint32_t low = LogitLowest<T>::word;
+        w[u] = make_uint4(low, low, low, low);
+        if (k >= whole0 && k < whole1) w[u] = __ldg(reinterpret_cast<const uint4*>(row + base + k * N));
+      }
+    };
+    auto take = [&](const uint4 (&w)[U]) {
+      raise(logits_most(kind, w));
       const uint64_t neg_2 = pack_f2(-m, -m);
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -176,6 +176,30 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
           s2 = add_f2(s2, wt);
           e2 = fma_f2(wt, d, e2);
         }
+    };
+    uint4 wa[U], wb[U];                        // one is on its way while the other is taken
+    fetch(tid, wa);
+    for (int k = tid; k < n_vec; k += 2 * U * TH) {
+      fetch(k + U * TH, wb);
+      take(wa);
+      fetch(k + 2 * U * TH, wa);
+      take(wb);
+    }
+    // The vectors at the row's ends.
+    for (int end = 0; end < 2; ++end) {
+      const int k = end ? n_vec - 1 : 0;
+      if (k < 0 || k >= n_vec || k % TH != tid || (k >= whole0 && k < whole1) || (end && k == 0)) continue;
+      float f[N], most = -INFINITY;
+      logits_load<T>(row, base + k * N, lo, hi, lowest, f);
+#pragma unroll
+      for (int x = 0; x < N; ++x) most = fmaxf(most, f[x]);
+      raise(most);
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        const float d = f[x] - m, w = ex2_approx(d * L2E);
+        s2 = add_f2(s2, pack_f2(w, 0.f));
+        e2 = add_f2(e2, pack_f2(w * d, 0.f));
+      }
     }
     float a, b;
     unpack_f2(s2, a, b);
@@ -218,101 +242,142 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
       red_s[warp][2] = e;
     }
   }
-  key_s[tid] = nan ? 0xffffffffu : logit_key(mine);
-  if (tid == 0) n_pool = n_win = n_tie = n_put = 0;
+  key_s[tid] = tid < n_vec ? (nan ? 0xffffffffu : logit_key(mine)) : 0u;
+  if (tid == 0) n_pool = 0;
   __syncthreads();
   // Joins n triples (m, S, E).
-  auto join = [&](const float (*red)[3], int n, float& gm, float& gs, float& ge) {
-    gm = -INFINITY;
+  auto join = [&](const float (*red)[3], int n, float* out) {
+    float gm = -INFINITY, gs = 0.f, ge = 0.f;
     for (int w = 0; w < n; ++w) gm = fmaxf(gm, red[w][0]);
-    gs = ge = 0.f;
     const float ref = gm == -INFINITY ? 0.f : gm;
     for (int w = 0; w < n; ++w) {
       const float d = red[w][0] - ref, r = ex2_approx(d * L2E);
       ge += r * fmaf(fmaxf(d, -1e30f), red[w][1], red[w][2]);
       gs += r * red[w][1];
     }
+    out[0] = gm;
+    out[1] = gs;
+    out[2] = ge;
   };
-  float gm, gs, ge;
-  join(red_s, LOGPROBS_WARPS, gm, gs, ge);
+  if (tid == 32) join(red_s, LOGPROBS_WARPS, all_s);
 
   // --- the n largest of the block, best_s, in order
-  if (top > 0) {
-    const int active = min(TH, n_vec);        // threads with elements
-    // The n-th largest of the maxima (of all of them where there are fewer): the largest key that `want` maxima reach.
-    const int want = min(top, active);
-    if (warp == 0) {
-      uint32_t k[TH / 32];
+  const int active = min(TH, n_vec);          // threads with elements
+  const int want = min(top, active);
+  if (warp == 0 && top > 0) {
+    // A bar that `want` of the maxima reach at least, and few more: the want-th of 32, each the largest of eight.
+    uint32_t k[TH / 32], most = 0;
 #pragma unroll
-      for (int i = 0; i < TH / 32; ++i) k[i] = lane + 32 * i < active ? key_s[lane + 32 * i] : 0u;
-      uint32_t at = 0;
+    for (int i = 0; i < TH / 32; ++i) {
+      k[i] = key_s[lane + 32 * i];
+      most = max(most, k[i]);
+    }
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+      for (int step = size >> 1; step >= 1; step >>= 1) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, most, step);
+        most = ((lane & size) == 0) == ((lane & step) == 0) ? max(most, other) : min(most, other);      // falling
+      }
+    uint32_t at = __shfl_sync(0xffffffffu, most, want - 1);
+    // The threads above it, and those that equal it.
+    int n = 0, ties = 0;
+    auto count = [&]() {
+      n = ties = 0;
+#pragma unroll
+      for (int i = 0; i < TH / 32; ++i) {
+        n += k[i] > at;
+        ties += k[i] == at;
+      }
+      n = __reduce_add_sync(0xffffffffu, n);
+      ties = __reduce_add_sync(0xffffffffu, ties);
+    };
+    count();
+    if (n + ties > LOGPROBS_SHARES) {
+      // Too many: the want-th largest of all, the largest key that `want` maxima reach, bit by bit.
+      at = 0;
       for (int bit = 31; bit >= 0; --bit) {
         const uint32_t test = at | (1u << bit);
         int c = 0;
 #pragma unroll
         for (int i = 0; i < TH / 32; ++i) c += k[i] >= test;
-        c = __reduce_add_sync(0xffffffffu, c);
-        if (c >= want) {
-          at = test;
-          if (c == want) {                    // the smallest of those that reach it is what is looked for
-            uint32_t low = 0xffffffffu;
-#pragma unroll
-            for (int i = 0; i < TH / 32; ++i)
-              if (k[i] >= test) low = min(low, k[i]);
-            at = __reduce_min_sync(0xffffffffu, low);
-            break;
-          }
-        }
+        if (__reduce_add_sync(0xffffffffu, c) >= want) at = test;
       }
-      if (lane == 0) bar_s = at;
+      count();
     }
-    __syncthreads();
+    const bool room = n + ties <= LOGPROBS_SHARES;
+    int put = 0;
+#pragma unroll
+    for (int i = 0; i < TH / 32; ++i) {
+      const bool in = k[i] > at || (room && k[i] == at);
+      const unsigned m = __ballot_sync(0xffffffffu, in);
+      if (in) win_s[put + __popc(m & ((1u << lane) - 1u))] = lane + 32 * i;
+      put += __popc(m);
+    }
+    if (lane == 0) {
+      bar_s = at;
+      n_above_s = n;
+      n_win_s = room ? n + ties : 0;
+    }
+  }
+  __syncthreads();
+  if (top > 0) {
     const uint32_t bar = bar_s;
-    const bool above = tid < active && key_s[tid] > bar, equal = tid < active && key_s[tid] == bar;
-    if (above) win_s[atomicAdd(&n_win, 1)] = tid;      // (in any order: what comes of it is put in order below)
-    if (equal) atomicAdd(&n_tie, 1);
-    __syncthreads();
-    const int n_above = n_win, ties = n_tie;
-    if (n_above + ties <= want) {
-      if (equal) win_s[n_above + atomicAdd(&n_put, 1)] = tid;
-    } else {
-      // Of the threads whose maxima are equal those whose first such element comes first.
-      int first = 0x7fffffff;
-      if (equal) {
-        for (int k = tid; k < n_vec && first == 0x7fffffff; k += TH) {
-          float f[N];
-          logits_load<T>(row, base + k * N, lo, hi, 0.f, f);
-#pragma unroll
-          for (int x = N - 1; x >= 0; --x) {
-            const int i = base + k * N + x;
-            if (i >= lo && i < hi && logit_key(f[x]) == bar) first = i;
-          }
-        }
-      }
-      first_s[tid] = first;
-      __syncthreads();
-      if (equal) {
-        int before = 0;
-        for (int x = 0; x < active; ++x) before += first_s[x] < first;
-        if (before < want - n_above) win_s[n_above + before] = tid;
-      }
-    }
-    __syncthreads();
-    // Their shares once more, one by a warp.
     const int per = (n_vec + TH - 1) / TH;              // vectors a thread, at most
-    auto each = [&](auto&& use) {                       // use(order) for the elements of the winners' shares that reach the bar
-      for (int w = warp; w < want; w += LOGPROBS_WARPS) {
+    int n_win = n_win_s;
+    if (n_win == 0) {
+      // Of the threads whose maxima are equal those whose first such element comes first.
+      n_win = want;
+      const int n_above = n_above_s;
+      for (int x = warp; x < TH; x += LOGPROBS_WARPS) {
+        if (key_s[x] != bar) {
+          if (lane == 0) first_s[x] = 0x7fffffff;
+          continue;
+        }
+        int first = 0x7fffffff;
         for (int j = lane; j < per; j += 32) {
-          const int k = win_s[w] + j * TH;
+          const int k = x + j * TH;
           if (k >= n_vec) break;
           float f[N];
           logits_load<T>(row, base + k * N, lo, hi, 0.f, f);
 #pragma unroll
-          for (int x = 0; x < N; ++x) {
-            const int i = base + k * N + x;
-            const uint32_t key = logit_key(f[x]);
-            if (i >= lo && i < hi && (key >= bar || want < top)) use(logit_order(key, i));
+          for (int y = 0; y < N; ++y) {
+            const int i = base + k * N + y;
+            if (i >= lo && i < hi && logit_key(f[y]) == bar) first = min(first, i);
           }
+          if (first != 0x7fffffff) break;
+        }
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (lane == 0) first_s[x] = first;
+      }
+      __syncthreads();
+      if (key_s[tid] == bar) {
+        int before = 0;
+        for (int x = 0; x < active; ++x) before += first_s[x] < first_s[tid];
+        if (before < want - n_above) win_s[n_above + before] = tid;
+      }
+      __syncthreads();
+    }
+    // Their shares once more, two at a time by a warp: what reaches the bar (all of them, where there are fewer threads with
+    // elements than elements wanted).
+    auto each = [&](auto&& use) {
+      for (int w = warp; w < n_win; w += 2 * LOGPROBS_WARPS) {
+        for (int j = lane; j < per; j += 32) {
+          float f[2][N];
+          int first[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int x = w + y * LOGPROBS_WARPS, k = x < n_win ? win_s[x] + j * TH : n_vec;
+            first[y] = k < n_vec ? base + k * N : hi;
+            logits_load<T>(row, first[y], lo, hi, 0.f, f[y]);
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+              const uint32_t key = logit_key(f[y][x]);
+              if ((key >= bar || want < top) && first[y] + x >= lo && first[y] + x < hi) use(logit_order(key, first[y] + x));
+            }
         }
       }
     };
@@ -368,14 +433,14 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
       asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(first_block(&peer_best[rank][tid])), "l"(o) : "memory");
     }
     if (tid == 0) {
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][0])), "f"(gm) : "memory");
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][1])), "f"(gs) : "memory");
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][2])), "f"(ge) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][0])), "f"(all_s[0]) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][1])), "f"(all_s[1]) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first_block(&peer_red[rank][2])), "f"(all_s[2]) : "memory");
     }
     cluster_arrive_release();
     if (rank != 0) return;
     cluster_wait_acquire();
-    join(peer_red, LOGPROBS_CLUSTER, gm, gs, ge);
+    if (tid == TH - 1) join(peer_red, LOGPROBS_CLUSTER, all_s);
     if (tid < LOGPROBS_CLUSTER * p.top) {
       const unsigned long long o = peer_best[tid / p.top][tid % p.top];
       int before = 0;
@@ -385,7 +450,7 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
     }
     __syncthreads();
   }
-  const float ls = logf(gs);
+  const float gm = all_s[0], gs = all_s[1], ge = all_s[2], ls = logf(gs);
   if (tid == 0) {
     p.lp[t] = (chosen - gm) - ls;
     if (p.entropy) p.entropy[t] = ls - ge / gs;

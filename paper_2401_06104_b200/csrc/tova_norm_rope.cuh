@@ -15,12 +15,14 @@
 #pragma once
 
 #include "tova_rope.cuh"
+#include "tova_tc.cuh"
 
 namespace tova {
 
 constexpr int NORM_THREADS = 256;
 constexpr int NORM_MAX_TOKENS = 4;                 // tokens a block has angles for at a time
-enum : int { NORM_HALF = 0, NORM_INTERLEAVED = 1, NORM_HALF_ODD = 2 };     // the last: pairs that split vectors
+// Half layout: whole heads; parts of heads; pairs that split vectors.
+enum : int { NORM_HALF = 0, NORM_INTERLEAVED = 1, NORM_HALF_ODD = 2, NORM_HALF_PART = 3 };
 
 struct NormRopeParams {
   const void* x[2];             // q, k: element strides between the rows of consecutive (token, sequence) pairs
@@ -33,6 +35,7 @@ struct NormRopeParams {
   const int32_t* positions;     // [T,B] or NULL: first_pos + token
   long long rows;               // T * B
   int first_pos, B, rot, tokens_per_block;
+  unsigned magic[3];            // ceil(2^32 / heads) for q, k and both: head row i belongs to token i * magic / 2^32
   float factor, eps;
   double turns[ROPE_MAX_PAIRS];
 };
@@ -77,7 +80,13 @@ struct NormShape {
       r.v[1] = __ldcs(reinterpret_cast<const uint4*>(row + b));
     }
   }
-  __device__ __forceinline__ static void store(T* row, int c, int half, const float (&f)[2][N]) {
+  __device__ __forceinline__ static void store(T* row, int c, int half, const uint64_t (&g)[2][N / 2]) {
+    float f[2][N];
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      unpack_f2(g[0][k / 2], f[0][k], f[0][k + 1]);
+      unpack_f2(g[1][k / 2], f[1][k], f[1][k + 1]);
+    }
     if constexpr (MODE == NORM_HALF_ODD) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
@@ -105,32 +114,50 @@ struct NormShape {
     }
   }
   // The lane's pairs are (a + k, b + k) for its two vectors; else they are neighbours in both.
-  __device__ __forceinline__ static bool apart(int c, int half) { return MODE == NORM_HALF && c * N < half; }
+  __device__ __forceinline__ static bool apart(int c, int half) { return MODE == NORM_HALF || (MODE == NORM_HALF_PART && c * N < half); }
   __device__ __forceinline__ static void vectors(int c, int half, int& a, int& b) {
     a = apart(c, half) ? c * N : 2 * c * N;
     b = apart(c, half) ? c * N + half : 2 * c * N + N;
   }
-  __device__ __forceinline__ static void split(const Raw& r, int c, int half, float (&f)[2][N]) {
+  // The pairs' first and second components, two pairs packed.
+  __device__ __forceinline__ static void split(const Raw& r, int c, int half, uint64_t (&f)[2][N / 2]) {
     float u[2][N];
     Vec16<T>::unpack(r.v[0], u[0]);
     Vec16<T>::unpack(r.v[1], u[1]);
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
+    for (int k = 0; k < N; k += 2) {
       if (MODE == NORM_HALF_ODD || apart(c, half)) {
-        f[0][k] = u[0][k];
-        f[1][k] = u[1][k];
+        f[0][k / 2] = pack_f2(u[0][k], u[0][k + 1]);
+        f[1][k / 2] = pack_f2(u[1][k], u[1][k + 1]);
       } else {
-        f[0][k] = u[(2 * k) / N][(2 * k) % N];
-        f[1][k] = u[(2 * k) / N][(2 * k) % N + 1];
+        f[0][k / 2] = pack_f2(u[(2 * k) / N][(2 * k) % N], u[(2 * k) / N][(2 * k) % N + 2]);
+        f[1][k / 2] = pack_f2(u[(2 * k) / N][(2 * k) % N + 1], u[(2 * k) / N][(2 * k) % N + 3]);
       }
     }
   }
-  __device__ __forceinline__ static void table(const float* t, int c, float (&f)[N]) {
+  __device__ __forceinline__ static void table(const float* t, int c, uint64_t (&f)[N / 2]) {
 #pragma unroll
     for (int k = 0; k < N; k += 4) {
-      const float4 x = *reinterpret_cast<const float4*>(t + place(c, k));
-      f[k] = x.x; f[k + 1] = x.y; f[k + 2] = x.z; f[k + 3] = x.w;
+      const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(t + place(c, k));
+      f[k / 2] = x.x;
+      f[k / 2 + 1] = x.y;
     }
+  }
+  // Token and head of head row i (of `heads` a token).
+  __device__ __forceinline__ static void locate(int i, int heads, unsigned magic, int& tok, int& head) {
+    tok = heads == 1 ? i : (int)__umulhi((unsigned)i, magic);
+    head = i - tok * heads;
+  }
+  __device__ __forceinline__ static float squares(const uint64_t (&x)[2][N / 2]) {
+    uint64_t q = mul_f2(x[0][0], x[0][0]);
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+      if (k > 0) q = fma_f2(x[0][k], x[0][k], q);
+      q = fma_f2(x[1][k], x[1][k], q);
+    }
+    float a, b;
+    unpack_f2(q, a, b);
+    return sum(a + b);
   }
   __device__ __forceinline__ static float sum(float x) {
 #pragma unroll
@@ -174,8 +201,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) tova_norm_rope_kernel(const _
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = min(i0 + u * S::GROUPS + group, total - 1);       // (rows behind the last are formed once more, and not stored)
-      tok[u] = i / per_tok;
-      head[u] = i - tok[u] * per_tok;
+      S::locate(i, per_tok, p.magic[2], tok[u], head[u]);
       which[u] = head[u] >= p.heads[0];
       if (which[u]) head[u] -= p.heads[0];
       S::load(static_cast<const T*>(p.x[which[u]]) + (row0 + tok[u]) * p.x_stride[which[u]] + (long long)head[u] * D, c, half, raw[u]);
@@ -194,20 +220,19 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) tova_norm_rope_kernel(const _
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u * S::GROUPS >= total) break;
-      float x[2][N], co[N], si[N], w[2][N], sum = 0.f;
+      uint64_t x[2][N / 2], co[N / 2], si[N / 2], w[2][N / 2];
       S::split(raw[u], c, half, x);
-#pragma unroll
-      for (int k = 0; k < N; ++k) sum = fmaf(x[0][k], x[0][k], fmaf(x[1][k], x[1][k], sum));
-      const float r = rsqrtf(S::sum(sum) * (1.f / D) + p.eps);
+      const float r = rsqrtf(S::squares(x) * (1.f / D) + p.eps);
+      const uint64_t r2 = pack_f2(r, r), minus = pack_f2(-1.f, -1.f);
       S::table(cs[tok[u]], c, co);
       S::table(sn[tok[u]], c, si);
       S::table(w_s[which[u]][0], c, w[0]);
       S::table(w_s[which[u]][1], c, w[1]);
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const float a = x[0][k] * r * w[0][k], b = x[1][k] * r * w[1][k];
-        x[0][k] = a * co[k] - b * si[k];
-        x[1][k] = b * co[k] + a * si[k];
+      for (int k = 0; k < N / 2; ++k) {
+        const uint64_t a = mul_f2(mul_f2(x[0][k], r2), w[0][k]), b = mul_f2(mul_f2(x[1][k], r2), w[1][k]);
+        x[0][k] = fma_f2(a, co[k], mul_f2(mul_f2(b, minus), si[k]));
+        x[1][k] = fma_f2(b, co[k], mul_f2(a, si[k]));
       }
       if (i0 + u * S::GROUPS + group < total)
         S::store(static_cast<T*>(p.y[which[u]]) + (row0 + tok[u]) * p.y_stride[which[u]] + (long long)head[u] * D, c, half, x);
@@ -227,14 +252,20 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int which = 0; which < 2; ++which) {
     const int heads = p.heads[which];
-    float w[2][N], dw[2][N];
+    uint64_t w[2][N / 2], dw[2][N / 2];
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      int a, b;
-      S::components(S::pair(c, k), half, a, b);
-      w[0][k] = p.w[which] ? (float)static_cast<const T*>(p.w[which])[a] : 1.f;
-      w[1][k] = p.w[which] ? (float)static_cast<const T*>(p.w[which])[b] : 1.f;
-      dw[0][k] = dw[1][k] = 0.f;
+    for (int k = 0; k < N; k += 2) {
+      float v[2][2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        int a, b;
+        S::components(S::pair(c, k + x), half, a, b);
+        v[0][x] = p.w[which] ? (float)static_cast<const T*>(p.w[which])[a] : 1.f;
+        v[1][x] = p.w[which] ? (float)static_cast<const T*>(p.w[which])[b] : 1.f;
+      }
+      w[0][k / 2] = pack_f2(v[0][0], v[0][1]);
+      w[1][k / 2] = pack_f2(v[1][0], v[1][1]);
+      dw[0][k / 2] = dw[1][k / 2] = pack_f2(0.f, 0.f);
     }
     for (long long row0 = (long long)blockIdx.x * p.tokens_per_block; row0 < p.rows && heads > 0; row0 += (long long)gridDim.x * p.tokens_per_block) {
       const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
@@ -245,8 +276,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int i = min(i0 + u * S::GROUPS + group, total - 1);
-          tok[u] = i / heads;
-          head[u] = i - tok[u] * heads;
+          S::locate(i, heads, p.magic[which], tok[u], head[u]);
           S::load(static_cast<const T*>(p.x[which]) + (row0 + tok[u]) * p.x_stride[which] + (long long)head[u] * D, c, half, raw[u]);
           S::load(static_cast<const T*>(p.dy[which]) + (row0 + tok[u]) * p.dy_stride[which] + (long long)head[u] * D, c, half, graw[u]);
         }
@@ -259,33 +289,35 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
         for (int u = 0; u < U; ++u) {
           if (i0 + u * S::GROUPS >= total) break;
           const bool in = i0 + u * S::GROUPS + group < total;
-          float x[2][N], g[2][N], co[N], si[N], sum = 0.f;
+          uint64_t x[2][N / 2], g[2][N / 2], co[N / 2], si[N / 2];
           S::split(raw[u], c, half, x);
-#pragma unroll
-          for (int k = 0; k < N; ++k) sum = fmaf(x[0][k], x[0][k], fmaf(x[1][k], x[1][k], sum));
-          const float r = rsqrtf(S::sum(sum) * (1.f / D) + p.eps);
+          const float r = rsqrtf(S::squares(x) * (1.f / D) + p.eps);
+          const uint64_t r2 = pack_f2(r, r), minus = pack_f2(-1.f, -1.f);
           S::split(graw[u], c, half, g);
           S::table(cs[tok[u]], c, co);
           S::table(sn[tok[u]], c, si);
-          float along = 0.f;
+          uint64_t sum2 = pack_f2(0.f, 0.f);
 #pragma unroll
-          for (int k = 0; k < N; ++k) {
-            const float a = g[0][k] * co[k] + g[1][k] * si[k], b = g[1][k] * co[k] - g[0][k] * si[k];
-            x[0][k] *= r;
-            x[1][k] *= r;
+          for (int k = 0; k < N / 2; ++k) {
+            const uint64_t a = fma_f2(g[0][k], co[k], mul_f2(g[1][k], si[k])), b = fma_f2(g[1][k], co[k], mul_f2(mul_f2(g[0][k], minus), si[k]));
+            x[0][k] = mul_f2(x[0][k], r2);
+            x[1][k] = mul_f2(x[1][k], r2);
             if (in) {
-              dw[0][k] = fmaf(a, x[0][k], dw[0][k]);
-              dw[1][k] = fmaf(b, x[1][k], dw[1][k]);
+              dw[0][k] = fma_f2(a, x[0][k], dw[0][k]);
+              dw[1][k] = fma_f2(b, x[1][k], dw[1][k]);
             }
-            g[0][k] = a * w[0][k];
-            g[1][k] = b * w[1][k];
-            along = fmaf(g[0][k], x[0][k], fmaf(g[1][k], x[1][k], along));
+            g[0][k] = mul_f2(a, w[0][k]);
+            g[1][k] = mul_f2(b, w[1][k]);
+            sum2 = fma_f2(g[0][k], x[0][k], fma_f2(g[1][k], x[1][k], sum2));
           }
-          along = S::sum(along) * (1.f / D);
+          float s0, s1;
+          unpack_f2(sum2, s0, s1);
+          const float along = S::sum(s0 + s1) * (-1.f / D);
+          const uint64_t along2 = pack_f2(along, along);
 #pragma unroll
-          for (int k = 0; k < N; ++k) {
-            g[0][k] = r * (g[0][k] - x[0][k] * along);
-            g[1][k] = r * (g[1][k] - x[1][k] * along);
+          for (int k = 0; k < N / 2; ++k) {
+            g[0][k] = mul_f2(r2, fma_f2(x[0][k], along2, g[0][k]));
+            g[1][k] = mul_f2(r2, fma_f2(x[1][k], along2, g[1][k]));
           }
           if (in) S::store(static_cast<T*>(p.y[which]) + (row0 + tok[u]) * p.y_stride[which] + (long long)head[u] * D, c, half, g);
         }
@@ -297,7 +329,9 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        float t = dw[x][k];
+        float both[2];
+        unpack_f2(dw[x][k / 2], both[0], both[1]);
+        float t = both[k & 1];
 #pragma unroll
         for (int o = S::LANES; o <= 16; o <<= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
         int a, b;

@@ -76,7 +76,10 @@ long long norm_back_blocks(const tova_rope_config& c, int32_t n_tokens, int sm_c
 template <typename T, int D>
 cudaError_t norm_launch(const tova::NormRopeParams& p, const tova_rope_config& c, bool back, unsigned grid, cudaStream_t st) {
   constexpr int TH = tova::NORM_THREADS, N = tova::Vec16<T>::N;
-  const int mode = c.layout == TOVA_ROPE_INTERLEAVED ? tova::NORM_INTERLEAVED : (c.rotary_dim / 2) % N == 0 ? tova::NORM_HALF : tova::NORM_HALF_ODD;
+  const int mode = c.layout == TOVA_ROPE_INTERLEAVED ? tova::NORM_INTERLEAVED
+                   : c.rotary_dim == c.head_dim      ? tova::NORM_HALF
+                   : (c.rotary_dim / 2) % N == 0     ? tova::NORM_HALF_PART
+                                                     : tova::NORM_HALF_ODD;
 #define TOVA_NORM_GO(M)                                                                    \
   if (back) tova::tova_norm_rope_back_kernel<T, D, M><<<grid, TH, 0, st>>>(p);             \
   else tova::tova_norm_rope_kernel<T, D, M><<<grid, TH, 0, st>>>(p);
@@ -84,6 +87,8 @@ cudaError_t norm_launch(const tova::NormRopeParams& p, const tova_rope_config& c
     TOVA_NORM_GO(tova::NORM_HALF)
   } else if (mode == tova::NORM_INTERLEAVED) {
     TOVA_NORM_GO(tova::NORM_INTERLEAVED)
+  } else if (mode == tova::NORM_HALF_PART) {
+    TOVA_NORM_GO(tova::NORM_HALF_PART)
   } else {
     TOVA_NORM_GO(tova::NORM_HALF_ODD)
   }
@@ -101,6 +106,8 @@ void norm_fill(tova::NormRopeParams& p, const tova_rope* r, int32_t n_tokens, co
   const tova_rope_config& c = r->cfg;
   p.heads[0] = c.n_q_heads;
   p.heads[1] = k ? c.n_kv_heads : 0;
+  const int heads[3] = {p.heads[0], p.heads[1], p.heads[0] + p.heads[1]};
+  for (int i = 0; i < 3; ++i) p.magic[i] = heads[i] > 1 ? (unsigned)(((1ull << 32) + heads[i] - 1) / heads[i]) : 0;
   p.w[0] = qw; p.w[1] = kw;
   p.positions = positions;
   p.rows = (long long)n_tokens * c.batch;
