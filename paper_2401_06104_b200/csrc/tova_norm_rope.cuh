@@ -20,7 +20,9 @@
 namespace tova {
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_MAX_TOKENS = 4;                 // tokens a block has angles for at a time
+constexpr int NORM_MAX_TOKENS = 4;                 // tokens of a block, forward
+constexpr int NORM_BACK_THREADS = 256, NORM_BACK_BLOCKS = 2;      // gradient: blocks resident on an SM
+constexpr int NORM_BACK_TOKENS = 8;                // tokens a block has angles for at a time
 // Half layout: whole heads; parts of heads; pairs that split vectors.
 enum : int { NORM_HALF = 0, NORM_INTERLEAVED = 1, NORM_HALF_ODD = 2, NORM_HALF_PART = 3 };
 
@@ -34,7 +36,8 @@ struct NormRopeParams {
   int heads[2];                 // heads of q, of k (0: no k)
   const int32_t* positions;     // [T,B] or NULL: first_pos + token
   long long rows;               // T * B
-  int first_pos, B, rot, tokens_per_block;
+  int first_pos, B, rot;
+  int tokens_per_block;         // (gradient: in all)
   unsigned magic[3];            // ceil(2^32 / heads) for q, k and both: head row i belongs to token i * magic / 2^32
   float factor, eps;
   double turns[ROPE_MAX_PAIRS];
@@ -44,7 +47,7 @@ struct NormRopeParams {
 // are pairs that turn by nothing.
 template <typename T, int D, int MODE>
 struct NormShape {
-  static constexpr int N = Vec16<T>::N, LANES = D / (2 * N), GROUPS = NORM_THREADS / LANES;     // rows at a time
+  static constexpr int N = Vec16<T>::N, LANES = D / (2 * N);
   // Pair k of lane c, and its two components.
   __device__ __forceinline__ static int pair(int c, int k) { return MODE == NORM_HALF_ODD ? k * LANES + c : c * N + k; }
   __device__ __forceinline__ static void components(int i, int half, int& a, int& b) {
@@ -167,7 +170,7 @@ struct NormShape {
   // Angles of the block's tokens.
   __device__ __forceinline__ static void angles(const NormRopeParams& p, long long row0, int n_tok, float (*cs)[D / 2], float (*sn)[D / 2]) {
     const int half = p.rot >> 1;
-    for (int i = threadIdx.x; i < n_tok * (D / 2); i += NORM_THREADS) {
+    for (int i = threadIdx.x; i < n_tok * (D / 2); i += blockDim.x) {
       const int t = i / (D / 2), at = i - t * (D / 2), k = at / LANES, c = at - k * LANES, j = pair(c, k);
       float s = 0.f, co = 1.f;
       if (j < half) {
@@ -189,18 +192,18 @@ struct NormShape {
 template <typename T, int D, int MODE>
 __global__ void __launch_bounds__(NORM_THREADS, 4) tova_norm_rope_kernel(const __grid_constant__ NormRopeParams p) {
   using S = NormShape<T, D, MODE>;
-  constexpr int N = S::N, U = 2;
+  constexpr int N = S::N, U = 2, GROUPS = NORM_THREADS / S::LANES;      // rows at a time
   __shared__ __align__(16) float cs[NORM_MAX_TOKENS][D / 2], sn[NORM_MAX_TOKENS][D / 2], w_s[2][2][D / 2];
   const int group = threadIdx.x / S::LANES, c = threadIdx.x % S::LANES, half = p.rot >> 1;
   const long long row0 = (long long)blockIdx.x * p.tokens_per_block;
   const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
   const int per_tok = p.heads[0] + p.heads[1], total = n_tok * per_tok;
-  for (int i0 = 0; i0 < total; i0 += U * S::GROUPS) {
+  for (int i0 = 0; i0 < total; i0 += U * GROUPS) {
     typename S::Raw raw[U];
     int tok[U], which[U], head[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = min(i0 + u * S::GROUPS + group, total - 1);       // (rows behind the last are formed once more, and not stored)
+      const int i = min(i0 + u * GROUPS + group, total - 1);       // (rows behind the last are formed once more, and not stored)
       S::locate(i, per_tok, p.magic[2], tok[u], head[u]);
       which[u] = head[u] >= p.heads[0];
       if (which[u]) head[u] -= p.heads[0];
@@ -219,7 +222,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) tova_norm_rope_kernel(const _
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u * S::GROUPS >= total) break;
+      if (i0 + u * GROUPS >= total) break;
       uint64_t x[2][N / 2], co[N / 2], si[N / 2], w[2][N / 2];
       S::split(raw[u], c, half, x);
       const float r = rsqrtf(S::squares(x) * (1.f / D) + p.eps);
@@ -234,20 +237,20 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) tova_norm_rope_kernel(const _
         x[0][k] = fma_f2(a, co[k], mul_f2(mul_f2(b, minus), si[k]));
         x[1][k] = fma_f2(b, co[k], mul_f2(a, si[k]));
       }
-      if (i0 + u * S::GROUPS + group < total)
+      if (i0 + u * GROUPS + group < total)
         S::store(static_cast<T*>(p.y[which[u]]) + (row0 + tok[u]) * p.y_stride[which[u]] + (long long)head[u] * D, c, half, x);
     }
   }
 }
 
-// Backward.  Blocks walk over the tokens, once for q and once for k, whose weights and weights' gradients a lane then holds in
-// registers; dw_part[block] is what the block's rows add to the weights' gradients.
+// Backward.  A block walks over its share of the tokens, once for q and once for k, whose weights and weights' gradients a lane
+// then holds in registers; dw_part[block] is what the block's rows add to the weights' gradients.
 template <typename T, int D, int MODE>
-__global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(const __grid_constant__ NormRopeParams p) {
+__global__ void __launch_bounds__(NORM_BACK_THREADS, NORM_BACK_BLOCKS) tova_norm_rope_back_kernel(const __grid_constant__ NormRopeParams p) {
   using S = NormShape<T, D, MODE>;
-  constexpr int N = S::N, U = 2;
-  __shared__ __align__(16) float cs[NORM_MAX_TOKENS][D / 2], sn[NORM_MAX_TOKENS][D / 2];
-  __shared__ float sum_s[NORM_THREADS / 32][D];
+  constexpr int N = S::N, U = 2, GROUPS = NORM_BACK_THREADS / S::LANES;
+  __shared__ __align__(16) float cs[NORM_BACK_TOKENS][D / 2], sn[NORM_BACK_TOKENS][D / 2];
+  __shared__ float sum_s[NORM_BACK_THREADS / 32][D];
   const int group = threadIdx.x / S::LANES, c = threadIdx.x % S::LANES, half = p.rot >> 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int which = 0; which < 2; ++which) {
@@ -267,15 +270,16 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
       w[1][k / 2] = pack_f2(v[1][0], v[1][1]);
       dw[0][k / 2] = dw[1][k / 2] = pack_f2(0.f, 0.f);
     }
-    for (long long row0 = (long long)blockIdx.x * p.tokens_per_block; row0 < p.rows && heads > 0; row0 += (long long)gridDim.x * p.tokens_per_block) {
-      const int n_tok = (int)min((long long)p.tokens_per_block, p.rows - row0);
+    const long long first = (long long)blockIdx.x * p.tokens_per_block, behind = min(p.rows, first + p.tokens_per_block);
+    for (long long row0 = first; row0 < behind && heads > 0; row0 += NORM_BACK_TOKENS) {
+      const int n_tok = (int)min((long long)NORM_BACK_TOKENS, behind - row0);
       const int total = n_tok * heads;
-      for (int i0 = 0; i0 < total; i0 += U * S::GROUPS) {
+      for (int i0 = 0; i0 < total; i0 += U * GROUPS) {
         typename S::Raw raw[U], graw[U];
         int tok[U], head[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int i = min(i0 + u * S::GROUPS + group, total - 1);
+          const int i = min(i0 + u * GROUPS + group, total - 1);
           S::locate(i, heads, p.magic[which], tok[u], head[u]);
           S::load(static_cast<const T*>(p.x[which]) + (row0 + tok[u]) * p.x_stride[which] + (long long)head[u] * D, c, half, raw[u]);
           S::load(static_cast<const T*>(p.dy[which]) + (row0 + tok[u]) * p.dy_stride[which] + (long long)head[u] * D, c, half, graw[u]);
@@ -287,8 +291,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (i0 + u * S::GROUPS >= total) break;
-          const bool in = i0 + u * S::GROUPS + group < total;
+          if (i0 + u * GROUPS >= total) break;
+          const bool in = i0 + u * GROUPS + group < total;
           uint64_t x[2][N / 2], g[2][N / 2], co[N / 2], si[N / 2];
           S::split(raw[u], c, half, x);
           const float r = rsqrtf(S::squares(x) * (1.f / D) + p.eps);
@@ -339,10 +343,10 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) tova_norm_rope_back_kernel(co
         if (lane < S::LANES) sum_s[warp][x ? b : a] = t;
       }
     __syncthreads();
-    for (int d = threadIdx.x; d < D; d += NORM_THREADS) {
+    for (int d = threadIdx.x; d < D; d += NORM_BACK_THREADS) {
       float t = 0.f;
 #pragma unroll
-      for (int x = 0; x < NORM_THREADS / 32; ++x) t += sum_s[x][d];
+      for (int x = 0; x < NORM_BACK_THREADS / 32; ++x) t += sum_s[x][d];
       p.dw_part[((long long)blockIdx.x * 2 + which) * D + d] = t;
     }
   }

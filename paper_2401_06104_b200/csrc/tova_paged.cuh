@@ -108,7 +108,7 @@ constexpr int PAGED_WARPS = 4, PAGED_THREADS = 32 * PAGED_WARPS, PAGED_UNIT = 16
 constexpr float PAGED_NOTHING = -1.f;      // the sum that stands for "no row seen"
 
 struct PagedCut {
-  int pieces, b, job, part;                // pieces (0: there is none such) of a job that starts in one block's run
+  int pieces, block, part;                 // pieces of a job (0: it was not cut), the block that its first lies in, that one's place
 };
 
 struct PagedParams {
@@ -118,7 +118,7 @@ struct PagedParams {
   void* out;                               // [B,H,D]
   float2* part_ml;                         // [2 * blocks][HEADS]
   float* part_acc;                         // [2 * blocks][HEADS][D]
-  PagedCut* cuts;                          // [blocks]
+  PagedCut* cuts;                          // [B * jobs]
   long long q_stride;
   int B, H, Hkv, G, hgroups, jobs;         // jobs of a sequence: Hkv * hgroups
   int n_pages, max_pages, shift, n_live, least;
@@ -596,7 +596,6 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
     __syncthreads();
     PagedRun r = run_s;
     const long long share = r.end - r.at;       // (only the last block's may be shorter, and it cuts nothing)
-    PagedCut cut{};
     while (r.at < r.end) {
       while (r.at >= r.base + (long long)r.units * p.jobs) {
         r.base += (long long)r.units * p.jobs;
@@ -608,11 +607,12 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
       const int hk = job / p.hgroups, hg = job - hk * p.hgroups, len = paged_len(p, r.b);
       const bool whole = u0 == 0 && u1 == r.units;
       const int part = 2 * blockIdx.x + (r.first ? 0 : 1);
-      if (u0 == 0 && !whole) {
-        cut.pieces = (int)((r.at + r.units - 1) / share) - blockIdx.x + 1;
-        cut.b = r.b;
-        cut.job = job;
+      if (u0 == 0 && tid == 0) {
+        PagedCut cut;
+        cut.pieces = whole ? 0 : (int)((r.at + r.units - 1) / share) - blockIdx.x + 1;
+        cut.block = blockIdx.x;
         cut.part = part;
+        p.cuts[(long long)r.b * p.jobs + job] = cut;
       }
       Core::run(p, r.b, hk, hg, u0 * PAGED_UNIT, min(len, u1 * PAGED_UNIT), &acc_s[warp][0][0], ml_s[warp]);
       __syncthreads();
@@ -632,33 +632,66 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
       r.first = false;
       r.at += u1 - u0;
     }
-    if (tid == 0) p.cuts[blockIdx.x] = cut;
     pdl_launch_dependents();
   }
 }
 
-// Joins the parts of the jobs that were cut: grid = blocks of the first kernel, D threads.
-template <typename Core>
-__global__ void __launch_bounds__(Core::D) tova_paged_join_kernel(const __grid_constant__ PagedParams p) {
-  constexpr int D = Core::D, HEADS = Core::HEADS;
+// Joins the parts of the jobs that were cut.  WIDE (few jobs, many parts each): a block per job and head, grid = (jobs, HEADS),
+// whose warps share out the parts; else a warp per head, grid = (jobs, HEADS / 8).
+constexpr int PAGED_JOIN_WARPS = 8, PAGED_JOIN_THREADS = 32 * PAGED_JOIN_WARPS;
+template <typename Core, bool WIDE>
+__global__ void __launch_bounds__(PAGED_JOIN_THREADS) tova_paged_join_kernel(const __grid_constant__ PagedParams p) {
+  constexpr int D = Core::D, HEADS = Core::HEADS, LANES = D / 4, AT = 32 / LANES;      // lanes a part's row, parts a warp takes at a time
+  __shared__ float4 acc_s[WIDE ? PAGED_JOIN_WARPS : 1][LANES];
+  __shared__ float sum_s[WIDE ? PAGED_JOIN_WARPS : 1];
   pdl_wait();
   const PagedCut cut = p.cuts[blockIdx.x];
   if (cut.pieces == 0) return;
-  const int hk = cut.job / p.hgroups, hg = cut.job - hk * p.hgroups, d = threadIdx.x;
-  const int heads = min(HEADS, p.G - hg * HEADS);
+  const int b = blockIdx.x / p.jobs, job = blockIdx.x - b * p.jobs, hk = job / p.hgroups, hg = job - hk * p.hgroups;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int h = WIDE ? blockIdx.y : blockIdx.y * PAGED_JOIN_WARPS + warp;
+  if (h >= min(HEADS, p.G - hg * HEADS)) return;
   // The parts behind the first are the first ones of the blocks that follow.
-  auto part = [&](int c) { return c == 0 ? cut.part : 2 * ((int)blockIdx.x + c); };
-  for (int h = 0; h < heads; ++h) {
-    PagedJoin j;
-    j.start();
-    for (int c = 0; c < cut.pieces; ++c) j.look(p.part_ml[part(c) * HEADS + h]);
-    float y = 0.f;
+  auto part = [&](int c) { return c == 0 ? cut.part : 2 * (cut.block + c); };
+  PagedJoin j;
+  j.start();
+  for (int c = lane; c < cut.pieces; c += 32) j.look(p.part_ml[part(c) * HEADS + h]);
+  j.base = warp_max(j.base);
+  j.seen = __any_sync(0xffffffffu, j.seen) != 0;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int first = (WIDE ? warp : 0) * AT + lane / LANES, step = (WIDE ? PAGED_JOIN_WARPS : 1) * AT, d = lane % LANES;
 #pragma unroll 4
-    for (int c = 0; c < cut.pieces; ++c) {
-      const float f = j.factor(p.part_ml[part(c) * HEADS + h]);
-      if (f != 0.f) y = fmaf(f, p.part_acc[((long long)part(c) * HEADS + h) * D + d], y);
+  for (int c = first; c < cut.pieces; c += step) {
+    const float4 a = *reinterpret_cast<const float4*>(p.part_acc + ((long long)part(c) * HEADS + h) * D + d * 4);
+    const float f = j.factor(p.part_ml[part(c) * HEADS + h]);
+    if (f != 0.f) y = make_float4(fmaf(f, a.x, y.x), fmaf(f, a.y, y.y), fmaf(f, a.z, y.z), fmaf(f, a.w, y.w));
+  }
+  float l = j.l;
+  if constexpr (AT == 2) {
+    l += __shfl_xor_sync(0xffffffffu, l, LANES);
+    y.x += __shfl_xor_sync(0xffffffffu, y.x, LANES);
+    y.y += __shfl_xor_sync(0xffffffffu, y.y, LANES);
+    y.z += __shfl_xor_sync(0xffffffffu, y.z, LANES);
+    y.w += __shfl_xor_sync(0xffffffffu, y.w, LANES);
+  }
+  if constexpr (WIDE) {
+    if (lane < LANES) acc_s[warp][d] = y;
+    if (lane == 0) sum_s[warp] = l;
+    __syncthreads();
+    if (warp != 0) return;
+    l = 0.f;
+    y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < PAGED_JOIN_WARPS; ++w) {
+      const float4 a = acc_s[w][d];
+      l += sum_s[w];
+      y = make_float4(y.x + a.x, y.y + a.y, y.z + a.z, y.w + a.w);
     }
-    paged_store<typename Core::T>(p, cut.b, hk * p.G + hg * HEADS + h, D, d, j.seen ? y / j.l : 0.f);
+  }
+  if (lane < LANES) {
+    const float r = j.seen ? 1.f / l : 0.f, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) paged_store<typename Core::T>(p, b, hk * p.G + hg * HEADS + h, D, d * 4 + e, j.seen ? v[e] * r : 0.f);
   }
 }
 

@@ -66,22 +66,22 @@ inline size_t round_up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 // ---------------------------------------------------------------------------
 namespace {
 
-// Blocks of the gradient's kernel: a few per SM, none without tokens.
+// Blocks of the gradient's kernel: as many as are resident at a time, none without tokens; even shares of the tokens.
 long long norm_back_blocks(const tova_rope_config& c, int32_t n_tokens, int sm_count, int* tokens_per_block) {
-  const long long rows = (long long)n_tokens * c.batch, most = 4LL * sm_count;
-  *tokens_per_block = (int)std::min<long long>(tova::NORM_MAX_TOKENS, std::max<long long>(1, rows / most));
-  return std::min(most, (rows + *tokens_per_block - 1) / *tokens_per_block);
+  const long long rows = (long long)n_tokens * c.batch, most = (long long)tova::NORM_BACK_BLOCKS * sm_count;
+  *tokens_per_block = (int)((rows + most - 1) / most);
+  return rows == 0 ? 0 : (rows + *tokens_per_block - 1) / *tokens_per_block;
 }
 
 template <typename T, int D>
 cudaError_t norm_launch(const tova::NormRopeParams& p, const tova_rope_config& c, bool back, unsigned grid, cudaStream_t st) {
-  constexpr int TH = tova::NORM_THREADS, N = tova::Vec16<T>::N;
+  constexpr int TH = tova::NORM_THREADS, TB = tova::NORM_BACK_THREADS, N = tova::Vec16<T>::N;
   const int mode = c.layout == TOVA_ROPE_INTERLEAVED ? tova::NORM_INTERLEAVED
                    : c.rotary_dim == c.head_dim      ? tova::NORM_HALF
                    : (c.rotary_dim / 2) % N == 0     ? tova::NORM_HALF_PART
                                                      : tova::NORM_HALF_ODD;
 #define TOVA_NORM_GO(M)                                                                    \
-  if (back) tova::tova_norm_rope_back_kernel<T, D, M><<<grid, TH, 0, st>>>(p);             \
+  if (back) tova::tova_norm_rope_back_kernel<T, D, M><<<grid, TB, 0, st>>>(p);             \
   else tova::tova_norm_rope_kernel<T, D, M><<<grid, TH, 0, st>>>(p);
   if (mode == tova::NORM_HALF) {
     TOVA_NORM_GO(tova::NORM_HALF)
@@ -153,8 +153,8 @@ extern "C" int tova_norm_rope_apply(const tova_rope* r, const void* q, int64_t q
 extern "C" size_t tova_norm_rope_workspace_bytes(const tova_rope* r, int32_t n_tokens) {
   DeviceInfo dev;
   if (!r || n_tokens < 0 || !device_info(&dev)) return (size_t)-1;
-  // (for every number of tokens up to this one: there may be more blocks for fewer tokens, never more than 4 per SM)
-  return (size_t)std::min<long long>(4LL * dev.sm_count, (long long)n_tokens * r->cfg.batch) * 2 * r->cfg.head_dim * sizeof(float);
+  // (for every number of tokens up to this one: there may be more blocks for fewer tokens, never more than are resident)
+  return (size_t)std::min<long long>((long long)tova::NORM_BACK_BLOCKS * dev.sm_count, (long long)n_tokens * r->cfg.batch) * 2 * r->cfg.head_dim * sizeof(float);
 }
 
 extern "C" int tova_norm_rope_backward(const tova_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
@@ -223,6 +223,7 @@ struct PagedPlan {
   int heads, hgroups, jobs;        // query heads a block takes, groups of them in a KV head, jobs of a sequence
   int splits;                      // > 0: a cluster of so many blocks a job; 0: even shares
   int blocks, least;
+  bool wide_join;                  // many parts a job
   size_t acc_bytes, ml_bytes, bytes;
 };
 PagedPlan paged_plan(const tova_paged_config& c, int32_t n_live, int sm_count, bool up_to = false) {
@@ -241,7 +242,8 @@ PagedPlan paged_plan(const tova_paged_config& c, int32_t n_live, int sm_count, b
     t.blocks = (int)std::min<long long>(resident, std::max<long long>(1, jobs * std::max<long long>(1, units)));
     t.acc_bytes = (size_t)t.blocks * 2 * t.heads * c.head_dim * sizeof(float);
     t.ml_bytes = (size_t)t.blocks * 2 * t.heads * sizeof(float2);
-    t.bytes = t.acc_bytes + t.ml_bytes + round_up((size_t)t.blocks * sizeof(tova::PagedCut), 16);
+    t.bytes = t.acc_bytes + t.ml_bytes + round_up((size_t)jobs * sizeof(tova::PagedCut), 16);
+    t.wide_join = t.blocks > 4 * jobs;
   }
   return t;
 }
@@ -252,7 +254,9 @@ cudaError_t paged_launch(const tova::PagedParams& p, const PagedPlan& t, cudaStr
     return start(tova::tova_paged_kernel<Core, true>, dim3((unsigned)t.splits, (unsigned)(p.B * p.jobs)), tova::PAGED_THREADS, 0, t.splits, false, st, p);
   cudaError_t e = start(tova::tova_paged_kernel<Core, false>, dim3((unsigned)t.blocks), tova::PAGED_THREADS, 0, 1, false, st, p);
   if (e != cudaSuccess) return e;
-  return start(tova::tova_paged_join_kernel<Core>, dim3((unsigned)t.blocks), Core::D, 0, 1, true, st, p);
+  const unsigned jobs = (unsigned)(p.B * p.jobs);
+  if (t.wide_join) return start(tova::tova_paged_join_kernel<Core, true>, dim3(jobs, Core::HEADS), tova::PAGED_JOIN_THREADS, 0, 1, true, st, p);
+  return start(tova::tova_paged_join_kernel<Core, false>, dim3(jobs, (Core::HEADS + 7) / 8), tova::PAGED_JOIN_THREADS, 0, 1, true, st, p);
 }
 template <int D>
 cudaError_t paged_run(const tova::PagedParams& p, const PagedPlan& t, bool bf16, cudaStream_t st) {
