@@ -220,17 +220,19 @@ struct PagedMma {
     look(j0 + PAGED_UNIT, next_page);
     for (; j0 < r1; j0 += PAGED_UNIT) {
       const uint32_t next_rows = rows_of(j0 + PAGED_UNIT, next_page);
-      float s[NT][4];
+      float s[NT][4], chain[4][NT][4];                   // (four chains of products)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) chain[y][n][0] = chain[y][n][1] = chain[y][n][2] = chain[y][n][3] = 0.f;
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
         const uint32_t a0[4] = {kr[0][x].x, kr[1][x].x, kr[0][x].y, kr[1][x].y};
         const uint32_t a1[4] = {kr[0][x].z, kr[1][x].z, kr[0][x].w, kr[1][x].w};
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          mma_bf16(s[n], a0, qf[n][x][0], qf[n][x][1]);
-          mma_bf16(s[n], a1, qf[n][x][2], qf[n][x][3]);
+          mma_bf16(chain[(2 * x) & 3][n], a0, qf[n][x][0], qf[n][x][1]);
+          mma_bf16(chain[(2 * x + 1) & 3][n], a1, qf[n][x][2], qf[n][x][3]);
         }
       }
       load_k(j0 + PAGED_UNIT, next_page, next_rows);
@@ -241,6 +243,7 @@ struct PagedMma {
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+          s[n][e] = (chain[0][n][e] + chain[1][n][e]) + (chain[2][n][e] + chain[3][n][e]);
           s[n][e] = (e < 2 ? in0 : in1) ? s[n][e] * p.scale2 : -INFINITY;
           beyond |= s[n][e] > ref[n][e & 1] + 16.f;
         }
@@ -460,11 +463,26 @@ struct PagedJoin {
     l = fmaf(f, ml.y, l);
     return f;
   }
+  // y += this part's four components.
+  __device__ __forceinline__ void add(float2 ml, const float4& a, float4& y) {
+    const float f = factor(ml);
+    if (f != 0.f) y = make_float4(fmaf(f, a.x, y.x), fmaf(f, a.y, y.y), fmaf(f, a.z, y.z), fmaf(f, a.w, y.w));
+  }
 };
 
+// Four components of a result: y / l, zeros where no row was seen.
 template <typename T>
-__device__ __forceinline__ void paged_store(const PagedParams& p, int b, int head, int D, int d, float x) {
-  static_cast<T*>(p.out)[((long long)b * p.H + head) * D + d] = (T)x;
+__device__ __forceinline__ void paged_store(const PagedParams& p, int b, int head, int D, int d, const float4& y, float l) {
+  const float r = 1.f / l;
+  const bool none = l == PAGED_NOTHING;
+  const float v[4] = {none ? 0.f : y.x * r, none ? 0.f : y.y * r, none ? 0.f : y.z * r, none ? 0.f : y.w * r};
+  T* out = static_cast<T*>(p.out) + ((long long)b * p.H + head) * D + d;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(out) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  }
 }
 
 // A block's run of units.
@@ -483,18 +501,19 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
   __shared__ float2 cta_ml[HEADS];
   __shared__ PagedRun run_s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // The warps' sums of head h, component d; l: the sum, ref: their reference.
+  // The warps' sums of head h, components d .. d + 3; l: the sum, ref: their reference.
   auto joined = [&](int h, int d, float& ref, float& l) {
     PagedJoin j;
     j.start();
-#pragma unroll
-    for (int w = 0; w < PAGED_WARPS; ++w) j.look(ml_s[w][h]);
-    float x = 0.f;
+    float2 ml[PAGED_WARPS];
 #pragma unroll
     for (int w = 0; w < PAGED_WARPS; ++w) {
-      const float f = j.factor(ml_s[w][h]);
-      if (f != 0.f) x = fmaf(f, acc_s[w][h][d], x);
+      ml[w] = ml_s[w][h];
+      j.look(ml[w]);
     }
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < PAGED_WARPS; ++w) j.add(ml[w], *reinterpret_cast<const float4*>(&acc_s[w][h][d]), x);
     ref = j.base;
     l = j.seen ? j.l : PAGED_NOTHING;
     return x;
@@ -508,20 +527,20 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
     __syncthreads();
     const int heads = min(HEADS, p.G - hg * HEADS);
     if (splits == 1) {
-      for (int e = tid; e < heads * D; e += PAGED_THREADS) {
-        const int h = e / D, d = e - h * D;
+      for (int e = tid; e < heads * (D / 4); e += PAGED_THREADS) {
+        const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
         float ref, l;
-        const float x = joined(h, d, ref, l);
-        paged_store<T>(p, b, hk * p.G + hg * HEADS + h, D, d, l == PAGED_NOTHING ? 0.f : x / l);
+        const float4 x = joined(h, d, ref, l);
+        paged_store<T>(p, b, hk * p.G + hg * HEADS + h, D, d, x, l);
       }
       return;
     }
     // (each thread writes over what only it reads)
-    for (int e = tid; e < heads * D; e += PAGED_THREADS) {
-      const int h = e / D, d = e - h * D;
+    for (int e = tid; e < heads * (D / 4); e += PAGED_THREADS) {
+      const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
       float ref, l;
-      const float x = joined(h, d, ref, l);
-      acc_s[0][h][d] = x;
+      const float4 x = joined(h, d, ref, l);
+      *reinterpret_cast<float4*>(&acc_s[0][h][d]) = x;
       if (d == 0) cta_ml[h] = make_float2(ref, l);
     }
     cluster_arrive_release();
@@ -531,29 +550,29 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(x)), "r"(r));
       return a;
     };
-    for (int e = rank * PAGED_THREADS + tid; e < heads * D; e += splits * PAGED_THREADS) {
-      const int h = e / D, d = e - h * D;
+    for (int e = rank * PAGED_THREADS + tid; e < heads * (D / 4); e += splits * PAGED_THREADS) {
+      const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
       float2 ml[8];
-      float x[8];
+      float4 x[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
         if (r >= splits) break;
         asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[r].x), "=f"(ml[r].y) : "r"(peer(&cta_ml[h], r)) : "memory");
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x[r]) : "r"(peer(&acc_s[0][h][d], r)) : "memory");
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(x[r].x), "=f"(x[r].y), "=f"(x[r].z), "=f"(x[r].w)
+                     : "r"(peer(&acc_s[0][h][d], r))
+                     : "memory");
       }
       PagedJoin j;
       j.start();
 #pragma unroll
       for (int r = 0; r < 8; ++r)
         if (r < splits) j.look(ml[r]);
-      float y = 0.f;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int r = 0; r < 8; ++r)
-        if (r < splits) {
-          const float f = j.factor(ml[r]);
-          if (f != 0.f) y = fmaf(f, x[r], y);
-        }
-      paged_store<T>(p, b, hk * p.G + hg * HEADS + h, D, d, j.seen ? y / j.l : 0.f);
+        if (r < splits) j.add(ml[r], x[r], y);
+      paged_store<T>(p, b, hk * p.G + hg * HEADS + h, D, d, y, j.seen ? j.l : PAGED_NOTHING);
     }
     cluster_arrive_release();             // nobody leaves while another reads its sums
     cluster_wait_acquire();
@@ -617,14 +636,14 @@ __global__ void __launch_bounds__(PAGED_THREADS, Core::MIN_BLOCKS) tova_paged_ke
       Core::run(p, r.b, hk, hg, u0 * PAGED_UNIT, min(len, u1 * PAGED_UNIT), &acc_s[warp][0][0], ml_s[warp]);
       __syncthreads();
       const int heads = min(HEADS, p.G - hg * HEADS);
-      for (int e = tid; e < heads * D; e += PAGED_THREADS) {
-        const int h = e / D, d = e - h * D;
+      for (int e = tid; e < heads * (D / 4); e += PAGED_THREADS) {
+        const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
         float ref, l;
-        const float y = joined(h, d, ref, l);
+        const float4 y = joined(h, d, ref, l);
         if (whole) {
-          paged_store<T>(p, r.b, hk * p.G + hg * HEADS + h, D, d, l == PAGED_NOTHING ? 0.f : y / l);
+          paged_store<T>(p, r.b, hk * p.G + hg * HEADS + h, D, d, y, l);
         } else {
-          p.part_acc[((long long)part * HEADS + h) * D + d] = y;
+          *reinterpret_cast<float4*>(p.part_acc + ((long long)part * HEADS + h) * D + d) = y;
           if (d == 0) p.part_ml[part * HEADS + h] = make_float2(ref, l);
         }
       }
@@ -663,8 +682,7 @@ __global__ void __launch_bounds__(PAGED_JOIN_THREADS) tova_paged_join_kernel(con
 #pragma unroll 4
   for (int c = first; c < cut.pieces; c += step) {
     const float4 a = *reinterpret_cast<const float4*>(p.part_acc + ((long long)part(c) * HEADS + h) * D + d * 4);
-    const float f = j.factor(p.part_ml[part(c) * HEADS + h]);
-    if (f != 0.f) y = make_float4(fmaf(f, a.x, y.x), fmaf(f, a.y, y.y), fmaf(f, a.z, y.z), fmaf(f, a.w, y.w));
+    j.add(p.part_ml[part(c) * HEADS + h], a, y);
   }
   float l = j.l;
   if constexpr (AT == 2) {
@@ -688,11 +706,7 @@ __global__ void __launch_bounds__(PAGED_JOIN_THREADS) tova_paged_join_kernel(con
       y = make_float4(y.x + a.x, y.y + a.y, y.z + a.z, y.w + a.w);
     }
   }
-  if (lane < LANES) {
-    const float r = j.seen ? 1.f / l : 0.f, v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) paged_store<typename Core::T>(p, b, hk * p.G + hg * HEADS + h, D, d * 4 + e, j.seen ? v[e] * r : 0.f);
-  }
+  if (lane < LANES) paged_store<typename Core::T>(p, b, hk * p.G + hg * HEADS + h, D, d * 4, y, j.seen ? l : PAGED_NOTHING);
 }
 
 }  // namespace tova
