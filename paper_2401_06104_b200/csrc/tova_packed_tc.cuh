@@ -9,7 +9,7 @@
 //   1 copying thread    Q, then K and V tiles of 128 tokens by tiled TMA into a ring of slots (128-byte swizzle)
 //   1 issuing warp      S_t = Q_t K^T (128 x 128, fp32 in TMEM) and O_t += P_t V of the two tiles in turn, PV_0(j) S_0(j+1)
 //                       PV_1(j) S_1(j+1): one tile's contractions run while the other's soft-max does
-//   8 warps a tile      two threads a row: logits from TMEM, weights as bf16 back over them, where they are the A operand of
+//   4 warps a tile      a thread per row: logits from TMEM, weights as bf16 back over them, where they are the A operand of
 //                       O += P V.  The weights' reference is a whole number, 0 at first and hardly ever moved (see tova_tree_tc.cuh): a
 //                       tile needs no maximum, only where its weights sum to more than 2^32, or a row's first ones to less than
 //                       2^-32, is it done over.  The sum is over the rounded weights, so that the weights that multiply V add up
@@ -29,8 +29,8 @@ template <int D>
 struct PackedTcShape {
   static constexpr int ROWS = 128, COLS = 128;
   static constexpr int TILE = ROWS * D * 2;                    // bytes of a tile of Q, K or V
-  static constexpr int SLOTS = D == 128 ? 4 : 8;
-  static constexpr int SOFT_WARPS = 16, COPIER = 16, ISSUER = 17, CHECKER = 18, CHECK_WARPS = 2;   // first warp of each role
+  static constexpr int SLOTS = D == 128 ? 5 : 8;
+  static constexpr int SOFT_WARPS = 8, COPIER = 8, ISSUER = 9, CHECKER = 10, CHECK_WARPS = 2;      // first warp of each role
   static constexpr int THREADS = 32 * (CHECKER + CHECK_WARPS);
   static constexpr int SMEM = (2 + SLOTS) * TILE + 1024;
 };
@@ -100,13 +100,10 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
   unsigned char *q_s = smem, *slot_s = smem + 2 * S::TILE;     // boxes of [128 rows][128 bytes]
   // landed and free again: Q of a tile, a slot; S computed, weights written, O complete; diagonal tiles checked, an item's rows
   // written (by items of even and odd number)
-  __shared__ __align__(8) uint64_t q_full[2], q_free[2], full[S::SLOTS], empty[S::SLOTS], bar_s[2], bar_p[2], bar_o[2], bar_odd[2], bar_done[2], bar_pair[8];
+  __shared__ __align__(8) uint64_t q_full[2], q_free[2], full[S::SLOTS], empty[S::SLOTS], bar_s[2], bar_p[2], bar_o[2], bar_odd[2], bar_done[2];
   __shared__ uint32_t tmem_base_s;
   __shared__ int odd_s[2][S::CHECK_WARPS];
   __shared__ int4 own_s;
-  // For the two warps of 32 rows, see the soft-max: the rows' references, their maxima, the halves' sums, and how far each is.
-  __shared__ float ref_s[2 * R], top_s[2 * R], sum_s[2][2 * R];
-  __shared__ int lock_s[8], go_s[8], done_s[2][8], want_s[2][8];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
@@ -118,15 +115,13 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
       mbar_init(&q_full[t], 1);
       mbar_init(&q_free[t], 1);
       mbar_init(&bar_s[t], 1);
-      mbar_init(&bar_p[t], 8);
+      mbar_init(&bar_p[t], 4);
       mbar_init(&bar_o[t], 1);
       mbar_init(&bar_odd[t], S::CHECK_WARPS);
       mbar_init(&bar_done[t], S::SOFT_WARPS);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(&bar_pair[i], 2);
     mbar_fence_init();
   }
-  if (tid < 8) lock_s[tid] = go_s[tid] = done_s[0][tid] = done_s[1][tid] = want_s[0][tid] = want_s[1][tid] = 0;
   if (warp == S::ISSUER) {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_s)), "r"(512) : "memory");
@@ -249,7 +244,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
           if (leader) {
 #pragma unroll
             for (int kk = 0; kk < C / 16; ++kk)
-              umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + (kk >> 2) * 64 + (kk & 3) * 8, at(v_t, kk * 2048), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+              umma_bf16_a_tmem(tmem + 256 * t + 128, tmem + 256 * t + kk * 8, at(v_t, kk * 2048), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
             if (j + 1 == it.n[t]) umma_commit(&bar_o[t]);
             if (t == last) umma_commit(&empty[v_slot]);
           }
@@ -314,70 +309,44 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
       ring += 2 * it.most;
     }
   } else {
-    // ============================== soft-max: two threads per row ==============================
-    // Warps 0-3 of a tile take the first 64 columns of its rows, warps 4-7 the others (a warp reaches the 32 TMEM lanes of its
-    // quarter): four warps a scheduler, since one warp's chain of loads, exponentials and conversions leaves it idle half the
-    // time.  The two do not meet on the way: a row's reference lies in shared memory, and whoever finds that it has to be moved
-    // does that for both, while the other waits for the next tile (which is not computed before both have reported this one),
-    // or, if it found so too, for the new reference.
-    const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, pair = t * 4 + quarter, row = quarter * 32 + lane;
-    const uint32_t base = tmem + 256 * t + ((uint32_t)(quarter * 32) << 16);
+    // ============================== soft-max: a thread per row ==============================
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t base = tmem + 256 * t + ((uint32_t)((warp & 3) * 32) << 16);
     const uint64_t scale_2 = pack_f2(p.scale2, p.scale2);
-    volatile float* const my_ref = &ref_s[t * R + row];
     uint32_t tiles = 0, outs = 0;
-    // A word that another warp writes: waits, for two seconds at most, until it is `from` or more.
-    auto reach = [&](volatile int* word, int from, volatile int* other_word) {
-      const unsigned long long t0 = global_ns();
-      while (*word < from && !(other_word && *other_word >= from))
-        if (global_ns() - t0 > WAIT_LIMIT_NS) return false;
-      return true;
-    };
     for (int item = 0; walk.next(p, it); ++item) {
       const int n = t ? it.n[1] : it.n[0], q0 = t ? it.q0[1] : it.q0[0], head = t ? it.head[1] : it.head[0];
-      float ref = 0.f, l = 0.f;                                // this half's sum, against the reference
-      // The reference as the other warp may have moved it.
-      auto follow = [&]() {
-        const float now = *my_ref;
-        if (now != ref) {
-          if (l != 0.f) l *= ex2_approx((ref == -INFINITY ? 0.f : ref) - now);
-          ref = now;
-        }
-      };
+      float m_ref = 0.f, l = 0.f;
       for (int j = 0; j < n && ok; ++j) {
         ok = warp_wait(&bar_s[t], tiles & 1);
         if (!ok) break;
         ++tiles;
         tc_fence_after();
-        if (j == 0) {
-          if (half == 0) *my_ref = 0.f;
-        } else {
-          follow();
-        }
         const bool masked = j * C >= q0;                       // the diagonal
-        uint32_t w[C / 4];                                     // packed weights
+        uint32_t w[C / 2];                                     // packed weights
         float sum;
-        auto logits = [&](int c, uint32_t (&s)[32]) {
-          tmem_ld32_start(base + 64 * half + 32 * c, s);
-          tmem_ld32_wait(s);
+        auto mask = [&](int c, uint32_t (&s)[32]) {
           if (masked) {
-            const int left = row - 64 * half - 32 * c;         // columns up to the row's own
-            const uint32_t see = left >= 31 ? 0xffffffffu : left >= 0 ? (2u << left) - 1u : 0u;
+            const uint32_t see = row >= 32 * c + 31 ? 0xffffffffu : row >= 32 * c ? (2u << (row - 32 * c)) - 1u : 0u;
 #pragma unroll
             for (int x = 0; x < 32; ++x) s[x] = ((see >> x) & 1u) ? s[x] : 0xff800000u;
           }
         };
         auto weights = [&]() {
-          const float r = ref == -INFINITY ? 0.f : ref;
-          const uint64_t neg_2 = pack_f2(-r, -r);
+          const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+          const uint64_t neg_2 = pack_f2(-ref, -ref);
           uint64_t sum2[2] = {pack_f2(0.f, 0.f), pack_f2(0.f, 0.f)};
+          uint32_t s[2][32];
+          tmem_ld32_start(base, s[0]);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t s[32];
-            logits(c, s);
+          for (int c = 0; c < C / 32; ++c) {
+            tmem_ld32_wait(s[c & 1]);
+            if (c + 1 < C / 32) tmem_ld32_start(base + 32 * (c + 1), s[(c + 1) & 1]);
+            mask(c, s[c & 1]);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float x0, x1;
-              unpack_f2(fma_f2(pack_f2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), scale_2, neg_2), x0, x1);
+              unpack_f2(fma_f2(pack_f2(__uint_as_float(s[c & 1][2 * e]), __uint_as_float(s[c & 1][2 * e + 1])), scale_2, neg_2), x0, x1);
               const uint32_t u = pack_bf16(ex2_approx(x0), ex2_approx(x1));
               sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
               w[16 * c + e] = u;
@@ -388,118 +357,56 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
           sum = s0 + s1;
         };
         weights();
-        // The reference is moved where weights grow too large, or where nothing has been summed so far and the first ones are all
-        // very small (below 2^-32 of a weight of 1: later ones might lose their smallest).
-        const bool fresh = j == 0 || ref == -INFINITY;
-        if (__any_sync(0xffffffffu, sum > TREE_TC_MOST || (fresh && sum < 1.f / TREE_TC_MOST && !(masked && row < 64 * half)))) {
+        // The reference is moved where weights grow too large, or where a row's first ones are all very small (below 2^-32 of a
+        // weight of 1: later ones might lose their smallest).
+        if (__any_sync(0xffffffffu, !(sum <= TREE_TC_MOST) || m_ref == -INFINITY || (j == 0 && sum < 1.f / TREE_TC_MOST))) {
           float top = -INFINITY;
-#pragma unroll 1
-          for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int c = 0; c < C / 32; ++c) {
             uint32_t s[32];
-            logits(c, s);
+            tmem_ld32_start(base + 32 * c, s);
+            tmem_ld32_wait(s);
+            mask(c, s);
 #pragma unroll
             for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(s[x]));
           }
           top *= p.scale2;
-          const int id = (int)tiles;
-          int first = 0;
-          if (lane == 0) first = atomicMax(&lock_s[pair], id) < id;
-          first = __shfl_sync(0xffffffffu, first, 0);
-          if (first) {
-            ok = __all_sync(0xffffffffu, reach(&done_s[half ^ 1][pair], id, &want_s[half ^ 1][pair])) != 0;
-            if (!ok) break;
-            __threadfence_block();
-            tc_fence_after();
-            const bool other_done = *(volatile int*)&done_s[half ^ 1][pair] >= id;
-            const uint32_t theirs = base + 64 * (half ^ 1);    // the other's weights, if it has stored them
-            bool some = false;                                 // it has weights that are not zero
-            if (other_done) {
-#pragma unroll 1
-              for (int c = 0; c < 32; c += 16) {
-                uint32_t v[16];
-                tmem_ld16(theirs + c, v);
+          // (a reference that is right already stays: another row of the warp asked)
+          const bool beyond = top > m_ref + 16.f || j == 0 || (m_ref == -INFINITY && top > -INFINITY);
+          const float m_new = beyond ? ceilf(top) : m_ref;
+          const float corr = beyond && j > 0 ? ex2_approx(m_ref - m_new) : 1.f;       // a power of two, or 0
+          m_ref = m_new;
+          l *= corr;
+          // (S of this tile was issued behind O of the one before, which is complete therefore)
+          if (j > 0) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) some |= v[k] != 0;
-              }
-            } else {
-              top = fmaxf(top, *(volatile float*)&top_s[t * R + row]);
-            }
-            // (a reference that is right already stays: another row of the warp asked)
-            const float was = ref == -INFINITY ? 0.f : ref;
-            float now = ref;
-            if (top > was + 16.f || (fresh && !some)) now = ceilf(top);
-            else if (fresh) now = was;
-            const float corr = now == -INFINITY ? 1.f : ex2_approx(was - now);       // a power of two, or 0
-            if (!fresh) l *= corr;
-            if (j > 0) {
-              // (S of this tile was issued behind O of the one before, which is complete therefore)
-#pragma unroll 1
-              for (int c = 0; c < D; c += 16) tree_tc_scale16(base + 128 + c, fresh ? 1.f : corr);
-            }
-            if (other_done) {
-              const __nv_bfloat162 f = __floats2bfloat162_rn(some ? corr : 1.f, some ? corr : 1.f);
-#pragma unroll 1
-              for (int c = 0; c < 32; c += 16) {
-                uint32_t v[16];
-                tmem_ld16(theirs + c, v);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                  const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[k]), f);
-                  v[k] = *reinterpret_cast<const uint32_t*>(&x);
-                }
-                tmem_st16(theirs + c, v);
-              }
-            }
-            ref = now;
-            *my_ref = now;
-            __threadfence_block();
-            __syncwarp();
-            if (lane == 0) *(volatile int*)&go_s[pair] = id;
-          } else {
-            *(volatile float*)&top_s[t * R + row] = top;
-            __threadfence_block();
-            __syncwarp();
-            if (lane == 0) *(volatile int*)&want_s[half][pair] = id;
-            ok = __all_sync(0xffffffffu, reach(&go_s[pair], id, nullptr)) != 0;
-            if (!ok) break;
-            __threadfence_block();
-            follow();
+            for (int c = 0; c < D; c += 16) tree_tc_scale16(base + 128 + c, corr);
           }
           weights();
         }
         l += sum;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < C / 32; ++c) {
           uint32_t (&wc)[16] = *reinterpret_cast<uint32_t (*)[16]>(&w[16 * c]);
-          tmem_st16(base + 64 * half + 16 * c, wc);             // over this half's logits, which have been read
+          tmem_st16(base + 16 * c, wc);                        // over logits that have been read
         }
         tmem_st_wait();
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          *(volatile int*)&done_s[half][pair] = (int)tiles;
-          mbar_arrive(&bar_p[t]);
-        }
+        warp_arrive(&bar_p[t], lane);
       }
       if (n > 0) {
         ok = ok && warp_wait(&bar_o[t], outs & 1);
         ok = ok && warp_wait(&bar_odd[item & 1], (uint32_t)((item >> 1) & 1));
+        if (ok) ++outs;
         tc_fence_after();
-        // The row's sum: both halves'.
-        if (ok) follow();
-        sum_s[half][t * R + row] = l;
-        warp_arrive(&bar_pair[pair], lane);
-        ok = ok && warp_wait(&bar_pair[pair], outs & 1);
-        ++outs;
-        l += sum_s[half ^ 1][t * R + row];
         const bool odd = ok && (odd_s[item & 1][0] | odd_s[item & 1][1]) != 0;
         const int tok = it.t0 + q0 + row;
         const bool in = tok < it.t1;
         const float r = 1.f / l;
         const int first = tok - (lane & 3);                    // of the four rows whose pieces this lane stores
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + ((long long)first * p.H + head) * D;
-#pragma unroll 1
-        for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
           float o[32];
           if (ok) {
             tmem_ld32(base + 128 + c, o);
