@@ -111,13 +111,13 @@ __global__ void __launch_bounds__(PACKED_PLAN_THREADS) tova_packed_plan_kernel(c
 // components of the result, a row's 16 threads are neighbouring lanes.  grid = (tiles, H).
 constexpr int PACKED_ALU_ROWS = 64, PACKED_ALU_THREADS = 256;
 template <int D>
-constexpr int packed_alu_smem() { return (3 * 64 * (D + 4) + 64 * 68) * 4; }
+constexpr int packed_alu_smem() { return (2 * 64 * (D + 4) + 64 * 68) * 4; }      // (two blocks an SM)
 
 template <typename T, int D>
-__global__ void __launch_bounds__(PACKED_ALU_THREADS) tova_packed_alu_kernel(const __grid_constant__ PackedParams p) {
+__global__ void __launch_bounds__(PACKED_ALU_THREADS, 2) tova_packed_alu_kernel(const __grid_constant__ PackedParams p) {
   constexpr int R = PACKED_ALU_ROWS, LD = D + 4, LP = 68, N = Vec16<T>::N;
   extern __shared__ __align__(16) float packed_alu_raw[];
-  float *q_s = packed_alu_raw, *k_s = q_s + R * LD, *v_s = k_s + R * LD, *p_s = v_s + R * LD;
+  float *q_s = packed_alu_raw, *k_s = q_s + R * LD, *v_s = k_s, *p_s = k_s + R * LD;      // (V takes the place of K)
   __shared__ int4 found_s;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   pdl_wait();
@@ -162,7 +162,6 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS) tova_packed_alu_kernel(con
     __syncthreads();
     const int n = min(R, t1 - (t0 + j * R));
     load(k_s, p.k, p.k_stride, t0 + j * R, hk, n);
-    load(v_s, p.v, p.v_stride, t0 + j * R, hk, n);
     __syncthreads();
     float s[4][4];
 #pragma unroll
@@ -182,6 +181,8 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS) tova_packed_alu_kernel(con
         for (int c = 0; c < 4; ++c)
           s[i][c] = fmaf(a[i].w, b[c].w, fmaf(a[i].z, b[c].z, fmaf(a[i].y, b[c].y, fmaf(a[i].x, b[c].x, s[i][c]))));
     }
+    __syncthreads();
+    load(v_s, p.v, p.v_stride, t0 + j * R, hk, n);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = ty * 4 + i;
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS) tova_packed_alu_kernel(con
         p_s[r * LP + tx + 16 * c] = w;
       }
     }
-    __syncwarp();               // a row's weights are written and read by the same half warp
+    __syncthreads();            // (V has landed; a row's weights are written and read by the same half warp)
     // A masked weight is 0, and 0 times a value that is not finite would be NaN: on the diagonal the columns end with the row.
     if (j < tile) {
 #pragma unroll 4

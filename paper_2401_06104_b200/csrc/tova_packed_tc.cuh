@@ -25,6 +25,11 @@
 
 namespace tova {
 
+// Two bf16 values, each added to a fp32 sum.
+__device__ __forceinline__ void add_bf16x2(uint32_t u, float& lo, float& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.bf16 %0, a, %0;\n\tadd.rn.f32.bf16 %1, b, %1;\n\t}" : "+f"(lo), "+f"(hi) : "r"(u));
+}
+
 template <int D>
 struct PackedTcShape {
   static constexpr int ROWS = 128, COLS = 128;
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
         auto weights = [&]() {
           const float ref = m_ref == -INFINITY ? 0.f : m_ref;
           const uint64_t neg_2 = pack_f2(-ref, -ref);
-          uint64_t sum2[2] = {pack_f2(0.f, 0.f), pack_f2(0.f, 0.f)};
+          float sums[2] = {0.f, 0.f};
           uint32_t s[2][32];
           tmem_ld32_start(base, s[0]);
 #pragma unroll
@@ -348,13 +353,11 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
               float x0, x1;
               unpack_f2(fma_f2(pack_f2(__uint_as_float(s[c & 1][2 * e]), __uint_as_float(s[c & 1][2 * e + 1])), scale_2, neg_2), x0, x1);
               const uint32_t u = pack_bf16(ex2_approx(x0), ex2_approx(x1));
-              sum2[e & 1] = add_f2(sum2[e & 1], pack_f2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
+              add_bf16x2(u, sums[0], sums[1]);
               w[16 * c + e] = u;
             }
           }
-          float s0, s1;
-          unpack_f2(add_f2(sum2[0], sum2[1]), s0, s1);
-          sum = s0 + s1;
+          sum = sums[0] + sums[1];
         };
         weights();
         // The reference is moved where weights grow too large, or where a row's first ones are all very small (below 2^-32 of a
