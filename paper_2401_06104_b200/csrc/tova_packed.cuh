@@ -150,11 +150,12 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS, 2) tova_packed_alu_kernel(
     }
   };
   load(q_s, p.q, p.q_stride, row0, h, rows);
-  float o[4][D / 16], m[4], l[4];
+  uint64_t o[4][D / 32];                   // pairs of components
+  float m[4], l[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
+    for (int c = 0; c < D / 32; ++c) o[i][c] = 0ull;
     m[i] = -INFINITY;
     l[i] = 0.f;
   }
@@ -164,22 +165,32 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS, 2) tova_packed_alu_kernel(
     load(k_s, p.k, p.k_stride, t0 + j * R, hk, n);
     __syncthreads();
     float s[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
-#pragma unroll 4
-    for (int d = 0; d < D; d += 4) {
-      float4 a[4], b[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(q_s + (ty * 4 + i) * LD + d);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const float4*>(k_s + (tx + 16 * c) * LD + d);
+    {
+      uint64_t s2[4][4];                     // even and odd components, packed
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          s[i][c] = fmaf(a[i].w, b[c].w, fmaf(a[i].z, b[c].z, fmaf(a[i].y, b[c].y, fmaf(a[i].x, b[c].x, s[i][c]))));
+        for (int c = 0; c < 4; ++c) s2[i][c] = 0ull;
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        ulonglong2 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const ulonglong2*>(q_s + (ty * 4 + i) * LD + d);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const ulonglong2*>(k_s + (tx + 16 * c) * LD + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s2[i][c] = fma_f2(a[i].y, b[c].y, fma_f2(a[i].x, b[c].x, s2[i][c]));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float lo, hi;
+          unpack_f2(s2[i][c], lo, hi);
+          s[i][c] = lo + hi;
+        }
     }
     __syncthreads();
     load(v_s, p.v, p.v_stride, t0 + j * R, hk, n);
@@ -198,7 +209,7 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS, 2) tova_packed_alu_kernel(
       m[i] = top;
       l[i] *= f;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
+      for (int c = 0; c < D / 32; ++c) o[i][c] = mul_f2(o[i][c], pack_f2(f, f));
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const float w = exp2f(s[i][c] - base);
@@ -215,33 +226,36 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS, 2) tova_packed_alu_kernel(
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(p_s + (ty * 4 + i) * LP + k);
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 4; ++x) {
+          uint64_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float y = x == 0 ? a[i].x : x == 1 ? a[i].y : x == 2 ? a[i].z : a[i].w;
+            w[i] = pack_f2(y, y);
+          }
 #pragma unroll
           for (int c = 0; c < D / 64; ++c) {
-            const float4 b = *reinterpret_cast<const float4*>(v_s + (k + x) * LD + c * 64 + tx * 4);
+            const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(v_s + (k + x) * LD + c * 64 + tx * 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float w = x == 0 ? a[i].x : x == 1 ? a[i].y : x == 2 ? a[i].z : a[i].w;
-              o[i][4 * c] = fmaf(w, b.x, o[i][4 * c]);
-              o[i][4 * c + 1] = fmaf(w, b.y, o[i][4 * c + 1]);
-              o[i][4 * c + 2] = fmaf(w, b.z, o[i][4 * c + 2]);
-              o[i][4 * c + 3] = fmaf(w, b.w, o[i][4 * c + 3]);
+              o[i][2 * c] = fma_f2(w[i], b.x, o[i][2 * c]);
+              o[i][2 * c + 1] = fma_f2(w[i], b.y, o[i][2 * c + 1]);
             }
           }
+        }
       }
     } else {
       for (int k = 0; k < min(rows, ty * 4 + 4); ++k) {
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
-          const float4 b = *reinterpret_cast<const float4*>(v_s + k * LD + c * 64 + tx * 4);
+          const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(v_s + k * LD + c * 64 + tx * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             if (k > ty * 4 + i) continue;
-            const float w = p_s[(ty * 4 + i) * LP + k];
-            o[i][4 * c] = fmaf(w, b.x, o[i][4 * c]);
-            o[i][4 * c + 1] = fmaf(w, b.y, o[i][4 * c + 1]);
-            o[i][4 * c + 2] = fmaf(w, b.z, o[i][4 * c + 2]);
-            o[i][4 * c + 3] = fmaf(w, b.w, o[i][4 * c + 3]);
+            const float y = p_s[(ty * 4 + i) * LP + k];
+            const uint64_t w = pack_f2(y, y);
+            o[i][2 * c] = fma_f2(w, b.x, o[i][2 * c]);
+            o[i][2 * c + 1] = fma_f2(w, b.y, o[i][2 * c + 1]);
           }
         }
       }
@@ -257,7 +271,12 @@ __global__ void __launch_bounds__(PACKED_ALU_THREADS, 2) tova_packed_alu_kernel(
     T* out = static_cast<T*>(p.out) + ((long long)(row0 + r) * p.H + h) * D + tx * 4;
     const float inv = 1.f / l[i];
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) out[(c >> 2) * 64 + (c & 3)] = (T)(o[i][c] * inv);
+    for (int c = 0; c < D / 32; ++c) {
+      float lo, hi;
+      unpack_f2(o[i][c], lo, hi);
+      out[(c >> 1) * 64 + 2 * (c & 1)] = (T)(lo * inv);
+      out[(c >> 1) * 64 + 2 * (c & 1) + 1] = (T)(hi * inv);
+    }
   }
 }
 
