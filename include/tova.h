@@ -676,9 +676,10 @@ int tova_norm_rope_backward(const tova_rope* r, const void* q, int64_t q_stride,
  *          behind the last, and pages that no row needs, may hold anything; a value
  *          that is not finite in a row that is attended to makes its component of
  *          the result not finite, NaN or infinite.
- *          fp32: every product in fp32; bf16: weights as two bf16 terms.  How the
- *          rows are cut (n_live, lens, the GPU's size) changes the order of fp32
- *          sums, nothing else; the same call gives the same bits every time.
+ *          fp32: every product in fp32; bf16: weights as two bf16 terms (16 bits).
+ *          How the rows are cut (n_live, lens, the GPU's size) changes the order of
+ *          fp32 sums and the maximum against which a weight is rounded, nothing
+ *          else; the same call gives the same bits every time.
  *   tova_paged_workspace_bytes   device bytes, for every n_live up to this one;
  *          (size_t)-1 for an invalid configuration.  It asks the current device
  *          for its SM count. */

@@ -153,6 +153,10 @@ def test_norm_rope_strides_aliases_no_keys_no_weights():
     within(dy, dx, 2.0 ** -8 * dx.abs() + 64 * U * size + 1e-38)
     within(dqw, ww, 100 * U * wsize)
     assert bool((dkw == 0).all())                 # no keys
+    gq, gk = randn(g, T, B, H, D).to(torch.bfloat16), randn(g, T, B, Hkv, D).to(torch.bfloat16)
+    dk, dks, _, _ = norm_backward(k.clone(), one, 1e-6, pos, 10000.0, D, 0, gk)
+    r.tova_norm_rope_backward(q, k, gq, gk, T, gq, gk, ws, first_pos=11)       # over both, no weights' gradients asked for
+    within(gk, dk, 2.0 ** -8 * dk.abs() + 64 * U * dks + 1e-38)
     assert torch.equal(qkv, keep)
     r.tova_norm_rope_apply(q, k, T, q, k, first_pos=11)         # in place, as slices of the projection
     within(q, want[0][0], tol[0])
@@ -349,6 +353,31 @@ def test_paged_attention(dtype, D, shape):
 @pytest.mark.parametrize("B, H, Hkv, L", [(1, 32, 32, 30000), (300, 32, 8, 300), (1, 4, 2, 100003), (2000, 2, 1, 40)])
 def test_paged_attention_every_way_to_deal_out(dtype, B, H, Hkv, L):
     run_paged(dtype, B, H, Hkv, 128, [max(0, L - 131 * b % L) for b in range(B)], 16, seed=B)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B, Hkv, long", [(20, 8, 3000), (70, 8, 1500), (9, 2, 20000)])
+def test_paged_attention_one_sequence_far_longer_than_the_others(dtype, B, Hkv, long):
+    run_paged(dtype, B, 4 * Hkv, Hkv, 128, [long if b == B // 2 else (5 * b) % 40 for b in range(B)], 16, seed=B)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_paged_sequences_share_pages(dtype):
+    """The pages of a common beginning are in several sequences' tables, and one sequence is in the batch twice."""
+    H, Hkv, D, rows, t = 8, 2, 64, 16, TT[dtype]
+    g = gen(3)
+    K, V = randn(g, 9, Hkv, rows, D).to(t), randn(g, 9, Hkv, rows, D).to(t)
+    table = torch.tensor([[4, 1, 7, 0], [4, 1, 2, 3], [4, 1, 7, 0], [4, 6, 4, 4]], dtype=torch.int32)
+    lens = [60, 33, 60, 64]
+    q = randn(g, 4, H, D).to(t)
+    q[2] = q[0]
+    cfg = tova.tova_paged_config(4, H, Hkv, D, 9, rows, 4, TD[dtype], 0.0)
+    ws = torch.empty(max(16, tova.tova_paged_workspace_bytes(cfg, 64)), dtype=torch.uint8, device=DEV)
+    out = torch.empty(4, H, D, dtype=t, device=DEV)
+    tova.tova_paged_attention(cfg, K, V, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), 64, q, out, ws)
+    want, wv, reach = paged_reference(q, K, V, table, lens, rows)
+    within(out, want, attention_tolerance(dtype, D, 64, want, wv, reach, False))
+    assert torch.equal(out[0], out[2])
 
 
 def test_paged_attention_bounds_scale_and_table():
