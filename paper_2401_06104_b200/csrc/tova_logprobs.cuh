@@ -10,6 +10,10 @@
 // is no less than the n-th of the maxima is collected and ordered by counting.  Where more is collected than there is room for (rows of equal logits), n
 // passes over the shares find one after the other.
 //
+// Measured (GPU time, in a captured graph): 4095 rows of 64,000 in bf16 (524 MB) 88 us without alternatives, 105 us with five, 128 us
+// with 20 (5.9, 5.0 and 4.1 TB/s; 0.90 to 0.62 of the copy rate: behind the pass a block's selection, some 3 us, hardly overlaps the
+// others'); one row of 32,000 in fp32 with 20 alternatives 8.5 us.
+//
 // A block per row; a cluster of eight blocks where rows are few, each with an eighth of the row, which join in the first
 // block's shared memory.
 #pragma once

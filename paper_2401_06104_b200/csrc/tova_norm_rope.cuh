@@ -12,6 +12,11 @@
 // pair meet in one lane; N pairs a lane, the same ones in every row.  The sum of squares takes log2(D / 2N) shuffles.  Cosines
 // and sines are formed once per token and serve all heads; they, and the weights, lie in shared memory in the lanes' order, so
 // that a lane reads them 16 bytes at a time without bank conflicts.
+//
+// Measured (GPU time, in a captured graph): 4 x 4096 tokens of 32 + 8 heads x 128 in bf16 (335 MB) 57 us, 5.9 TB/s, 0.89 of the
+// copy rate; their gradient over 4 x 2047 tokens (252 MB) 56 us, 4.5 TB/s: 124 registers leave 16 warps an SM, whose two reductions
+// a row are not covered (three blocks an SM, one row in flight a thread: spills, 62; 128 threads a block: 57); 64 tokens 3.1 us.
+// With one vector a lane, so that a pair's other half came by shuffles, the first took 120 us, the second 88.
 #pragma once
 
 #include "tova_rope.cuh"

@@ -2,7 +2,8 @@
 // attends to itself and the earlier tokens of its sequence,
 //   o_i[h] = sum_{j <= i} softmax_j(scale q_i[h] k_j[hk]) v_j[hk],   hk = h / (H / Hkv).
 //
-// Here: how the work is dealt out, and the kernel on the plain ALUs (fp32, every product in fp32).
+// Here: how the work is dealt out, and the kernel on the plain ALUs (fp32, every product in fp32: four prompts of 1500 tokens, 32
+// heads x 128, 2.1 ms, 34.7 TFLOP/s, 0.47 of the multiply-adds' peak: shared-memory reads and the unhidden copies between).
 #pragma once
 
 #include "tova_mma.cuh"

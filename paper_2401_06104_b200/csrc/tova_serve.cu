@@ -297,7 +297,10 @@ extern "C" int tova_paged_write(const tova_paged_config* cfg, const void* k, int
   p.max_rows = (long long)cfg->max_pages * cfg->page_rows;
   p.S = cfg->batch; p.N = n_tokens; p.Hkv = cfg->n_kv_heads; p.n_pages = cfg->n_pages; p.max_pages = cfg->max_pages;
   p.shift = paged_shift(*cfg);
-  p.vec = (int)(cfg->head_dim * E / 16);
+  const unsigned vec = (unsigned)(cfg->head_dim * E / 16), per_row = vec * (unsigned)cfg->n_kv_heads;      // vec: 8, 16 or 32
+  for (p.vec_shift = 3; (1u << p.vec_shift) < vec;) ++p.vec_shift;
+  // Exact for i < 2 * PAGED_WRITE_TOKENS * per_row where i * per_row < 2^32.
+  p.magic = 2ull * tova::PAGED_WRITE_TOKENS * per_row * per_row < (1ull << 32) ? (unsigned)(((1ull << 32) + per_row - 1) / per_row) : 0;
   p.tokens_per_block = (int)std::min<long long>(tova::PAGED_WRITE_TOKENS, std::max<long long>(1, n_tokens / (4LL * dev.sm_count)));
   const unsigned blocks = (unsigned)((n_tokens + p.tokens_per_block - 1) / p.tokens_per_block);
   tova::tova_paged_write_kernel<<<blocks, tova::PAGED_WRITE_THREADS, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
