@@ -404,9 +404,10 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
         tc_fence_before();
         warp_arrive(&bar_p[t], lane);
       }
+      // (Also by warps without a tile: else they could report several items written while the others are still at the first.)
+      ok = ok && warp_wait(&bar_odd[item & 1], (uint32_t)((item >> 1) & 1));
       if (n > 0) {
         ok = ok && warp_wait(&bar_o[t], outs & 1);
-        ok = ok && warp_wait(&bar_odd[item & 1], (uint32_t)((item >> 1) & 1));
         if (ok) ++outs;
         tc_fence_after();
         const bool odd = ok && (odd_s[item & 1][0] | odd_s[item & 1][1]) != 0;

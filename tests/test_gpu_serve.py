@@ -599,6 +599,12 @@ def test_packed_attention_scale_and_logits_of_any_size(dtype):
     run_packed(dtype, 4, 2, 128, [260], gain=30.0)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H, Hkv, lens", [(32, 32, [1] * 40 + [114, 5]), (32, 32, [3] * 28), (9, 3, [100] * 200), (32, 32, [129, 1, 128, 300, 2] * 9)])
+def test_packed_many_items_a_block_some_without_a_second_tile(D, H, Hkv, lens):
+    run_packed("bf16", H, Hkv, D, lens)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_packed_attention_many_sequences(dtype):
     run_packed(dtype, 4, 2, 64, [(7 * i) % 40 for i in range(2000)])
