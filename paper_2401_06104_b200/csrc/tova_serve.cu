@@ -370,7 +370,8 @@ PackedPlan packed_plan(const tova_packed_config& c, int32_t n_tokens, int sm_cou
   t.rows = !bf16 ? tova::PACKED_ALU_ROWS : t.pairs ? 128 : 256;
   t.room = n_tokens / t.rows + std::min(c.n_seqs, n_tokens);
   t.heads = t.pairs ? c.n_q_heads / 2 : c.n_q_heads;
-  t.list = (long long)t.room * t.heads > sm_count;
+  // (a block that finds its own tile walks through the sequences, 32 at a time)
+  t.list = (long long)t.room * t.heads > sm_count || c.n_seqs > 256;
   t.bytes = t.list ? 16 + (size_t)t.room * sizeof(int4) : 0;
   return t;
 }

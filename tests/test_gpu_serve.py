@@ -608,6 +608,8 @@ def test_packed_many_items_a_block_some_without_a_second_tile(D, H, Hkv, lens):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_packed_attention_many_sequences(dtype):
     run_packed(dtype, 4, 2, 64, [(7 * i) % 40 for i in range(2000)])
+    run_packed(dtype, 4, 2, 64, [0] * 3000 + [9, 0, 70] + [0] * 2000, pad=0)      # nearly all of them empty
+    run_packed(dtype, 2, 2, 128, [0] * 200 + [130] + [0] * 50)
 
 
 def test_packed_offsets_that_are_not_rising_or_lie_outside():
