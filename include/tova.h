@@ -671,7 +671,7 @@ int tova_norm_rope_backward(const tova_rope* r, const void* q, int64_t q_stride,
  *          0..lens[b]-1 (its own among them, if it has been written): q [B,H,D]
  *          (q_stride elements between sequences, 0 = contiguous), out [B,H,D] in
  *          cfg->dtype.  lens [B] are taken as 0..n_live, n_live <= max_pages *
- *          page_rows being the most rows that any sequence has.  No rows: zeros.
+ *          page_rows (and 2^30) being the most rows that any sequence has.  No rows: zeros.
  *          A row of logits that are NaN, or all minus infinity, gives NaN.  Rows
  *          behind the last, and pages that no row needs, may hold anything; a value
  *          that is not finite in a row that is attended to makes its component of
@@ -681,7 +681,7 @@ int tova_norm_rope_backward(const tova_rope* r, const void* q, int64_t q_stride,
  *          fp32 sums and the maximum against which a weight is rounded, nothing
  *          else; the same call gives the same bits every time.
  *   tova_paged_workspace_bytes   device bytes, for every n_live up to this one;
- *          (size_t)-1 for an invalid configuration.  It asks the current device
+ *          (size_t)-1 for an invalid configuration or n_live.  It asks the current device
  *          for its SM count. */
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads, head_dim; /* as in tova_config                         */

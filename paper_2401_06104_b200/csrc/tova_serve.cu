@@ -212,6 +212,10 @@ int paged_check(const tova_paged_config* c) {
   if ((c->head_dim != 64 && c->head_dim != 128) || !known_dtype(c->dtype)) return TOVA_ERR_UNSUPPORTED;
   return TOVA_OK;
 }
+// Rows that a call may be bounded by: the table's, at most 2^30 (row numbers and what is added to them stay below 2^31).
+bool paged_bound_ok(const tova_paged_config& c, int32_t n_live) {
+  return n_live >= 0 && n_live <= (1 << 30) && n_live <= (long long)c.max_pages * c.page_rows;
+}
 int paged_shift(const tova_paged_config& c) {
   int s = 0;
   while ((1 << s) < c.page_rows) ++s;
@@ -309,7 +313,7 @@ extern "C" int tova_paged_write(const tova_paged_config* cfg, const void* k, int
 
 extern "C" size_t tova_paged_workspace_bytes(const tova_paged_config* cfg, int32_t n_live) {
   DeviceInfo dev;
-  if (paged_check(cfg) != TOVA_OK || n_live < 0 || n_live > (long long)cfg->max_pages * cfg->page_rows || !device_info(&dev)) return (size_t)-1;
+  if (paged_check(cfg) != TOVA_OK || !paged_bound_ok(*cfg, n_live) || !device_info(&dev)) return (size_t)-1;
   return paged_plan(*cfg, n_live, dev.sm_count, true).bytes;
 }
 
@@ -317,7 +321,7 @@ extern "C" int tova_paged_attention(const tova_paged_config* cfg, const void* K,
                                     const int32_t* lens, int32_t n_live, const void* q, int64_t q_stride, void* out, void* workspace,
                                     size_t workspace_bytes, void* cuda_stream) {
   if (int rc = paged_check(cfg)) return rc;
-  if (n_live < 0 || n_live > (long long)cfg->max_pages * cfg->page_rows) return TOVA_ERR_BAD_SHAPE;
+  if (!paged_bound_ok(*cfg, n_live)) return TOVA_ERR_BAD_SHAPE;
   if (!K || !V || !page_table || !lens || !q || !out) return TOVA_ERR_NULL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return TOVA_ERR_ALIGN;
   if (q_stride < 0) return TOVA_ERR_BAD_SHAPE;
