@@ -47,6 +47,20 @@ struct PackedTcShape {
   static constexpr int SMEM = (2 + SLOTS) * TILE + 1024;
 };
 
+// Where a block's copies lie: copy x of the present item has place at + x in the order of all of the block's, in a ring of SLOTS.
+// The count starts anew a whole number of turns back before it grows large (a long sequence with many heads has more than 2^31).
+template <int SLOTS>
+struct PackedRing {
+  int at = 0;
+  __host__ __device__ __forceinline__ int slot(int x) const { return (at + x) % SLOTS; }
+  __host__ __device__ __forceinline__ uint32_t phase(int x) const { return (uint32_t)((at + x) / SLOTS) & 1u; }
+  __host__ __device__ __forceinline__ bool again(int x) const { return at + x >= SLOTS; }        // another copy was there before
+  __host__ __device__ __forceinline__ void pass(int copies) {
+    at += copies;
+    if (at >= 4 * SLOTS) at = 2 * SLOTS + at % (2 * SLOTS);
+  }
+};
+
 // An item: tokens and heads of its two tiles, columns in tiles of 128.
 struct PackedItem {
   int t0, t1;                  // first token of the sequence, the first behind it
@@ -157,7 +171,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
   walk.start(p, own);
   PackedItem it;
   // Copies are made and consumed in the order K0 V0 K1 V1 ...; the ring's positions go on from item to item.
-  int ring = 0;
+  PackedRing<S::SLOTS> ring;
 
   if (warp == S::COPIER) {
     // ============================== copying thread ==============================
@@ -171,8 +185,8 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
       while (ok && walk.next(p, it)) {
         const int hk = it.head[0] / p.G;
         for (int x = 0; x < 2 * it.most && ok; ++x) {
-          const int pos = ring + x, slot = pos % S::SLOTS;
-          if (pos >= S::SLOTS) ok = mbar_wait_bounded(&empty[slot], (uint32_t)((pos / S::SLOTS - 1) & 1));
+          const int slot = ring.slot(x);
+          if (ring.again(x)) ok = mbar_wait_bounded(&empty[slot], ring.phase(x) ^ 1u);
           if (!ok) break;
           box(slot_s + slot * S::TILE, (x & 1) ? &map_v : &map_k, hk, it.t0 + (x >> 1) * C, &full[slot]);
           if (x == 0) {
@@ -186,7 +200,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
             }
           }
         }
-        ring += 2 * it.most;
+        ring.pass(2 * it.most);
       }
       // (Where a wait ran out it took two seconds, and whatever was on its way has landed since.)
     }
@@ -281,8 +295,8 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
       // They follow every copy, and a slot is free again only when they have seen what was in it: a wait by parity must be
       // neither ahead of its barrier by a phase nor behind by two.
       for (int x = 0; x < 2 * it.most && ok; ++x) {
-        const int pos = ring + x, slot = pos % S::SLOTS;
-        ok = warp_wait(&full[slot], (uint32_t)((pos / S::SLOTS) & 1));
+        const int slot = ring.slot(x);
+        ok = warp_wait(&full[slot], ring.phase(x));
         if (!ok) break;
         if ((x & 1) && (x >> 1) >= it.checked) {
           unsigned char* v_t = slot_s + slot * S::TILE;
@@ -318,7 +332,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
       odd = __any_sync(0xffffffffu, odd) != 0;
       if (lane == 0) odd_s[item & 1][w] = odd;
       warp_arrive(&bar_odd[item & 1], lane);
-      ring += 2 * it.most;
+      ring.pass(2 * it.most);
     }
   } else {
     // ============================== soft-max: a thread per row ==============================
