@@ -39,15 +39,17 @@ struct LogprobsParams {
   int T, V, top;
 };
 
-// A key that orders logits: larger is earlier.  -0 counts as 0; a NaN comes before everything.
+// A key that orders logits: larger is earlier.  -0 counts as 0; a NaN comes before everything, and leaves room for a start before
+// the first of all (the order of a NaN at token 0 is below ~0).
+constexpr uint32_t LOGIT_KEY_NAN = 0xfffffffeu;
 __device__ __forceinline__ uint32_t logit_key(float x) {
-  if (x != x) return 0xffffffffu;
+  if (x != x) return LOGIT_KEY_NAN;
   const uint32_t u = __float_as_uint(x + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 // The logit of a key (of a NaN: a NaN).
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
-// ... with the token: distinct for all elements of a row, and never 0.
+// ... with the token: distinct for all elements of a row, never 0 and never ~0.
 __device__ __forceinline__ unsigned long long logit_order(uint32_t key, int token) {
   return ((unsigned long long)key << 32) | (0xffffffffu - (uint32_t)token);
 }
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(LOGPROBS_THREADS, LOGPROBS_BLOCKS) tova_logpro
       red_s[warp][2] = e;
     }
   }
-  key_s[tid] = tid < n_vec ? (nan ? 0xffffffffu : logit_key(mine)) : 0u;
+  key_s[tid] = tid < n_vec ? (nan ? LOGIT_KEY_NAN : logit_key(mine)) : 0u;
   if (tid == 0) n_pool = 0;
   __syncthreads();
   // Joins n triples (m, S, E).

@@ -1,0 +1,33 @@
+"""GPU tests of the operators for sequences of different lengths where they are read most strictly: orders of NaN, bits that
+must not depend on other tokens, values that are not finite under vanishing weights, offsets that fall or lie outside, workspaces
+and captured calls."""
+import math
+
+import pytest
+import torch
+
+import paper_2401_06104_b200 as tova
+from test_gpu_serve import (DEV, TD, TT, attention_tolerance, gen, make_table, offsets_of, packed_reference, paged_reference,
+                            randn, run_logprobs, within)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------- log probabilities
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T, V, top", [(1, 5, 5), (2, 2000, 20), (200, 2000, 20), (160, 64000, 5), (160, 32000, 20), (2, 128256, 20), (2, 400000, 32)])
+def test_logprobs_rows_of_many_nan_are_ordered_by_their_tokens(dtype, T, V, top):
+    """NaN come first, equal ones in the order of their tokens: rows of nothing else, of NaN in half or most of the places, of
+    both signs; in rows of a block and of a cluster, with more and with fewer of them than are collected at a time."""
+    g, n = gen(V + T), torch.arange(V, device=DEV)
+    nan = torch.tensor([math.nan, -math.nan], device=DEV)
+    one = randn(g, V)
+    rows = [torch.full((V,), math.nan, device=DEV), torch.where(n % 2 == 0, nan[0], one), torch.where(n % 3 > 0, nan[1], one),
+            torch.where(n >= V // 2, nan[n % 2], torch.full_like(one, math.inf))]
+    x = torch.stack([rows[i % len(rows)] for i in range(max(T, len(rows)))]).to(TT[dtype])
+    tok = torch.zeros(x.shape[0], dtype=torch.int32, device=DEV)
+    lp, ent, ids, tlp = run_logprobs(x, tok, top, dtype)
+    assert bool(lp.isnan().all()) and bool(ent.isnan().all()) and bool(tlp.isnan().all())
+    key = torch.where(x.isnan(), torch.full((), math.inf, device=DEV, dtype=torch.float64), x.double().clamp(max=1e300))
+    assert torch.equal(ids.long(), torch.sort(key, dim=-1, descending=True, stable=True)[1][:, :top])
