@@ -381,9 +381,11 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
           sum = sums[0] + sums[1];
         };
         weights();
-        // The reference is moved where weights grow too large, or where a row's first ones are all very small (below 2^-32 of a
-        // weight of 1: later ones might lose their smallest).
-        if (__any_sync(0xffffffffu, !(sum <= TREE_TC_MOST) || m_ref == -INFINITY || (j == 0 && sum < 1.f / TREE_TC_MOST))) {
+        // A row's reference is moved where its weights grow too large, or where its first ones are all very small (below 2^-32 of a
+        // weight of 1: later ones might lose their smallest).  The warp's other rows form theirs anew against the reference that they
+        // have: the same bits, so that a row's result does not depend on what later tokens, or other sequences, ask for.
+        const bool ask = !(sum <= TREE_TC_MOST) || m_ref == -INFINITY || (j == 0 && sum < 1.f / TREE_TC_MOST);
+        if (__any_sync(0xffffffffu, ask)) {
           float top = -INFINITY;
 #pragma unroll
           for (int c = 0; c < C / 32; ++c) {
@@ -395,8 +397,8 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
             for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(s[x]));
           }
           top *= p.scale2;
-          // (a reference that is right already stays: another row of the warp asked)
-          const bool beyond = top > m_ref + 16.f || j == 0 || (m_ref == -INFINITY && top > -INFINITY);
+          // (without a finite logit so far, or with a NaN among them, there may be none to move to)
+          const bool beyond = ask && (top > m_ref + 16.f || j == 0 || (m_ref == -INFINITY && top > -INFINITY));
           const float m_new = beyond ? ceilf(top) : m_ref;
           const float corr = beyond && j > 0 ? ex2_approx(m_ref - m_new) : 1.f;       // a power of two, or 0
           m_ref = m_new;

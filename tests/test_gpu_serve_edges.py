@@ -31,3 +31,37 @@ def test_logprobs_rows_of_many_nan_are_ordered_by_their_tokens(dtype, T, V, top)
     assert bool(lp.isnan().all()) and bool(ent.isnan().all()) and bool(tlp.isnan().all())
     key = torch.where(x.isnan(), torch.full((), math.inf, device=DEV, dtype=torch.float64), x.double().clamp(max=1e300))
     assert torch.equal(ids.long(), torch.sort(key, dim=-1, descending=True, stable=True)[1][:, :top])
+
+
+# -------------------------------------------------------------------------------------------- packed prompts
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H, Hkv", [(16, 4), (9, 9)])
+@pytest.mark.parametrize("far", [30.0, math.nan])
+def test_packed_tokens_keep_their_bits_whatever_others_hold(dtype, D, H, Hkv, far):
+    """Logits of some size; then other sequences, the later tokens of a sequence from the middle of a warp's rows on (in the first
+    tile and in the second), and the rows behind the last sequence get queries and keys far larger, or NaN.  What no token sees
+    changes none of its bits."""
+    S, L = 50, 200
+    g, t, N = gen(D + H), TT[dtype], 50 * 200
+    q, k = (randn(g, N + 70, H, D) * 5).to(t), randn(g, N + 70, Hkv, D).to(t)
+    v = randn(g, N + 70, Hkv, D).to(t)
+    off = offsets_of([L] * S)
+    cfg = tova.tova_packed_config(S, H, Hkv, D, TD[dtype], 0.0)
+    ws = torch.empty(max(16, tova.tova_packed_workspace_bytes(cfg, N + 70)), dtype=torch.uint8, device=DEV)
+
+    def go(q, k):
+        out = torch.full((N + 70, H, D), 77.0, dtype=t, device=DEV)
+        tova.tova_packed_attention(cfg, q, k, v, N + 70, off, out, ws)
+        return out[:N].view(S, L, H, D)
+    clean = go(q, k)
+    place = torch.arange(N + 70, device=DEV)
+    for first in (48, 150):                        # the first token of each sequence that changes; all of every other sequence
+        change = ((place // L) % 2 == 1) | (place % L >= first) | (place >= N)
+        q2, k2 = (torch.where(change[:, None, None], x * far, x) for x in (q, k))
+        out = go(q2, k2)
+        assert torch.equal(out[::2, :first], clean[::2, :first])
+    change = ((place // L) % 2 == 1) | (place >= N)
+    q2, k2 = (torch.where(change[:, None, None], x * far, x) for x in (q, k))
+    assert torch.equal(go(q2, k2)[::2], clean[::2])
