@@ -467,15 +467,18 @@ struct PagedJoin {
     seen |= ml.y != PAGED_NOTHING;
   }
   __device__ __forceinline__ float factor(float2 ml) {       // (after all have been looked at)
+    // Without a row, or without a logit above minus infinity where another part has one: nothing for the sum, and 0 times the
+    // part's weighted sum, which is 0 unless it is not finite.
     if (ml.y == PAGED_NOTHING || (ml.x == -INFINITY && base != -INFINITY && ml.y == 0.f)) return 0.f;
     const float f = ml.x == -INFINITY ? 1.f : exp2f(ml.x - base);
     l = fmaf(f, ml.y, l);
     return f;
   }
-  // y += this part's four components.
+  // y += this part's four components; where the factor is 0 too: an infinity or a NaN among a part's values stays one, wherever
+  // the largest logit lies.
   __device__ __forceinline__ void add(float2 ml, const float4& a, float4& y) {
     const float f = factor(ml);
-    if (f != 0.f) y = make_float4(fmaf(f, a.x, y.x), fmaf(f, a.y, y.y), fmaf(f, a.z, y.z), fmaf(f, a.w, y.w));
+    y = make_float4(fmaf(f, a.x, y.x), fmaf(f, a.y, y.y), fmaf(f, a.z, y.z), fmaf(f, a.w, y.w));
   }
 };
 

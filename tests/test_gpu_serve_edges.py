@@ -65,3 +65,47 @@ def test_packed_tokens_keep_their_bits_whatever_others_hold(dtype, D, H, Hkv, fa
     change = ((place // L) % 2 == 1) | (place >= N)
     q2, k2 = (torch.where(change[:, None, None], x * far, x) for x in (q, k))
     assert torch.equal(go(q2, k2)[::2], clean[::2])
+
+# --------------------------------------------------------------------------------------------- a state in pages
+
+WAYS = {"one block": (2, 8, 2, 50), "cluster": (2, 8, 2, 1000), "shares": (1, 8, 2, 40000), "many parts": (1, 32, 1, 70000), "many": (400, 8, 2, 200)}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("logits", ["far below", "minus infinity"])
+def test_paged_values_that_are_not_finite_reach_the_result_under_any_weight(dtype, way, logits):
+    """All rows but the first 16 have a logit so far below the largest that their weights are 0, or minus infinity; an infinity or
+    a NaN in one of them still makes its component, and no other, not finite, wherever the row lies."""
+    B, H, Hkv, L = WAYS[way]
+    D, rows, t = 64, 16, TT[dtype]
+    g = gen(L)
+    table, pages = make_table([L] * B, rows, 3)
+    K, V = randn(g, pages, Hkv, rows, D).to(t), randn(g, pages, Hkv, rows, D).to(t)
+    b, tb = B - 1, table.to(DEV)
+    rest = table[b, 1:(L + rows - 1) // rows].long().to(DEV)
+    K[rest] = -40.0 if logits == "far below" else -math.inf
+    q = (randn(g, B, H, D).abs() + 0.5).to(t)      # logits of the rest: below -8 sqrt(64) * 40 / 16 ln 2 ... far below -2^7 in powers of two
+    cfg = tova.tova_paged_config(B, H, Hkv, D, pages, rows, table.shape[1], TD[dtype], 0.0)
+    ws = torch.empty(max(16, tova.tova_paged_workspace_bytes(cfg, L)), dtype=torch.uint8, device=DEV)
+    lens = torch.full((B,), L, dtype=torch.int32, device=DEV)
+
+    def go():
+        out = torch.full((B, H, D), 77.0, dtype=t, device=DEV)
+        tova.tova_paged_attention(cfg, K, V, tb, lens, L, q, out, ws)
+        return out
+    clean = go()
+    assert bool(clean.isfinite().all())
+    G = H // Hkv
+    hk = Hkv - 1
+    for j in (16, 33, L // 2, L - 1):
+        for bad in (math.inf, -math.inf, math.nan):
+            at = (int(table[b, j // rows]), hk, j % rows, 5)
+            keep = V[at].clone()
+            V[at] = bad
+            out = go()
+            V[at] = keep
+            mine = out[b, hk * G:(hk + 1) * G, 5]
+            assert not bool(mine.isfinite().any()), (j, bad, mine)
+            mine.copy_(clean[b, hk * G:(hk + 1) * G, 5])
+            assert torch.equal(out, clean), (j, bad)
