@@ -620,9 +620,13 @@ int tova_verify_draft(const tova_verify_config* cfg, const void* target, const v
  * nothing kept between calls, any stream, argument errors found on the host
  * before anything is launched.  Two calls that may run at the same time, captured
  * ones among them, need a workspace each.  Packed tokens: [N,...], the tokens of
- * sequence b are offsets[b] .. offsets[b+1] - 1, rows behind offsets[S] are left
- * alone.  Lengths, offsets and page tables are read on the device at the time of
- * the call's execution, so that a captured call follows them.
+ * sequence b are offsets[b] .. offsets[b+1] - 1, rows that belong to no sequence
+ * are left alone.  Offsets rise; values outside 0..N are taken as the nearest of
+ * them, a sequence that would end before it starts is empty.  (Where they fall
+ * all the same, a token that lies in several sequences counts as one of them's,
+ * some tokens may be left out, and nothing else is touched.)  Lengths, offsets and
+ * page tables are read on the device at the time of the call's execution, so that
+ * a captured call follows them.
  * ------------------------------------------------------------------------- */
 
 /* Norms of queries and keys, each head by itself, with the rotation of
@@ -662,8 +666,8 @@ int tova_norm_rope_backward(const tova_rope* r, const void* q, int64_t q_stride,
  * 0..n_pages-1 holds no rows: what would be written there is dropped, what would
  * be read there has no weight.
  *   tova_paged_write   rows k, v [N,Hkv,D] (strides as for tova_rope_apply) of
- *          packed tokens: token i of sequence b goes to row first_rows[b] +
- *          i - offsets[b] (first_rows [B] int32, NULL: 0).  offsets NULL: one token
+ *          packed tokens: a sequence's first goes to row first_rows[b] (int32, NULL:
+ *          0), the next ones behind it.  offsets [B+1] int32, NULL: one token
  *          a sequence, N <= B of them.  Rows that the table has no entry for are
  *          dropped.  Where two tokens of a call go to the same place (pages that
  *          sequences share) each 16 bytes there are one of theirs.
@@ -703,9 +707,7 @@ int tova_paged_attention(const tova_paged_config* cfg, const void* K, const void
  * to the earlier tokens of its sequence (Eq. 4 and 7 while nothing is dropped).
  *   q [N,H,D], k, v [N,Hkv,D]   strides as for tova_rope_apply (v may be a slice of
  *          the projection), out [N,H,D], all in cfg->dtype
- *   offsets [S+1] int32         rising; values outside 0..N are taken as the
- *          nearest of them, a sequence that would end before it starts is empty.
- *          Rows that belong to no sequence are not written
+ *   offsets [S+1] int32         Rows that belong to no sequence are not written
  * Logits, soft-max and sums are fp32; fp32 configurations form every product in
  * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the
  * result is.  A token's result does not depend on later tokens or on other

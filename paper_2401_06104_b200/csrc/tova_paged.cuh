@@ -29,9 +29,10 @@ struct PagedWriteParams {
   unsigned magic;               // ceil(2^32 / (vectors of a token's row)), or 0: too many for it to divide exactly
 };
 
-// The sequence that packed token i belongs to: the last b with offsets[b] <= i, looked for by a whole warp (32 places at a
-// time); -1 where there is none, or i lies behind the sequence's end.
-__device__ __forceinline__ int packed_sequence(const int32_t* offsets, int S, int i, int lane) {
+// The sequence that packed token i, 0 <= i < N, belongs to (the last b with offsets[b] <= i, looked for by a whole warp, 32 places at
+// a time) and its first token; -1 where there is none, or i lies behind the sequence's end.  Offsets outside 0..N are the nearest of
+// them, as in packed attention.
+__device__ __forceinline__ int packed_sequence(const int32_t* offsets, int S, int i, int lane, int& first) {
   int lo = 0, hi = S;                      // offsets[lo] <= i (if any), the answer lies in lo .. hi - 1
   for (;;) {
     const int step = (hi - lo + 31) / 32;
@@ -42,6 +43,7 @@ __device__ __forceinline__ int packed_sequence(const int32_t* offsets, int S, in
     hi = min(hi, lo + step);
     if (step == 1) break;
   }
+  first = max(offsets[lo], 0);             // (no more than i; the end's bound is above i)
   return i < offsets[lo + 1] ? lo : -1;
 }
 
@@ -68,10 +70,11 @@ __global__ void __launch_bounds__(PAGED_WRITE_THREADS) tova_paged_write_kernel(c
     if (e0 == (int)threadIdx.x) {
       for (int t = warp; t < n_tok; t += PAGED_WRITE_THREADS / 32) {
         const int i = i0 + t;
-        const int b = p.offsets ? packed_sequence(p.offsets, p.S, i, lane) : i;
+        int first = i;
+        const int b = p.offsets ? packed_sequence(p.offsets, p.S, i, lane, first) : i;
         long long to = -1;
         if (b >= 0) {
-          const long long j = (long long)(p.first ? p.first[b] : 0) + (p.offsets ? i - p.offsets[b] : 0);
+          const long long j = (long long)(p.first ? p.first[b] : 0) + (i - first);
           if (j >= 0 && j < p.max_rows) {
             const int page = p.table[(long long)b * p.max_pages + (j >> p.shift)];
             if (page >= 0 && page < p.n_pages)

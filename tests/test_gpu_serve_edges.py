@@ -109,3 +109,53 @@ def test_paged_values_that_are_not_finite_reach_the_result_under_any_weight(dtyp
             assert not bool(mine.isfinite().any()), (j, bad, mine)
             mine.copy_(clean[b, hk * G:(hk + 1) * G, 5])
             assert torch.equal(out, clean), (j, bad)
+
+
+def token_places(off, N):
+    """The (sequence, row) pairs that each packed token belongs to: sequence b has the tokens from offsets[b], held to 0..N, to
+    the one before offsets[b + 1], held the same way."""
+    places = [[] for _ in range(N)]
+    for b in range(len(off) - 1):
+        a = min(max(off[b], 0), N)
+        for i in range(a, min(max(off[b + 1], a), N)):
+            places[i].append((b, i - a))
+    return places
+
+
+OFFSETS = {
+    "outside": [-4, 100, 200, 2 ** 31 - 1], "far outside": [-2 ** 31, 7, 7, 2 ** 31 - 1], "behind the tokens": [0, 10, 5000, 6000], "below 0": [-9, -3, 60, 250],
+    "all the same": [9, 9, 9, 9], "begin late, end early": [7, 20, 20, 240], "one ends before it starts": [-4, 100, 90, 150, 2 ** 31 - 1],
+    "many outside": [3 * i - 300 for i in range(230)], "falls back": [0, 200, 90, 120], "falls below 0": [50, -3, 60, 260],
+    "many, falling": [0] + [(37 * i) % 257 for i in range(200)] + [230],
+}
+
+
+@pytest.mark.parametrize("case", OFFSETS)
+def test_paged_write_reads_offsets_as_packed_attention_does(case):
+    """Every token goes to the row that packed attention has it at: values outside 0..N are the nearest of them, a sequence that
+    would end before it starts is empty.  Where offsets fall, a token that several sequences hold goes to one of its places, some
+    go to none, and nothing else is written."""
+    off, N, Hkv, D, rows = OFFSETS[case], 250, 2, 64, 4
+    S = len(off) - 1
+    g = gen(S)
+    first = [(3 * b) % 5 for b in range(S)]
+    most = 65                                      # pages a sequence: up to N + 4 rows
+    pages = S * most
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(S)).to(torch.int32).view(S, most)
+    k, v = randn(g, N, Hkv, D) + 10, randn(g, N, Hkv, D) + 10
+    K = torch.zeros(pages, Hkv, rows, D, device=DEV)
+    V = torch.zeros_like(K)
+    cfg = tova.tova_paged_config(S, Hkv, Hkv, D, pages, rows, most, TD["fp32"], 0.0)
+    tova.tova_paged_write(cfg, k, v, N, table.to(DEV), K, V, first_rows=torch.tensor(first, dtype=torch.int32, device=DEV),
+                          offsets=torch.tensor(off, dtype=torch.int32, device=DEV))
+    for i, places in enumerate(token_places(off, N)):
+        found = 0
+        for b, r in places:
+            j = first[b] + r
+            at = (int(table[b, j // rows]), slice(None), j % rows)
+            if torch.equal(K[at], k[i]) and torch.equal(V[at], v[i]):
+                found += 1
+                K[at] = 0.0
+                V[at] = 0.0
+        assert found == (1 if places else 0) or (found == 0 and "fall" in case), (i, places, found)
+    assert not bool(K.any()) and not bool(V.any())
