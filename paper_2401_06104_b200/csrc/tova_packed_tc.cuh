@@ -37,6 +37,8 @@ __device__ __forceinline__ void add_bf16x2(uint32_t u, float& lo, float& hi) {
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.bf16 %0, a, %0;\n\tadd.rn.f32.bf16 %1, b, %1;\n\t}" : "+f"(lo), "+f"(hi) : "r"(u));
 }
 
+constexpr float PACKED_TC_FAR = 4194304.f;      // 2^22: up to here a rounded product of a logit is off by a quarter at most
+
 template <int D>
 struct PackedTcShape {
   static constexpr int ROWS = 128, COLS = 128;
@@ -358,9 +360,11 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
             for (int x = 0; x < 32; ++x) s[x] = ((see >> x) & 1u) ? s[x] : 0xff800000u;
           }
         };
-        auto weights = [&]() {
+        // `far`: a logit's product with the scale is rounded by itself where the reference, which is a logit's rounded product too,
+        // is so large that the two would not meet otherwise.
+        auto weights = [&](bool far) {
           const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-          const uint64_t neg_2 = pack_f2(-ref, -ref);
+          const uint64_t neg_2 = pack_f2(-ref, -ref), mul_2 = far ? pack_f2(1.f, 1.f) : scale_2;
           float sums[2] = {0.f, 0.f};
           uint32_t s[2][32];
           tmem_ld32_start(base, s[0]);
@@ -372,7 +376,9 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float x0, x1;
-              unpack_f2(fma_f2(pack_f2(__uint_as_float(s[c & 1][2 * e]), __uint_as_float(s[c & 1][2 * e + 1])), scale_2, neg_2), x0, x1);
+              uint64_t x = pack_f2(__uint_as_float(s[c & 1][2 * e]), __uint_as_float(s[c & 1][2 * e + 1]));
+              if (far) x = mul_f2(x, scale_2);
+              unpack_f2(fma_f2(x, mul_2, neg_2), x0, x1);
               const uint32_t u = pack_bf16(ex2_approx(x0), ex2_approx(x1));
               add_bf16x2(u, sums[0], sums[1]);
               w[16 * c + e] = u;
@@ -380,11 +386,11 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
           }
           sum = sums[0] + sums[1];
         };
-        weights();
+        weights(false);
         // A row's reference is moved where its weights grow too large, or where its first ones are all very small (below 2^-32 of a
         // weight of 1: later ones might lose their smallest).  The warp's other rows form theirs anew against the reference that they
         // have: the same bits, so that a row's result does not depend on what later tokens, or other sequences, ask for.
-        const bool ask = !(sum <= TREE_TC_MOST) || m_ref == -INFINITY || (j == 0 && sum < 1.f / TREE_TC_MOST);
+        const bool ask = !(sum <= TREE_TC_MOST) || fabsf(m_ref) > PACKED_TC_FAR || (j == 0 && sum < 1.f / TREE_TC_MOST);
         if (__any_sync(0xffffffffu, ask)) {
           float top = -INFINITY;
 #pragma unroll
@@ -408,7 +414,7 @@ __global__ void __launch_bounds__(PackedTcShape<D>::THREADS, 1)
 #pragma unroll
             for (int c = 0; c < D; c += 16) tree_tc_scale16(base + 128 + c, corr);
           }
-          weights();
+          weights(fabsf(m_ref) > PACKED_TC_FAR && m_ref != -INFINITY);
         }
         l += sum;
 #pragma unroll

@@ -67,6 +67,57 @@ def test_packed_tokens_keep_their_bits_whatever_others_hold(dtype, D, H, Hkv, fa
     assert torch.equal(go(q2, k2)[::2], clean[::2])
 
 
+def far_logits(g, N, H, Hkv, D, size, kind, t):
+    """Queries and keys along one component, so that logits are whole multiples of 2^size in every arithmetic (-7 .. 7, -7 .. -1, or
+    falling and rising with the token): all weight lies on the rows of the largest multiple."""
+    c = {"any": lambda: torch.randint(-7, 8, (N, Hkv), generator=g, device=DEV), "negative": lambda: torch.randint(-7, 0, (N, Hkv), generator=g, device=DEV),
+         "rising": lambda: (torch.arange(N, device=DEV) // 9)[:, None].expand(N, Hkv), "falling": lambda: -(torch.arange(N, device=DEV) // 9)[:, None].expand(N, Hkv)}[kind]()
+    q, k = torch.zeros(N, H, D, device=DEV), torch.zeros(N, Hkv, D, device=DEV)
+    q[..., 3], k[..., 3] = 2.0 ** (size - size // 2 + 3), c * 2.0 ** (size // 2)
+    return q.to(t), k.to(t), c.double()
+
+
+FAR = [(size, kind) for size in (7, 19, 27, 31, 40, 100) for kind in ("any", "negative", "rising", "falling")]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size, kind", FAR)
+def test_attention_with_finite_logits_of_any_size(dtype, size, kind):
+    """Soft-max of logits that lie 2^7 and more apart is the mean over the rows of the largest, at any size below fp32's range: in
+    packed prompts and over pages.  Weights are 1 or 0 (2^-128 and less), so only sums of n values and the result round."""
+    t, H, Hkv, D, lens, rows = TT[dtype], 6, 3, 64, [300, 1, 77, 40], 16
+    g, N = gen(size), sum(lens)
+    q, k, c = far_logits(g, N, H, Hkv, D, size, kind, t)
+    v = randn(g, N, Hkv, D).to(t)
+    cfg = tova.tova_packed_config(len(lens), H, Hkv, D, TD[dtype], 1.0 / 8)
+    ws = torch.empty(max(16, tova.tova_packed_workspace_bytes(cfg, N)), dtype=torch.uint8, device=DEV)
+    out = torch.full((N, H, D), 77.0, dtype=t, device=DEV)
+    off = offsets_of(lens)
+    tova.tova_packed_attention(cfg, q, k, v, N, off, out, ws)
+    want, size_v = torch.empty(N, H, D, dtype=torch.float64, device=DEV), torch.empty(N, H, D, dtype=torch.float64, device=DEV)
+    a = 0
+    for n in lens:
+        see = torch.ones(n, n, dtype=torch.bool, device=DEV).tril()
+        for h in range(H):
+            x = c[a:a + n, h // (H // Hkv)].expand(n, n).masked_fill(~see, -math.inf)
+            w = (x == x.amax(-1, keepdim=True)).double()
+            w /= w.sum(-1, keepdim=True)
+            want[a:a + n, h], size_v[a:a + n, h] = w @ v[a:a + n, h // (H // Hkv)].double(), w @ v[a:a + n, h // (H // Hkv)].double().abs()
+        a += n
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    tol = half * want.abs() + (2 * max(lens) + 16) * 2.0 ** -24 * size_v + 1e-30
+    within(out, want, tol)
+    table, pages = make_table(lens, rows, 1)
+    K, V = torch.zeros(pages, Hkv, rows, D, dtype=t, device=DEV), torch.zeros(pages, Hkv, rows, D, dtype=t, device=DEV)
+    pc = tova.tova_paged_config(len(lens), H, Hkv, D, pages, rows, table.shape[1], TD[dtype], 1.0 / 8)
+    tova.tova_paged_write(pc, k, v, N, table.to(DEV), K, V, offsets=off)
+    pw = torch.empty(max(16, tova.tova_paged_workspace_bytes(pc, max(lens))), dtype=torch.uint8, device=DEV)
+    last = (off[1:] - 1).long()
+    po = torch.full((len(lens), H, D), 77.0, dtype=t, device=DEV)
+    tova.tova_paged_attention(pc, K, V, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), max(lens), q[last].contiguous(), po, pw)
+    within(po, want[last], tol[last])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_packed_attention_with_a_list_in_captured_graphs_at_once(dtype):
     """Calls that make a list of their tiles first (more sequences, or more work, than blocks find by themselves), captured, and
