@@ -542,7 +542,9 @@ int tova_quant_read(const tova_quant_config* cfg, const void* k_codes, const flo
  *   q [N,B,H,D], k, v [N,B,Hkv,D], out [N,B,H,D]   all in cfg->dtype
  * Logits, soft-max and sums are fp32; fp32 configurations form every product in
  * fp32, bf16 ones on the tensor cores with the weights rounded to bf16, as the
- * result is (an answer for one token is so less exact than tova_decode_step's).
+ * result is (an answer for one token is so less exact than tova_decode_step's);
+ * there, logits of 2^30 and more give NaN where N nodes times the query heads of a
+ * KV head are more than 64.
  * n_live, lens, the other sequences and the GPU's size decide how the columns are
  * cut: they change the order of fp32 sums and, in bf16, the maximum against which a
  * weight is rounded, and nothing else.  The same call gives the same bits every time.

@@ -16,6 +16,8 @@
 // Measured (GPU time, in a captured graph): 4 x 4096 tokens of 32 + 8 heads x 128 in bf16 (335 MB) 57 us, 5.9 TB/s, 0.89 of the
 // copy rate; their gradient over 4 x 2047 tokens (252 MB) 56 us, 4.5 TB/s: 124 registers leave 16 warps an SM, whose two reductions
 // a row are not covered (three blocks an SM, one row in flight a thread: spills, 62; 128 threads a block: 57); 64 tokens 3.1 us.
+// fp32: the first 107 us (6.3 TB/s), the gradient 89 (5.7).  64 or 96 of 128 components turning: 61 and 58-59 us; 20 (pairs that split
+// vectors, single components) 117 and 96; interleaved 60 and 57.
 // With one vector a lane, so that a pair's other half came by shuffles, the first took 120 us, the second 88.
 #pragma once
 

@@ -11,8 +11,8 @@
 //                       PV_1(j) S_1(j+1): one tile's contractions run while the other's soft-max does
 //   4 warps a tile      a thread per row: logits from TMEM, weights as bf16 back over them, where they are the A operand of
 //                       O += P V.  The weights' reference is a whole number, 0 at first and hardly ever moved (see tova_tree_tc.cuh): a
-//                       tile needs no maximum, only where its weights sum to more than 2^32, or a row's first ones to less than
-//                       2^-32, is it done over.  The sum is over the rounded weights, so that the weights that multiply V add up
+//                       tile needs no maximum, only where a row's weights sum to more than 2^32, its first ones to less than
+//                       2^-32, or its reference is beyond 2^22, is it done over.  The sum is over the rounded weights, so that the weights that multiply V add up
 //                       to one.  At the end the row of O, divided by its sum.
 //   2 checking warps    V tiles on the diagonal hold values of later tokens, and of other sequences, under weights of 0; where
 //                       one is not finite it becomes 0, and the rows that do see it get it added in the end.
@@ -20,7 +20,8 @@
 // yet to write.
 //
 // Measured (GPU time, in a captured graph): seven prompts from 8191 tokens down, 32 query over 8 KV heads x 128 (875 GFLOP) 750 us,
-// 1160 TFLOP/s, 0.70 of the measured bf16 rate; nine prompts of up to 200 tokens, 8 over 2 heads x 64, 8.6 us.  What bounds the
+// 1160 TFLOP/s, 0.70 of the measured bf16 rate (call after call, at the clocks of the power cap, 884 us); one prompt of 1024 / 2048 /
+// 4096 tokens 23 / 42 / 127 us; nine prompts of up to 200 tokens, 8 over 2 heads x 64, 8.6 us.  What bounds the
 // first: a round of both tiles takes 3500 cycles, its contractions 2050 of them.  The soft-max of a tile takes 2100 (exponentials
 // 1024 of them, TMEM loads and stores 700) and overlaps the other's contractions, not its own.  Not kept: two threads a row (2 %,
 // with a protocol for moving a reference that two warps share), an issuing warp for each tile (1.35 times as long: their

@@ -13,8 +13,8 @@ namespace tova {
 // Rows into pages: token i of the packed rows belongs to the sequence b with offsets[b] <= i < offsets[b + 1] (one token a
 // sequence where there are no offsets) and becomes its row first[b] + i - offsets[b].  DRAM bound; a block takes a few tokens,
 // whose rows are on their way before their places have been looked up.  Measured (GPU time, in a captured graph): 20,342 tokens of
-// 8 heads x 128 in bf16 (167 MB) 29.7 us, 5.6 TB/s, 0.85 of the copy rate (34 with divisions by run-time sizes, 33 with 16 tokens
-// a block); 64 tokens 2.2 us.
+// 8 heads x 128 in bf16 (167 MB) 29.1 us, 5.7 TB/s, 0.87 of the copy rate, in fp32 56.8 us, 0.89 (bf16: 34 with divisions by run-time
+// sizes, 33 with 16 tokens a block); 64 tokens 2.3 us.
 constexpr int PAGED_WRITE_THREADS = 256;
 constexpr int PAGED_WRITE_TOKENS = 4;
 
